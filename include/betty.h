@@ -111,7 +111,11 @@ typedef enum {
 } betty_param_kind;
 
 typedef enum { BETTY_NEUMANN = 0, BETTY_CG = 1, BETTY_FD = 2 } betty_method;
-typedef enum { BETTY_ACT_RELU = 0, BETTY_ACT_GELU = 1 } betty_activation; /* GELU: erf form */
+typedef enum {
+  BETTY_ACT_RELU = 0,
+  BETTY_ACT_GELU = 1,  /* erf form */
+  BETTY_ACT_SILU = 2   /* z sigmoid(z); the betty_act8 calls only, not the levels' hidden layers */
+} betty_activation;
 typedef enum { BETTY_F32 = 0, BETTY_BF16 = 1, BETTY_I32 = 2, BETTY_F16 = 3 } betty_dtype;
 
 /* How a problem's gradient step is taken (the paper lets each problem bring its own optimiser: SGD with
@@ -325,6 +329,87 @@ typedef struct {
 betty_status betty_gemm_bf16(int32_t M, int32_t N, int32_t n_pairs, const betty_gemm_operands* pairs,
                              float* C, int64_t ldc, float beta, int32_t path, void* ws, size_t ws_bytes,
                              void* stream);
+
+/* ---- Operators of a trained residual block ----
+ * For problems whose network is not one of the cost families above: a block  u = N(x),  y = experts(u),
+ * x' = x + s a(g) N(y)  of a language model, forward and backward, next to the optimisers and the finite-difference
+ * products of gradients that the caller takes with them.  All matrices are row-major DEVICE memory with a leading
+ * dimension in values (rows may be padded or be slices of wider rows); addresses need only their type's own alignment, 16-byte
+ * aligned addresses and leading dimensions (and widths that are multiples of 8) take the faster accesses.  Parameter
+ * blocks and their gradients are fp32 and 16-byte aligned, as above.  Outputs are overwritten, sums are fp32 in a
+ * fixed order: the same call gives the same bits.  Zero rows are valid.  In-place use is possible where it is said. */
+
+typedef enum {
+  BETTY_NORM_NONE = 0,   /* N(v) = v */
+  BETTY_NORM_RMS = 1,    /* v / sqrt(mean(v^2) + eps) */
+  BETTY_NORM_LAYER = 2   /* the same of v - mean(v) */
+} betty_norm;
+typedef enum {
+  BETTY_GATE_NONE = 0,   /* a = 1 */
+  BETTY_GATE_LINEAR = 1, /* a(g) = g */
+  BETTY_GATE_SIGMOID = 2 /* a(g) = sigmoid(g) */
+} betty_gate;
+typedef struct {
+  int64_t d;             /* width of a row, 1 .. 16384 (else BETTY_ERR_SHAPE / BETTY_ERR_UNSUPPORTED) */
+  int32_t x_dtype;       /* the residual stream x, x', dx', dx: BETTY_F32, or the same as y_dtype */
+  int32_t y_dtype;       /* y, gate, u and their gradients: BETTY_F32, BETTY_BF16 or BETTY_F16 */
+  int32_t pre, post;     /* betty_norm: before the (next) block, after the block */
+  int32_t gate;          /* betty_gate */
+  int32_t bias;          /* != 0: the norms have biases */
+  int64_t rows_per_gate; /* >= 1: row i uses row i / rows_per_gate of the gate (1: a gate of its own) */
+  float eps;             /* >= 0 */
+} betty_block_norm_cfg;
+
+/* The norms after a block and before the next one, with the block's gate and residual scale, in one pass:
+ *   z = N_post(y) * w_post (+ b_post);   x' = x + s * a(g) * z;   u = N_pre(x') * w_pre (+ b_pre).
+ * params: [w_pre, w_post, s (, b_pre, b_post)], d floats each.  The entry norm reads x' before it is rounded to
+ * x_dtype.  y = NULL: no block before (u = N_pre(x) * w_pre (+ b_pre), x_out is not written).  u = NULL: no block
+ * after.  x_out may be x. */
+betty_status betty_block_norm(const betty_block_norm_cfg* cfg, const float* params, int64_t rows, const void* x, int64_t ldx,
+                              const void* y, int64_t ldy, const void* gate, int64_t ldg, void* x_out, int64_t ldxo, void* u,
+                              int64_t ldu, void* stream);
+
+/* Workspace of the backward call on up to `rows` rows (on the current device). */
+betty_status betty_block_norm_workspace_size(const betty_block_norm_cfg* cfg, int64_t rows, size_t* bytes);
+
+/* Gradients of betty_block_norm from its stored x' and its inputs y and gate (no statistics are kept):
+ * du (NULL: u was not used) and dx_out (the gradient that reaches x' from elsewhere; NULL: none), not both NULL, give
+ * dx, dy, dgate [ceil(rows / rows_per_gate), d] (summed over the rows that share a gate row) and
+ * dparams (layout of params).  y = NULL: dx and dparams only.  du = NULL: x_out is not read and may be NULL.  dx may be
+ * dx_out; dy may be y, dgate may be gate when rows_per_gate is 1. */
+betty_status betty_block_norm_backward(const betty_block_norm_cfg* cfg, const float* params, int64_t rows, const void* x_out,
+                                       int64_t ldxo, const void* y, int64_t ldy, const void* gate, int64_t ldg, const void* du,
+                                       int64_t lddu, const void* dx_out, int64_t lddxo, void* dx, int64_t lddx, void* dy,
+                                       int64_t lddy, void* dgate, int64_t lddg, float* dparams, void* ws, size_t ws_bytes,
+                                       void* stream);
+
+typedef struct {
+  int64_t cols;          /* width of the activation, >= 1 */
+  int32_t dtype;         /* z, the activation and their gradients: BETTY_F32, BETTY_BF16 or BETTY_F16 */
+  int32_t act;           /* betty_activation */
+  int32_t gated;         /* != 0: z is [gate | value], 2 * cols wide, and the activation act(gate) * value */
+} betty_act8_cfg;
+
+/* A hidden layer's activation with an 8-bit checkpoint of its pre-activation z [rows, cols or 2 * cols]:
+ *   act = act(z)  or  act(z_gate) * z_value   (NULL: the checkpoint only)
+ * and per group of 128 values of a row (of each half of a gated row; the last group may be short), with
+ * top = max |z| of the group and every operation rounded to fp32,
+ *   q = rint(z * (127 * (1 / top))) as int8,   scale = top * (1 / 127).
+ * A group with top < 1e-30 is held as zeros; a group with an infinity or a NaN gets the scale NaN.
+ * q [rows, width of z], scales [rows, halves * ceil(cols / 128)]. */
+betty_status betty_act8_store(const betty_act8_cfg* cfg, int64_t rows, const void* z, int64_t ldz, void* act, int64_t lda,
+                              int8_t* q, int64_t ldq, float* scales, int64_t lds, void* stream);
+
+/* The values a checkpoint stands for: z = q * scale, rounded to dtype. */
+betty_status betty_act8_restore(const betty_act8_cfg* cfg, int64_t rows, const int8_t* q, int64_t ldq, const float* scales,
+                                int64_t lds, void* z, int64_t ldz, void* stream);
+
+/* The layer's backward pass from the checkpoint (z~ = q * scale): dz = da * act'(z~), gated
+ * dz = [da * z~_value * act'(z~_gate) | da * act(z~_gate)], and the activation at z~ (what the next layer's weight
+ * gradient needs).  dz or act may be NULL; da is read for dz only. */
+betty_status betty_act8_backward(const betty_act8_cfg* cfg, int64_t rows, const int8_t* q, int64_t ldq, const float* scales,
+                                 int64_t lds, const void* da, int64_t ldda, void* dz, int64_t lddz, void* act, int64_t lda,
+                                 void* stream);
 
 /* The dataflow graph of Sec. 3.1: directed edges between problem indices.  An upper-to-lower edge
  * (from > to in the paper's ordering) says that theta_from constrains problem `to`; a lower-to-upper

@@ -19,7 +19,9 @@ BETTY_OK = 0
  LOSS_WEIGHTNET_DETECT, LOSS_MLP_CE_CORRECT) = range(8)
 PARAM_VECTOR, PARAM_MLP, PARAM_WEIGHTNET, PARAM_LOGWD, PARAM_CORRECTNET = range(5)
 BETTY_NEUMANN, BETTY_CG, BETTY_FD = range(3)
-ACT_RELU, ACT_GELU = range(2)
+ACT_RELU, ACT_GELU, ACT_SILU = range(3)
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+GATE_NONE, GATE_LINEAR, GATE_SIGMOID = range(3)
 BETTY_F32, BETTY_BF16, BETTY_I32, BETTY_F16 = range(4)
 BETTY_OPT_GD, BETTY_OPT_MOMENTUM, BETTY_OPT_ADAM = range(3)
 BETTY_LR_CONSTANT, BETTY_LR_MULTISTEP, BETTY_LR_COSINE = range(3)
@@ -69,6 +71,15 @@ class _GemmOperands(C.Structure):
                 ("ldb", C.c_int64), ("b_transposed", C.c_int32), ("K", C.c_int32), ("alpha", C.c_float)]
 
 
+class _BlockNormCfg(C.Structure):
+    _fields_ = [("d", C.c_int64), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("pre", C.c_int32), ("post", C.c_int32),
+                ("gate", C.c_int32), ("bias", C.c_int32), ("rows_per_gate", C.c_int64), ("eps", C.c_float)]
+
+
+class _Act8Cfg(C.Structure):
+    _fields_ = [("cols", C.c_int64), ("dtype", C.c_int32), ("act", C.c_int32), ("gated", C.c_int32)]
+
+
 _lib = None
 
 
@@ -105,6 +116,14 @@ def lib():
     }
     sig["betty_hvp_logreg_static"] = [VP, C.c_int64, C.c_int64, VP, VP, VP, VP, VP, VP]
     sig["betty_gemm_bf16"] = [I32, I32, I32, C.POINTER(_GemmOperands), VP, C.c_int64, F, I32, VP, SZ, VP]
+    I64, BN, A8 = C.c_int64, C.POINTER(_BlockNormCfg), C.POINTER(_Act8Cfg)
+    mat = [VP, I64]
+    sig["betty_block_norm"] = [BN, VP, I64] + 5 * mat + [VP]
+    sig["betty_block_norm_workspace_size"] = [BN, I64, C.POINTER(SZ)]
+    sig["betty_block_norm_backward"] = [BN, VP, I64] + 8 * mat + [VP, VP, SZ, VP]
+    sig["betty_act8_store"] = [A8, I64] + 4 * mat + [VP]
+    sig["betty_act8_restore"] = [A8, I64] + 3 * mat + [VP]
+    sig["betty_act8_backward"] = [A8, I64] + 5 * mat + [VP]
     EP, IP = C.POINTER(_Edge), C.POINTER(I32)
     sig["betty_find_paths"] = [I32, EP, I32, EP, I32, I32, IP, I32, IP, I32, IP, IP]
     sig["betty_selftest_wait_timeout"] = [VP, SZ, VP]
@@ -292,6 +311,17 @@ class Workspace:
         betty_reset_status(self)
 
 
+    @classmethod
+    def of_bytes(cls, nbytes: int, device="cuda") -> "Workspace":
+        """Scratch for calls that say how much they need themselves (the operators of a residual block)."""
+        ws = cls.__new__(cls)
+        ws.nbytes = max(int(nbytes), 256)
+        ws.buf = torch.empty(ws.nbytes + 256, dtype=torch.uint8, device=device)
+        ws.ptr = ws.buf.data_ptr() + (-ws.buf.data_ptr()) % 256
+        betty_reset_status(ws)
+        return ws
+
+
 def betty_reset_status(ws: Workspace, stream=None) -> None:
     _check(lib().betty_reset_status(ws.ptr, ws.nbytes, _stream(stream)), "betty_reset_status")
 
@@ -420,6 +450,146 @@ def betty_engine_run(levels: Sequence[Level], u2l, l2u, per_level: Sequence[Meth
                                   int(n_iterations), log, log_capacity, C.byref(n), ws.ptr, ws.nbytes, _stream(stream)),
            "betty_engine_run")
     return [log[i] for i in range(min(n.value, log_capacity))]
+
+
+# ---- operators of a trained residual block ----
+def _mat(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, name: str):
+    """Address and leading dimension of a [rows, cols] matrix with consecutive values in a row."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"{name} must be a {dtype} CUDA tensor, got {t.dtype} on {t.device}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must have the shape ({rows}, {cols}), got {tuple(t.shape)}")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1 and rows > 0:
+        raise ValueError(f"{name} must have consecutive values in a row, got strides {t.stride()}")
+    return t.data_ptr(), ld
+
+
+_FLOAT = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def _float_dtype(t: torch.dtype) -> int:
+    if t not in _FLOAT:
+        raise ValueError(f"fp32, bf16 or fp16 tensors are taken, got {t}")
+    return _DT[t]
+
+
+class BlockNorm:
+    """Configuration of betty_block_norm (betty.h): the norms before (`pre`) and after (`post`) a block, its gate and the
+    rows that share a gate row.  Parameters are one fp32 tensor [3, d] = (w_pre, w_post, residual scale), with bias
+    [5, d] = (..., b_pre, b_post)."""
+
+    def __init__(self, d: int, pre: int = NORM_RMS, post: int = NORM_RMS, gate: int = GATE_NONE, rows_per_gate: int = 1,
+                 eps: float = 1e-6, bias: bool = False):
+        self.d, self.bias, self.rows_per_gate = int(d), bool(bias), int(rows_per_gate)
+        self._fields = (int(pre), int(post), int(gate), int(self.bias), self.rows_per_gate, float(eps))
+        self._refs = {}
+
+    def _ref(self, tx: torch.dtype, ty: torch.dtype):
+        """The C descriptor for these types (one per pair of types, so that calls of several threads share none in change)."""
+        r = self._refs.get((tx, ty))
+        if r is None:
+            r = self._refs[tx, ty] = C.byref(_BlockNormCfg(self.d, _float_dtype(tx), _float_dtype(ty), *self._fields))
+        return r
+
+    def _params(self, t: torch.Tensor, name: str) -> int:
+        n = 5 if self.bias else 3
+        if t.dtype is not torch.float32 or not t.is_cuda or not t.is_contiguous() or t.numel() != n * self.d:
+            raise ValueError(f"{name} must be a contiguous fp32 CUDA tensor of {n} x {self.d} values")
+        return t.data_ptr()
+
+    def _gate(self, t, rows: int, dtype, name: str):
+        return _mat(t, -(-rows // self.rows_per_gate), self.d, dtype, name)
+
+
+def betty_block_norm(cfg: BlockNorm, params: torch.Tensor, x: torch.Tensor, y: Optional[torch.Tensor], gate: Optional[torch.Tensor],
+                     x_out: Optional[torch.Tensor], u: Optional[torch.Tensor], stream=None) -> None:
+    """x_out = x + s a(gate) N_post(y), u = N_pre(x_out); y None: u = N_pre(x); u None: no entry norm."""
+    rows, d = x.shape[0], cfg.d
+    like = y if y is not None else u
+    if like is None:
+        raise ValueError("one of y and u has to be given")
+    tx, ty = x.dtype, like.dtype
+    _check(lib().betty_block_norm(cfg._ref(tx, ty), cfg._params(params, "params"), rows, *_mat(x, rows, d, tx, "x"), *_mat(y, rows, d, ty, "y"),
+                                  *cfg._gate(gate, rows, ty, "gate"), *_mat(x_out, rows, d, tx, "x_out"), *_mat(u, rows, d, ty, "u"),
+                                  _stream(stream)), "betty_block_norm")
+
+
+def betty_block_norm_workspace_size(cfg: BlockNorm, rows: int) -> int:
+    out = C.c_size_t(0)
+    _check(lib().betty_block_norm_workspace_size(cfg._ref(torch.float32, torch.float32), int(rows), C.byref(out)), "betty_block_norm_workspace_size")
+    return int(out.value)
+
+
+def betty_block_norm_backward(cfg: BlockNorm, params: torch.Tensor, x_out: Optional[torch.Tensor], y: Optional[torch.Tensor],
+                              gate: Optional[torch.Tensor], du: Optional[torch.Tensor], dx_out: Optional[torch.Tensor],
+                              dx: torch.Tensor, dy: Optional[torch.Tensor], dgate: Optional[torch.Tensor], dparams: torch.Tensor,
+                              ws: Workspace, stream=None) -> None:
+    """Gradients of betty_block_norm from x_out, y and gate; du and dx_out are the gradients of u and x_out."""
+    rows, d = dx.shape[0], cfg.d
+    like = y if y is not None else du
+    if like is None:
+        raise ValueError("one of y and du has to be given")
+    tx, ty = dx.dtype, like.dtype
+    _check(lib().betty_block_norm_backward(
+        cfg._ref(tx, ty), cfg._params(params, "params"), rows, *_mat(x_out, rows, d, tx, "x_out"), *_mat(y, rows, d, ty, "y"),
+        *cfg._gate(gate, rows, ty, "gate"), *_mat(du, rows, d, ty, "du"), *_mat(dx_out, rows, d, tx, "dx_out"),
+        *_mat(dx, rows, d, tx, "dx"), *_mat(dy, rows, d, ty, "dy"), *cfg._gate(dgate, rows, ty, "dgate"),
+        cfg._params(dparams, "dparams"), ws.ptr, ws.nbytes, _stream(stream)), "betty_block_norm_backward")
+
+
+class Act8:
+    """Configuration of the betty_act8 calls (betty.h): a hidden layer of `cols` activations, gated when its
+    pre-activation is [gate | value], 2 * cols wide."""
+
+    def __init__(self, cols: int, act: int = ACT_GELU, gated: bool = False):
+        self.cols, self.gated = int(cols), bool(gated)
+        self.width = self.cols * (2 if self.gated else 1)
+        self.n_scales = (self.width // max(self.cols, 1)) * -(-self.cols // 128)
+        self._fields = (int(act), int(self.gated))
+        self._refs = {}
+
+    def _ref(self, t: torch.dtype):
+        r = self._refs.get(t)
+        if r is None:
+            r = self._refs[t] = C.byref(_Act8Cfg(self.cols, _float_dtype(t), *self._fields))
+        return r
+
+    def empty(self, rows: int, device="cuda"):
+        """An unfilled checkpoint: (q, scales)."""
+        return (torch.empty(rows, self.width, dtype=torch.int8, device=device),
+                torch.empty(rows, self.n_scales, dtype=torch.float32, device=device))
+
+
+def betty_act8_store(cfg: Act8, z: torch.Tensor, act: Optional[torch.Tensor], q: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """act = the layer's activation (None: not wanted); (q, scales) = the 8-bit checkpoint of z."""
+    rows, t = z.shape[0], z.dtype
+    _check(lib().betty_act8_store(cfg._ref(t), rows, *_mat(z, rows, cfg.width, t, "z"), *_mat(act, rows, cfg.cols, t, "act"),
+                                  *_mat(q, rows, cfg.width, torch.int8, "q"), *_mat(scales, rows, cfg.n_scales, torch.float32, "scales"),
+                                  _stream(stream)), "betty_act8_store")
+
+
+def betty_act8_restore(cfg: Act8, q: torch.Tensor, scales: torch.Tensor, z: torch.Tensor, stream=None) -> None:
+    """z = the values the checkpoint stands for."""
+    rows = z.shape[0]
+    _check(lib().betty_act8_restore(cfg._ref(z.dtype), rows, *_mat(q, rows, cfg.width, torch.int8, "q"),
+                                    *_mat(scales, rows, cfg.n_scales, torch.float32, "scales"), *_mat(z, rows, cfg.width, z.dtype, "z"),
+                                    _stream(stream)), "betty_act8_restore")
+
+
+def betty_act8_backward(cfg: Act8, q: torch.Tensor, scales: torch.Tensor, da: Optional[torch.Tensor], dz: Optional[torch.Tensor],
+                        act: Optional[torch.Tensor], stream=None) -> None:
+    """dz = the gradient of the pre-activation from da, act = the activation, both at the checkpoint's values."""
+    like = dz if dz is not None else act
+    if like is None:
+        raise ValueError("one of dz and act has to be given")
+    rows, t = like.shape[0], like.dtype
+    _check(lib().betty_act8_backward(cfg._ref(t), rows, *_mat(q, rows, cfg.width, torch.int8, "q"),
+                                     *_mat(scales, rows, cfg.n_scales, torch.float32, "scales"), *_mat(da, rows, cfg.cols, t, "da"),
+                                     *_mat(dz, rows, cfg.width, t, "dz"), *_mat(act, rows, cfg.cols, t, "act"), _stream(stream)),
+           "betty_act8_backward")
 
 
 def betty_selftest_wait_timeout(ws: Workspace, stream=None) -> None:

@@ -981,6 +981,7 @@ betty_status mlpfam_validate(const betty_level* L) {
   const Parts P = parts_of(L);
   if (!P.mlp || !P.mlp->params) return BETTY_ERR_INVALID_ARG;
   if (L->loss == BETTY_LOSS_MLP_CE_REWEIGHT && L->param_kind != BETTY_PARAM_MLP) return BETTY_ERR_INVALID_ARG;
+  if (P.mlp->activation == BETTY_ACT_SILU) return BETTY_ERR_UNSUPPORTED;
   Net n;
   BETTY_TRY(net_layout(P.mlp, n));
   if (L->n < 0 || L->d != n.w[0]) return BETTY_ERR_SHAPE;
