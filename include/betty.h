@@ -411,6 +411,36 @@ betty_status betty_act8_backward(const betty_act8_cfg* cfg, int64_t rows, const 
                                  int64_t lds, const void* da, int64_t ldda, void* dz, int64_t lddz, void* act, int64_t lda,
                                  void* stream);
 
+typedef struct {
+  int32_t n_groups;      /* experts, 1 .. 1024 */
+  int32_t dtype;         /* operands: BETTY_BF16 or BETTY_F16; fp32 accumulation */
+  int64_t in, out;       /* W_e is [out, in] */
+} betty_grouped_cfg;
+
+/* Products of a batch whose rows are sorted by expert with the experts' matrices.  offsets (DEVICE int32
+ * [n_groups + 1], ascending from 0 to at most rows): rows offsets[e] .. offsets[e+1]-1 belong to expert e, which may have
+ * none; they are read on the device only.  Offsets out of order or range are clamped and recorded as
+ * BETTY_ERR_INVALID_ARG in the status block.  Matrices W, dW: [n_groups][out][in] with leading dimension ldw and
+ * group_stride values from one to the next.  Result types: BETTY_F32 or the operands' type.
+ *   forward          Y [rows, out]:  Y_i = W_e X_i,       zeros in rows beyond offsets[n_groups]
+ *   backward_data    dX [rows, in]:  dX_i = W_e^T dY_i,   zeros in rows beyond offsets[n_groups]
+ *   backward_weight  dW_e = sum of dY_i X_i^T over the expert's rows, zeros for an expert without rows
+ * Results must not overlap operands.  Limits: rows <= 2^30, in and out <= 2^24 (else BETTY_ERR_UNSUPPORTED). */
+betty_status betty_grouped_forward(const betty_grouped_cfg* cfg, int64_t rows, const int32_t* offsets, const void* X, int64_t ldx,
+                                   const void* W, int64_t ldw, int64_t group_stride, void* Y, int64_t ldy, int32_t y_dtype,
+                                   void* ws, size_t ws_bytes, void* stream);
+betty_status betty_grouped_backward_data(const betty_grouped_cfg* cfg, int64_t rows, const int32_t* offsets, const void* dY,
+                                         int64_t lddy, const void* W, int64_t ldw, int64_t group_stride, void* dX, int64_t lddx,
+                                         int32_t dx_dtype, void* ws, size_t ws_bytes, void* stream);
+betty_status betty_grouped_backward_weight(const betty_grouped_cfg* cfg, int64_t rows, const int32_t* offsets, const void* dY,
+                                           int64_t lddy, const void* X, int64_t ldx, void* dW, int64_t lddw, int64_t group_stride,
+                                           int32_t dw_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace of any of the three on up to `rows` rows.  any_layout != 0: room for aligned copies of the operands too,
+ * which the calls make of operands that do not start on 16-byte boundaries or whose leading dimensions (group strides)
+ * are not multiples of 8; without that room such operands return BETTY_ERR_WORKSPACE. */
+betty_status betty_grouped_workspace_size(const betty_grouped_cfg* cfg, int64_t rows, int32_t any_layout, size_t* bytes);
+
 /* The dataflow graph of Sec. 3.1: directed edges between problem indices.  An upper-to-lower edge
  * (from > to in the paper's ordering) says that theta_from constrains problem `to`; a lower-to-upper
  * edge says that theta*_from constrains problem `to`. */

@@ -76,6 +76,10 @@ class _BlockNormCfg(C.Structure):
                 ("gate", C.c_int32), ("bias", C.c_int32), ("rows_per_gate", C.c_int64), ("eps", C.c_float)]
 
 
+class _GroupedCfg(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("dtype", C.c_int32), ("n_in", C.c_int64), ("n_out", C.c_int64)]
+
+
 class _Act8Cfg(C.Structure):
     _fields_ = [("cols", C.c_int64), ("dtype", C.c_int32), ("act", C.c_int32), ("gated", C.c_int32)]
 
@@ -124,6 +128,10 @@ def lib():
     sig["betty_act8_store"] = [A8, I64] + 4 * mat + [VP]
     sig["betty_act8_restore"] = [A8, I64] + 3 * mat + [VP]
     sig["betty_act8_backward"] = [A8, I64] + 5 * mat + [VP]
+    GC = C.POINTER(_GroupedCfg)
+    sig["betty_grouped_workspace_size"] = [GC, I64, I32, C.POINTER(SZ)]
+    sig["betty_grouped_forward"] = sig["betty_grouped_backward_data"] = [GC, I64, VP] + 2 * mat + [I64] + mat + [I32, VP, SZ, VP]
+    sig["betty_grouped_backward_weight"] = [GC, I64, VP] + 3 * mat + [I64, I32, VP, SZ, VP]
     EP, IP = C.POINTER(_Edge), C.POINTER(I32)
     sig["betty_find_paths"] = [I32, EP, I32, EP, I32, I32, IP, I32, IP, I32, IP, IP]
     sig["betty_selftest_wait_timeout"] = [VP, SZ, VP]
@@ -590,6 +598,67 @@ def betty_act8_backward(cfg: Act8, q: torch.Tensor, scales: torch.Tensor, da: Op
                                      *_mat(scales, rows, cfg.n_scales, torch.float32, "scales"), *_mat(da, rows, cfg.cols, t, "da"),
                                      *_mat(dz, rows, cfg.width, t, "dz"), *_mat(act, rows, cfg.cols, t, "act"), _stream(stream)),
            "betty_act8_backward")
+
+
+class Grouped:
+    """Configuration of the betty_grouped calls (betty.h): `n_groups` experts with matrices [n_out, n_in], operands of
+    `dtype` (BETTY_BF16 or BETTY_F16)."""
+
+    def __init__(self, n_groups: int, n_in: int, n_out: int, dtype: int = BETTY_BF16):
+        self.n_groups, self.n_in, self.n_out = int(n_groups), int(n_in), int(n_out)
+        self.torch_dtype = {BETTY_BF16: torch.bfloat16, BETTY_F16: torch.float16}.get(int(dtype))
+        self._ref = C.byref(_GroupedCfg(self.n_groups, int(dtype), self.n_in, self.n_out))
+
+    def _offsets(self, t: torch.Tensor) -> int:
+        if t.dtype is not torch.int32 or not t.is_cuda or not t.is_contiguous() or t.numel() != self.n_groups + 1:
+            raise ValueError(f"offsets must be {self.n_groups + 1} contiguous int32 values on the GPU")
+        return t.data_ptr()
+
+    def _matrices(self, t: torch.Tensor, dtype: torch.dtype, name: str):
+        if t.dtype is not dtype or not t.is_cuda:
+            raise ValueError(f"{name} must be a {dtype} CUDA tensor, got {t.dtype} on {t.device}")
+        if t.dim() != 3 or t.shape[0] != self.n_groups or t.shape[1] != self.n_out or t.shape[2] != self.n_in:
+            raise ValueError(f"{name} must have the shape ({self.n_groups}, {self.n_out}, {self.n_in}), got {tuple(t.shape)}")
+        gs, ld, inner = t.stride()
+        if inner != 1 and self.n_in > 1:
+            raise ValueError(f"{name} must have consecutive values in a row, got strides {t.stride()}")
+        return t.data_ptr(), ld, gs
+
+
+def betty_grouped_workspace_size(cfg: Grouped, rows: int, any_layout: Optional[bool] = None) -> int:
+    """any_layout: room for aligned copies of the operands; default: where contiguous operands would need them."""
+    if any_layout is None:
+        any_layout = cfg.n_in % 8 != 0 or cfg.n_out % 8 != 0
+    out = C.c_size_t(0)
+    _check(lib().betty_grouped_workspace_size(cfg._ref, int(rows), int(any_layout), C.byref(out)), "betty_grouped_workspace_size")
+    return int(out.value)
+
+
+def betty_grouped_forward(cfg: Grouped, offsets: torch.Tensor, x: torch.Tensor, w: torch.Tensor, y: torch.Tensor, ws: Workspace,
+                          stream=None) -> None:
+    """y[i] = w[e] x[i] for the rows i of expert e."""
+    rows, t = x.shape[0], cfg.torch_dtype
+    _check(lib().betty_grouped_forward(cfg._ref, rows, cfg._offsets(offsets), *_mat(x, rows, cfg.n_in, t, "x"), *cfg._matrices(w, t, "w"),
+                                       *_mat(y, rows, cfg.n_out, y.dtype, "y"), _DT.get(y.dtype, -1), ws.ptr, ws.nbytes, _stream(stream)),
+           "betty_grouped_forward")
+
+
+def betty_grouped_backward_data(cfg: Grouped, offsets: torch.Tensor, dy: torch.Tensor, w: torch.Tensor, dx: torch.Tensor, ws: Workspace,
+                                stream=None) -> None:
+    """dx[i] = w[e]^T dy[i] for the rows i of expert e."""
+    rows, t = dy.shape[0], cfg.torch_dtype
+    _check(lib().betty_grouped_backward_data(cfg._ref, rows, cfg._offsets(offsets), *_mat(dy, rows, cfg.n_out, t, "dy"),
+                                             *cfg._matrices(w, t, "w"), *_mat(dx, rows, cfg.n_in, dx.dtype, "dx"), _DT.get(dx.dtype, -1),
+                                             ws.ptr, ws.nbytes, _stream(stream)), "betty_grouped_backward_data")
+
+
+def betty_grouped_backward_weight(cfg: Grouped, offsets: torch.Tensor, dy: torch.Tensor, x: torch.Tensor, dw: torch.Tensor, ws: Workspace,
+                                  stream=None) -> None:
+    """dw[e] = sum over the rows i of expert e of dy[i] x[i]^T."""
+    rows, t = dy.shape[0], cfg.torch_dtype
+    _check(lib().betty_grouped_backward_weight(cfg._ref, rows, cfg._offsets(offsets), *_mat(dy, rows, cfg.n_out, t, "dy"),
+                                               *_mat(x, rows, cfg.n_in, t, "x"), *cfg._matrices(dw, dw.dtype, "dw"), _DT.get(dw.dtype, -1),
+                                               ws.ptr, ws.nbytes, _stream(stream)), "betty_grouped_backward_weight")
 
 
 def betty_selftest_wait_timeout(ws: Workspace, stream=None) -> None:
