@@ -5,29 +5,46 @@ namespace betty {
 namespace blocknorm {
 
 // Bound by memory: per value of a 16-bit row 3 reads and 2 writes, ~20 operations.  Thread groups walk the rows with the
-// parameters in registers and the next row's values already requested while the present row is summed.
-template <typename TX, typename TY, bool ALIGNED, int CH, bool GENERAL>
-__global__ void __launch_bounds__(MAX_G) k_forward(const Args a) {
-  __shared__ float red[2 * RED_VALUES * 32];
+// parameters in registers and the next rows' values already on their way.
+template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
+__global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
+  __shared__ float red[2 * RED_VALUES * 16];
+  extern __shared__ __align__(16) char slots[];
   pdl_enter();
-  const int G = a.G, d = a.d, t = threadIdx.x & (G - 1);
-  const int64_t step = (int64_t)gridDim.x * (blockDim.x / G);
-  int64_t row = (int64_t)blockIdx.x * (blockDim.x / G) + threadIdx.x / G;
+  const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G, subs = blockDim.x / G;
+  const int64_t step = (int64_t)gridDim.x * subs;
+  int64_t row = (int64_t)blockIdx.x * subs + sub;
   const bool has_y = a.y != nullptr, has_g = a.gate != BETTY_GATE_NONE && has_y, has_u = a.u != nullptr;
-  int half = 0;
+  const int bytes_x = CH * 8 * G * (int)sizeof(TX), bytes_y = CH * 8 * G * (int)sizeof(TY);
+  char* ring = slots + (size_t)sub * (a.ahead + 1) * a.slot_bytes;
+  auto gate_row = [&](int64_t r) { return (const TY*)a.g + (int64_t)((unsigned)r / a.per_gate) * a.ldg; };
+  auto fetch = [&](int64_t r, int slot) {
+    if constexpr (PIPE) {
+      if (r < a.rows) {
+        char* p = ring + slot * a.slot_bytes;
+        copy_row<GR, CH>(p, (const TX*)a.x + r * a.ldx, t, G, d);
+        if (has_y) copy_row<GR, CH>(p + bytes_x, (const TY*)a.y + r * a.ldy, t, G, d);
+        if (has_g) copy_row<GR, CH>(p + bytes_x + bytes_y, gate_row(r), t, G, d);
+      }
+      copies_commit();
+    }
+  };
+  int half = 0, slot = 0;
+  if (PIPE)
+    for (int i = 0; i < a.ahead; ++i) fetch(row + i * step, i);
   float wp[CH][8], ws[CH][8], bp[GENERAL ? CH : 1][8], bs[GENERAL ? CH : 1][8];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     float s[8];
-    load_param8<ALIGNED>(wp[c], a.params, c, t, G, d);
-    load_param8<ALIGNED>(ws[c], a.params + d, c, t, G, d);
-    load_param8<ALIGNED>(s, a.params + 2 * (int64_t)d, c, t, G, d);
+    load_param8<GR>(wp[c], a.params, c, t, G, d);
+    load_param8<GR>(ws[c], a.params + d, c, t, G, d);
+    load_param8<GR>(s, a.params + 2 * (int64_t)d, c, t, G, d);
     if (GENERAL) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) { bp[c][k] = 0.f; bs[c][k] = 0.f; }
       if (a.bias) {
-        load_param8<ALIGNED>(bp[c], a.params + 3 * (int64_t)d, c, t, G, d);
-        load_param8<ALIGNED>(bs[c], a.params + 4 * (int64_t)d, c, t, G, d);
+        load_param8<GR>(bp[c], a.params + 3 * (int64_t)d, c, t, G, d);
+        load_param8<GR>(bs[c], a.params + 4 * (int64_t)d, c, t, G, d);
       }
     }
 #pragma unroll
@@ -36,33 +53,27 @@ __global__ void __launch_bounds__(MAX_G) k_forward(const Args a) {
       if (GENERAL) bs[c][k] *= s[k];
     }
   }
-  Raw8<TX> xr[CH];
-  Raw8<TY> yr[CH], gr[CH];
-  auto request = [&](int64_t r) {
-    const TX* x = (const TX*)a.x + r * a.ldx;
-    const TY* y = (const TY*)a.y + r * a.ldy;
-    const TY* g = has_g ? (const TY*)a.g + (int64_t)((unsigned)r / a.per_gate) * a.ldg : nullptr;
+  for (; row < a.rows; row += step) {
+    const char* p = nullptr;
+    if (PIPE) {
+      fetch(row + a.ahead * step, slot == 0 ? a.ahead : slot - 1);
+      copies_wait(a.ahead);
+      p = ring + slot * a.slot_bytes;
+      slot = slot == a.ahead ? 0 : slot + 1;
+    }
+    float x[CH][8], y[CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      load8<ALIGNED>(xr[c], x, c, t, G, d);
-      if (has_y) load8<ALIGNED>(yr[c], y, c, t, G, d);
-      if (has_g) load8<ALIGNED>(gr[c], g, c, t, G, d);
-    }
-  };
-  if (row < a.rows) request(row);
-  for (; row < a.rows; row += step) {
-    float x[CH][8], y[CH][8], ag[CH][8];
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        x[c][k] = to_f(xr[c].v[k]);
-        y[c][k] = has_y ? to_f(yr[c].v[k]) : 0.f;
-        ag[c][k] = has_g ? to_f(gr[c].v[k]) : 1.f;
+      if constexpr (PIPE) {
+        read_slot<GR, TX>(x[c], p, c, t, G, d);
+        if (has_y) read_slot<GR, TY>(y[c], p + bytes_x, c, t, G, d);
+      } else {
+        load8<GR>(x[c], (const TX*)a.x + row * a.ldx, c, t, G, d);
+        if (has_y) load8<GR>(y[c], (const TY*)a.y + row * a.ldy, c, t, G, d);
       }
-    if (row + step < a.rows) request(row + step);
+    }
     if (has_y) {
-      float mean = 0.f, r = 1.f;
+      float r = 1.f;
       if (GENERAL && a.post == BETTY_NORM_LAYER) {
         float v[1] = {0.f};
 #pragma unroll
@@ -70,11 +81,11 @@ __global__ void __launch_bounds__(MAX_G) k_forward(const Args a) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[0] += y[c][k];
         row_sums<1>(v, red, half, G, t);
-        mean = v[0] * a.inv_d;
+        const float mean = v[0] * a.inv_d;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[c][k] = column<ALIGNED>(c, k, t, G) < d ? y[c][k] - mean : 0.f;
+          for (int k = 0; k < 8; ++k) y[c][k] = column<GR>(c, k, t, G) < d ? y[c][k] - mean : 0.f;
       }
       if (a.post != BETTY_NORM_NONE) {
         float v[1] = {0.f};
@@ -85,20 +96,23 @@ __global__ void __launch_bounds__(MAX_G) k_forward(const Args a) {
         row_sums<1>(v, red, half, G, t);
         r = rsqrtf(fmaf(v[0], a.inv_d, a.eps));
       }
-      if (a.gate == BETTY_GATE_SIGMOID)
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) ag[c][k] = sigmoid_f(ag[c][k]);
       TX* xo = (TX*)a.x_out + row * a.ldxo;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
+        float g[8];
+        if (has_g) {
+          if constexpr (PIPE) read_slot<GR, TY>(g, p + bytes_x + bytes_y, c, t, G, d);
+          else load8<GR>(g, gate_row(row), c, t, G, d);
+          if (a.gate == BETTY_GATE_SIGMOID)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) g[k] = sigmoid_f(g[k]);
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float z = GENERAL ? fmaf(y[c][k] * r, ws[c][k], bs[c][k]) : y[c][k] * r * ws[c][k];
-          x[c][k] = fmaf(ag[c][k], z, x[c][k]);
+          x[c][k] = has_g ? fmaf(g[k], z, x[c][k]) : x[c][k] + z;
         }
-        store8<ALIGNED>(xo, x[c], c, t, G, d);
+        store8<GR>(xo, x[c], c, t, G, d);
       }
     }
     if (has_u) {          // the entry norm reads x' before its rounding
@@ -108,13 +122,13 @@ __global__ void __launch_bounds__(MAX_G) k_forward(const Args a) {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[0] += x[c][k];
+          for (int k = 0; k < 8; ++k) v[0] += column<GR>(c, k, t, G) < d ? x[c][k] : 0.f;
         row_sums<1>(v, red, half, G, t);
         const float mean = v[0] * a.inv_d;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) x[c][k] = column<ALIGNED>(c, k, t, G) < d ? x[c][k] - mean : 0.f;
+          for (int k = 0; k < 8; ++k) x[c][k] = column<GR>(c, k, t, G) < d ? x[c][k] - mean : 0.f;
       }
       if (a.pre != BETTY_NORM_NONE) {
         float v[1] = {0.f};
@@ -131,51 +145,87 @@ __global__ void __launch_bounds__(MAX_G) k_forward(const Args a) {
         float o[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) o[k] = GENERAL ? fmaf(x[c][k] * r, wp[c][k], bp[c][k]) : x[c][k] * r * wp[c][k];
-        store8<ALIGNED>(u, o, c, t, G, d);
+        store8<GR>(u, o, c, t, G, d);
       }
     }
   }
 }
 
-template <typename TX, typename TY, bool ALIGNED, int CH, bool GENERAL>
-static betty_status launch_forward(cudaStream_t stream, const Args& a) {
-  const int threads = a.G == 32 ? SMALL_THREADS : a.G, per_block = threads / a.G;
-  static std::atomic<int> resident[16];         // blocks per SM, by the logarithm of the block size
-  int lg = 0;
-  while ((1 << lg) < threads) ++lg;
-  int occ = resident[lg].load(std::memory_order_relaxed);
-  if (!occ) {
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_forward<TX, TY, ALIGNED, CH, GENERAL>, threads, 0) != cudaSuccess || occ < 1) {
-      (void)cudaGetLastError();
-      return BETTY_ERR_CUDA;
-    }
-    resident[lg].store(occ, std::memory_order_relaxed);
-  }
-  const int64_t want = (a.rows + per_block - 1) / per_block, most = (int64_t)occ * current_sm_count();
-  launch_pdl(k_forward<TX, TY, ALIGNED, CH, GENERAL>, dim3((unsigned)(want < most ? want : most)), dim3(threads), 0, stream, a);
+template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
+static betty_status launch_forward(cudaStream_t stream, const Args& a, const Layout& l) {
+  static SmemLimit limit = {};
+  if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_forward<TX, TY, GR, PIPE, CH, GENERAL>, limit, l.smem));
+  const int per_block = l.threads / l.G;
+  const int64_t want = (a.rows + per_block - 1) / per_block, most = (int64_t)l.blocks_per_sm * current_sm_count();
+  launch_pdl(k_forward<TX, TY, GR, PIPE, CH, GENERAL>, dim3((unsigned)(want < most ? want : most)), dim3(l.threads), l.smem, stream, a);
   BETTY_LAUNCH_CHECK();
   return BETTY_OK;
 }
-template <typename TX, typename TY, bool ALIGNED, bool GENERAL>
-static betty_status forward_chunks(cudaStream_t stream, const Args& a) {
-  switch (chunks_of(a.d, a.G)) {
-    case 1: return launch_forward<TX, TY, ALIGNED, 1, GENERAL>(stream, a);
-    case 2: return launch_forward<TX, TY, ALIGNED, 2, GENERAL>(stream, a);
-    default: return launch_forward<TX, TY, ALIGNED, 4, GENERAL>(stream, a);
+template <typename TX, typename TY, bool GENERAL>
+static betty_status forward_layout(cudaStream_t stream, const Args& a, const Layout& l) {
+  if (l.granule == 8) {
+    if (!l.ahead) return launch_forward<TX, TY, 8, false, 4, GENERAL>(stream, a, l);
+    return l.chunks == 1 ? launch_forward<TX, TY, 8, true, 1, GENERAL>(stream, a, l) : launch_forward<TX, TY, 8, true, 2, GENERAL>(stream, a, l);
   }
+  if constexpr (sizeof(TY) == 4) {
+    if (l.ahead) return launch_forward<TX, TY, 1, true, 1, GENERAL>(stream, a, l);
+  } else {
+    if (l.ahead) return launch_forward<TX, TY, 2, true, 1, GENERAL>(stream, a, l);
+    if (l.chunks == 1) return launch_forward<TX, TY, 1, false, 1, GENERAL>(stream, a, l);
+  }
+  return launch_forward<TX, TY, 1, false, 4, GENERAL>(stream, a, l);
 }
 template <typename TX, typename TY>
-static betty_status forward_typed(cudaStream_t stream, const Args& a, bool aligned) {
+static betty_status forward_typed(cudaStream_t stream, const Args& a, const Layout& l) {
   const bool general = a.bias || a.pre == BETTY_NORM_LAYER || a.post == BETTY_NORM_LAYER;
-  if (aligned) return general ? forward_chunks<TX, TY, true, true>(stream, a) : forward_chunks<TX, TY, true, false>(stream, a);
-  return general ? forward_chunks<TX, TY, false, true>(stream, a) : forward_chunks<TX, TY, false, false>(stream, a);
+  return general ? forward_layout<TX, TY, true>(stream, a, l) : forward_layout<TX, TY, false>(stream, a, l);
 }
-betty_status forward(cudaStream_t stream, const Args& a, int xd, int yd, bool aligned) {
-  if (xd == BETTY_F32 && yd == BETTY_F32) return forward_typed<float, float>(stream, a, aligned);
-  if (xd == BETTY_F32 && yd == BETTY_BF16) return forward_typed<float, __nv_bfloat16>(stream, a, aligned);
-  if (xd == BETTY_F32 && yd == BETTY_F16) return forward_typed<float, __half>(stream, a, aligned);
-  if (xd == BETTY_BF16 && yd == BETTY_BF16) return forward_typed<__nv_bfloat16, __nv_bfloat16>(stream, a, aligned);
-  return forward_typed<__half, __half>(stream, a, aligned);
+betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int granule) {
+  const int ys = (a.y ? 1 : 0) + (a.y && a.gate != BETTY_GATE_NONE ? 1 : 0);
+  const Layout l = layout_of(a.d, xd, yd, granule, 1, ys, 512, 1);
+  a.G = l.G; a.ahead = l.ahead; a.slot_bytes = l.slot_bytes;
+  if (xd == BETTY_F32 && yd == BETTY_F32) return forward_typed<float, float>(stream, a, l);
+  if (xd == BETTY_F32 && yd == BETTY_BF16) return forward_typed<float, __nv_bfloat16>(stream, a, l);
+  if (xd == BETTY_F32 && yd == BETTY_F16) return forward_typed<float, __half>(stream, a, l);
+  if (xd == BETTY_BF16 && yd == BETTY_BF16) return forward_typed<__nv_bfloat16, __nv_bfloat16>(stream, a, l);
+  return forward_typed<__half, __half>(stream, a, l);
+}
+
+// Aligned rows: `chunks` chunks per thread where MAX_G threads then cover the row.  Rows that cannot be fetched ahead (16-bit
+// values on odd addresses; rows so wide that two do not fit the shared memory) are read where they are used, the widest
+// with four chunks per thread.
+Layout layout_of(int64_t d, int xd, int yd, int granule, int streams_x, int streams_y, int threads_per_sm, int chunks) {
+  Layout l = {};
+  const int bx = xd == BETTY_F32 ? 4 : 2, by = yd == BETTY_F32 ? 4 : 2;
+  bool pipe = granule == 8 || by == 4 || granule == 2;
+  l.granule = granule == 2 && by == 4 ? 1 : granule;
+  l.chunks = granule == 8 ? chunks : 1;
+  for (;;) {
+    l.G = 32;
+    while (l.G < MAX_G && (int64_t)l.G * 8 * l.chunks < d) l.G *= 2;
+    if ((int64_t)l.G * 8 * l.chunks < d) {
+      l.chunks = l.chunks == 1 && granule == 8 ? 2 : MAX_CH;
+      if (l.chunks == MAX_CH) pipe = false;
+      continue;
+    }
+    l.threads = l.G == 32 ? SMALL_THREADS : l.G;
+    l.blocks_per_sm = threads_per_sm / l.threads > 0 ? threads_per_sm / l.threads : 1;
+    l.slot_bytes = l.chunks * 8 * l.G * (streams_x * bx + streams_y * by);
+    l.ahead = 0; l.smem = 0;
+    if (!pipe) {
+      if (granule == 2) l.granule = 1;
+      return l;
+    }
+    const int64_t budget = (int64_t)(220 * 1024) / l.blocks_per_sm - 2048, slot = (int64_t)l.slot_bytes * (l.threads / l.G);
+    l.ahead = (int)(budget / slot) - 1;
+    if (l.ahead > MAX_AHEAD) l.ahead = MAX_AHEAD;
+    if (l.ahead >= 1) {
+      l.smem = (size_t)(l.ahead + 1) * slot;
+      return l;
+    }
+    pipe = false;                      // two rows do not fit
+    l.chunks = MAX_CH;
+  }
 }
 
 // ------------------------------------------------------------------ arguments
@@ -193,17 +243,20 @@ static betty_status check_cfg(const betty_block_norm_cfg* c, int64_t rows) {
   if (c->d > MAX_D || rows > INT32_MAX || c->rows_per_gate > INT32_MAX) return BETTY_ERR_UNSUPPORTED;
   return BETTY_OK;
 }
-// a [rows, d] matrix: its stride covers a row and its address a value; `aligned` is cleared when 16-byte accesses do not fit
-static betty_status check_matrix(const void* p, int64_t ld, int64_t rows, int64_t d, int dtype, bool& aligned) {
+// a [rows, d] matrix: its stride covers a row and its address a value; `granule` (see block_norm.cuh) shrinks to what its
+// rows' addresses allow
+static betty_status check_matrix(const void* p, int64_t ld, int64_t rows, int64_t d, int dtype, int& granule) {
   if (!p) return BETTY_OK;
   if (rows > 1 && ld < d) return BETTY_ERR_SHAPE;
-  const int64_t b = size_of(dtype);
+  const int64_t b = size_of(dtype), bytes = rows > 1 ? ld * b : 0;
   if ((uintptr_t)p % b) return BETTY_ERR_ALIGNMENT;
-  if (!aligned16(p) || (rows > 1 && (ld * b) % 16)) aligned = false;
+  if (granule == 8 && ((uintptr_t)p % 16 || bytes % 16)) granule = 2;
+  if (granule == 2 && ((uintptr_t)p % 4 || bytes % 4)) granule = 1;
   return BETTY_OK;
 }
+static inline int widest_granule(int64_t d) { return d % 8 == 0 ? 8 : (d % 2 == 0 ? 2 : 1); }
 static void common_args(Args& a, const betty_block_norm_cfg* c, int64_t rows, const float* params) {
-  a.rows = rows; a.d = (int)c->d; a.G = threads_per_row(c->d);
+  a.rows = rows; a.d = (int)c->d;
   a.pre = c->pre; a.post = c->post; a.gate = c->gate; a.bias = c->bias != 0;
   a.per_gate = (unsigned)c->rows_per_gate;
   a.eps = c->eps; a.inv_d = 1.f / (float)c->d; a.params = params;
@@ -224,25 +277,33 @@ extern "C" betty_status betty_block_norm(const betty_block_norm_cfg* cfg, const 
   if (!params || !x || (!y && !u) || (y && !x_out) || (y && cfg->gate != BETTY_GATE_NONE && !gate)) return BETTY_ERR_INVALID_ARG;
   if (!aligned16(params)) return BETTY_ERR_ALIGNMENT;
   const int64_t d = cfg->d;
-  bool aligned = d % 8 == 0;
-  BETTY_TRY(check_matrix(x, ldx, rows, d, cfg->x_dtype, aligned));
-  BETTY_TRY(check_matrix(y, ldy, rows, d, cfg->y_dtype, aligned));
-  if (y) BETTY_TRY(check_matrix(x_out, ldxo, rows, d, cfg->x_dtype, aligned));
+  int granule = widest_granule(d);
+  BETTY_TRY(check_matrix(x, ldx, rows, d, cfg->x_dtype, granule));
+  BETTY_TRY(check_matrix(y, ldy, rows, d, cfg->y_dtype, granule));
+  if (y) BETTY_TRY(check_matrix(x_out, ldxo, rows, d, cfg->x_dtype, granule));
   if (y && cfg->gate != BETTY_GATE_NONE)
-    BETTY_TRY(check_matrix(gate, ldg, (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate, d, cfg->y_dtype, aligned));
-  BETTY_TRY(check_matrix(u, ldu, rows, d, cfg->y_dtype, aligned));
+    BETTY_TRY(check_matrix(gate, ldg, (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate, d, cfg->y_dtype, granule));
+  BETTY_TRY(check_matrix(u, ldu, rows, d, cfg->y_dtype, granule));
   Args a = {};
   common_args(a, cfg, rows, params);
   a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy; a.g = gate; a.ldg = ldg;
   a.x_out = x_out; a.ldxo = ldxo; a.u = u; a.ldu = ldu;
-  return forward((cudaStream_t)stream, a, cfg->x_dtype, cfg->y_dtype, aligned);
+  return forward((cudaStream_t)stream, a, cfg->x_dtype, cfg->y_dtype, granule);
 }
 
 extern "C" betty_status betty_block_norm_workspace_size(const betty_block_norm_cfg* cfg, int64_t rows, size_t* bytes) {
   if (!bytes) return BETTY_ERR_INVALID_ARG;
   BETTY_TRY(check_cfg(cfg, rows));
-  const int G = threads_per_row(cfg->d);
-  const int64_t blocks = backward_blocks(rows, G), walkers = blocks * (G == 32 ? SMALL_THREADS / 32 : 1);
+  int64_t blocks = 0, walkers = 0;
+  // whatever the matrices' types and addresses will be
+  for (int granule : {8, 2, 1})
+    for (int xd : {BETTY_F32, BETTY_BF16})
+      for (int yd : {BETTY_F32, BETTY_BF16}) {
+        const Layout l = backward_layout(cfg->d, xd, yd, granule);
+        const int64_t n = backward_blocks(rows, l), w = n * (l.threads / l.G);
+        if (n > blocks) blocks = n;
+        if (w > walkers) walkers = w;
+      }
   const int64_t gates = (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate;
   int64_t floats = blocks * quantities(cfg) * cfg->d;
   if (cfg->gate != BETTY_GATE_NONE && cfg->rows_per_gate > 1) floats += (walkers + gates) * cfg->d;
@@ -262,19 +323,19 @@ extern "C" betty_status betty_block_norm_backward(const betty_block_norm_cfg* cf
   const int64_t d = cfg->d;
   const bool gated = y && cfg->gate != BETTY_GATE_NONE;
   Args a = {};
-  bool aligned = d % 8 == 0;
+  int granule = widest_granule(d);
   if (rows > 0) {
     if ((!x_out && du) || (!du && !dx_out) || (!y && !du) || !dx || (y && !dy) || (gated && (!gate || !dgate))) return BETTY_ERR_INVALID_ARG;
     const int64_t gates = (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate;
-    BETTY_TRY(check_matrix(x_out, ldxo, rows, d, cfg->x_dtype, aligned));
-    BETTY_TRY(check_matrix(y, ldy, rows, d, cfg->y_dtype, aligned));
-    BETTY_TRY(check_matrix(du, lddu, rows, d, cfg->y_dtype, aligned));
-    BETTY_TRY(check_matrix(dx_out, lddxo, rows, d, cfg->x_dtype, aligned));
-    BETTY_TRY(check_matrix(dx, lddx, rows, d, cfg->x_dtype, aligned));
-    if (y) BETTY_TRY(check_matrix(dy, lddy, rows, d, cfg->y_dtype, aligned));
+    BETTY_TRY(check_matrix(x_out, ldxo, rows, d, cfg->x_dtype, granule));
+    BETTY_TRY(check_matrix(y, ldy, rows, d, cfg->y_dtype, granule));
+    BETTY_TRY(check_matrix(du, lddu, rows, d, cfg->y_dtype, granule));
+    BETTY_TRY(check_matrix(dx_out, lddxo, rows, d, cfg->x_dtype, granule));
+    BETTY_TRY(check_matrix(dx, lddx, rows, d, cfg->x_dtype, granule));
+    if (y) BETTY_TRY(check_matrix(dy, lddy, rows, d, cfg->y_dtype, granule));
     if (gated) {
-      BETTY_TRY(check_matrix(gate, ldg, gates, d, cfg->y_dtype, aligned));
-      BETTY_TRY(check_matrix(dgate, lddg, gates, d, cfg->y_dtype, aligned));
+      BETTY_TRY(check_matrix(gate, ldg, gates, d, cfg->y_dtype, granule));
+      BETTY_TRY(check_matrix(dgate, lddg, gates, d, cfg->y_dtype, granule));
     }
   }
   common_args(a, cfg, rows, params);
@@ -282,11 +343,12 @@ extern "C" betty_status betty_block_norm_backward(const betty_block_norm_cfg* cf
   a.x = x_out; a.ldx = ldxo; a.y = y; a.ldy = ldy; a.g = gate; a.ldg = ldg; a.du = du; a.lddu = lddu; a.dxo = dx_out; a.lddxo = lddxo;
   a.dx = dx; a.lddx = lddx; a.dy = dy; a.lddy = lddy; a.dg = dgate; a.lddg = lddg;
   Arena arena(ws, ws_bytes);
-  const int blocks = backward_blocks(rows, a.G);
-  a.walkers = blocks * (a.G == 32 ? SMALL_THREADS / 32 : 1);
+  const Layout l = backward_layout(d, cfg->x_dtype, cfg->y_dtype, granule);
+  const int blocks = backward_blocks(rows, l);
+  a.walkers = blocks * (l.threads / l.G);
   a.col_partials = arena.alloc<float>((size_t)blocks * quantities(cfg) * d);
   if (gated && cfg->rows_per_gate > 1)
     a.gate_partials = arena.alloc<float>((size_t)(a.walkers + (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate) * d);
   if (arena.overflow) return BETTY_ERR_WORKSPACE;
-  return backward((cudaStream_t)stream, a, cfg->x_dtype, cfg->y_dtype, aligned, dparams);
+  return backward((cudaStream_t)stream, a, l, cfg->x_dtype, cfg->y_dtype, dparams);
 }
