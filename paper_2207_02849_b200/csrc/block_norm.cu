@@ -5,23 +5,27 @@ namespace betty {
 namespace blocknorm {
 
 // Bound by memory: per value of a 16-bit row 3 reads and 2 writes, ~20 operations.  Thread groups walk the rows with the
-// parameters in registers and the next rows' values already on their way.
-template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
+// parameters in registers and the next rows' values already on their way, R rows at a time: a row's own chain (values, sum,
+// barrier, values, sum, barrier) is several times longer than the memory needs for it, and the rows of a batch share it.
+template <typename TX, typename TY, int GR, bool PIPE, int CH, int R, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
   __shared__ float red[2 * RED_VALUES * 16];
   extern __shared__ __align__(16) char slots[];
   pdl_enter();
   const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G, subs = blockDim.x / G;
-  const int64_t step = (int64_t)gridDim.x * subs;
-  int64_t row = (int64_t)blockIdx.x * subs + sub;
+  const int64_t step = (int64_t)gridDim.x * subs * R;
+  int64_t row = ((int64_t)blockIdx.x * subs + sub) * R;
   const bool has_y = a.y != nullptr, has_g = a.gate != BETTY_GATE_NONE && has_y, has_u = a.u != nullptr;
   const int bytes_x = CH * 8 * G * (int)sizeof(TX), bytes_y = CH * 8 * G * (int)sizeof(TY);
-  char* ring = slots + (size_t)sub * (a.ahead + 1) * a.slot_bytes;
-  auto gate_row = [&](int64_t r) { return (const TY*)a.g + (int64_t)((unsigned)r / a.per_gate) * a.ldg; };
-  auto fetch = [&](int64_t r, int slot) {
+  char* ring = slots + (size_t)sub * (a.ahead + 1) * R * a.slot_bytes;
+  auto gate_row = [&](int64_t r) { return (const TY*)a.g + (a.per_gate == 1 ? r : (int64_t)((unsigned)r / a.per_gate)) * a.ldg; };
+  auto fetch = [&](int64_t first, int slot) {
     if constexpr (PIPE) {
-      if (r < a.rows) {
-        char* p = ring + slot * a.slot_bytes;
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int64_t r = first + i;
+        if (r >= a.rows) break;
+        char* p = ring + (slot * R + i) * a.slot_bytes;
         copy_row<GR, CH>(p, (const TX*)a.x + r * a.ldx, t, G, d);
         if (has_y) copy_row<GR, CH>(p + bytes_x, (const TY*)a.y + r * a.ldy, t, G, d);
         if (has_g) copy_row<GR, CH>(p + bytes_x + bytes_y, gate_row(r), t, G, d);
@@ -30,8 +34,15 @@ __global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
     }
   };
   int half = 0, slot = 0;
-  if (PIPE)
+  if constexpr (PIPE) {
+    for (int i = 0; i < (a.ahead + 1) * R && CH * 8 * G > d; ++i) {
+      char* p = ring + i * a.slot_bytes;
+      clear_beyond<GR, CH, TX>(p, t, G, d);
+      if (has_y) clear_beyond<GR, CH, TY>(p + bytes_x, t, G, d);
+      if (has_g) clear_beyond<GR, CH, TY>(p + bytes_x + bytes_y, t, G, d);
+    }
     for (int i = 0; i < a.ahead; ++i) fetch(row + i * step, i);
+  }
   float wp[CH][8], ws[CH][8], bp[GENERAL ? CH : 1][8], bs[GENERAL ? CH : 1][8];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -53,127 +64,134 @@ __global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
       if (GENERAL) bs[c][k] *= s[k];
     }
   }
+  float mask[GENERAL ? CH : 1][8 / GR];      // 1 for columns of the row, 0 beyond it
+  if (GENERAL)
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int k = 0; k < 8; k += GR) mask[c][k / GR] = column<GR>(c, k, t, G) < d ? 1.f : 0.f;
+  // 1 / rms of each row (after its mean is taken off), or 1
+  auto normalise = [&](float (&v)[R][CH][8], int kind, float (&r)[R]) {
+    if (GENERAL && kind == BETTY_NORM_LAYER) {
+      float s[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        s[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[i] += v[i][c][k];
+      }
+      row_sums<R>(s, red, half, G, t);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const float mean = s[i] * a.inv_d;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[i][c][k] = fmaf(-mean, mask[c][k / GR], v[i][c][k]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) r[i] = 1.f;
+    if (kind != BETTY_NORM_NONE) {
+      float s[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        s[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s[i] = fmaf(v[i][c][k], v[i][c][k], s[i]);
+      }
+      row_sums<R>(s, red, half, G, t);
+#pragma unroll
+      for (int i = 0; i < R; ++i) r[i] = rsqrtf(fmaf(s[i], a.inv_d, a.eps));
+    }
+  };
   for (; row < a.rows; row += step) {
     const char* p = nullptr;
     if (PIPE) {
       fetch(row + a.ahead * step, slot == 0 ? a.ahead : slot - 1);
       copies_wait(a.ahead);
-      p = ring + slot * a.slot_bytes;
+      p = ring + slot * R * a.slot_bytes;
       slot = slot == a.ahead ? 0 : slot + 1;
     }
-    float x[CH][8], y[CH][8];
+    float x[R][CH][8], y[R][CH][8], r[R];
+    // rows past the last one hold whatever their slots hold; they take part in the sums and are not stored
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if constexpr (PIPE) {
-        read_slot<GR, TX>(x[c], p, c, t, G, d);
-        if (has_y) read_slot<GR, TY>(y[c], p + bytes_x, c, t, G, d);
-      } else {
-        load8<GR>(x[c], (const TX*)a.x + row * a.ldx, c, t, G, d);
-        if (has_y) load8<GR>(y[c], (const TY*)a.y + row * a.ldy, c, t, G, d);
-      }
-    }
-    if (has_y) {
-      float r = 1.f;
-      if (GENERAL && a.post == BETTY_NORM_LAYER) {
-        float v[1] = {0.f};
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[0] += y[c][k];
-        row_sums<1>(v, red, half, G, t);
-        const float mean = v[0] * a.inv_d;
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[c][k] = column<GR>(c, k, t, G) < d ? y[c][k] - mean : 0.f;
-      }
-      if (a.post != BETTY_NORM_NONE) {
-        float v[1] = {0.f};
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[0] = fmaf(y[c][k], y[c][k], v[0]);
-        row_sums<1>(v, red, half, G, t);
-        r = rsqrtf(fmaf(v[0], a.inv_d, a.eps));
-      }
-      TX* xo = (TX*)a.x_out + row * a.ldxo;
+    for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        float g[8];
-        if (has_g) {
-          if constexpr (PIPE) read_slot<GR, TY>(g, p + bytes_x + bytes_y, c, t, G, d);
-          else load8<GR>(g, gate_row(row), c, t, G, d);
-          if (a.gate == BETTY_GATE_SIGMOID)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) g[k] = sigmoid_f(g[k]);
+        if constexpr (PIPE) {
+          read_slot<GR, TX>(x[i][c], p + i * a.slot_bytes, c, t, G);
+          if (has_y) read_slot<GR, TY>(y[i][c], p + i * a.slot_bytes + bytes_x, c, t, G);
+        } else {
+          load8<GR>(x[i][c], (const TX*)a.x + row * a.ldx, c, t, G, d);
+          if (has_y) load8<GR>(y[i][c], (const TY*)a.y + row * a.ldy, c, t, G, d);
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float z = GENERAL ? fmaf(y[c][k] * r, ws[c][k], bs[c][k]) : y[c][k] * r * ws[c][k];
-          x[c][k] = has_g ? fmaf(g[k], z, x[c][k]) : x[c][k] + z;
-        }
-        store8<GR>(xo, x[c], c, t, G, d);
       }
+    if (has_y) {
+      normalise(y, a.post, r);
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          float g[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) g[k] = 1.f;
+          if (has_g) {
+            if constexpr (PIPE) read_slot<GR, TY>(g, p + i * a.slot_bytes + bytes_x + bytes_y, c, t, G);
+            else load8<GR>(g, gate_row(row), c, t, G, d);
+            if (a.gate == BETTY_GATE_SIGMOID)
+#pragma unroll
+              for (int k = 0; k < 8; ++k) g[k] = sigmoid_f(g[k]);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float z = GENERAL ? fmaf(y[i][c][k] * r[i], ws[c][k], bs[c][k]) : y[i][c][k] * r[i] * ws[c][k];
+            x[i][c][k] = fmaf(g[k], z, x[i][c][k]);
+          }
+          if (R == 1 || row + i < a.rows) store8<GR>((TX*)a.x_out + (row + i) * a.ldxo, x[i][c], c, t, G, d);
+        }
     }
     if (has_u) {          // the entry norm reads x' before its rounding
-      float r = 1.f;
-      if (GENERAL && a.pre == BETTY_NORM_LAYER) {
-        float v[1] = {0.f};
+      normalise(x, a.pre, r);
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+      for (int i = 0; i < R; ++i)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[0] += column<GR>(c, k, t, G) < d ? x[c][k] : 0.f;
-        row_sums<1>(v, red, half, G, t);
-        const float mean = v[0] * a.inv_d;
+        for (int c = 0; c < CH; ++c) {
+          float o[8];
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) x[c][k] = column<GR>(c, k, t, G) < d ? x[c][k] - mean : 0.f;
-      }
-      if (a.pre != BETTY_NORM_NONE) {
-        float v[1] = {0.f};
-#pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[0] = fmaf(x[c][k], x[c][k], v[0]);
-        row_sums<1>(v, red, half, G, t);
-        r = rsqrtf(fmaf(v[0], a.inv_d, a.eps));
-      }
-      TY* u = (TY*)a.u + row * a.ldu;
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        float o[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = GENERAL ? fmaf(x[c][k] * r, wp[c][k], bp[c][k]) : x[c][k] * r * wp[c][k];
-        store8<GR>(u, o, c, t, G, d);
-      }
+          for (int k = 0; k < 8; ++k) o[k] = GENERAL ? fmaf(x[i][c][k] * r[i], wp[c][k], bp[c][k]) : x[i][c][k] * r[i] * wp[c][k];
+          if (R == 1 || row + i < a.rows) store8<GR>((TY*)a.u + (row + i) * a.ldu, o, c, t, G, d);
+        }
     }
   }
 }
 
-template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
+template <typename TX, typename TY, int GR, bool PIPE, int CH, int R, bool GENERAL>
 static betty_status launch_forward(cudaStream_t stream, const Args& a, const Layout& l) {
   static SmemLimit limit = {};
-  if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_forward<TX, TY, GR, PIPE, CH, GENERAL>, limit, l.smem));
-  const int per_block = l.threads / l.G;
+  if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_forward<TX, TY, GR, PIPE, CH, R, GENERAL>, limit, l.smem));
+  const int per_block = l.threads / l.G * R;
   const int64_t want = (a.rows + per_block - 1) / per_block, most = (int64_t)l.blocks_per_sm * current_sm_count();
-  launch_pdl(k_forward<TX, TY, GR, PIPE, CH, GENERAL>, dim3((unsigned)(want < most ? want : most)), dim3(l.threads), l.smem, stream, a);
+  launch_pdl(k_forward<TX, TY, GR, PIPE, CH, R, GENERAL>, dim3((unsigned)(want < most ? want : most)), dim3(l.threads), l.smem, stream, a);
   BETTY_LAUNCH_CHECK();
   return BETTY_OK;
 }
+// the wide kernel's chunks per thread and rows at a time: what 128 registers hold
+static constexpr int FWD_CHUNKS = 2;
+static constexpr int forward_batch(bool general) { return general ? 1 : 2; }
 template <typename TX, typename TY, bool GENERAL>
 static betty_status forward_layout(cudaStream_t stream, const Args& a, const Layout& l) {
+  constexpr int R = forward_batch(GENERAL), CH = FWD_CHUNKS, GR = sizeof(TY) == 4 ? 1 : 2;
   if (l.granule == 8) {
-    if (!l.ahead) return launch_forward<TX, TY, 8, false, 4, GENERAL>(stream, a, l);
-    return l.chunks == 1 ? launch_forward<TX, TY, 8, true, 1, GENERAL>(stream, a, l) : launch_forward<TX, TY, 8, true, 2, GENERAL>(stream, a, l);
+    if (!l.ahead) return launch_forward<TX, TY, 8, false, 4, 1, GENERAL>(stream, a, l);
+    return l.wide ? launch_forward<TX, TY, 8, true, CH, R, GENERAL>(stream, a, l) : launch_forward<TX, TY, 8, true, 1, 1, GENERAL>(stream, a, l);
   }
-  if constexpr (sizeof(TY) == 4) {
-    if (l.ahead) return launch_forward<TX, TY, 1, true, 1, GENERAL>(stream, a, l);
-  } else {
-    if (l.ahead) return launch_forward<TX, TY, 2, true, 1, GENERAL>(stream, a, l);
-    if (l.chunks == 1) return launch_forward<TX, TY, 1, false, 1, GENERAL>(stream, a, l);
-  }
-  return launch_forward<TX, TY, 1, false, 4, GENERAL>(stream, a, l);
+  if (!l.ahead) return launch_forward<TX, TY, 1, false, 4, 1, GENERAL>(stream, a, l);
+  return l.wide ? launch_forward<TX, TY, GR, true, CH, R, GENERAL>(stream, a, l) : launch_forward<TX, TY, GR, true, 1, 1, GENERAL>(stream, a, l);
 }
 template <typename TX, typename TY>
 static betty_status forward_typed(cudaStream_t stream, const Args& a, const Layout& l) {
@@ -182,7 +200,8 @@ static betty_status forward_typed(cudaStream_t stream, const Args& a, const Layo
 }
 betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int granule) {
   const int ys = (a.y ? 1 : 0) + (a.y && a.gate != BETTY_GATE_NONE ? 1 : 0);
-  const Layout l = layout_of(a.d, xd, yd, granule, 1, ys, 512, 1);
+  const bool general = a.bias || a.pre == BETTY_NORM_LAYER || a.post == BETTY_NORM_LAYER;
+  const Layout l = layout_of(a.d, a.rows, xd, yd, granule, {1, ys, FWD_CHUNKS, forward_batch(general), 0});
   a.G = l.G; a.ahead = l.ahead; a.slot_bytes = l.slot_bytes;
   if (xd == BETTY_F32 && yd == BETTY_F32) return forward_typed<float, float>(stream, a, l);
   if (xd == BETTY_F32 && yd == BETTY_BF16) return forward_typed<float, __nv_bfloat16>(stream, a, l);
@@ -191,40 +210,40 @@ betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int granule) 
   return forward_typed<__half, __half>(stream, a, l);
 }
 
-// Aligned rows: `chunks` chunks per thread where MAX_G threads then cover the row.  Rows that cannot be fetched ahead (16-bit
-// values on odd addresses; rows so wide that two do not fit the shared memory) are read where they are used, the widest
-// with four chunks per thread.
-Layout layout_of(int64_t d, int xd, int yd, int granule, int streams_x, int streams_y, int threads_per_sm, int chunks) {
-  Layout l = {};
-  const int bx = xd == BETTY_F32 ? 4 : 2, by = yd == BETTY_F32 ? 4 : 2;
-  bool pipe = granule == 8 || by == 4 || granule == 2;
-  l.granule = granule == 2 && by == 4 ? 1 : granule;
-  l.chunks = granule == 8 ? chunks : 1;
-  for (;;) {
+// Many rows take the wide kernel (several chunks per thread: a row's fixed cost, its sums and addresses, is shared by more
+// values); rows that would leave thread groups idle take one chunk per thread.  Rows that cannot be fetched ahead (16-bit
+// values on odd addresses; rows so wide that two batches do not fit the shared memory) are read where they are used, four
+// chunks per thread.
+Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int granule, const Needs& n) {
+  const int bx = xd == BETTY_F32 ? 4 : 2, by = yd == BETTY_F32 ? 4 : 2, sms = current_sm_count();
+  const bool pipe = granule == 8 || by == 4 || granule == 2;
+  for (int attempt = pipe ? 0 : 2; ; ++attempt) {            // wide, one chunk per thread, not fetched ahead
+    Layout l = {};
+    l.granule = granule == 2 && by == 4 ? 1 : granule;
+    l.wide = attempt == 0;
+    l.chunks = attempt == 0 ? n.wide_chunks : (attempt == 1 ? 1 : MAX_CH);
+    const int batch = attempt == 0 ? n.batch : 1;
     l.G = 32;
     while (l.G < MAX_G && (int64_t)l.G * 8 * l.chunks < d) l.G *= 2;
-    if ((int64_t)l.G * 8 * l.chunks < d) {
-      l.chunks = l.chunks == 1 && granule == 8 ? 2 : MAX_CH;
-      if (l.chunks == MAX_CH) pipe = false;
-      continue;
-    }
+    if ((int64_t)l.G * 8 * l.chunks < d) continue;
     l.threads = l.G == 32 ? SMALL_THREADS : l.G;
-    l.blocks_per_sm = threads_per_sm / l.threads > 0 ? threads_per_sm / l.threads : 1;
-    l.slot_bytes = l.chunks * 8 * l.G * (streams_x * bx + streams_y * by);
-    l.ahead = 0; l.smem = 0;
-    if (!pipe) {
+    const int groups = l.threads / l.G;
+    l.blocks_per_sm = MAX_G / l.threads;
+    l.slot_bytes = l.chunks * 8 * l.G * (n.streams_x * bx + n.streams_y * by);
+    const size_t acc = (size_t)n.acc_arrays * groups * l.chunks * 8 * l.G * sizeof(float);
+    if (attempt == 2) {
+      l.smem = acc;
+      l.slot_bytes = 0;
       if (granule == 2) l.granule = 1;
       return l;
     }
-    const int64_t budget = (int64_t)(220 * 1024) / l.blocks_per_sm - 2048, slot = (int64_t)l.slot_bytes * (l.threads / l.G);
+    if (attempt == 0 && d <= (int64_t)MAX_G * 8 && rows < (int64_t)2 * batch * groups * l.blocks_per_sm * sms) continue;
+    const int64_t slot = (int64_t)l.slot_bytes * groups * batch, budget = (int64_t)(222 * 1024) / l.blocks_per_sm - 2048 - (int64_t)acc;
     l.ahead = (int)(budget / slot) - 1;
+    if (l.ahead < 1) continue;
     if (l.ahead > MAX_AHEAD) l.ahead = MAX_AHEAD;
-    if (l.ahead >= 1) {
-      l.smem = (size_t)(l.ahead + 1) * slot;
-      return l;
-    }
-    pipe = false;                      // two rows do not fit
-    l.chunks = MAX_CH;
+    l.smem = acc + (size_t)(l.ahead + 1) * slot;
+    return l;
   }
 }
 
@@ -299,7 +318,7 @@ extern "C" betty_status betty_block_norm_workspace_size(const betty_block_norm_c
   for (int granule : {8, 2, 1})
     for (int xd : {BETTY_F32, BETTY_BF16})
       for (int yd : {BETTY_F32, BETTY_BF16}) {
-        const Layout l = backward_layout(cfg->d, xd, yd, granule);
+        const Layout l = backward_layout(cfg, rows, xd, yd, granule);
         const int64_t n = backward_blocks(rows, l), w = n * (l.threads / l.G);
         if (n > blocks) blocks = n;
         if (w > walkers) walkers = w;
@@ -343,7 +362,7 @@ extern "C" betty_status betty_block_norm_backward(const betty_block_norm_cfg* cf
   a.x = x_out; a.ldx = ldxo; a.y = y; a.ldy = ldy; a.g = gate; a.ldg = ldg; a.du = du; a.lddu = lddu; a.dxo = dx_out; a.lddxo = lddxo;
   a.dx = dx; a.lddx = lddx; a.dy = dy; a.lddy = lddy; a.dg = dgate; a.lddg = lddg;
   Arena arena(ws, ws_bytes);
-  const Layout l = backward_layout(d, cfg->x_dtype, cfg->y_dtype, granule);
+  const Layout l = backward_layout(cfg, rows, cfg->x_dtype, cfg->y_dtype, granule);
   const int blocks = backward_blocks(rows, l);
   a.walkers = blocks * (l.threads / l.G);
   a.col_partials = arena.alloc<float>((size_t)blocks * quantities(cfg) * d);

@@ -29,29 +29,46 @@ template <> __device__ __forceinline__ float from_f(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
 
+// two neighbouring values into one 32-bit word, one conversion instruction
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *(const uint32_t*)&v;
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *(const uint32_t*)&v;
+}
+template <typename T> __device__ __forceinline__ void unpack2(uint32_t w, float& a, float& b);
+template <> __device__ __forceinline__ void unpack2<__nv_bfloat16>(uint32_t w, float& a, float& b) {
+  a = __uint_as_float(w << 16);
+  b = __uint_as_float(w & 0xffff0000u);
+}
+template <> __device__ __forceinline__ void unpack2<__half>(uint32_t w, float& a, float& b) {
+  const float2 v = __half22float2(*(const __half2*)&w);
+  a = v.x; b = v.y;
+}
+
 // column of a thread's value k (0 .. 7) of chunk c
 template <int GR>
 __device__ __forceinline__ int column(int c, int k, int t, int G) {
   return ((c * (8 / GR) + k / GR) * G + t) * GR + k % GR;
 }
 
-template <typename T> struct alignas(16) Raw8 { T v[8]; };
-
 // chunk c of a row in global memory; columns beyond d are 0
 template <int GR, typename T>
 __device__ __forceinline__ void load8(float (&o)[8], const T* row, int c, int t, int G, int d) {
-  if (GR == 8) {
-    Raw8<T> r;
+  if constexpr (GR == 8) {
     const int j = (c * G + t) * 8;
-    if (j < d) {
+    uint4 w[sizeof(T) / 2];
 #pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) ((uint4*)r.v)[i] = *(const uint4*)((const char*)(row + j) + 16 * i);
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = j < d ? *(const uint4*)((const char*)(row + j) + 16 * i) : make_uint4(0, 0, 0, 0);
+    if constexpr (sizeof(T) == 4) {
+      o[0] = __uint_as_float(w[0].x); o[1] = __uint_as_float(w[0].y); o[2] = __uint_as_float(w[0].z); o[3] = __uint_as_float(w[0].w);
+      o[4] = __uint_as_float(w[1].x); o[5] = __uint_as_float(w[1].y); o[6] = __uint_as_float(w[1].z); o[7] = __uint_as_float(w[1].w);
     } else {
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) ((uint4*)r.v)[i] = make_uint4(0, 0, 0, 0);
+      unpack2<T>(w[0].x, o[0], o[1]); unpack2<T>(w[0].y, o[2], o[3]); unpack2<T>(w[0].z, o[4], o[5]); unpack2<T>(w[0].w, o[6], o[7]);
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = to_f(r.v[k]);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
@@ -62,23 +79,21 @@ __device__ __forceinline__ void load8(float (&o)[8], const T* row, int c, int t,
 }
 template <int GR, typename T>
 __device__ __forceinline__ void store8(T* row, const float (&v)[8], int c, int t, int G, int d) {
-  if (GR == 8) {
+  if constexpr (GR == 8) {
     const int j = (c * G + t) * 8;
     if (j < d) {
-      Raw8<T> r;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) r.v[k] = from_f<T>(v[k]);
-#pragma unroll
-      for (int i = 0; i < (int)sizeof(T) / 2; ++i) *(uint4*)((char*)(row + j) + 16 * i) = ((const uint4*)r.v)[i];
+      if constexpr (sizeof(T) == 4) {
+        *(float4*)(row + j) = make_float4(v[0], v[1], v[2], v[3]);
+        *(float4*)(row + j + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      } else {
+        *(uint4*)(row + j) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
+      }
     }
-  } else if (GR == 2 && sizeof(T) == 2) {
+  } else if constexpr (GR == 2 && sizeof(T) == 2) {
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {             // rows start on 4-byte boundaries and d is even
       const int j = column<GR>(c, k, t, G);
-      if (j < d) {
-        struct alignas(4) Pair { T a, b; } p = {from_f<T>(v[k]), from_f<T>(v[k + 1])};
-        *(uint32_t*)(row + j) = *(const uint32_t*)&p;
-      }
+      if (j < d) *(uint32_t*)(row + j) = pack2<T>(v[k], v[k + 1]);
     }
   } else {
 #pragma unroll
@@ -115,20 +130,35 @@ __device__ __forceinline__ void copy_row(char* slot, const T* row, int t, int G,
     }
   }
 }
-template <int GR, typename T>
-__device__ __forceinline__ void read_slot(float (&o)[8], const char* slot, int c, int t, int G, int d) {
-  constexpr int bytes = GR * (int)sizeof(T), piece = bytes >= 16 ? 16 : 4, per = bytes / piece;
-  Raw8<T> r;
-#pragma unroll
-  for (int n = 0; n < 8 / GR; ++n)
-#pragma unroll
-    for (int i = 0; i < per; ++i) {
-      const char* src = slot + (((c * (8 / GR) + n) * per + i) * G + t) * piece;
-      if (piece == 16) ((uint4*)r.v)[n * per + i] = *(const uint4*)src;
-      else ((uint32_t*)r.v)[n * per + i] = *(const uint32_t*)src;
+// zeros for the columns beyond d, written once: no copy touches them, so that reading a slot needs no comparison
+template <int GR, int CH, typename T>
+__device__ __forceinline__ void clear_beyond(char* slot, int t, int G, int d) {
+  constexpr int words = GR * (int)sizeof(T) / 4;
+  for (int n = 0; n < CH * 8 / GR; ++n)
+    if ((n * G + t) * GR >= d) {
+      constexpr int bytes = GR * (int)sizeof(T), piece = bytes >= 16 ? 16 : 4;
+      for (int i = 0; i < words; ++i) *(uint32_t*)(slot + (n * (bytes / piece) + i * 4 / piece) * G * piece + t * piece + i * 4 % piece) = 0u;
     }
+}
+template <int GR, typename T>
+__device__ __forceinline__ void read_slot(float (&o)[8], const char* slot, int c, int t, int G) {
+  constexpr int bytes = GR * (int)sizeof(T), piece = bytes >= 16 ? 16 : 4, pieces = 8 * (int)sizeof(T) / piece;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) o[k] = column<GR>(c, k, t, G) < d ? to_f(r.v[k]) : 0.f;
+  for (int i = 0; i < pieces; ++i) {
+    const char* src = slot + ((c * pieces + i) * G + t) * piece;
+    constexpr int per = piece / (int)sizeof(T);          // values in a piece
+    if constexpr (piece == 16 && sizeof(T) == 4) {
+      const float4 w = *(const float4*)src;
+      o[i * per] = w.x; o[i * per + 1] = w.y; o[i * per + 2] = w.z; o[i * per + 3] = w.w;
+    } else if constexpr (piece == 16) {
+      const uint4 w = *(const uint4*)src;
+      unpack2<T>(w.x, o[0], o[1]); unpack2<T>(w.y, o[2], o[3]); unpack2<T>(w.z, o[4], o[5]); unpack2<T>(w.w, o[6], o[7]);
+    } else if constexpr (sizeof(T) == 4) {
+      o[i] = *(const float*)src;
+    } else {
+      unpack2<T>(*(const uint32_t*)src, o[2 * i], o[2 * i + 1]);
+    }
+  }
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // until at most `later` of this thread's groups are still in flight
@@ -139,31 +169,62 @@ __device__ __forceinline__ void copies_wait(int later) {
 }
 static constexpr int MAX_AHEAD = 3;
 
-// Sums of NV values over the G threads of a row, every thread receiving the same bits.  A butterfly within each warp,
-// then (G > 32) the warps' sums through shared memory and a second butterfly.  `red` has two halves used in turn, so
-// one block barrier per call is enough.
-static constexpr int RED_VALUES = 3;
+// Sums of NV values over the G threads of a row, every thread receiving the same bits.  Within a warp the values are
+// folded while they are reduced: each of the first steps halves the number of values a lane carries, so that P values cost
+// P - 1 exchanges and log2(32 / P) further ones instead of 5 P.  Across warps every lane then takes one (value, warp) pair
+// from shared memory.  `red` has two halves used in turn, so one block barrier per call is enough.
+static constexpr int RED_VALUES = 8;
 template <int NV>
 __device__ __forceinline__ void row_sums(float (&v)[NV], float* red, int& half, int G, int t) {
+  constexpr int P = NV <= 1 ? 1 : (NV <= 2 ? 2 : (NV <= 4 ? 4 : 8));
+  const int lane = t & 31;
+  float u[P];
 #pragma unroll
-  for (int o = 16; o; o >>= 1)
+  for (int i = 0; i < P; ++i) u[i] = i < NV ? v[i < NV ? i : 0] : 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-  if (G > 32) {
-    float* r = red + half * (RED_VALUES * 16);
-    half ^= 1;
-    const int warps = G >> 5;
-    if ((t & 31) == 0)
+  for (int n = P, o = 16; o; o >>= 1) {
+    if (n > 1) {
+      n >>= 1;
+      const bool up = lane & o;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) r[i * 16 + (t >> 5)] = v[i];
-    __syncthreads();
-    // every half warp adds the (at most 16) warps' sums
+      for (int i = 0; i < n; ++i) {
+        const float send = up ? u[i] : u[i + n], keep = up ? u[i + n] : u[i];
+        u[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+      }
+    } else {
+      u[0] += __shfl_xor_sync(0xffffffffu, u[0], o);
+    }
+  }
+  if (G == 32) {           // value i now is in lanes i * 32 / P ...
 #pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] = (t & 15) < warps ? r[i * 16 + (t & 15)] : 0.f;
+    for (int i = 0; i < NV; ++i) v[i] = P == 1 ? u[0] : __shfl_sync(0xffffffffu, u[0], i * (32 / P));
+    return;
+  }
+  float* r = red + half * (RED_VALUES * 16);
+  half ^= 1;
+  const int warps = G >> 5, lg = 31 - __clz(warps);
+  if (lane % (32 / P) == 0) r[((lane / (32 / P)) << lg) + (t >> 5)] = u[0];
+  __syncthreads();
+  constexpr int LOADS = P * 16 > 32 ? P * 16 / 32 : 1;       // at most 16 warps
+  float w[LOADS];
 #pragma unroll
-    for (int o = 8; o; o >>= 1)
+  for (int j = 0; j < LOADS; ++j) {
+    const int e = lane + 32 * j;
+    w[j] = r[e & ((P << lg) - 1)];
+  }
 #pragma unroll
-      for (int i = 0; i < NV; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  for (int o = 8; o; o >>= 1)
+    if (o < warps)
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) w[j] += __shfl_xor_sync(0xffffffffu, w[j], o);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {                              // pair e = i * warps + ... is in lane e % 32 of load e / 32
+    const int e = i << lg;
+    float x = w[0];
+#pragma unroll
+    for (int j = 1; j < LOADS; ++j)
+      if ((e >> 5) == j) x = w[j];
+    v[i] = __shfl_sync(0xffffffffu, x, e & 31);
   }
 }
 
@@ -172,7 +233,7 @@ __device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.f, 1.f
 struct Args {
   int64_t rows;
   int d, G;
-  int ahead;                // rows fetched ahead of the present one, 1 .. MAX_AHEAD (kernels that fetch ahead)
+  int ahead;                // batches of rows fetched ahead of the present one, 1 .. MAX_AHEAD (kernels that fetch ahead)
   int slot_bytes;           // of one row, all streams
   int pre, post, gate, bias;
   unsigned per_gate;
@@ -199,15 +260,19 @@ struct Layout {
   int G, chunks;            // threads per row, chunks of 8 values per thread
   int threads;              // of a block
   int blocks_per_sm;        // that the grid counts on
-  int ahead, slot_bytes;    // ahead 0: rows are read from global memory where they are used
+  bool wide;                // two chunks and several rows at a time: many rows; else the shortest way for a few
+  int ahead, slot_bytes;    // batches fetched ahead; 0: rows are read from global memory where they are used
   size_t smem;
 };
 
-// streams of the residual stream's type and of the block's type that a row fetches; threads_per_sm: what the kernel's
-// registers allow; chunks: values per thread / 8 to aim for where rows are aligned
-Layout layout_of(int64_t d, int x_dtype, int y_dtype, int granule, int streams_x, int streams_y, int threads_per_sm, int chunks);
+struct Needs {
+  int streams_x, streams_y; // rows fetched of the residual stream's and of the block's type
+  int wide_chunks, batch;   // of the wide kernel
+  int acc_arrays;           // fp32 values of a row kept in shared memory
+};
+Layout layout_of(int64_t d, int64_t rows, int x_dtype, int y_dtype, int granule, const Needs& n);
 betty_status forward(cudaStream_t stream, Args& a, int x_dtype, int y_dtype, int granule);
-Layout backward_layout(int64_t d, int x_dtype, int y_dtype, int granule);
+Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int x_dtype, int y_dtype, int granule);
 int backward_blocks(int64_t rows, const Layout& l);
 betty_status backward(cudaStream_t stream, Args& a, const Layout& l, int x_dtype, int y_dtype, float* dparams);
 

@@ -18,20 +18,55 @@ namespace blocknorm {
 __host__ __device__ __forceinline__ int64_t share_start(int64_t w, int64_t rows, int64_t walkers) { return w * rows / walkers; }
 __device__ __forceinline__ int64_t walker_of(int64_t row, int64_t rows, int64_t walkers) { return ((row + 1) * walkers - 1) / rows; }
 
-// Each walker (thread group) takes a contiguous share of the rows, so that the column sums (parameter gradients, gates of
-// several rows) stay in its registers; it writes them once, and k_backward_sums adds the walkers' sums in order.
-// Per row: the norms' sums over the fetched values, then dX (and with it everything that hangs off dm), then dy.
+// dm of one chunk, 8 fp32 values, kept in the thread's own slots of x' and du: where x' is fp32 each in its column's place,
+// else values 0 .. 3 in the 16 bytes of x' and 4 .. 7 in those of du, or (granules of two) a granule's two values in its
+// words of x' and of du.  Columns beyond d keep their zeros.
+template <int GR, typename TX>
+__device__ __forceinline__ int park_at(int at_u, int c, int k, int t, int G) {      // k: a multiple of 4 (GR = 8) or any
+  if (GR == 8) return sizeof(TX) == 4 ? ((c * 2 + k / 4) * G + t) * 16 : (c * G + t) * 16 + (k / 4) * at_u;
+  return sizeof(TX) == 4 ? ((c * 8 + k) * G + t) * 4 : ((c * 4 + k / 2) * G + t) * 4 + (k % 2) * at_u;
+}
+template <int GR, typename TX>
+__device__ __forceinline__ void park(char* slot, int at_u, const float (&v)[8], int c, int t, int G, int d) {
+  static_assert(GR == 8 || sizeof(TX) == 4 || GR == 2, "16-bit rows are fetched in granules of 8 or 2");
+#pragma unroll
+  for (int k = 0; k < 8; k += GR == 8 ? 4 : 1)
+    if (column<GR>(c, k, t, G) < d) {
+      char* at = slot + park_at<GR, TX>(at_u, c, k, t, G);
+      if constexpr (GR == 8) *(float4*)at = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+      else *(float*)at = v[k];
+    }
+}
+template <int GR, typename TX>
+__device__ __forceinline__ void unpark(float (&v)[8], const char* slot, int at_u, int c, int t, int G) {
+#pragma unroll
+  for (int k = 0; k < 8; k += GR == 8 ? 4 : 1) {
+    const char* at = slot + park_at<GR, TX>(at_u, c, k, t, G);
+    if constexpr (GR == 8) {
+      const float4 w = *(const float4*)at;
+      v[k] = w.x; v[k + 1] = w.y; v[k + 2] = w.z; v[k + 3] = w.w;
+    } else {
+      v[k] = *(const float*)at;
+    }
+  }
+}
+
+// Each walker (thread group) takes a contiguous share of the rows, so that the column sums stay in its registers; it writes
+// them once, and k_backward_sums adds the blocks' sums in order.  Per row: the norms' sums over the fetched values, then dX
+// (and with it everything that hangs off dm), then dy.  dm waits for its row's sum in the slots of x' and du, which are read
+// by then.  A gate shared by rows needs one sum H = sum dX m per gate: dg = a'(g) s w_post H and A gains a(g) H when the
+// walker leaves the gate, so A waits in shared memory.
 template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   __shared__ float red[2 * RED_VALUES * 16];
-  extern __shared__ __align__(16) char slots[];      // fetched rows; G = 32: at the end the warps' column sums
+  extern __shared__ __align__(16) char slots[];
   pdl_enter();
-  const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G;
-  const int64_t walker = (int64_t)blockIdx.x * (blockDim.x / G) + sub;
+  const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G, subs = blockDim.x / G;
+  const int64_t walker = (int64_t)blockIdx.x * subs + sub;
   const int64_t first = share_start(walker, a.rows, a.walkers), last = share_start(walker + 1, a.rows, a.walkers);
   const bool has_y = a.y != nullptr, has_g = a.gate != BETTY_GATE_NONE, has_u = a.du != nullptr, has_o = a.dxo != nullptr;
   const bool pre_layer = GENERAL && a.pre == BETTY_NORM_LAYER && has_u, post_layer = GENERAL && a.post == BETTY_NORM_LAYER && has_y;
-  const bool shared_gate = has_g && a.per_gate > 1;
+  const bool shared_gate = has_g && a.per_gate > 1, row_gate = has_g && !shared_gate;
   const float* w_pre = a.params;
   const float* w_post = a.params + d;
   const float* s_res = a.params + 2 * (int64_t)d;
@@ -39,7 +74,8 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   const int bx = CH * 8 * G * (int)sizeof(TX), by = CH * 8 * G * (int)sizeof(TY);
   const int at_o = bx, at_y = 2 * bx, at_u = 2 * bx + by, at_g = 2 * bx + 2 * by;
   char* ring = slots + (size_t)sub * (a.ahead + 1) * a.slot_bytes;
-  auto gate_row = [&](int64_t r) { return (const TY*)a.g + (int64_t)((unsigned)r / a.per_gate) * a.ldg; };
+  // [A (, B)][value][thread] of a walker whose gates are shared
+  float* acc_s = (float*)(slots + (size_t)subs * (a.ahead + 1) * a.slot_bytes) + (size_t)sub * (GENERAL ? 2 : 1) * CH * 8 * G + t;
   auto fetch = [&](int64_t r, int slot) {
     if constexpr (PIPE) {
       if (r < last) {
@@ -50,84 +86,91 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         }
         if (has_o) copy_row<GR, CH>(p + at_o, (const TX*)a.dxo + r * a.lddxo, t, G, d);
         if (has_y) copy_row<GR, CH>(p + at_y, (const TY*)a.y + r * a.ldy, t, G, d);
-        if (has_g) copy_row<GR, CH>(p + at_g, gate_row(r), t, G, d);
+        if (row_gate) copy_row<GR, CH>(p + at_g, (const TY*)a.g + r * a.ldg, t, G, d);
       }
       copies_commit();
     }
   };
   // one chunk of a stream of the present row
-  const char* p = nullptr;
-  auto get = [&](auto* base, int64_t row, int64_t ld, int at, int c, float (&v)[8]) {
+  char* p = nullptr;
+  int64_t row = first;
+  auto get = [&](auto* base, int64_t ld, int at, int c, float (&v)[8]) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(base)>::type>::type T;
-    if constexpr (PIPE) read_slot<GR, T>(v, p + at, c, t, G, d);
+    if constexpr (PIPE) read_slot<GR, T>(v, p + at, c, t, G);
     else load8<GR, T>(v, base + row * ld, c, t, G, d);
   };
-  // parameters of one chunk: kept in registers where a thread holds one chunk, else read again (they stay in L1)
-  constexpr int KEEP = CH == 1 ? 1 : 0;
-  float kp[KEEP ? 8 : 1], kws[KEEP ? 8 : 1];
-  auto param_pre = [&](int c, float (&v)[8]) {
-    if constexpr (KEEP) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = kp[k];
-    } else load_param8<GR>(v, w_pre, c, t, G, d);
-  };
-  auto param_post = [&](int c, float (&v)[8]) {      // w_post * s
-    if constexpr (KEEP) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = kws[k];
-    } else {
-      float s[8];
-      load_param8<GR>(v, w_post, c, t, G, d);
-      load_param8<GR>(s, s_res, c, t, G, d);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] *= s[k];
-    }
-  };
   int half = 0, slot = 0;
-  if (PIPE)
+  if constexpr (PIPE) {
+    for (int i = 0; i <= a.ahead && CH * 8 * G > d; ++i) {
+      char* s = ring + i * a.slot_bytes;
+      clear_beyond<GR, CH, TX>(s, t, G, d);
+      clear_beyond<GR, CH, TX>(s + at_o, t, G, d);
+      clear_beyond<GR, CH, TY>(s + at_y, t, G, d);
+      clear_beyond<GR, CH, TY>(s + at_u, t, G, d);
+      if (row_gate) clear_beyond<GR, CH, TY>(s + at_g, t, G, d);
+    }
     for (int i = 0; i < a.ahead; ++i) fetch(first + i, i);
-  if constexpr (KEEP) {
-    float s[8];
-    load_param8<GR>(kp, w_pre, 0, t, G, d);
-    load_param8<GR>(kws, w_post, 0, t, G, d);
-    load_param8<GR>(s, s_res, 0, t, G, d);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) kws[k] *= s[k];
   }
-  float accC[CH][8], accA[CH][8], accD[GENERAL ? CH : 1][8], accB[GENERAL ? CH : 1][8], accG[CH][8];
+  // w_pre and w_post * s stay in registers (CH <= 2) or are read again
+  constexpr bool KEEP = CH <= 2;
+  float kp[KEEP ? CH : 1][8], kws[KEEP ? CH : 1][8], mask[GENERAL ? CH : 1][8 / GR];
+  auto params_of = [&](int c, float (&wp)[8], float (&ws)[8]) {
+    float s[8];
+    load_param8<GR>(wp, w_pre, c, t, G, d);
+    load_param8<GR>(ws, w_post, c, t, G, d);
+    load_param8<GR>(s, s_res, c, t, G, d);
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+    for (int k = 0; k < 8; ++k) ws[k] *= s[k];
+  };
+  float accC[CH][8], accA[CH][8], accD[GENERAL ? CH : 1][8], accB[GENERAL ? CH : 1][8];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if constexpr (KEEP) params_of(c, kp[c], kws[c]);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      accC[c][k] = 0.f; accA[c][k] = 0.f; accG[c][k] = 0.f;
+      accC[c][k] = 0.f; accA[c][k] = 0.f;
       if (GENERAL) { accD[c][k] = 0.f; accB[c][k] = 0.f; }
+      if (shared_gate) {
+        acc_s[(c * 8 + k) * G] = 0.f;
+        if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = 0.f;
+      }
     }
-  for (int64_t row = first; row < last; ++row) {
+    if (GENERAL)
+#pragma unroll
+      for (int k = 0; k < 8; k += GR) mask[c][k / GR] = column<GR>(c, k, t, G) < d ? 1.f : 0.f;   // 0 beyond the row
+  }
+  const TX* xs = (const TX*)a.x;
+  const TX* os = (const TX*)a.dxo;
+  const TY* ys = (const TY*)a.y;
+  const TY* us = (const TY*)a.du;
+  int64_t gate = 0, gate_end = 0;          // of a shared gate: the present row's, and the row after its last
+  if (shared_gate && first < last) {
+    gate = (unsigned)first / a.per_gate;
+    gate_end = (gate + 1) * a.per_gate;
+  }
+  for (; row < last; ++row) {
     if (PIPE) {
       fetch(row + a.ahead, slot == 0 ? a.ahead : slot - 1);
       copies_wait(a.ahead);
       p = ring + slot * a.slot_bytes;
       slot = slot == a.ahead ? 0 : slot + 1;
     }
-    const TX* xs = (const TX*)a.x;
-    const TX* os = (const TX*)a.dxo;
-    const TY* ys = (const TY*)a.y;
-    const TY* us = (const TY*)a.du;
     float mean_dn = 0.f, mx = 0.f, my = 0.f;
     if (pre_layer || post_layer) {
       float v[3] = {0.f, 0.f, 0.f};
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        float x[8], y[8], du[8], w[8];
         if (pre_layer) {
-          get(xs, row, a.ldx, 0, c, x);
-          get(us, row, a.lddu, at_u, c, du);
-          param_pre(c, w);
+          float x[8], du[8], w[8], ws[8];
+          get(xs, a.ldx, 0, c, x);
+          get(us, a.lddu, at_u, c, du);
+          if constexpr (!KEEP) params_of(c, w, ws);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) { v[0] += x[k]; v[2] = fmaf(du[k], w[k], v[2]); }
+          for (int k = 0; k < 8; ++k) { v[0] += x[k]; v[2] = fmaf(du[k], KEEP ? kp[KEEP ? c : 0][k] : w[k], v[2]); }
         }
         if (post_layer) {
-          get(ys, row, a.ldy, at_y, c, y);
+          float y[8];
+          get(ys, a.ldy, at_y, c, y);
 #pragma unroll
           for (int k = 0; k < 8; ++k) v[1] += y[k];
         }
@@ -142,23 +185,23 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         if (has_u) {
-          float x[8], du[8], w[8];
-          get(xs, row, a.ldx, 0, c, x);
-          get(us, row, a.lddu, at_u, c, du);
-          param_pre(c, w);
+          float x[8], du[8], w[8], ws[8];
+          get(xs, a.ldx, 0, c, x);
+          get(us, a.lddu, at_u, c, du);
+          if constexpr (!KEEP) params_of(c, w, ws);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            if (GENERAL) x[k] = column<GR>(c, k, t, G) < d ? x[k] - mx : 0.f;
+            if (GENERAL) x[k] = fmaf(-mx, mask[c][k / GR], x[k]);
             v[0] = fmaf(x[k], x[k], v[0]);
-            v[1] = fmaf(du[k] * w[k], x[k], v[1]);
+            v[1] = fmaf(du[k] * (KEEP ? kp[KEEP ? c : 0][k] : w[k]), x[k], v[1]);
           }
         }
         if (has_y) {
           float y[8];
-          get(ys, row, a.ldy, at_y, c, y);
+          get(ys, a.ldy, at_y, c, y);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            if (GENERAL) y[k] = column<GR>(c, k, t, G) < d ? y[k] - my : 0.f;
+            if (GENERAL) y[k] = fmaf(-my, mask[c][k / GR], y[k]);
             v[2] = fmaf(y[k], y[k], v[2]);
           }
         }
@@ -170,100 +213,172 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       }
       if (a.post != BETTY_NORM_NONE && has_y) q = rsqrtf(fmaf(v[2], a.inv_d, a.eps));
     }
-    TX* dx = (TX*)a.dx + row * a.lddx;
     float v[2] = {0.f, 0.f};
-    float m[CH][8], dm[CH][8];
+    // dm of the row: in registers where a thread holds one chunk (or nothing is fetched ahead), else over x' and du
+    constexpr bool PARK = PIPE && CH > 1;
+    float dm[PARK ? 1 : CH][8];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float dX[8];
-      if (has_o) get(os, row, a.lddxo, at_o, c, dX);
+      float dX[8], w[8], ws[8];
+      if constexpr (!KEEP) params_of(c, w, ws);
+      if (has_o) get(os, a.lddxo, at_o, c, dX);
       else
 #pragma unroll
         for (int k = 0; k < 8; ++k) dX[k] = 0.f;
       if (has_u) {
-        float x[8], du[8], w[8];
-        get(xs, row, a.ldx, 0, c, x);
-        get(us, row, a.lddu, at_u, c, du);
-        param_pre(c, w);
+        float x[8], du[8];
+        get(xs, a.ldx, 0, c, x);
+        get(us, a.lddu, at_u, c, du);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const float n = (GENERAL ? x[k] - mx : x[k]) * r;
+          const float n = (GENERAL ? fmaf(-mx, mask[c][k / GR], x[k]) : x[k]) * r;
           accC[c][k] = fmaf(du[k], n, accC[c][k]);
           if (GENERAL) accD[c][k] += du[k];
-          float dn = fmaf(-n, proj, du[k] * w[k]);
+          float dn = fmaf(-n, proj, du[k] * (KEEP ? kp[KEEP ? c : 0][k] : w[k]));
           if (GENERAL) dn -= mean_dn;
           dX[k] = fmaf(r, dn, dX[k]);
         }
       }
-      store8<GR>(dx, dX, c, t, G, d);
+      store8<GR>((TX*)a.dx + row * a.lddx, dX, c, t, G, d);
       if (!has_y) continue;
-      float ws[8], g[8], b[8], y[8];
-      param_post(c, ws);
-      get(ys, row, a.ldy, at_y, c, y);
-      if (has_g) get((const TY*)a.g, (int64_t)((unsigned)row / a.per_gate), a.ldg, at_g, c, g);
-      if (GENERAL && a.bias) {
-        float s[8];
-        load_param8<GR>(b, b_post, c, t, G, d);
-        load_param8<GR>(s, s_res, c, t, G, d);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) b[k] *= s[k];
-      }
-      float dg[8];
+      float y[8], g[8], base[8];
+      get(ys, a.ldy, at_y, c, y);
+      if (shared_gate) load8<GR, TY>(g, (const TY*)a.g + gate * a.ldg, c, t, G, d);
+      else if (row_gate) get((const TY*)a.g, a.ldg, at_g, c, g);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float mk = (GENERAL ? (column<GR>(c, k, t, G) < d ? y[k] - my : 0.f) : y[k]) * q;
-        float act = 1.f, slope = 1.f;
-        if (a.gate == BETTY_GATE_LINEAR) act = g[k];
-        if (a.gate == BETTY_GATE_SIGMOID) { act = sigmoid_f(g[k]); slope = act * (1.f - act); }
-        const float base = dX[k] * act, dmk = base * ws[k];
-        accA[c][k] = fmaf(base, mk, accA[c][k]);
-        float z = mk * ws[k];
-        if (GENERAL) {
-          accB[c][k] += base;
-          if (a.bias) z += b[k];
-        }
-        dg[k] = dX[k] * z * slope;
-        accG[c][k] += dg[k];
-        v[0] = fmaf(dmk, mk, v[0]);
-        v[1] += dmk;
-        m[c][k] = mk;
-        dm[c][k] = dmk;
+        y[k] = (GENERAL ? fmaf(-my, mask[c][k / GR], y[k]) : y[k]) * q;      // m
+        if constexpr (KEEP) ws[k] = kws[KEEP ? c : 0][k];
       }
-      if (has_g && !shared_gate) store8<GR>((TY*)a.dg + row * a.lddg, dg, c, t, G, d);
+      if (has_g) {
+        float slope[8];
+        if (a.gate == BETTY_GATE_SIGMOID) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) { g[k] = sigmoid_f(g[k]); slope[k] = g[k] * (1.f - g[k]); }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) slope[k] = 1.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) base[k] = dX[k] * g[k];
+        if (shared_gate) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            accA[c][k] = fmaf(dX[k], y[k], accA[c][k]);
+            if (GENERAL) accB[c][k] += dX[k];
+          }
+        } else {
+          float dg[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dg[k] = y[k] * ws[k];
+          if (GENERAL && a.bias) {
+            float b[8], s[8];
+            load_param8<GR>(b, b_post, c, t, G, d);
+            load_param8<GR>(s, s_res, c, t, G, d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dg[k] = fmaf(b[k], s[k], dg[k]);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dg[k] *= dX[k] * slope[k];
+          store8<GR>((TY*)a.dg + row * a.lddg, dg, c, t, G, d);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) base[k] = dX[k];
+      }
+      if (!shared_gate)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          accA[c][k] = fmaf(base[k], y[k], accA[c][k]);
+          if (GENERAL) accB[c][k] += base[k];
+        }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        base[k] *= ws[k];                                                    // dm
+        v[0] = fmaf(base[k], y[k], v[0]);
+        if (GENERAL) v[1] += base[k];
+      }
+      if constexpr (PARK) {
+        park<GR, TX>(p, at_u, base, c, t, G, d);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dm[PARK ? 0 : c][k] = base[k];
+      }
     }
     if (!has_y) continue;
-    if (a.post != BETTY_NORM_NONE) row_sums<2>(v, red, half, G, t);
+    if (a.post != BETTY_NORM_NONE) {
+      if (GENERAL) row_sums<2>(v, red, half, G, t);
+      else {
+        float one[1] = {v[0]};
+        row_sums<1>(one, red, half, G, t);
+        v[0] = one[0];
+      }
+    }
     const float pm = a.post != BETTY_NORM_NONE ? v[0] * a.inv_d : 0.f, mean_dm = post_layer ? v[1] * a.inv_d : 0.f;
-    TY* dy = (TY*)a.dy + row * a.lddy;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float o[8];
+      float o[8], y[8];
+      get(ys, a.ldy, at_y, c, y);
+      if constexpr (PARK) unpark<GR, TX>(o, p, at_u, c, t, G);
+      else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = dm[PARK ? 0 : c][k];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        o[k] = fmaf(-m[c][k], pm, dm[c][k]);
+        const float m = (GENERAL ? fmaf(-my, mask[c][k / GR], y[k]) : y[k]) * q;
+        o[k] = fmaf(-m, pm, o[k]);
         if (GENERAL) o[k] -= mean_dm;
         o[k] *= q;
       }
-      store8<GR>(dy, o, c, t, G, d);
+      store8<GR>((TY*)a.dy + row * a.lddy, o, c, t, G, d);
     }
-    if (shared_gate) {
-      const unsigned gate = (unsigned)row / a.per_gate;
-      const int64_t g0 = (int64_t)gate * a.per_gate;
-      const int64_t g1 = g0 + a.per_gate < a.rows ? g0 + a.per_gate : a.rows;
-      if (row + 1 == g1 || row + 1 == last) {
-        const bool whole = g0 >= first && g1 <= last;
+    if (shared_gate && (row + 1 == gate_end || row + 1 == last)) {           // the walker leaves the gate
+      const int64_t g0 = gate * a.per_gate, g1 = gate_end < a.rows ? gate_end : a.rows;
+      const bool whole = g0 >= first && g1 <= last;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          if (whole) store8<GR>((TY*)a.dg + gate * a.lddg, accG[c], c, t, G, d);
-          else store8<GR>(a.gate_partials + (walker + gate) * d, accG[c], c, t, G, d);
+      for (int c = 0; c < CH; ++c) {
+        float g[8], dg[8], w[8], ws[8];
+        if constexpr (!KEEP) params_of(c, w, ws);
+        load8<GR, TY>(g, (const TY*)a.g + gate * a.ldg, c, t, G, d);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) accG[c][k] = 0.f;
+        for (int k = 0; k < 8; ++k) dg[k] = accA[c][k] * (KEEP ? kws[KEEP ? c : 0][k] : ws[k]);
+        if (GENERAL && a.bias) {
+          float b[8], s[8];
+          load_param8<GR>(b, b_post, c, t, G, d);
+          load_param8<GR>(s, s_res, c, t, G, d);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dg[k] = fmaf(b[k] * s[k], accB[c][k], dg[k]);
         }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (a.gate == BETTY_GATE_SIGMOID) {
+            g[k] = sigmoid_f(g[k]);
+            dg[k] *= g[k] * (1.f - g[k]);
+          }
+          acc_s[(c * 8 + k) * G] = fmaf(g[k], accA[c][k], acc_s[(c * 8 + k) * G]);
+          accA[c][k] = 0.f;
+          if (GENERAL) {
+            acc_s[(CH * 8 + c * 8 + k) * G] = fmaf(g[k], accB[c][k], acc_s[(CH * 8 + c * 8 + k) * G]);
+            accB[c][k] = 0.f;
+          }
+        }
+        if (whole) store8<GR>((TY*)a.dg + gate * a.lddg, dg, c, t, G, d);
+        else store8<GR>(a.gate_partials + (walker + gate) * d, dg, c, t, G, d);
       }
+      ++gate;
+      gate_end += a.per_gate;
     }
   }
   const int nq = a.bias ? 4 : 2;
   float* out = a.col_partials + (int64_t)blockIdx.x * nq * d;
+  if (shared_gate)
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        accA[c][k] = acc_s[(c * 8 + k) * G];
+        if (GENERAL) accB[c][k] = acc_s[(CH * 8 + c * 8 + k) * G];
+      }
   if (G > 32) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -277,7 +392,6 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   } else {                                    // a warp per walker: the block's warps are added in order through shared memory
     float* combine = (float*)slots;
     constexpr int W = CH * 256;               // columns a warp can hold
-    const int warps = blockDim.x >> 5;
     for (int qn = 0; qn < nq; ++qn) {
       __syncthreads();
 #pragma unroll
@@ -291,7 +405,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       __syncthreads();
       for (int j = threadIdx.x; j < d; j += blockDim.x) {
         float s = 0.f;
-        for (int w = 0; w < warps; ++w) s += combine[w * W + j];
+        for (int w = 0; w < subs; ++w) s += combine[w * W + j];
         out[(int64_t)qn * d + j] = s;
       }
     }
@@ -364,8 +478,14 @@ int backward_blocks(int64_t rows, const Layout& l) {
   const int64_t want = (rows + per_block - 1) / per_block, most = (int64_t)current_sm_count() * l.blocks_per_sm;
   return (int)(want < 1 ? 1 : (want < most ? want : most));
 }
-Layout backward_layout(int64_t d, int xd, int yd, int granule) {
-  Layout l = layout_of(d, xd, yd, granule, 2, 3, 512, 1);
+static inline bool is_general(int bias, int pre, int post) { return bias || pre == BETTY_NORM_LAYER || post == BETTY_NORM_LAYER; }
+// chunks per thread of the wide kernel: the layer norms' and biases' sums leave registers for one
+static constexpr int backward_chunks(bool general) { return general ? 1 : 2; }
+Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int xd, int yd, int granule) {
+  const bool gated = c->gate != BETTY_GATE_NONE, general = is_general(c->bias, c->pre, c->post);
+  const bool row_gate = gated && c->rows_per_gate == 1;             // a gate shared by rows stays in L1
+  Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, gated && !row_gate ? (general ? 2 : 1) : 0};
+  Layout l = layout_of(c->d, rows, xd, yd, granule, n);
   const size_t combine = l.G == 32 ? (size_t)(l.threads / 32) * l.chunks * 256 * sizeof(float) : 0;
   if (l.smem < combine) l.smem = combine;
   return l;
@@ -391,23 +511,17 @@ static betty_status launch_backward(cudaStream_t stream, const Args& a, const La
 }
 template <typename TX, typename TY, bool GENERAL>
 static betty_status backward_shape(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
-  if (l.granule == 8) {
-    if (!l.ahead) return launch_backward<TX, TY, 8, false, 4, GENERAL>(stream, a, l, dparams);
-    return l.chunks == 1 ? launch_backward<TX, TY, 8, true, 1, GENERAL>(stream, a, l, dparams)
-                         : launch_backward<TX, TY, 8, true, 2, GENERAL>(stream, a, l, dparams);
-  }
-  if constexpr (sizeof(TY) == 4) {
-    if (l.ahead) return launch_backward<TX, TY, 1, true, 1, GENERAL>(stream, a, l, dparams);
-  } else {
-    if (l.ahead) return launch_backward<TX, TY, 2, true, 1, GENERAL>(stream, a, l, dparams);
-    if (l.chunks == 1) return launch_backward<TX, TY, 1, false, 1, GENERAL>(stream, a, l, dparams);
-  }
-  return launch_backward<TX, TY, 1, false, 4, GENERAL>(stream, a, l, dparams);
+  constexpr int CH = backward_chunks(GENERAL), GR = sizeof(TY) == 4 ? 1 : 2;
+  if (!l.ahead)
+    return l.granule == 8 ? launch_backward<TX, TY, 8, false, 4, GENERAL>(stream, a, l, dparams)
+                          : launch_backward<TX, TY, 1, false, 4, GENERAL>(stream, a, l, dparams);
+  if (l.granule == 8)
+    return l.wide ? launch_backward<TX, TY, 8, true, CH, GENERAL>(stream, a, l, dparams) : launch_backward<TX, TY, 8, true, 1, GENERAL>(stream, a, l, dparams);
+  return l.wide ? launch_backward<TX, TY, GR, true, CH, GENERAL>(stream, a, l, dparams) : launch_backward<TX, TY, GR, true, 1, GENERAL>(stream, a, l, dparams);
 }
 template <typename TX, typename TY>
 static betty_status backward_typed(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
-  const bool general = a.bias || a.pre == BETTY_NORM_LAYER || a.post == BETTY_NORM_LAYER;
-  return general ? backward_shape<TX, TY, true>(stream, a, l, dparams) : backward_shape<TX, TY, false>(stream, a, l, dparams);
+  return is_general(a.bias, a.pre, a.post) ? backward_shape<TX, TY, true>(stream, a, l, dparams) : backward_shape<TX, TY, false>(stream, a, l, dparams);
 }
 betty_status backward(cudaStream_t stream, Args& a, const Layout& l, int xd, int yd, float* dparams) {
   a.G = l.G; a.ahead = l.ahead; a.slot_bytes = l.slot_bytes;

@@ -143,6 +143,39 @@ def test_forward_and_backward_over_sizes(rows, d, kind, act, per_gate, bias):
     _check_backward(bt, q, args)
 
 
+@pytest.mark.parametrize("rows,d", [(5000, 96), (5000, 130), (4800, 77), (2500, 1000), (2500, 1002), (700, 4096), (700, 2050), (700, 2051),
+                                    (320, 5000), (320, 5002), (320, 8191)])
+@pytest.mark.parametrize("kind,act,per_gate,bias", [("rms", "linear", 1, False), ("layer", "sigmoid", 1, True), ("rms", "sigmoid", 90, False),
+                                                    ("layer", "linear", 33, True)])
+def test_many_rows(rows, d, kind, act, per_gate, bias):
+    """Enough rows for every thread group to walk several.  (Column sums of 5000 rows: each walker adds at most 34 of them, the
+    walkers' sums are added over at most 2 x 148: 2e-6 of the sum of magnitudes holds as for fewer rows.)"""
+    import paper_2207_02849_b200 as bt
+    for tx, ty in ((F, F), (BF, BF), (F, HF)):
+        q = _problem(rows + d, rows, d, tx, ty, act, per_gate, bias)
+        args = (d, kind, kind, act, per_gate, bias, 1e-5)
+        x_out, u = torch.full_like(q["x"], float("nan")), torch.full_like(q["y"], float("nan"))
+        bt.betty_block_norm(_cfg(bt, *args), q["params"], q["x"], q["y"], q["gate"], x_out, u)
+        _check_forward(q, args, x_out, u)
+        _check_backward(bt, q, args)
+
+
+def test_a_nan_row_among_many_stays_by_itself():
+    import paper_2207_02849_b200 as bt
+    for d in (2000, 2002, 2051):
+        q = _problem(1, 900, d, F, F, "linear", 1, False)
+        q["x"][450, 3] = float("nan")
+        q["y"][300, d - 1] = float("inf")
+        cfg = _cfg(bt, d, "rms", "rms", "linear", 1, False, 1e-6)
+        ws = bt.Workspace.of_bytes(bt.betty_block_norm_workspace_size(cfg, 900))
+        outs = [torch.full_like(q[k], float("nan")) for k in ("x", "y", "gate", "params")]
+        bt.betty_block_norm_backward(cfg, q["params"], q["x"], q["y"], q["gate"], q["du"], q["dxo"], *outs, ws)
+        keep = [i for i in range(900) if i not in (300, 450)]
+        for t in outs[:3]:
+            assert bool(torch.isfinite(t[keep]).all())
+        assert bool(torch.isnan(outs[0][450]).all())
+
+
 @pytest.mark.parametrize("tx,ty", TYPES)
 @pytest.mark.parametrize("pre,post", list(itertools.product(ref.KINDS, ref.KINDS)))
 def test_every_pair_of_norms_and_types(tx, ty, pre, post):
