@@ -34,15 +34,8 @@ __global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
     }
   };
   int half = 0, slot = 0;
-  if constexpr (PIPE) {
-    for (int i = 0; i < (a.ahead + 1) * R && CH * 8 * G > d; ++i) {
-      char* p = ring + i * a.slot_bytes;
-      clear_beyond<GR, CH, TX>(p, t, G, d);
-      if (has_y) clear_beyond<GR, CH, TY>(p + bytes_x, t, G, d);
-      if (has_g) clear_beyond<GR, CH, TY>(p + bytes_x + bytes_y, t, G, d);
-    }
+  if (PIPE)
     for (int i = 0; i < a.ahead; ++i) fetch(row + i * step, i);
-  }
   float wp[CH][8], ws[CH][8], bp[GENERAL ? CH : 1][8], bs[GENERAL ? CH : 1][8];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -364,7 +357,8 @@ extern "C" betty_status betty_block_norm_backward(const betty_block_norm_cfg* cf
   Arena arena(ws, ws_bytes);
   const Layout l = backward_layout(cfg, rows, cfg->x_dtype, cfg->y_dtype, granule);
   const int blocks = backward_blocks(rows, l);
-  a.walkers = blocks * (l.threads / l.G);
+  a.walkers = blocks * (l.threads / l.G);         // as many as there are rows at most: no share is empty
+  if (a.walkers > rows) a.walkers = rows > 0 ? (int)rows : 1;
   a.col_partials = arena.alloc<float>((size_t)blocks * quantities(cfg) * d);
   if (gated && cfg->rows_per_gate > 1)
     a.gate_partials = arena.alloc<float>((size_t)(a.walkers + (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate) * d);

@@ -112,33 +112,24 @@ __device__ __forceinline__ void load_param8(float (&v)[8], const float* row, int
 // bytes at a time), a few rows before their use: no registers are held by data in flight, and as nobody reads another
 // thread's slots, waiting for one's own copies is all the synchronisation there is.
 // A slot holds CH * 8 values of every stream, interleaved over the G threads so that a warp's accesses are contiguous.
+// Columns beyond d are filled with zeros (a copy of no bytes), so that reading a slot needs no comparison.
 template <int GR, int CH, typename T>
 __device__ __forceinline__ void copy_row(char* slot, const T* row, int t, int G, int d) {
   constexpr int bytes = GR * (int)sizeof(T), piece = bytes >= 16 ? 16 : 4, per = bytes / piece;
   static_assert(bytes % 4 == 0, "cp.async moves 4 or 16 bytes");
+  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot) + t * piece;
 #pragma unroll
   for (int n = 0; n < CH * 8 / GR; ++n) {
-    const int j = (n * G + t) * GR;
-    if (j < d) {
+    const int j = (n * G + t) * GR, size = j < d ? piece : 0;
+    const char* src = (const char*)(row + (j < d ? j : 0));
 #pragma unroll
-      for (int i = 0; i < per; ++i) {
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot + (((n * per + i) * G + t) * piece));
-        const char* src = (const char*)(row + j) + i * piece;
-        if (piece == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-        else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-      }
+    for (int i = 0; i < per; ++i) {
+      if (piece == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (n * per + i) * G * piece), "l"(src + i * piece), "r"(size) : "memory");
+      else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + (n * per + i) * G * piece), "l"(src + i * piece), "r"(size) : "memory");
     }
   }
-}
-// zeros for the columns beyond d, written once: no copy touches them, so that reading a slot needs no comparison
-template <int GR, int CH, typename T>
-__device__ __forceinline__ void clear_beyond(char* slot, int t, int G, int d) {
-  constexpr int words = GR * (int)sizeof(T) / 4;
-  for (int n = 0; n < CH * 8 / GR; ++n)
-    if ((n * G + t) * GR >= d) {
-      constexpr int bytes = GR * (int)sizeof(T), piece = bytes >= 16 ? 16 : 4;
-      for (int i = 0; i < words; ++i) *(uint32_t*)(slot + (n * (bytes / piece) + i * 4 / piece) * G * piece + t * piece + i * 4 % piece) = 0u;
-    }
 }
 template <int GR, typename T>
 __device__ __forceinline__ void read_slot(float (&o)[8], const char* slot, int c, int t, int G) {
@@ -228,6 +219,37 @@ __device__ __forceinline__ void row_sums(float (&v)[NV], float* red, int& half, 
   }
 }
 
+// ---- pairs of fp32 values: one instruction for two products or sums ----
+struct alignas(8) f2 { float x, y; };
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ f2 both(float v) { return f2{v, v}; }
+__device__ __forceinline__ void pairs(f2 (&o)[4], const float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = f2{v[2 * k], v[2 * k + 1]};
+}
+__device__ __forceinline__ void singles(float (&o)[8], const f2 (&v)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) { o[2 * k] = v[k].x; o[2 * k + 1] = v[k].y; }
+}
+
 __device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
 
 struct Args {
@@ -251,7 +273,7 @@ struct Args {
   void* dg; int64_t lddg;
   float* gate_partials;                // [walkers + gates, d] (gates of several rows)
   float* col_partials;                 // [blocks, quantities, d]
-  int walkers;                         // row-holding thread groups of the whole grid
+  int walkers;                         // thread groups with rows, at most one per row
 };
 
 // How a call's rows are laid over threads.

@@ -18,55 +18,29 @@ namespace blocknorm {
 __host__ __device__ __forceinline__ int64_t share_start(int64_t w, int64_t rows, int64_t walkers) { return w * rows / walkers; }
 __device__ __forceinline__ int64_t walker_of(int64_t row, int64_t rows, int64_t walkers) { return ((row + 1) * walkers - 1) / rows; }
 
-// dm of one chunk, 8 fp32 values, kept in the thread's own slots of x' and du: where x' is fp32 each in its column's place,
-// else values 0 .. 3 in the 16 bytes of x' and 4 .. 7 in those of du, or (granules of two) a granule's two values in its
-// words of x' and of du.  Columns beyond d keep their zeros.
-template <int GR, typename TX>
-__device__ __forceinline__ int park_at(int at_u, int c, int k, int t, int G) {      // k: a multiple of 4 (GR = 8) or any
-  if (GR == 8) return sizeof(TX) == 4 ? ((c * 2 + k / 4) * G + t) * 16 : (c * G + t) * 16 + (k / 4) * at_u;
-  return sizeof(TX) == 4 ? ((c * 8 + k) * G + t) * 4 : ((c * 4 + k / 2) * G + t) * 4 + (k % 2) * at_u;
-}
-template <int GR, typename TX>
-__device__ __forceinline__ void park(char* slot, int at_u, const float (&v)[8], int c, int t, int G, int d) {
-  static_assert(GR == 8 || sizeof(TX) == 4 || GR == 2, "16-bit rows are fetched in granules of 8 or 2");
-#pragma unroll
-  for (int k = 0; k < 8; k += GR == 8 ? 4 : 1)
-    if (column<GR>(c, k, t, G) < d) {
-      char* at = slot + park_at<GR, TX>(at_u, c, k, t, G);
-      if constexpr (GR == 8) *(float4*)at = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
-      else *(float*)at = v[k];
-    }
-}
-template <int GR, typename TX>
-__device__ __forceinline__ void unpark(float (&v)[8], const char* slot, int at_u, int c, int t, int G) {
-#pragma unroll
-  for (int k = 0; k < 8; k += GR == 8 ? 4 : 1) {
-    const char* at = slot + park_at<GR, TX>(at_u, c, k, t, G);
-    if constexpr (GR == 8) {
-      const float4 w = *(const float4*)at;
-      v[k] = w.x; v[k + 1] = w.y; v[k + 2] = w.z; v[k + 3] = w.w;
-    } else {
-      v[k] = *(const float*)at;
-    }
-  }
-}
-
 // Each walker (thread group) takes a contiguous share of the rows, so that the column sums stay in its registers; it writes
-// them once, and k_backward_sums adds the blocks' sums in order.  Per row: the norms' sums over the fetched values, then dX
-// (and with it everything that hangs off dm), then dy.  dm waits for its row's sum in the slots of x' and du, which are read
-// by then.  A gate shared by rows needs one sum H = sum dX m per gate: dg = a'(g) s w_post H and A gains a(g) H when the
-// walker leaves the gate, so A waits in shared memory.
+// them once, and k_backward_sums adds the blocks' sums in order.  A row's chain is what bounds this kernel, so with RMS
+// norms a row costs one sum over its threads: with c = a w_post s y the mean of dm m is a combination of sums that do not
+// wait for dX,
+//
+//   <dm m> d = q (sum dx' c + r sum dn0 c - r^2 proj sum x' c),   dn0 = du w_pre,   proj = <dn n>
+//
+// and then dX, dm, dy and all products of the row come out in one go.  Layer norms take the means first and <dm>, <dm m>
+// from dm itself: their combination would cancel two differences that are scaled up by 1 / sigma each where rows are flat.
+// A gate shared by rows needs one sum H = sum dX m per gate: dg = a'(g) s w_post H, and A gains a(g) H when the walker
+// leaves the gate, so A waits in shared memory.
 template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   __shared__ float red[2 * RED_VALUES * 16];
-  extern __shared__ __align__(16) char slots[];
+  extern __shared__ __align__(16) char slots[];      // fetched rows; G = 32: at the end the warps' column sums
   pdl_enter();
   const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G, subs = blockDim.x / G;
   const int64_t walker = (int64_t)blockIdx.x * subs + sub;
-  const int64_t first = share_start(walker, a.rows, a.walkers), last = share_start(walker + 1, a.rows, a.walkers);
+  const int64_t first = walker < a.walkers ? share_start(walker, a.rows, a.walkers) : a.rows;
+  const int64_t last = walker < a.walkers ? share_start(walker + 1, a.rows, a.walkers) : a.rows;
   const bool has_y = a.y != nullptr, has_g = a.gate != BETTY_GATE_NONE, has_u = a.du != nullptr, has_o = a.dxo != nullptr;
   const bool pre_layer = GENERAL && a.pre == BETTY_NORM_LAYER && has_u, post_layer = GENERAL && a.post == BETTY_NORM_LAYER && has_y;
-  const bool shared_gate = has_g && a.per_gate > 1, row_gate = has_g && !shared_gate;
+  const bool shared_gate = has_g && a.per_gate > 1, row_gate = has_g && !shared_gate, bias = GENERAL && a.bias;
   const float* w_pre = a.params;
   const float* w_post = a.params + d;
   const float* s_res = a.params + 2 * (int64_t)d;
@@ -76,77 +50,97 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   char* ring = slots + (size_t)sub * (a.ahead + 1) * a.slot_bytes;
   // [A (, B)][value][thread] of a walker whose gates are shared
   float* acc_s = (float*)(slots + (size_t)subs * (a.ahead + 1) * a.slot_bytes) + (size_t)sub * (GENERAL ? 2 : 1) * CH * 8 * G + t;
+  const TX* xs = (const TX*)a.x;
+  const TX* os = (const TX*)a.dxo;
+  const TY* ys = (const TY*)a.y;
+  const TY* us = (const TY*)a.du;
+  const TY* gs = (const TY*)a.g;
   auto fetch = [&](int64_t r, int slot) {
     if constexpr (PIPE) {
       if (r < last) {
         char* p = ring + slot * a.slot_bytes;
         if (has_u) {
-          copy_row<GR, CH>(p, (const TX*)a.x + r * a.ldx, t, G, d);
-          copy_row<GR, CH>(p + at_u, (const TY*)a.du + r * a.lddu, t, G, d);
+          copy_row<GR, CH>(p, xs + r * a.ldx, t, G, d);
+          copy_row<GR, CH>(p + at_u, us + r * a.lddu, t, G, d);
         }
-        if (has_o) copy_row<GR, CH>(p + at_o, (const TX*)a.dxo + r * a.lddxo, t, G, d);
-        if (has_y) copy_row<GR, CH>(p + at_y, (const TY*)a.y + r * a.ldy, t, G, d);
-        if (row_gate) copy_row<GR, CH>(p + at_g, (const TY*)a.g + r * a.ldg, t, G, d);
+        if (has_o) copy_row<GR, CH>(p + at_o, os + r * a.lddxo, t, G, d);
+        if (has_y) copy_row<GR, CH>(p + at_y, ys + r * a.ldy, t, G, d);
+        if (row_gate) copy_row<GR, CH>(p + at_g, gs + r * a.ldg, t, G, d);
       }
       copies_commit();
     }
   };
   // one chunk of a stream of the present row
-  char* p = nullptr;
+  const char* p = nullptr;
   int64_t row = first;
-  auto get = [&](auto* base, int64_t ld, int at, int c, float (&v)[8]) {
+  auto get = [&](auto* base, int64_t ld, int at, int c, f2 (&o)[4]) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(base)>::type>::type T;
+    float v[8];
     if constexpr (PIPE) read_slot<GR, T>(v, p + at, c, t, G);
     else load8<GR, T>(v, base + row * ld, c, t, G, d);
+    pairs(o, v);
+  };
+  auto param = [&](const float* base, int c, f2 (&o)[4]) {
+    float v[8];
+    load_param8<GR>(v, base, c, t, G, d);
+    pairs(o, v);
   };
   int half = 0, slot = 0;
-  if constexpr (PIPE) {
-    for (int i = 0; i <= a.ahead && CH * 8 * G > d; ++i) {
-      char* s = ring + i * a.slot_bytes;
-      clear_beyond<GR, CH, TX>(s, t, G, d);
-      clear_beyond<GR, CH, TX>(s + at_o, t, G, d);
-      clear_beyond<GR, CH, TY>(s + at_y, t, G, d);
-      clear_beyond<GR, CH, TY>(s + at_u, t, G, d);
-      if (row_gate) clear_beyond<GR, CH, TY>(s + at_g, t, G, d);
-    }
+  if (PIPE)
     for (int i = 0; i < a.ahead; ++i) fetch(first + i, i);
-  }
-  // w_pre and w_post * s stay in registers (CH <= 2) or are read again
-  constexpr bool KEEP = CH <= 2;
-  float kp[KEEP ? CH : 1][8], kws[KEEP ? CH : 1][8], mask[GENERAL ? CH : 1][8 / GR];
-  auto params_of = [&](int c, float (&wp)[8], float (&ws)[8]) {
-    float s[8];
-    load_param8<GR>(wp, w_pre, c, t, G, d);
-    load_param8<GR>(ws, w_post, c, t, G, d);
-    load_param8<GR>(s, s_res, c, t, G, d);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) ws[k] *= s[k];
-  };
-  float accC[CH][8], accA[CH][8], accD[GENERAL ? CH : 1][8], accB[GENERAL ? CH : 1][8];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    if constexpr (KEEP) params_of(c, kp[c], kws[c]);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      accC[c][k] = 0.f; accA[c][k] = 0.f;
-      if (GENERAL) { accD[c][k] = 0.f; accB[c][k] = 0.f; }
-      if (shared_gate) {
-        acc_s[(c * 8 + k) * G] = 0.f;
-        if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = 0.f;
-      }
-    }
-    if (GENERAL)
-#pragma unroll
-      for (int k = 0; k < 8; k += GR) mask[c][k / GR] = column<GR>(c, k, t, G) < d ? 1.f : 0.f;   // 0 beyond the row
-  }
-  const TX* xs = (const TX*)a.x;
-  const TX* os = (const TX*)a.dxo;
-  const TY* ys = (const TY*)a.y;
-  const TY* us = (const TY*)a.du;
+
   int64_t gate = 0, gate_end = 0;          // of a shared gate: the present row's, and the row after its last
   if (shared_gate && first < last) {
     gate = (unsigned)first / a.per_gate;
     gate_end = (gate + 1) * a.per_gate;
+  }
+  // w_pre, and e = w_post s (times a(g) of a shared gate): kept in registers, or (wide rows) formed where they are used
+  constexpr bool KEEP = CH <= 2;
+  f2 kw[KEEP ? CH : 1][4], ke[KEEP ? CH : 1][4];
+  auto make_e = [&](int c, f2 (&e)[4]) {
+    f2 s[4];
+    param(w_post, c, e);
+    param(s_res, c, s);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = mul2(e[k], s[k]);
+    if (shared_gate) {
+      float g[8];
+      load8<GR, TY>(g, gs + gate * a.ldg, c, t, G, d);
+      if (a.gate == BETTY_GATE_SIGMOID)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) g[k] = sigmoid_f(g[k]);
+      pairs(s, g);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] = mul2(e[k], s[k]);
+    }
+  };
+  auto coefficients = [&](int c, f2 (&w)[4], f2 (&e)[4]) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) { w[k] = kw[KEEP ? c : 0][k]; e[k] = ke[KEEP ? c : 0][k]; }
+    } else {
+      param(w_pre, c, w);
+      make_e(c, e);
+    }
+  };
+  f2 accC[CH][4], accA[CH][4], accD[GENERAL ? CH : 1][4], accB[GENERAL ? CH : 1][4], mask[GENERAL ? CH : 1][4];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if constexpr (KEEP) { param(w_pre, c, kw[c]); make_e(c, ke[c]); }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      accC[c][k] = accA[c][k] = both(0.f);
+      if (GENERAL) {
+        accD[c][k] = accB[c][k] = both(0.f);
+        mask[c][k] = f2{column<GR>(c, 2 * k, t, G) < d ? 1.f : 0.f, column<GR>(c, 2 * k + 1, t, G) < d ? 1.f : 0.f};   // 0 beyond the row
+      }
+    }
+    if (shared_gate)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        acc_s[(c * 8 + k) * G] = 0.f;
+        if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = 0.f;
+      }
   }
   for (; row < last; ++row) {
     if (PIPE) {
@@ -155,281 +149,302 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       p = ring + slot * a.slot_bytes;
       slot = slot == a.ahead ? 0 : slot + 1;
     }
-    float mean_dn = 0.f, mx = 0.f, my = 0.f;
+    float mx = 0.f, my = 0.f;
     if (pre_layer || post_layer) {
-      float v[3] = {0.f, 0.f, 0.f};
+      f2 sx = both(0.f), sy = both(0.f);
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
+        f2 v[4];
         if (pre_layer) {
-          float x[8], du[8], w[8], ws[8];
-          get(xs, a.ldx, 0, c, x);
-          get(us, a.lddu, at_u, c, du);
-          if constexpr (!KEEP) params_of(c, w, ws);
+          get(xs, a.ldx, 0, c, v);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) { v[0] += x[k]; v[2] = fmaf(du[k], KEEP ? kp[KEEP ? c : 0][k] : w[k], v[2]); }
+          for (int k = 0; k < 4; ++k) sx = add2(sx, v[k]);
         }
         if (post_layer) {
-          float y[8];
-          get(ys, a.ldy, at_y, c, y);
+          get(ys, a.ldy, at_y, c, v);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) v[1] += y[k];
+          for (int k = 0; k < 4; ++k) sy = add2(sy, v[k]);
         }
       }
-      row_sums<3>(v, red, half, G, t);
-      if (pre_layer) { mx = v[0] * a.inv_d; mean_dn = v[2] * a.inv_d; }
+      float v[2] = {sx.x + sx.y, sy.x + sy.y};
+      row_sums<2>(v, red, half, G, t);
+      if (pre_layer) mx = v[0] * a.inv_d;
       if (post_layer) my = v[1] * a.inv_d;
     }
-    float r = 1.f, q = 1.f, proj = 0.f;
+    // x2, dn0 x, y2, and dx' c, dn0 c, x c; layer norms dn0
+    constexpr int NS = GENERAL ? 4 : 6;
+    float S[NS];
     {
-      float v[3] = {0.f, 0.f, 0.f};
+      f2 s2[NS];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) s2[i] = both(0.f);
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
+        f2 x[4], u[4], w[4], e[4];
+        coefficients(c, w, e);
         if (has_u) {
-          float x[8], du[8], w[8], ws[8];
           get(xs, a.ldx, 0, c, x);
-          get(us, a.lddu, at_u, c, du);
-          if constexpr (!KEEP) params_of(c, w, ws);
+          get(us, a.lddu, at_u, c, u);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            if (GENERAL) x[k] = fmaf(-mx, mask[c][k / GR], x[k]);
-            v[0] = fmaf(x[k], x[k], v[0]);
-            v[1] = fmaf(du[k] * (KEEP ? kp[KEEP ? c : 0][k] : w[k]), x[k], v[1]);
+          for (int k = 0; k < 4; ++k) {
+            if (GENERAL) x[k] = fma2(both(-mx), mask[c][k], x[k]);
+            u[k] = mul2(u[k], w[k]);
+            s2[0] = fma2(x[k], x[k], s2[0]);
+            s2[1] = fma2(u[k], x[k], s2[1]);
+            if (GENERAL) s2[3] = add2(s2[3], u[k]);
           }
         }
         if (has_y) {
-          float y[8];
+          f2 y[4];
           get(ys, a.ldy, at_y, c, y);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            if (GENERAL) y[k] = fmaf(-my, mask[c][k / GR], y[k]);
-            v[2] = fmaf(y[k], y[k], v[2]);
+          for (int k = 0; k < 4; ++k) {
+            if (GENERAL) y[k] = fma2(both(-my), mask[c][k], y[k]);
+            s2[2] = fma2(y[k], y[k], s2[2]);
+          }
+          if constexpr (!GENERAL) {
+            if (row_gate) {
+              f2 g[4];
+              get(gs, a.ldg, at_g, c, g);
+              if (a.gate == BETTY_GATE_SIGMOID)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) g[k] = f2{sigmoid_f(g[k].x), sigmoid_f(g[k].y)};
+#pragma unroll
+              for (int k = 0; k < 4; ++k) e[k] = mul2(e[k], g[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = mul2(y[k], e[k]);               // c
+            if (has_u)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                s2[4] = fma2(u[k], y[k], s2[4]);
+                s2[5] = fma2(x[k], y[k], s2[5]);
+              }
+            if (has_o) {
+              f2 o[4];
+              get(os, a.lddxo, at_o, c, o);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) s2[3] = fma2(o[k], y[k], s2[3]);
+            }
           }
         }
       }
-      row_sums<3>(v, red, half, G, t);
-      if (a.pre != BETTY_NORM_NONE && has_u) {
-        r = rsqrtf(fmaf(v[0], a.inv_d, a.eps));
-        proj = r * v[1] * a.inv_d;
-      }
-      if (a.post != BETTY_NORM_NONE && has_y) q = rsqrtf(fmaf(v[2], a.inv_d, a.eps));
+#pragma unroll
+      for (int i = 0; i < NS; ++i) S[i] = s2[i].x + s2[i].y;
+      row_sums<NS>(S, red, half, G, t);
     }
-    float v[2] = {0.f, 0.f};
-    // dm of the row: in registers where a thread holds one chunk (or nothing is fetched ahead), else over x' and du
-    constexpr bool PARK = PIPE && CH > 1;
-    float dm[PARK ? 1 : CH][8];
+    float r = 1.f, q = 1.f, cx = 0.f, mean_dn = 0.f;      // dX = dx' + r (dn0 - <dn>) + cx (x - mean)
+    if (a.pre != BETTY_NORM_NONE && has_u) {
+      r = rsqrtf(fmaf(S[0], a.inv_d, a.eps));
+      cx = -r * r * r * S[1] * a.inv_d;
+      if (pre_layer) mean_dn = S[3] * a.inv_d;
+    }
+    float pm = 0.f;
+    if (a.post != BETTY_NORM_NONE && has_y) {
+      q = rsqrtf(fmaf(S[2], a.inv_d, a.eps));
+      if constexpr (!GENERAL) pm = q * fmaf(r, S[NS - 2], fmaf(cx, S[NS - 1], S[3])) * a.inv_d;
+    }
+    const f2 r2 = both(r), cx2 = both(cx), q2 = both(q), pq2 = both(-pm * q), dn2 = both(-mean_dn);
+    f2 dm[GENERAL ? CH : 1][4], sm = both(0.f), sd = both(0.f);       // layer norms: dm, sum dm m, sum dm
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float dX[8], w[8], ws[8];
-      if constexpr (!KEEP) params_of(c, w, ws);
+      f2 dX[4], w[4], e[4];
+      float out[8];
+      coefficients(c, w, e);
       if (has_o) get(os, a.lddxo, at_o, c, dX);
       else
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dX[k] = 0.f;
+        for (int k = 0; k < 4; ++k) dX[k] = both(0.f);
       if (has_u) {
-        float x[8], du[8];
+        f2 x[4], u[4];
         get(xs, a.ldx, 0, c, x);
-        get(us, a.lddu, at_u, c, du);
+        get(us, a.lddu, at_u, c, u);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float n = (GENERAL ? fmaf(-mx, mask[c][k / GR], x[k]) : x[k]) * r;
-          accC[c][k] = fmaf(du[k], n, accC[c][k]);
-          if (GENERAL) accD[c][k] += du[k];
-          float dn = fmaf(-n, proj, du[k] * (KEEP ? kp[KEEP ? c : 0][k] : w[k]));
-          if (GENERAL) dn -= mean_dn;
-          dX[k] = fmaf(r, dn, dX[k]);
+        for (int k = 0; k < 4; ++k) {
+          if (GENERAL) x[k] = fma2(both(-mx), mask[c][k], x[k]);
+          dX[k] = fma2(x[k], cx2, dX[k]);
+          f2 dn = mul2(u[k], w[k]);
+          if (GENERAL) dn = add2(dn, dn2);          // subtracted before the scaling: r can be large where a row is flat
+          dX[k] = fma2(dn, r2, dX[k]);
+          if (GENERAL) {
+            accD[c][k] = add2(accD[c][k], u[k]);
+          }
+          accC[c][k] = fma2(u[k], mul2(x[k], r2), accC[c][k]);
         }
       }
-      store8<GR>((TX*)a.dx + row * a.lddx, dX, c, t, G, d);
+      singles(out, dX);
+      store8<GR>((TX*)a.dx + row * a.lddx, out, c, t, G, d);
       if (!has_y) continue;
-      float y[8], g[8], base[8];
-      get(ys, a.ldy, at_y, c, y);
-      if (shared_gate) load8<GR, TY>(g, (const TY*)a.g + gate * a.ldg, c, t, G, d);
-      else if (row_gate) get((const TY*)a.g, a.ldg, at_g, c, g);
+      f2 m[4];
+      get(ys, a.ldy, at_y, c, m);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        y[k] = (GENERAL ? fmaf(-my, mask[c][k / GR], y[k]) : y[k]) * q;      // m
-        if constexpr (KEEP) ws[k] = kws[KEEP ? c : 0][k];
+      for (int k = 0; k < 4; ++k) {
+        if (GENERAL) m[k] = fma2(both(-my), mask[c][k], m[k]);
+        m[k] = mul2(m[k], q2);
       }
-      if (has_g) {
-        float slope[8];
-        if (a.gate == BETTY_GATE_SIGMOID) {
+      if (row_gate) {
+        f2 g[4], z[4];
+        get(gs, a.ldg, at_g, c, g);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) { g[k] = sigmoid_f(g[k]); slope[k] = g[k] * (1.f - g[k]); }
-        } else {
+        for (int k = 0; k < 4; ++k) z[k] = mul2(m[k], e[k]);
+        if (bias) {
+          f2 b[4], s[4];
+          param(b_post, c, b);
+          param(s_res, c, s);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) slope[k] = 1.f;
+          for (int k = 0; k < 4; ++k) z[k] = fma2(b[k], s[k], z[k]);
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) base[k] = dX[k] * g[k];
-        if (shared_gate) {
+        for (int k = 0; k < 4; ++k) z[k] = mul2(z[k], dX[k]);
+        if (a.gate == BETTY_GATE_SIGMOID)
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            accA[c][k] = fmaf(dX[k], y[k], accA[c][k]);
-            if (GENERAL) accB[c][k] += dX[k];
+          for (int k = 0; k < 4; ++k) {
+            g[k] = f2{sigmoid_f(g[k].x), sigmoid_f(g[k].y)};
+            z[k] = mul2(z[k], fma2(mul2(g[k], both(-1.f)), g[k], g[k]));
           }
+        singles(out, z);
+        store8<GR>((TY*)a.dg + row * a.lddg, out, c, t, G, d);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          dX[k] = mul2(dX[k], g[k]);
+          if (GENERAL) accB[c][k] = add2(accB[c][k], dX[k]);
+        }
+      } else if (GENERAL) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) accB[c][k] = add2(accB[c][k], dX[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        accA[c][k] = fma2(dX[k], m[k], accA[c][k]);
+        dX[k] = mul2(dX[k], e[k]);                                 // dm
+        if constexpr (GENERAL) {
+          dm[c][k] = dX[k];
+          sm = fma2(dX[k], m[k], sm);
+          sd = add2(sd, dX[k]);
         } else {
-          float dg[8];
+          const f2 o = fma2(dX[k], q2, mul2(m[k], pq2));           // q (dm - m <dm m>)
+          out[2 * k] = o.x; out[2 * k + 1] = o.y;
+        }
+      }
+      if (!GENERAL) store8<GR>((TY*)a.dy + row * a.lddy, out, c, t, G, d);
+    }
+    if constexpr (GENERAL) {
+      if (has_y) {
+        float v[2] = {sm.x + sm.y, sd.x + sd.y};
+        if (a.post != BETTY_NORM_NONE) row_sums<2>(v, red, half, G, t);
+        const float mean = post_layer ? v[1] * a.inv_d : 0.f;
+        pm = a.post != BETTY_NORM_NONE ? v[0] * a.inv_d : 0.f;
 #pragma unroll
-          for (int k = 0; k < 8; ++k) dg[k] = y[k] * ws[k];
-          if (GENERAL && a.bias) {
-            float b[8], s[8];
-            load_param8<GR>(b, b_post, c, t, G, d);
-            load_param8<GR>(s, s_res, c, t, G, d);
+        for (int c = 0; c < CH; ++c) {
+          f2 m[4];
+          float out[8];
+          get(ys, a.ldy, at_y, c, m);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) dg[k] = fmaf(b[k], s[k], dg[k]);
+          for (int k = 0; k < 4; ++k) {
+            m[k] = mul2(fma2(both(-my), mask[c][k], m[k]), q2);
+            const f2 o = mul2(fma2(m[k], both(-pm), add2(dm[c][k], both(-mean))), q2);      // q (dm - <dm> - m <dm m>)
+            out[2 * k] = o.x; out[2 * k + 1] = o.y;
           }
-#pragma unroll
-          for (int k = 0; k < 8; ++k) dg[k] *= dX[k] * slope[k];
-          store8<GR>((TY*)a.dg + row * a.lddg, dg, c, t, G, d);
+          store8<GR>((TY*)a.dy + row * a.lddy, out, c, t, G, d);
         }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) base[k] = dX[k];
-      }
-      if (!shared_gate)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          accA[c][k] = fmaf(base[k], y[k], accA[c][k]);
-          if (GENERAL) accB[c][k] += base[k];
-        }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        base[k] *= ws[k];                                                    // dm
-        v[0] = fmaf(base[k], y[k], v[0]);
-        if (GENERAL) v[1] += base[k];
-      }
-      if constexpr (PARK) {
-        park<GR, TX>(p, at_u, base, c, t, G, d);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dm[PARK ? 0 : c][k] = base[k];
       }
     }
-    if (!has_y) continue;
-    if (a.post != BETTY_NORM_NONE) {
-      if (GENERAL) row_sums<2>(v, red, half, G, t);
-      else {
-        float one[1] = {v[0]};
-        row_sums<1>(one, red, half, G, t);
-        v[0] = one[0];
-      }
-    }
-    const float pm = a.post != BETTY_NORM_NONE ? v[0] * a.inv_d : 0.f, mean_dm = post_layer ? v[1] * a.inv_d : 0.f;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      float o[8], y[8];
-      get(ys, a.ldy, at_y, c, y);
-      if constexpr (PARK) unpark<GR, TX>(o, p, at_u, c, t, G);
-      else
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = dm[PARK ? 0 : c][k];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float m = (GENERAL ? fmaf(-my, mask[c][k / GR], y[k]) : y[k]) * q;
-        o[k] = fmaf(-m, pm, o[k]);
-        if (GENERAL) o[k] -= mean_dm;
-        o[k] *= q;
-      }
-      store8<GR>((TY*)a.dy + row * a.lddy, o, c, t, G, d);
-    }
-    if (shared_gate && (row + 1 == gate_end || row + 1 == last)) {           // the walker leaves the gate
+    if (has_y && shared_gate && (row + 1 == gate_end || row + 1 == last)) {           // the walker leaves the gate
       const int64_t g0 = gate * a.per_gate, g1 = gate_end < a.rows ? gate_end : a.rows;
       const bool whole = g0 >= first && g1 <= last;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        float g[8], dg[8], w[8], ws[8];
-        if constexpr (!KEEP) params_of(c, w, ws);
-        load8<GR, TY>(g, (const TY*)a.g + gate * a.ldg, c, t, G, d);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dg[k] = accA[c][k] * (KEEP ? kws[KEEP ? c : 0][k] : ws[k]);
-        if (GENERAL && a.bias) {
-          float b[8], s[8];
-          load_param8<GR>(b, b_post, c, t, G, d);
-          load_param8<GR>(s, s_res, c, t, G, d);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) dg[k] = fmaf(b[k] * s[k], accB[c][k], dg[k]);
-        }
+        float g[8], dg[8], w[8], s[8], b[8];
+        load8<GR, TY>(g, gs + gate * a.ldg, c, t, G, d);
+        load_param8<GR>(w, w_post, c, t, G, d);
+        load_param8<GR>(s, s_res, c, t, G, d);
+        if (bias) load_param8<GR>(b, b_post, c, t, G, d);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
+          const float H = k & 1 ? accA[c][k / 2].y : accA[c][k / 2].x, E = !GENERAL ? 0.f : (k & 1 ? accB[GENERAL ? c : 0][k / 2].y : accB[GENERAL ? c : 0][k / 2].x);
+          dg[k] = s[k] * (bias ? fmaf(b[k], E, w[k] * H) : w[k] * H);
           if (a.gate == BETTY_GATE_SIGMOID) {
             g[k] = sigmoid_f(g[k]);
             dg[k] *= g[k] * (1.f - g[k]);
           }
-          acc_s[(c * 8 + k) * G] = fmaf(g[k], accA[c][k], acc_s[(c * 8 + k) * G]);
-          accA[c][k] = 0.f;
-          if (GENERAL) {
-            acc_s[(CH * 8 + c * 8 + k) * G] = fmaf(g[k], accB[c][k], acc_s[(CH * 8 + c * 8 + k) * G]);
-            accB[c][k] = 0.f;
-          }
+          acc_s[(c * 8 + k) * G] = fmaf(g[k], H, acc_s[(c * 8 + k) * G]);
+          if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = fmaf(g[k], E, acc_s[(CH * 8 + c * 8 + k) * G]);
         }
         if (whole) store8<GR>((TY*)a.dg + gate * a.lddg, dg, c, t, G, d);
         else store8<GR>(a.gate_partials + (walker + gate) * d, dg, c, t, G, d);
       }
       ++gate;
       gate_end += a.per_gate;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          accA[c][k] = both(0.f);
+          if (GENERAL) accB[c][k] = both(0.f);
+        }
+        if constexpr (KEEP)
+          if (row + 1 < last) make_e(c, ke[c]);
+      }
     }
   }
-  const int nq = a.bias ? 4 : 2;
-  float* out = a.col_partials + (int64_t)blockIdx.x * nq * d;
   if (shared_gate)
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        accA[c][k] = acc_s[(c * 8 + k) * G];
-        if (GENERAL) accB[c][k] = acc_s[(CH * 8 + c * 8 + k) * G];
+      for (int k = 0; k < 4; ++k) {
+        accA[c][k] = f2{acc_s[(c * 8 + 2 * k) * G], acc_s[(c * 8 + 2 * k + 1) * G]};
+        if (GENERAL) accB[c][k] = f2{acc_s[(CH * 8 + c * 8 + 2 * k) * G], acc_s[(CH * 8 + c * 8 + 2 * k + 1) * G]};
       }
-  if (G > 32) {
+  const int nq = a.bias ? 4 : 2;
+  float* out = a.col_partials + (int64_t)blockIdx.x * nq * d;
+  float* combine = (float*)slots;             // G = 32, a warp per walker: the block's warps are added in order
+  constexpr int W = CH * 256;                 // columns a warp can hold
+  for (int qn = 0; qn < nq; ++qn, out += d) {
+    if (G == 32) __syncthreads();
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      store8<GR>(out, accC[c], c, t, G, d);
-      store8<GR>(out + d, accA[c], c, t, G, d);
-      if (GENERAL && a.bias) {
-        store8<GR>(out + 2 * (int64_t)d, accD[c], c, t, G, d);
-        store8<GR>(out + 3 * (int64_t)d, accB[c], c, t, G, d);
-      }
+      float v[8];
+      if (qn == 0) singles(v, accC[c]);
+      else if (!GENERAL || qn == 1) singles(v, accA[c]);
+      else singles(v, qn == 2 ? accD[GENERAL ? c : 0] : accB[GENERAL ? c : 0]);
+      if (G > 32) store8<GR>(out, v, c, t, G, d);
+      else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) combine[sub * W + column<GR>(c, k, t, 32)] = v[k];
     }
-  } else {                                    // a warp per walker: the block's warps are added in order through shared memory
-    float* combine = (float*)slots;
-    constexpr int W = CH * 256;               // columns a warp can hold
-    for (int qn = 0; qn < nq; ++qn) {
-      __syncthreads();
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float s = qn == 0 ? accC[c][k] : accA[c][k];
-          if (GENERAL && qn >= 2) s = qn == 2 ? accD[c][k] : accB[c][k];
-          combine[sub * W + column<GR>(c, k, t, 32)] = s;
-        }
+    if (G == 32) {
       __syncthreads();
       for (int j = threadIdx.x; j < d; j += blockDim.x) {
         float s = 0.f;
         for (int w = 0; w < subs; ++w) s += combine[w * W + j];
-        out[(int64_t)qn * d + j] = s;
+        out[j] = s;
       }
     }
   }
 }
 
-// Adds the blocks' column sums and forms the parameter gradients (the first param_blocks blocks: 32 columns each, eight
-// slices of the list added in a fixed order), then the gates whose rows lie in several walkers' shares (256 columns each).
+// Adds the blocks' column sums and forms the parameter gradients (the first param_blocks blocks: 32 columns each, SLICES
+// slices of the list added in a fixed order), then the gates whose rows lie in several walkers' shares.
+static constexpr int SLICES = 16, GATE_COLUMNS = 128;
 template <typename TY>
-__global__ void __launch_bounds__(256) k_backward_sums(const Args a, int blocks, int param_blocks, float* __restrict__ dparams) {
-  __shared__ float part[4][8][32];
+__global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int blocks, int param_blocks, float* __restrict__ dparams) {
+  __shared__ float part[4][SLICES][32];
   pdl_enter();
   const int d = a.d;
   if ((int)blockIdx.x < param_blocks) {
     const int j = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, nq = a.bias ? 4 : 2;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (j < d)
-#pragma unroll 4
-      for (int b = slice; b < blocks; b += 8) {
-        const float* p = a.col_partials + (int64_t)b * nq * d + j;
-        v[0] += p[0];
-        v[1] += p[d];
-        if (nq == 4) { v[2] += p[2 * (int64_t)d]; v[3] += p[3 * (int64_t)d]; }
+    if (j < d) {
+      const float* p = a.col_partials + (int64_t)slice * nq * d + j;
+      const int64_t step = (int64_t)SLICES * nq * d;
+      if (nq == 2) {
+#pragma unroll 10
+        for (int b = slice; b < blocks; b += SLICES, p += step) { v[0] += p[0]; v[1] += p[d]; }
+      } else {
+#pragma unroll 5
+        for (int b = slice; b < blocks; b += SLICES, p += step) { v[0] += p[0]; v[1] += p[d]; v[2] += p[2 * (int64_t)d]; v[3] += p[3 * (int64_t)d]; }
       }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) part[i][slice][threadIdx.x & 31] = v[i];
     __syncthreads();
@@ -438,7 +453,7 @@ __global__ void __launch_bounds__(256) k_backward_sums(const Args a, int blocks,
       for (int i = 0; i < 4; ++i) {
         v[i] = 0.f;
 #pragma unroll
-        for (int s = 0; s < 8; ++s) v[i] += part[i][s][threadIdx.x];
+        for (int s = 0; s < SLICES; ++s) v[i] += part[i][s][threadIdx.x];
       }
       const float w = a.params[d + j], s = a.params[2 * (int64_t)d + j];
       dparams[j] = v[0];
@@ -453,8 +468,9 @@ __global__ void __launch_bounds__(256) k_backward_sums(const Args a, int blocks,
     }
     return;
   }
-  const int col_blocks = (d + 255) / 256;
-  const int item = (blockIdx.x - param_blocks) / col_blocks, j = ((blockIdx.x - param_blocks) % col_blocks) * 256 + threadIdx.x;
+  const int col_blocks = (d + GATE_COLUMNS - 1) / GATE_COLUMNS;
+  const int item = (blockIdx.x - param_blocks) / col_blocks, lane = threadIdx.x % GATE_COLUMNS, slice = threadIdx.x / GATE_COLUMNS;
+  const int j = ((blockIdx.x - param_blocks) % col_blocks) * GATE_COLUMNS + lane;
   const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
   int64_t gate = item;
   if (gates >= a.walkers) {      // more gates than shares: only the ones cut by the start of share item + 1 are open
@@ -465,12 +481,24 @@ __global__ void __launch_bounds__(256) k_backward_sums(const Args a, int blocks,
   }
   const int64_t g0 = gate * a.per_gate, g1 = g0 + a.per_gate < a.rows ? g0 + a.per_gate : a.rows;
   const int64_t lo = walker_of(g0, a.rows, a.walkers), hi = walker_of(g1 - 1, a.rows, a.walkers);
-  if (lo == hi || j >= d) return;
+  if (lo == hi) return;
+  // the walkers in between, in slices added in a fixed order; there are no more walkers than rows, so none is empty
+  constexpr int GS = 32 * SLICES / GATE_COLUMNS;
   float s = 0.f;
-#pragma unroll 4
-  for (int64_t w = lo; w <= hi; ++w)
-    if (share_start(w, a.rows, a.walkers) < share_start(w + 1, a.rows, a.walkers)) s += a.gate_partials[(w + gate) * d + j];
-  ((TY*)a.dg)[gate * a.lddg + j] = from_f<TY>(s);
+  if (j < d) {
+    const float* p = a.gate_partials + (lo + slice + gate) * d + j;
+#pragma unroll 8
+    for (int64_t w = lo + slice; w <= hi; w += GS, p += (int64_t)GS * d) s += *p;
+  }
+  float* sums = &part[0][0][0];
+  sums[slice * GATE_COLUMNS + lane] = s;
+  __syncthreads();
+  if (slice == 0 && j < d) {
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < GS; ++i) s += sums[i * GATE_COLUMNS + lane];
+    ((TY*)a.dg)[gate * a.lddg + j] = from_f<TY>(s);
+  }
 }
 
 int backward_blocks(int64_t rows, const Layout& l) {
@@ -495,7 +523,7 @@ template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
 static betty_status launch_backward(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
   static SmemLimit limit = {};
   if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_backward<TX, TY, GR, PIPE, CH, GENERAL>, limit, l.smem));
-  const int blocks = a.walkers / (l.threads / l.G);
+  const int blocks = backward_blocks(a.rows, l);
   launch_pdl(k_backward<TX, TY, GR, PIPE, CH, GENERAL>, dim3(blocks), dim3(l.threads), l.smem, stream, a);
   BETTY_LAUNCH_CHECK();
   const int param_blocks = (a.d + 31) / 32;
@@ -504,7 +532,8 @@ static betty_status launch_backward(cudaStream_t stream, const Args& a, const La
     const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
     items = gates < a.walkers ? gates : a.walkers - 1;
   }
-  launch_pdl(k_backward_sums<TY>, dim3((unsigned)(param_blocks + items * ((a.d + 255) / 256))), dim3(256), 0, stream, a, blocks, param_blocks,
+  launch_pdl(k_backward_sums<TY>, dim3((unsigned)(param_blocks + items * ((a.d + GATE_COLUMNS - 1) / GATE_COLUMNS))), dim3(32 * SLICES), 0, stream, a,
+             blocks, param_blocks,
              dparams);
   BETTY_LAUNCH_CHECK();
   return BETTY_OK;
