@@ -194,7 +194,7 @@ static betty_status forward_typed(cudaStream_t stream, const Args& a, const Layo
 betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int granule) {
   const int ys = (a.y ? 1 : 0) + (a.y && a.gate != BETTY_GATE_NONE ? 1 : 0);
   const bool general = a.bias || a.pre == BETTY_NORM_LAYER || a.post == BETTY_NORM_LAYER;
-  const Layout l = layout_of(a.d, a.rows, xd, yd, granule, {1, ys, FWD_CHUNKS, forward_batch(general), 0});
+  const Layout l = layout_of(a.d, a.rows, xd, yd, granule, {1, ys, FWD_CHUNKS, forward_batch(general), 0, 0});
   a.G = l.G; a.ahead = l.ahead; a.slot_bytes = l.slot_bytes;
   if (xd == BETTY_F32 && yd == BETTY_F32) return forward_typed<float, float>(stream, a, l);
   if (xd == BETTY_F32 && yd == BETTY_BF16) return forward_typed<float, __nv_bfloat16>(stream, a, l);
@@ -223,7 +223,7 @@ Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int granule, const Nee
     const int groups = l.threads / l.G;
     l.blocks_per_sm = MAX_G / l.threads;
     l.slot_bytes = l.chunks * 8 * l.G * (n.streams_x * bx + n.streams_y * by);
-    const size_t acc = (size_t)n.acc_arrays * groups * l.chunks * 8 * l.G * sizeof(float);
+    const size_t acc = (size_t)(n.acc_arrays * groups + n.param_arrays) * l.chunks * 8 * l.G * sizeof(float);
     if (attempt == 2) {
       l.smem = acc;
       l.slot_bytes = 0;

@@ -290,7 +290,8 @@ struct Layout {
 struct Needs {
   int streams_x, streams_y; // rows fetched of the residual stream's and of the block's type
   int wide_chunks, batch;   // of the wide kernel
-  int acc_arrays;           // fp32 values of a row kept in shared memory
+  int acc_arrays;           // fp32 values of a row that each thread group keeps in shared memory
+  int param_arrays;         // and that a block keeps once
 };
 Layout layout_of(int64_t d, int64_t rows, int x_dtype, int y_dtype, int granule, const Needs& n);
 betty_status forward(cudaStream_t stream, Args& a, int x_dtype, int y_dtype, int granule);

@@ -18,6 +18,9 @@ namespace blocknorm {
 __host__ __device__ __forceinline__ int64_t share_start(int64_t w, int64_t rows, int64_t walkers) { return w * rows / walkers; }
 __device__ __forceinline__ int64_t walker_of(int64_t row, int64_t rows, int64_t walkers) { return ((row + 1) * walkers - 1) / rows; }
 
+
+
+
 // Each walker (thread group) takes a contiguous share of the rows, so that the column sums stay in its registers; it writes
 // them once, and k_backward_sums adds the blocks' sums in order.  A row's chain is what bounds this kernel, so with RMS
 // norms a row costs one sum over its threads: with c = a w_post s y the mean of dm m is a combination of sums that do not
@@ -49,7 +52,13 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   const int at_o = bx, at_y = 2 * bx, at_u = 2 * bx + by, at_g = 2 * bx + 2 * by;
   char* ring = slots + (size_t)sub * (a.ahead + 1) * a.slot_bytes;
   // [A (, B)][value][thread] of a walker whose gates are shared
-  float* acc_s = (float*)(slots + (size_t)subs * (a.ahead + 1) * a.slot_bytes) + (size_t)sub * (GENERAL ? 2 : 1) * CH * 8 * G + t;
+  // w_pre of the block, then e of each walker: [half chunk][thread], read with 16-byte accesses
+  float4* w_s = (float4*)(slots + (size_t)subs * (a.ahead + 1) * a.slot_bytes) + t;
+  float4* e_s = w_s + (size_t)(sub + 1) * 2 * CH * G;
+  // A (and B) of a walker whose gates are shared: its block's row of the column sums, or where a warp holds a row (several
+  // walkers to a block) [value][thread] in shared memory
+  float* acc_s = (float*)(w_s - t + (size_t)(subs + 1) * 2 * CH * G) + (size_t)sub * (GENERAL ? 2 : 1) * CH * 8 * G + t;
+  float* const partials = a.col_partials + (int64_t)blockIdx.x * (a.bias ? 4 : 2) * d;
   const TX* xs = (const TX*)a.x;
   const TX* os = (const TX*)a.dxo;
   const TY* ys = (const TY*)a.y;
@@ -94,9 +103,8 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
     gate = (unsigned)first / a.per_gate;
     gate_end = (gate + 1) * a.per_gate;
   }
-  // w_pre, and e = w_post s (times a(g) of a shared gate): kept in registers, or (wide rows) formed where they are used
+  // w_pre and e = w_post s, times a(g) of a shared gate: in shared memory; wide rows form them where they are used
   constexpr bool KEEP = CH <= 2;
-  f2 kw[KEEP ? CH : 1][4], ke[KEEP ? CH : 1][4];
   auto make_e = [&](int c, f2 (&e)[4]) {
     f2 s[4];
     param(w_post, c, e);
@@ -114,10 +122,17 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       for (int k = 0; k < 4; ++k) e[k] = mul2(e[k], s[k]);
     }
   };
+  auto keep_e = [&](int c) {
+    f2 e[4];
+    make_e(c, e);
+    e_s[(2 * c) * G] = make_float4(e[0].x, e[0].y, e[1].x, e[1].y);
+    e_s[(2 * c + 1) * G] = make_float4(e[2].x, e[2].y, e[3].x, e[3].y);
+  };
   auto coefficients = [&](int c, f2 (&w)[4], f2 (&e)[4]) {
     if constexpr (KEEP) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) { w[k] = kw[KEEP ? c : 0][k]; e[k] = ke[KEEP ? c : 0][k]; }
+      const float4 a0 = w_s[(2 * c) * G], a1 = w_s[(2 * c + 1) * G], b0 = e_s[(2 * c) * G], b1 = e_s[(2 * c + 1) * G];
+      w[0] = f2{a0.x, a0.y}; w[1] = f2{a0.z, a0.w}; w[2] = f2{a1.x, a1.y}; w[3] = f2{a1.z, a1.w};
+      e[0] = f2{b0.x, b0.y}; e[1] = f2{b0.z, b0.w}; e[2] = f2{b1.x, b1.y}; e[3] = f2{b1.z, b1.w};
     } else {
       param(w_pre, c, w);
       make_e(c, e);
@@ -126,7 +141,13 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   f2 accC[CH][4], accA[CH][4], accD[GENERAL ? CH : 1][4], accB[GENERAL ? CH : 1][4], mask[GENERAL ? CH : 1][4];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    if constexpr (KEEP) { param(w_pre, c, kw[c]); make_e(c, ke[c]); }
+    if constexpr (KEEP) {
+      float w[8];
+      load_param8<GR>(w, w_pre, c, t, G, d);         // every thread group writes the same values, and reads its own writes
+      w_s[(2 * c) * G] = make_float4(w[0], w[1], w[2], w[3]);
+      w_s[(2 * c + 1) * G] = make_float4(w[4], w[5], w[6], w[7]);
+      keep_e(c);
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       accC[c][k] = accA[c][k] = both(0.f);
@@ -135,12 +156,21 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         mask[c][k] = f2{column<GR>(c, 2 * k, t, G) < d ? 1.f : 0.f, column<GR>(c, 2 * k + 1, t, G) < d ? 1.f : 0.f};   // 0 beyond the row
       }
     }
-    if (shared_gate)
+    if (shared_gate) {
+      float zero[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        acc_s[(c * 8 + k) * G] = 0.f;
-        if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = 0.f;
+        zero[k] = 0.f;
+        if (G == 32) {
+          acc_s[(c * 8 + k) * G] = 0.f;
+          if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = 0.f;
+        }
       }
+      if (G > 32) {
+        store8<GR>(partials + d, zero, c, t, G, d);
+        if (bias) store8<GR>(partials + 3 * (int64_t)d, zero, c, t, G, d);
+      }
+    }
   }
   for (; row < last; ++row) {
     if (PIPE) {
@@ -367,8 +397,26 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
             g[k] = sigmoid_f(g[k]);
             dg[k] *= g[k] * (1.f - g[k]);
           }
-          acc_s[(c * 8 + k) * G] = fmaf(g[k], H, acc_s[(c * 8 + k) * G]);
-          if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = fmaf(g[k], E, acc_s[(CH * 8 + c * 8 + k) * G]);
+          if (G == 32) {
+            acc_s[(c * 8 + k) * G] = fmaf(g[k], H, acc_s[(c * 8 + k) * G]);
+            if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = fmaf(g[k], E, acc_s[(CH * 8 + c * 8 + k) * G]);
+          } else {
+            w[k] = g[k] * H;
+            if (GENERAL) b[k] = g[k] * E;
+          }
+        }
+        if (G > 32) {
+          float was[8];
+          load8<GR, float>(was, partials + d, c, t, G, d);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) w[k] += was[k];
+          store8<GR>(partials + d, w, c, t, G, d);
+          if (bias) {
+            load8<GR, float>(was, partials + 3 * (int64_t)d, c, t, G, d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) b[k] += was[k];
+            store8<GR>(partials + 3 * (int64_t)d, b, c, t, G, d);
+          }
         }
         if (whole) store8<GR>((TY*)a.dg + gate * a.lddg, dg, c, t, G, d);
         else store8<GR>(a.gate_partials + (walker + gate) * d, dg, c, t, G, d);
@@ -383,11 +431,11 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
           if (GENERAL) accB[c][k] = both(0.f);
         }
         if constexpr (KEEP)
-          if (row + 1 < last) make_e(c, ke[c]);
+          if (row + 1 < last) keep_e(c);
       }
     }
   }
-  if (shared_gate)
+  if (shared_gate && G == 32)
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -396,10 +444,11 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         if (GENERAL) accB[c][k] = f2{acc_s[(CH * 8 + c * 8 + 2 * k) * G], acc_s[(CH * 8 + c * 8 + 2 * k + 1) * G]};
       }
   const int nq = a.bias ? 4 : 2;
-  float* out = a.col_partials + (int64_t)blockIdx.x * nq * d;
+  float* out = partials;
   float* combine = (float*)slots;             // G = 32, a warp per walker: the block's warps are added in order
   constexpr int W = CH * 256;                 // columns a warp can hold
   for (int qn = 0; qn < nq; ++qn, out += d) {
+    if (shared_gate && G > 32 && (qn & 1)) continue;       // A and B are there already
     if (G == 32) __syncthreads();
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -512,7 +561,8 @@ static constexpr int backward_chunks(bool general) { return general ? 1 : 2; }
 Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int xd, int yd, int granule) {
   const bool gated = c->gate != BETTY_GATE_NONE, general = is_general(c->bias, c->pre, c->post);
   const bool row_gate = gated && c->rows_per_gate == 1;             // a gate shared by rows stays in L1
-  Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, gated && !row_gate ? (general ? 2 : 1) : 0};
+  Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, 0, 1};
+  n.acc_arrays = gated && !row_gate && c->d <= 32 * 8 * MAX_CH ? 1 + (general ? 2 : 1) : 1;      // e; A (and B) where a warp holds a row
   Layout l = layout_of(c->d, rows, xd, yd, granule, n);
   const size_t combine = l.G == 32 ? (size_t)(l.threads / 32) * l.chunks * 256 * sizeof(float) : 0;
   if (l.smem < combine) l.smem = combine;
