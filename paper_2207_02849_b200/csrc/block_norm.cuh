@@ -11,14 +11,16 @@
 namespace betty {
 namespace blocknorm {
 
-// A row is held by G threads (a power of two, 32 .. MAX_G), CH * 8 values each, in granules of GR consecutive values that
-// every stream's layout lets a thread copy by itself: 8 where rows start on 16-byte boundaries, 2 where they start on 4-byte
-// boundaries (16-bit values), 1 elsewhere.  Neighbouring threads hold neighbouring granules.
+// A row is held by G threads (a power of two, 32 .. MAX_G), CH * 8 values each.  VEC: chunk c of thread t is the eight
+// values from (c * G + t) * 8 - shift, one or two 16-byte accesses, where shift is how far the row starts behind a 16-byte
+// boundary (counted modulo 8 values).  Rows of an odd width start at every shift in turn; the rows that one thread group
+// takes all have the same one ("class": rows of equal number modulo `classes`), so that a thread's columns, and with them
+// its parameters and column sums, stay the same.  Otherwise (matrices whose rows start at different shifts, or wider rows
+// than shared memory holds) values are accessed one by one: value k of chunk c is column (c * 8 + k) * G + t.
 static constexpr int MAX_G = 512;
 static constexpr int MAX_CH = 4;
 static constexpr int MAX_D = MAX_G * 8 * MAX_CH;
 static constexpr int SMALL_THREADS = 256;     // block size when a warp holds a row
-static constexpr int MAX_STREAMS = 5;
 
 template <typename T> __device__ __forceinline__ float to_f(T v);
 template <> __device__ __forceinline__ float to_f(float v) { return v; }
@@ -49,106 +51,135 @@ template <> __device__ __forceinline__ void unpack2<__half>(uint32_t w, float& a
   a = v.x; b = v.y;
 }
 
-// column of a thread's value k (0 .. 7) of chunk c
-template <int GR>
-__device__ __forceinline__ int column(int c, int k, int t, int G) {
-  return ((c * (8 / GR) + k / GR) * G + t) * GR + k % GR;
+// row `row` of a matrix with rows of `ld_bytes` bytes (both below 2^32: one wide multiply)
+template <typename T>
+__device__ __forceinline__ const T* row_at(const void* base, int64_t row, uint32_t ld_bytes) {
+  return (const T*)((const char*)base + (uint64_t)(uint32_t)row * ld_bytes);
+}
+template <typename T>
+__device__ __forceinline__ T* row_at(void* base, int64_t row, uint32_t ld_bytes) {
+  return (T*)((char*)base + (uint64_t)(uint32_t)row * ld_bytes);
 }
 
-// chunk c of a row in global memory; columns beyond d are 0
-template <int GR, typename T>
-__device__ __forceinline__ void load8(float (&o)[8], const T* row, int c, int t, int G, int d) {
-  if constexpr (GR == 8) {
-    const int j = (c * G + t) * 8;
-    uint4 w[sizeof(T) / 2];
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) w[i] = j < d ? *(const uint4*)((const char*)(row + j) + 16 * i) : make_uint4(0, 0, 0, 0);
-    if constexpr (sizeof(T) == 4) {
-      o[0] = __uint_as_float(w[0].x); o[1] = __uint_as_float(w[0].y); o[2] = __uint_as_float(w[0].z); o[3] = __uint_as_float(w[0].w);
-      o[4] = __uint_as_float(w[1].x); o[5] = __uint_as_float(w[1].y); o[6] = __uint_as_float(w[1].z); o[7] = __uint_as_float(w[1].w);
-    } else {
-      unpack2<T>(w[0].x, o[0], o[1]); unpack2<T>(w[0].y, o[2], o[3]); unpack2<T>(w[0].z, o[4], o[5]); unpack2<T>(w[0].w, o[6], o[7]);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int j = column<GR>(c, k, t, G);
-      o[k] = j < d ? to_f(row[j]) : 0.f;
-    }
-  }
+// where a thread's values lie in a row
+struct Place { int t, G, d, shift; };
+template <bool VEC>
+__device__ __forceinline__ int column(const Place& w, int c, int k) {
+  return VEC ? (c * w.G + w.t) * 8 + k - w.shift : (c * 8 + k) * w.G + w.t;
 }
-template <int GR, typename T>
-__device__ __forceinline__ void store8(T* row, const float (&v)[8], int c, int t, int G, int d) {
-  if constexpr (GR == 8) {
-    const int j = (c * G + t) * 8;
-    if (j < d) {
+template <bool VEC>
+__device__ __forceinline__ bool inside(const Place& w, int c, int k) { return (unsigned)column<VEC>(w, c, k) < (unsigned)w.d; }
+
+// chunk c of a row in global memory, value by value; columns outside the row are 0
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(float (&o)[8], const T* row, int c, const Place& w) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) o[k] = inside<VEC>(w, c, k) ? to_f(row[column<VEC>(w, c, k)]) : 0.f;
+}
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_each(T* row, const float (&v)[8], int c, const Place& w) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (inside<VEC>(w, c, k)) row[column<VEC>(w, c, k)] = from_f<T>(v[k]);
+}
+// rows of the call's matrices: 16 bytes at a time except at a shifted row's ends
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T* row, const float (&v)[8], int c, const Place& w) {
+  if constexpr (VEC) {
+    const int j = column<VEC>(w, c, 0);
+    if (j >= 0 && j + 8 <= w.d) {
       if constexpr (sizeof(T) == 4) {
         *(float4*)(row + j) = make_float4(v[0], v[1], v[2], v[3]);
         *(float4*)(row + j + 4) = make_float4(v[4], v[5], v[6], v[7]);
       } else {
         *(uint4*)(row + j) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7]));
       }
+      return;
     }
-  } else if constexpr (GR == 2 && sizeof(T) == 2) {
-#pragma unroll
-    for (int k = 0; k < 8; k += 2) {             // rows start on 4-byte boundaries and d is even
-      const int j = column<GR>(c, k, t, G);
-      if (j < d) *(uint32_t*)(row + j) = pack2<T>(v[k], v[k + 1]);
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int j = column<GR>(c, k, t, G);
-      if (j < d) row[j] = from_f<T>(v[k]);
-    }
+    if (j >= w.d) return;
   }
+  store_each<VEC>(row, v, c, w);
 }
-// parameters are fp32 and every block of them starts on a 16-byte boundary only when d is a multiple of 4
-template <int GR>
-__device__ __forceinline__ void load_param8(float (&v)[8], const float* row, int c, int t, int G, int d) { load8<GR, float>(v, row, c, t, G, d); }
+
+// ---- shared memory by 32-bit addresses: half the registers of generic pointers ----
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ float4 lds16f(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts16f(uint32_t a, float x, float y, float z, float w) {
+  asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(a), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
+}
+__device__ __forceinline__ float lds4f(uint32_t a) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void sts4f(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory"); }
+template <typename T> __device__ __forceinline__ void sts(uint32_t a, T v) {
+  if constexpr (sizeof(T) == 4) sts4f(a, v);
+  else asm volatile("st.shared.b16 [%0], %1;" ::"r"(a), "h"(*(const uint16_t*)&v) : "memory");
+}
 
 // ---- rows fetched ahead ----
-// Each thread copies the granules that it will itself read into its own slots of shared memory with cp.async (16 or 4
-// bytes at a time), a few rows before their use: no registers are held by data in flight, and as nobody reads another
-// thread's slots, waiting for one's own copies is all the synchronisation there is.
-// A slot holds CH * 8 values of every stream, interleaved over the G threads so that a warp's accesses are contiguous.
-// Columns beyond d are filled with zeros (a copy of no bytes), so that reading a slot needs no comparison.
-template <int GR, int CH, typename T>
-__device__ __forceinline__ void copy_row(char* slot, const T* row, int t, int G, int d) {
-  constexpr int bytes = GR * (int)sizeof(T), piece = bytes >= 16 ? 16 : 4, per = bytes / piece;
-  static_assert(bytes % 4 == 0, "cp.async moves 4 or 16 bytes");
-  const uint32_t dst = (uint32_t)__cvta_generic_to_shared(slot) + t * piece;
+// Each thread copies the 16-byte pieces that it will itself read into its own slots of shared memory with cp.async, a few
+// rows before their use: no registers are held by data in flight, and as nobody reads another thread's slots, waiting for
+// one's own copies is all the synchronisation there is.  A slot holds CH * 8 values of every stream, interleaved over the
+// G threads so that a warp's accesses are contiguous.  Columns from d on are filled with zeros (a copy of fewer bytes); the
+// values before column 0 of a shifted row are the end of the row before (never before the matrix: its first row has shift
+// 0) and are cleared by drop_head.
+template <int CH, typename T>
+__device__ __forceinline__ void copy_row(uint32_t slot, const T* row, const Place& w) {
+  constexpr int per = (int)sizeof(T) / 2, values = 16 / (int)sizeof(T);
+  const uint32_t dst = slot + w.t * 16;
+  const T* base = row - w.shift;
+  if (w.d == CH * 8 * w.G) {         // nothing to fill (and no shift: the threads then hold seven columns more than d)
 #pragma unroll
-  for (int n = 0; n < CH * 8 / GR; ++n) {
-    const int j = (n * G + t) * GR, size = j < d ? piece : 0;
-    const char* src = (const char*)(row + (j < d ? j : 0));
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < per; ++i)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;"
+                     ::"r"(dst + (c * per + i) * w.G * 16), "l"(base + (c * w.G + w.t) * 8 + i * values) : "memory");
+    return;
+  }
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
 #pragma unroll
     for (int i = 0; i < per; ++i) {
-      if (piece == 16)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + (n * per + i) * G * piece), "l"(src + i * piece), "r"(size) : "memory");
-      else
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + (n * per + i) * G * piece), "l"(src + i * piece), "r"(size) : "memory");
+      const int j = (c * w.G + w.t) * 8 + i * values, left = (w.d + w.shift - j) * (int)sizeof(T), size = left < 0 ? 0 : (left > 16 ? 16 : left);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                   ::"r"(dst + (c * per + i) * w.G * 16), "l"(size > 0 ? base + j : base), "r"(size) : "memory");
     }
-  }
 }
-template <int GR, typename T>
-__device__ __forceinline__ void read_slot(float (&o)[8], const char* slot, int c, int t, int G) {
-  constexpr int bytes = GR * (int)sizeof(T), piece = bytes >= 16 ? 16 : 4, pieces = 8 * (int)sizeof(T) / piece;
-#pragma unroll
-  for (int i = 0; i < pieces; ++i) {
-    const char* src = slot + ((c * pieces + i) * G + t) * piece;
-    constexpr int per = piece / (int)sizeof(T);          // values in a piece
-    if constexpr (piece == 16 && sizeof(T) == 4) {
-      const float4 w = *(const float4*)src;
-      o[i * per] = w.x; o[i * per + 1] = w.y; o[i * per + 2] = w.z; o[i * per + 3] = w.w;
-    } else if constexpr (piece == 16) {
-      const uint4 w = *(const uint4*)src;
-      unpack2<T>(w.x, o[0], o[1]); unpack2<T>(w.y, o[2], o[3]); unpack2<T>(w.z, o[4], o[5]); unpack2<T>(w.w, o[6], o[7]);
-    } else if constexpr (sizeof(T) == 4) {
-      o[i] = *(const float*)src;
-    } else {
-      unpack2<T>(*(const uint32_t*)src, o[2 * i], o[2 * i + 1]);
-    }
+// the same for a row at another shift than the thread's columns, value by value and not ahead
+template <int CH, bool VEC, typename T>
+__device__ __forceinline__ void fill_slot(uint32_t slot, const T* row, const Place& w) {
+#pragma unroll 1
+  for (int c = 0; c < CH; ++c)
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k)
+      sts<T>(slot + ((c * (int)sizeof(T) / 2 + k * (int)sizeof(T) / 16) * w.G + w.t) * 16 + k * (int)sizeof(T) % 16,
+             inside<VEC>(w, c, k) ? row[column<VEC>(w, c, k)] : from_f<T>(0.f));
+}
+template <typename T>
+__device__ __forceinline__ void drop_head(uint32_t slot, const Place& w) {
+  if (w.t == 0)
+    for (int k = 0; k < w.shift; ++k) sts<T>(slot + (k * (int)sizeof(T) / 16) * w.G * 16 + k * (int)sizeof(T) % 16, from_f<T>(0.f));
+}
+template <typename T>
+__device__ __forceinline__ void read_slot(float (&o)[8], uint32_t slot, int c, const Place& w) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = lds16f(slot + ((c * 2) * w.G + w.t) * 16), b = lds16f(slot + ((c * 2 + 1) * w.G + w.t) * 16);
+    o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w; o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+  } else {
+    const uint4 a = lds16(slot + (c * w.G + w.t) * 16);
+    unpack2<T>(a.x, o[0], o[1]); unpack2<T>(a.y, o[2], o[3]); unpack2<T>(a.z, o[4], o[5]); unpack2<T>(a.w, o[6], o[7]);
   }
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -162,8 +193,8 @@ static constexpr int MAX_AHEAD = 3;
 
 // Sums of NV values over the G threads of a row, every thread receiving the same bits.  Within a warp the values are
 // folded while they are reduced: each of the first steps halves the number of values a lane carries, so that P values cost
-// P - 1 exchanges and log2(32 / P) further ones instead of 5 P.  Across warps every lane then takes one (value, warp) pair
-// from shared memory.  `red` has two halves used in turn, so one block barrier per call is enough.
+// P - 1 exchanges and log2(32 / P) further ones instead of 5 P.  Across warps every thread then adds the warps' sums from
+// shared memory (broadcast reads).  `red` has two halves used in turn, so one block barrier per call is enough.
 static constexpr int RED_VALUES = 8;
 template <int NV>
 __device__ __forceinline__ void row_sums(float (&v)[NV], float* red, int& half, int G, int t) {
@@ -193,29 +224,28 @@ __device__ __forceinline__ void row_sums(float (&v)[NV], float* red, int& half, 
   }
   float* r = red + half * (RED_VALUES * 16);
   half ^= 1;
-  const int warps = G >> 5, lg = 31 - __clz(warps);
-  if (lane % (32 / P) == 0) r[((lane / (32 / P)) << lg) + (t >> 5)] = u[0];
+  const int warps = G >> 5;
+  if (lane % (32 / P) == 0) r[lane / (32 / P) * 16 + (t >> 5)] = u[0];
   __syncthreads();
-  constexpr int LOADS = P * 16 > 32 ? P * 16 / 32 : 1;       // at most 16 warps
-  float w[LOADS];
+  const float2* r2 = (const float2*)r;              // at least two warps; every thread adds them in the same order
 #pragma unroll
-  for (int j = 0; j < LOADS; ++j) {
-    const int e = lane + 32 * j;
-    w[j] = r[e & ((P << lg) - 1)];
+  for (int i = 0; i < NV; ++i) {
+    const float2 w = r2[i * 8];
+    v[i] = w.x + w.y;
   }
+  if (warps > 2) {
 #pragma unroll
-  for (int o = 8; o; o >>= 1)
-    if (o < warps)
+    for (int i = 0; i < NV; ++i) {
+      const float2 w = r2[i * 8 + 1];
+      v[i] += w.x + w.y;
+    }
+    for (int j = 4; j < warps; j += 4) {
 #pragma unroll
-      for (int j = 0; j < LOADS; ++j) w[j] += __shfl_xor_sync(0xffffffffu, w[j], o);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {                              // pair e = i * warps + ... is in lane e % 32 of load e / 32
-    const int e = i << lg;
-    float x = w[0];
-#pragma unroll
-    for (int j = 1; j < LOADS; ++j)
-      if ((e >> 5) == j) x = w[j];
-    v[i] = __shfl_sync(0xffffffffu, x, e & 31);
+      for (int i = 0; i < NV; ++i) {
+        const float4 w = *(const float4*)(r + i * 16 + j);
+        v[i] += (w.x + w.y) + (w.z + w.w);
+      }
+    }
   }
 }
 
@@ -255,30 +285,34 @@ __device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.f, 1.f
 struct Args {
   int64_t rows;
   int d, G;
+  int classes;              // 1, 2, 4 or 8: row r starts at the shift of row r % classes,
+  int ld8;                  // which is (r * ld8) modulo 8
   int ahead;                // batches of rows fetched ahead of the present one, 1 .. MAX_AHEAD (kernels that fetch ahead)
   int slot_bytes;           // of one row, all streams
   int pre, post, gate, bias;
   unsigned per_gate;
+  int gate_ahead;           // forward: the gate is among the streams fetched ahead
   float eps, inv_d;
   const float* params;      // [w_pre, w_post, s (, b_pre, b_post)], d values each
-  const void* x; int64_t ldx;          // forward: x; backward: x'
-  const void* y; int64_t ldy;          // may be null
-  const void* g; int64_t ldg;
-  void* x_out; int64_t ldxo;           // forward
-  void* u; int64_t ldu;                // forward, may be null
-  const void* du; int64_t lddu;        // backward, may be null
-  const void* dxo; int64_t lddxo;      // backward, may be null
-  void* dx; int64_t lddx;
-  void* dy; int64_t lddy;
-  void* dg; int64_t lddg;
-  float* gate_partials;                // [walkers + gates, d] (gates of several rows)
+  // matrices: address and bytes from one row to the next
+  const void* x; uint32_t ldx;          // forward: x; backward: x'
+  const void* y; uint32_t ldy;          // may be null
+  const void* g; uint32_t ldg;
+  void* x_out; uint32_t ldxo;           // forward
+  void* u; uint32_t ldu;                // forward, may be null
+  const void* du; uint32_t lddu;        // backward, may be null
+  const void* dxo; uint32_t lddxo;      // backward, may be null
+  void* dx; uint32_t lddx;
+  void* dy; uint32_t lddy;
+  void* dg; uint32_t lddg;
+  float* gate_partials;                // [classes][shares + gates][d] (gates of several rows)
   float* col_partials;                 // [blocks, quantities, d]
-  int walkers;                         // thread groups with rows, at most one per row
+  int shares;                          // backward: contiguous shares that the rows of a class are cut into
 };
 
 // How a call's rows are laid over threads.
 struct Layout {
-  int granule;              // 8, 2 or 1
+  bool vec;
   int G, chunks;            // threads per row, chunks of 8 values per thread
   int threads;              // of a block
   int blocks_per_sm;        // that the grid counts on
@@ -291,12 +325,12 @@ struct Needs {
   int streams_x, streams_y; // rows fetched of the residual stream's and of the block's type
   int wide_chunks, batch;   // of the wide kernel
   int acc_arrays;           // fp32 values of a row that each thread group keeps in shared memory
-  int param_arrays;         // and that a block keeps once
 };
-Layout layout_of(int64_t d, int64_t rows, int x_dtype, int y_dtype, int granule, const Needs& n);
-betty_status forward(cudaStream_t stream, Args& a, int x_dtype, int y_dtype, int granule);
-Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int x_dtype, int y_dtype, int granule);
-int backward_blocks(int64_t rows, const Layout& l);
+// classes: 0 where the matrices' rows do not start at one shift
+Layout layout_of(int64_t d, int64_t rows, int x_dtype, int y_dtype, int classes, const Needs& n);
+betty_status forward(cudaStream_t stream, Args& a, int x_dtype, int y_dtype, int classes);
+Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int x_dtype, int y_dtype, int classes);
+void backward_grid(int64_t rows, const Layout& l, int classes, int& blocks, int& shares);
 betty_status backward(cudaStream_t stream, Args& a, const Layout& l, int x_dtype, int y_dtype, float* dparams);
 
 }  // namespace blocknorm

@@ -14,12 +14,25 @@
 namespace betty {
 namespace blocknorm {
 
-// First row of a walker's share; the shares are contiguous and differ by at most one row.
-__host__ __device__ __forceinline__ int64_t share_start(int64_t w, int64_t rows, int64_t walkers) { return w * rows / walkers; }
-__device__ __forceinline__ int64_t walker_of(int64_t row, int64_t rows, int64_t walkers) { return ((row + 1) * walkers - 1) / rows; }
+// The rows of a class (row numbers equal modulo `classes`) are cut into `shares` contiguous shares, equal to within a row.
+__device__ __forceinline__ int64_t class_rows(const Args& a, int kind) { return a.rows > kind ? (a.rows - kind + a.classes - 1) / a.classes : 0; }
+__device__ __forceinline__ int64_t share_start(int64_t share, int64_t n, int shares) { return share * n / shares; }
+__device__ __forceinline__ int64_t share_of(int64_t i, int64_t n, int shares) { return ((i + 1) * shares - 1) / n; }
 
 
 
+
+// a row of sums in the workspace: 16 bytes at a time where that fits
+template <bool VEC>
+__device__ __forceinline__ void store_sums(float* row, const float (&v)[8], int c, const Place& w) {
+  if (VEC && w.shift == 0 && w.d % 4 == 0) store8<VEC>(row, v, c, w);
+  else store_each<VEC>(row, v, c, w);
+}
+// a walker's sum for a gate of several rows: shares and gates both grow along the rows, so no two pairs of a class meet
+__device__ __forceinline__ int64_t gate_slot(const Args& a, int kind, int64_t share, int64_t gate) {
+  const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
+  return kind * (a.shares + gates) + share + gate;
+}
 
 // Each walker (thread group) takes a contiguous share of the rows, so that the column sums stay in its registers; it writes
 // them once, and k_backward_sums adds the blocks' sums in order.  A row's chain is what bounds this kernel, so with RMS
@@ -32,15 +45,19 @@ __device__ __forceinline__ int64_t walker_of(int64_t row, int64_t rows, int64_t 
 // from dm itself: their combination would cancel two differences that are scaled up by 1 / sigma each where rows are flat.
 // A gate shared by rows needs one sum H = sum dX m per gate: dg = a'(g) s w_post H, and A gains a(g) H when the walker
 // leaves the gate, so A waits in shared memory.
-template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
+template <typename TX, typename TY, bool VEC, int CH, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   __shared__ float red[2 * RED_VALUES * 16];
   extern __shared__ __align__(16) char slots[];      // fetched rows; G = 32: at the end the warps' column sums
   pdl_enter();
   const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G, subs = blockDim.x / G;
-  const int64_t walker = (int64_t)blockIdx.x * subs + sub;
-  const int64_t first = walker < a.walkers ? share_start(walker, a.rows, a.walkers) : a.rows;
-  const int64_t last = walker < a.walkers ? share_start(walker + 1, a.rows, a.walkers) : a.rows;
+  // walker: share `share` of the rows kind, kind + classes, ...; `at` and `last` count those
+  const int walker = blockIdx.x * subs + sub, kind = walker % a.classes, share = walker / a.classes;
+  const int64_t n_rows = class_rows(a, kind);
+  const int64_t first = share < a.shares ? share_start(share, n_rows, a.shares) : n_rows;
+  const int64_t last = share < a.shares ? share_start(share + 1, n_rows, a.shares) : n_rows;
+  const Place pl = {t, G, d, VEC ? (int)((kind * a.ld8) & 7) : 0};
+  auto row_of = [&](int64_t i) { return kind + i * a.classes; };
   const bool has_y = a.y != nullptr, has_g = a.gate != BETTY_GATE_NONE, has_u = a.du != nullptr, has_o = a.dxo != nullptr;
   const bool pre_layer = GENERAL && a.pre == BETTY_NORM_LAYER && has_u, post_layer = GENERAL && a.post == BETTY_NORM_LAYER && has_y;
   const bool shared_gate = has_g && a.per_gate > 1, row_gate = has_g && !shared_gate, bias = GENERAL && a.bias;
@@ -50,57 +67,57 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   const float* b_post = a.params + 4 * (int64_t)d;
   const int bx = CH * 8 * G * (int)sizeof(TX), by = CH * 8 * G * (int)sizeof(TY);
   const int at_o = bx, at_y = 2 * bx, at_u = 2 * bx + by, at_g = 2 * bx + 2 * by;
-  char* ring = slots + (size_t)sub * (a.ahead + 1) * a.slot_bytes;
-  // [A (, B)][value][thread] of a walker whose gates are shared
-  // w_pre of the block, then e of each walker: [half chunk][thread], read with 16-byte accesses
-  float4* w_s = (float4*)(slots + (size_t)subs * (a.ahead + 1) * a.slot_bytes) + t;
-  float4* e_s = w_s + (size_t)(sub + 1) * 2 * CH * G;
-  // A (and B) of a walker whose gates are shared: its block's row of the column sums, or where a warp holds a row (several
-  // walkers to a block) [value][thread] in shared memory
-  float* acc_s = (float*)(w_s - t + (size_t)(subs + 1) * 2 * CH * G) + (size_t)sub * (GENERAL ? 2 : 1) * CH * 8 * G + t;
+  // shared memory: the walkers' slots; then for each walker w_pre and e of its columns, [half chunk][thread]; then A (and B)
+  // of walkers whose gates are shared, where a warp holds a row (several walkers to a block), [value][thread] (elsewhere A
+  // and B wait in the block's row of the column sums)
+  const uint32_t base_s = shared_address(slots), slots_end = base_s + subs * (a.ahead + 1) * a.slot_bytes;
+  const uint32_t ring = base_s + sub * (a.ahead + 1) * a.slot_bytes;
+  const uint32_t w_s = slots_end + (sub * 4 * CH * G + t) * 16, e_s = w_s + 2 * CH * G * 16;
+  const uint32_t acc_s = slots_end + subs * 4 * CH * G * 16 + (sub * (GENERAL ? 2 : 1) * CH * 8 * G + t) * 4;
   float* const partials = a.col_partials + (int64_t)blockIdx.x * (a.bias ? 4 : 2) * d;
-  const TX* xs = (const TX*)a.x;
-  const TX* os = (const TX*)a.dxo;
-  const TY* ys = (const TY*)a.y;
-  const TY* us = (const TY*)a.du;
-  const TY* gs = (const TY*)a.g;
-  auto fetch = [&](int64_t r, int slot) {
-    if constexpr (PIPE) {
-      if (r < last) {
-        char* p = ring + slot * a.slot_bytes;
+  const TX* const xs = (const TX*)a.x;
+  const TX* const os = (const TX*)a.dxo;
+  const TY* const ys = (const TY*)a.y;
+  const TY* const us = (const TY*)a.du;
+  const TY* const gs = (const TY*)a.g;
+  auto fetch = [&](int64_t i, int slot) {
+    if constexpr (VEC) {
+      if (i < last) {
+        const int64_t r = row_of(i);
+        const uint32_t p = ring + slot * a.slot_bytes;
         if (has_u) {
-          copy_row<GR, CH>(p, xs + r * a.ldx, t, G, d);
-          copy_row<GR, CH>(p + at_u, us + r * a.lddu, t, G, d);
+          copy_row<CH>(p, row_at<TX>(xs, r, a.ldx), pl);
+          copy_row<CH>(p + at_u, row_at<TY>(us, r, a.lddu), pl);
         }
-        if (has_o) copy_row<GR, CH>(p + at_o, os + r * a.lddxo, t, G, d);
-        if (has_y) copy_row<GR, CH>(p + at_y, ys + r * a.ldy, t, G, d);
-        if (row_gate) copy_row<GR, CH>(p + at_g, gs + r * a.ldg, t, G, d);
+        if (has_o) copy_row<CH>(p + at_o, row_at<TX>(os, r, a.lddxo), pl);
+        if (has_y) copy_row<CH>(p + at_y, row_at<TY>(ys, r, a.ldy), pl);
+        if (row_gate) copy_row<CH>(p + at_g, row_at<TY>(gs, r, a.ldg), pl);
       }
       copies_commit();
     }
   };
   // one chunk of a stream of the present row
-  const char* p = nullptr;
-  int64_t row = first;
-  auto get = [&](auto* base, int64_t ld, int at, int c, f2 (&o)[4]) {
+  uint32_t p = 0;
+  int64_t row = 0;
+  auto get = [&](auto* base, uint32_t ld, int at, int c, f2 (&o)[4]) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(base)>::type>::type T;
     float v[8];
-    if constexpr (PIPE) read_slot<GR, T>(v, p + at, c, t, G);
-    else load8<GR, T>(v, base + row * ld, c, t, G, d);
+    if constexpr (VEC) read_slot<T>(v, p + at, c, pl);
+    else load8<VEC, T>(v, row_at<T>(base, row, ld), c, pl);
     pairs(o, v);
   };
   auto param = [&](const float* base, int c, f2 (&o)[4]) {
     float v[8];
-    load_param8<GR>(v, base, c, t, G, d);
+    load8<VEC>(v, base, c, pl);
     pairs(o, v);
   };
   int half = 0, slot = 0;
-  if (PIPE)
+  if (VEC)
     for (int i = 0; i < a.ahead; ++i) fetch(first + i, i);
 
   int64_t gate = 0, gate_end = 0;          // of a shared gate: the present row's, and the row after its last
   if (shared_gate && first < last) {
-    gate = (unsigned)first / a.per_gate;
+    gate = (unsigned)row_of(first) / a.per_gate;
     gate_end = (gate + 1) * a.per_gate;
   }
   // w_pre and e = w_post s, times a(g) of a shared gate: in shared memory; wide rows form them where they are used
@@ -113,7 +130,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
     for (int k = 0; k < 4; ++k) e[k] = mul2(e[k], s[k]);
     if (shared_gate) {
       float g[8];
-      load8<GR, TY>(g, gs + gate * a.ldg, c, t, G, d);
+      load8<VEC>(g, row_at<TY>(gs, gate, a.ldg), c, pl);
       if (a.gate == BETTY_GATE_SIGMOID)
 #pragma unroll
         for (int k = 0; k < 8; ++k) g[k] = sigmoid_f(g[k]);
@@ -125,12 +142,13 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   auto keep_e = [&](int c) {
     f2 e[4];
     make_e(c, e);
-    e_s[(2 * c) * G] = make_float4(e[0].x, e[0].y, e[1].x, e[1].y);
-    e_s[(2 * c + 1) * G] = make_float4(e[2].x, e[2].y, e[3].x, e[3].y);
+    sts16f(e_s + (2 * c) * G * 16, e[0].x, e[0].y, e[1].x, e[1].y);
+    sts16f(e_s + (2 * c + 1) * G * 16, e[2].x, e[2].y, e[3].x, e[3].y);
   };
   auto coefficients = [&](int c, f2 (&w)[4], f2 (&e)[4]) {
     if constexpr (KEEP) {
-      const float4 a0 = w_s[(2 * c) * G], a1 = w_s[(2 * c + 1) * G], b0 = e_s[(2 * c) * G], b1 = e_s[(2 * c + 1) * G];
+      const float4 a0 = lds16f(w_s + (2 * c) * G * 16), a1 = lds16f(w_s + (2 * c + 1) * G * 16);
+      const float4 b0 = lds16f(e_s + (2 * c) * G * 16), b1 = lds16f(e_s + (2 * c + 1) * G * 16);
       w[0] = f2{a0.x, a0.y}; w[1] = f2{a0.z, a0.w}; w[2] = f2{a1.x, a1.y}; w[3] = f2{a1.z, a1.w};
       e[0] = f2{b0.x, b0.y}; e[1] = f2{b0.z, b0.w}; e[2] = f2{b1.x, b1.y}; e[3] = f2{b1.z, b1.w};
     } else {
@@ -143,9 +161,9 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   for (int c = 0; c < CH; ++c) {
     if constexpr (KEEP) {
       float w[8];
-      load_param8<GR>(w, w_pre, c, t, G, d);         // every thread group writes the same values, and reads its own writes
-      w_s[(2 * c) * G] = make_float4(w[0], w[1], w[2], w[3]);
-      w_s[(2 * c + 1) * G] = make_float4(w[4], w[5], w[6], w[7]);
+      load8<VEC>(w, w_pre, c, pl);
+      sts16f(w_s + (2 * c) * G * 16, w[0], w[1], w[2], w[3]);
+      sts16f(w_s + (2 * c + 1) * G * 16, w[4], w[5], w[6], w[7]);
       keep_e(c);
     }
 #pragma unroll
@@ -153,7 +171,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       accC[c][k] = accA[c][k] = both(0.f);
       if (GENERAL) {
         accD[c][k] = accB[c][k] = both(0.f);
-        mask[c][k] = f2{column<GR>(c, 2 * k, t, G) < d ? 1.f : 0.f, column<GR>(c, 2 * k + 1, t, G) < d ? 1.f : 0.f};   // 0 beyond the row
+        mask[c][k] = f2{inside<VEC>(pl, c, 2 * k) ? 1.f : 0.f, inside<VEC>(pl, c, 2 * k + 1) ? 1.f : 0.f};   // 0 outside the row
       }
     }
     if (shared_gate) {
@@ -162,22 +180,29 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       for (int k = 0; k < 8; ++k) {
         zero[k] = 0.f;
         if (G == 32) {
-          acc_s[(c * 8 + k) * G] = 0.f;
-          if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = 0.f;
+          sts4f(acc_s + (c * 8 + k) * G * 4, 0.f);
+          if (GENERAL) sts4f(acc_s + (CH * 8 + c * 8 + k) * G * 4, 0.f);
         }
       }
       if (G > 32) {
-        store8<GR>(partials + d, zero, c, t, G, d);
-        if (bias) store8<GR>(partials + 3 * (int64_t)d, zero, c, t, G, d);
+        store_sums<VEC>(partials + d, zero, c, pl);
+        if (bias) store_sums<VEC>(partials + 3 * (int64_t)d, zero, c, pl);
       }
     }
   }
-  for (; row < last; ++row) {
-    if (PIPE) {
-      fetch(row + a.ahead, slot == 0 ? a.ahead : slot - 1);
+  for (int64_t at = first; at < last; ++at) {
+    row = row_of(at);
+    if constexpr (VEC) {
+      fetch(at + a.ahead, slot == 0 ? a.ahead : slot - 1);
       copies_wait(a.ahead);
       p = ring + slot * a.slot_bytes;
       slot = slot == a.ahead ? 0 : slot + 1;
+      if (pl.shift) {
+        if (has_u) { drop_head<TX>(p, pl); drop_head<TY>(p + at_u, pl); }
+        if (has_o) drop_head<TX>(p + at_o, pl);
+        if (has_y) drop_head<TY>(p + at_y, pl);
+        if (row_gate) drop_head<TY>(p + at_g, pl);
+      }
     }
     float mx = 0.f, my = 0.f;
     if (pre_layer || post_layer) {
@@ -303,7 +328,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         }
       }
       singles(out, dX);
-      store8<GR>((TX*)a.dx + row * a.lddx, out, c, t, G, d);
+      store8<VEC>(row_at<TX>(a.dx, row, a.lddx), out, c, pl);
       if (!has_y) continue;
       f2 m[4];
       get(ys, a.ldy, at_y, c, m);
@@ -333,7 +358,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
             z[k] = mul2(z[k], fma2(mul2(g[k], both(-1.f)), g[k], g[k]));
           }
         singles(out, z);
-        store8<GR>((TY*)a.dg + row * a.lddg, out, c, t, G, d);
+        store8<VEC>(row_at<TY>(a.dg, row, a.lddg), out, c, pl);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           dX[k] = mul2(dX[k], g[k]);
@@ -356,7 +381,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
           out[2 * k] = o.x; out[2 * k + 1] = o.y;
         }
       }
-      if (!GENERAL) store8<GR>((TY*)a.dy + row * a.lddy, out, c, t, G, d);
+      if (!GENERAL) store8<VEC>(row_at<TY>(a.dy, row, a.lddy), out, c, pl);
     }
     if constexpr (GENERAL) {
       if (has_y) {
@@ -375,20 +400,20 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
             const f2 o = mul2(fma2(m[k], both(-pm), add2(dm[c][k], both(-mean))), q2);      // q (dm - <dm> - m <dm m>)
             out[2 * k] = o.x; out[2 * k + 1] = o.y;
           }
-          store8<GR>((TY*)a.dy + row * a.lddy, out, c, t, G, d);
+          store8<VEC>(row_at<TY>(a.dy, row, a.lddy), out, c, pl);
         }
       }
     }
-    if (has_y && shared_gate && (row + 1 == gate_end || row + 1 == last)) {           // the walker leaves the gate
+    if (has_y && shared_gate && (at + 1 == last || row + a.classes >= gate_end)) {           // the walker leaves the gate
       const int64_t g0 = gate * a.per_gate, g1 = gate_end < a.rows ? gate_end : a.rows;
-      const bool whole = g0 >= first && g1 <= last;
+      const bool whole = a.classes == 1 && g0 >= first && g1 <= last;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         float g[8], dg[8], w[8], s[8], b[8];
-        load8<GR, TY>(g, gs + gate * a.ldg, c, t, G, d);
-        load_param8<GR>(w, w_post, c, t, G, d);
-        load_param8<GR>(s, s_res, c, t, G, d);
-        if (bias) load_param8<GR>(b, b_post, c, t, G, d);
+        load8<VEC>(g, row_at<TY>(gs, gate, a.ldg), c, pl);
+        load8<VEC>(w, w_post, c, pl);
+        load8<VEC>(s, s_res, c, pl);
+        if (bias) load8<VEC>(b, b_post, c, pl);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float H = k & 1 ? accA[c][k / 2].y : accA[c][k / 2].x, E = !GENERAL ? 0.f : (k & 1 ? accB[GENERAL ? c : 0][k / 2].y : accB[GENERAL ? c : 0][k / 2].x);
@@ -398,8 +423,9 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
             dg[k] *= g[k] * (1.f - g[k]);
           }
           if (G == 32) {
-            acc_s[(c * 8 + k) * G] = fmaf(g[k], H, acc_s[(c * 8 + k) * G]);
-            if (GENERAL) acc_s[(CH * 8 + c * 8 + k) * G] = fmaf(g[k], E, acc_s[(CH * 8 + c * 8 + k) * G]);
+            const uint32_t at_a = acc_s + (c * 8 + k) * G * 4, at_b = at_a + CH * 8 * G * 4;
+            sts4f(at_a, fmaf(g[k], H, lds4f(at_a)));
+            if (GENERAL) sts4f(at_b, fmaf(g[k], E, lds4f(at_b)));
           } else {
             w[k] = g[k] * H;
             if (GENERAL) b[k] = g[k] * E;
@@ -407,22 +433,24 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         }
         if (G > 32) {
           float was[8];
-          load8<GR, float>(was, partials + d, c, t, G, d);
+          load8<VEC>(was, partials + d, c, pl);
 #pragma unroll
           for (int k = 0; k < 8; ++k) w[k] += was[k];
-          store8<GR>(partials + d, w, c, t, G, d);
+          store_sums<VEC>(partials + d, w, c, pl);
           if (bias) {
-            load8<GR, float>(was, partials + 3 * (int64_t)d, c, t, G, d);
+            load8<VEC>(was, partials + 3 * (int64_t)d, c, pl);
 #pragma unroll
             for (int k = 0; k < 8; ++k) b[k] += was[k];
-            store8<GR>(partials + 3 * (int64_t)d, b, c, t, G, d);
+            store_sums<VEC>(partials + 3 * (int64_t)d, b, c, pl);
           }
         }
-        if (whole) store8<GR>((TY*)a.dg + gate * a.lddg, dg, c, t, G, d);
-        else store8<GR>(a.gate_partials + (walker + gate) * d, dg, c, t, G, d);
+        if (whole) store_each<VEC>(row_at<TY>(a.dg, gate, a.lddg), dg, c, pl);
+        else store_sums<VEC>(a.gate_partials + gate_slot(a, kind, share, gate) * d, dg, c, pl);
       }
-      ++gate;
-      gate_end += a.per_gate;
+      if (at + 1 < last) {
+        gate = (unsigned)row_of(at + 1) / a.per_gate;
+        gate_end = (gate + 1) * a.per_gate;
+      }
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
 #pragma unroll
@@ -431,7 +459,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
           if (GENERAL) accB[c][k] = both(0.f);
         }
         if constexpr (KEEP)
-          if (row + 1 < last) keep_e(c);
+          if (at + 1 < last) keep_e(c);
       }
     }
   }
@@ -440,8 +468,8 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        accA[c][k] = f2{acc_s[(c * 8 + 2 * k) * G], acc_s[(c * 8 + 2 * k + 1) * G]};
-        if (GENERAL) accB[c][k] = f2{acc_s[(CH * 8 + c * 8 + 2 * k) * G], acc_s[(CH * 8 + c * 8 + 2 * k + 1) * G]};
+        accA[c][k] = f2{lds4f(acc_s + (c * 8 + 2 * k) * G * 4), lds4f(acc_s + (c * 8 + 2 * k + 1) * G * 4)};
+        if (GENERAL) accB[c][k] = f2{lds4f(acc_s + (CH * 8 + c * 8 + 2 * k) * G * 4), lds4f(acc_s + (CH * 8 + c * 8 + 2 * k + 1) * G * 4)};
       }
   const int nq = a.bias ? 4 : 2;
   float* out = partials;
@@ -456,16 +484,19 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       if (qn == 0) singles(v, accC[c]);
       else if (!GENERAL || qn == 1) singles(v, accA[c]);
       else singles(v, qn == 2 ? accD[GENERAL ? c : 0] : accB[GENERAL ? c : 0]);
-      if (G > 32) store8<GR>(out, v, c, t, G, d);
+      if (G > 32) store_sums<VEC>(out, v, c, pl);
       else
 #pragma unroll
-        for (int k = 0; k < 8; ++k) combine[sub * W + column<GR>(c, k, t, 32)] = v[k];
+        for (int k = 0; k < 8; ++k) combine[sub * W + (c * 8 + k) * 32 + t] = v[k];
     }
     if (G == 32) {
       __syncthreads();
       for (int j = threadIdx.x; j < d; j += blockDim.x) {
         float s = 0.f;
-        for (int w = 0; w < subs; ++w) s += combine[w * W + j];
+        for (int w = 0; w < subs; ++w) {              // column j is in another place in each class
+          const int shift = VEC ? (int)(((blockIdx.x * subs + w) % a.classes * a.ld8) & 7) : 0, jj = j + shift;
+          s += combine[w * W + (VEC ? (jj / 256 * 8 + jj % 8) * 32 + jj / 8 % 32 : j)];
+        }
         out[j] = s;
       }
     }
@@ -520,24 +551,34 @@ __global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int
   const int col_blocks = (d + GATE_COLUMNS - 1) / GATE_COLUMNS;
   const int item = (blockIdx.x - param_blocks) / col_blocks, lane = threadIdx.x % GATE_COLUMNS, slice = threadIdx.x / GATE_COLUMNS;
   const int j = ((blockIdx.x - param_blocks) % col_blocks) * GATE_COLUMNS + lane;
-  const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
   int64_t gate = item;
-  if (gates >= a.walkers) {      // more gates than shares: only the ones cut by the start of share item + 1 are open
-    const int64_t cut = share_start(item + 1, a.rows, a.walkers);
+  const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
+  if (a.classes == 1 && gates >= a.shares) {      // more gates than shares: only the ones cut by the start of share item + 1 are open
+    const int64_t cut = share_start(item + 1, a.rows, a.shares);
     gate = cut / a.per_gate;
     const int64_t g0 = gate * a.per_gate;
-    if (g0 == cut || walker_of(g0, a.rows, a.walkers) != item) return;
+    if (g0 == cut || share_of(g0, a.rows, a.shares) != item) return;
   }
   const int64_t g0 = gate * a.per_gate, g1 = g0 + a.per_gate < a.rows ? g0 + a.per_gate : a.rows;
-  const int64_t lo = walker_of(g0, a.rows, a.walkers), hi = walker_of(g1 - 1, a.rows, a.walkers);
-  if (lo == hi) return;
-  // the walkers in between, in slices added in a fixed order; there are no more walkers than rows, so none is empty
   constexpr int GS = 32 * SLICES / GATE_COLUMNS;
   float s = 0.f;
-  if (j < d) {
-    const float* p = a.gate_partials + (lo + slice + gate) * d + j;
+  for (int kind = 0; kind < a.classes; ++kind) {
+    // the class's rows of the gate, and the shares that hold them
+    const int64_t n = class_rows(a, kind), i0 = g0 > kind ? (g0 - kind + a.classes - 1) / a.classes : 0;
+    const int64_t i1 = g1 > kind ? (g1 - kind + a.classes - 1) / a.classes : 0;
+    if (i0 >= i1) continue;
+    const int64_t lo = share_of(i0, n, a.shares), hi = share_of(i1 - 1, n, a.shares);
+    if (a.classes == 1 && lo == hi) return;       // one walker had all of the gate's rows and has written dg
+    if (j < d) {
+      const float* p = a.gate_partials + gate_slot(a, kind, lo + slice, gate) * d + j;
+      if (n >= a.shares) {
 #pragma unroll 8
-    for (int64_t w = lo + slice; w <= hi; w += GS, p += (int64_t)GS * d) s += *p;
+        for (int64_t w = lo + slice; w <= hi; w += GS, p += (int64_t)GS * d) s += *p;
+      } else {                                    // some shares of the class may be empty: their slots hold nothing
+        for (int64_t w = lo + slice; w <= hi; w += GS, p += (int64_t)GS * d)
+          if (share_start(w, n, a.shares) < share_start(w + 1, n, a.shares)) s += *p;
+      }
+    }
   }
   float* sums = &part[0][0][0];
   sums[slice * GATE_COLUMNS + lane] = s;
@@ -546,41 +587,48 @@ __global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < GS; ++i) s += sums[i * GATE_COLUMNS + lane];
-    ((TY*)a.dg)[gate * a.lddg + j] = from_f<TY>(s);
+    row_at<TY>(a.dg, gate, a.lddg)[j] = from_f<TY>(s);
   }
 }
 
-int backward_blocks(int64_t rows, const Layout& l) {
-  const int per_block = l.threads / l.G;
-  const int64_t want = (rows + per_block - 1) / per_block, most = (int64_t)current_sm_count() * l.blocks_per_sm;
-  return (int)(want < 1 ? 1 : (want < most ? want : most));
+// Blocks of the grid, and shares of each class: as many thread groups as the device holds, at most one per row, at least one
+// per class.
+void backward_grid(int64_t rows, const Layout& l, int classes, int& blocks, int& shares) {
+  const int groups = l.threads / l.G;
+  const int64_t walkers = (int64_t)current_sm_count() * l.blocks_per_sm * groups, most = (rows + classes - 1) / classes;
+  int64_t n = walkers / classes;
+  if (n > most) n = most;
+  if (n < 1) n = 1;
+  shares = (int)n;
+  blocks = (int)((n * classes + groups - 1) / groups);
 }
 static inline bool is_general(int bias, int pre, int post) { return bias || pre == BETTY_NORM_LAYER || post == BETTY_NORM_LAYER; }
 // chunks per thread of the wide kernel: the layer norms' and biases' sums leave registers for one
 static constexpr int backward_chunks(bool general) { return general ? 1 : 2; }
-Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int xd, int yd, int granule) {
+Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int xd, int yd, int classes) {
   const bool gated = c->gate != BETTY_GATE_NONE, general = is_general(c->bias, c->pre, c->post);
   const bool row_gate = gated && c->rows_per_gate == 1;             // a gate shared by rows stays in L1
-  Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, 0, 1};
-  n.acc_arrays = gated && !row_gate && c->d <= 32 * 8 * MAX_CH ? 1 + (general ? 2 : 1) : 1;      // e; A (and B) where a warp holds a row
-  Layout l = layout_of(c->d, rows, xd, yd, granule, n);
+  Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, 0};
+  n.acc_arrays = gated && !row_gate && c->d <= 32 * 8 * MAX_CH ? 2 + (general ? 2 : 1) : 2;      // w_pre, e; A (and B) where a warp holds a row
+  Layout l = layout_of(c->d, rows, xd, yd, classes, n);
   const size_t combine = l.G == 32 ? (size_t)(l.threads / 32) * l.chunks * 256 * sizeof(float) : 0;
   if (l.smem < combine) l.smem = combine;
   return l;
 }
 
-template <typename TX, typename TY, int GR, bool PIPE, int CH, bool GENERAL>
+template <typename TX, typename TY, bool VEC, int CH, bool GENERAL>
 static betty_status launch_backward(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
   static SmemLimit limit = {};
-  if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_backward<TX, TY, GR, PIPE, CH, GENERAL>, limit, l.smem));
-  const int blocks = backward_blocks(a.rows, l);
-  launch_pdl(k_backward<TX, TY, GR, PIPE, CH, GENERAL>, dim3(blocks), dim3(l.threads), l.smem, stream, a);
+  if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_backward<TX, TY, VEC, CH, GENERAL>, limit, l.smem));
+  int blocks, shares;
+  backward_grid(a.rows, l, a.classes, blocks, shares);
+  launch_pdl(k_backward<TX, TY, VEC, CH, GENERAL>, dim3(blocks), dim3(l.threads), l.smem, stream, a);
   BETTY_LAUNCH_CHECK();
   const int param_blocks = (a.d + 31) / 32;
   int64_t items = 0;
   if (a.gate_partials && a.rows > 0) {
     const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
-    items = gates < a.walkers ? gates : a.walkers - 1;
+    items = a.classes > 1 || gates < a.shares ? gates : a.shares - 1;
   }
   launch_pdl(k_backward_sums<TY>, dim3((unsigned)(param_blocks + items * ((a.d + GATE_COLUMNS - 1) / GATE_COLUMNS))), dim3(32 * SLICES), 0, stream, a,
              blocks, param_blocks,
@@ -590,13 +638,9 @@ static betty_status launch_backward(cudaStream_t stream, const Args& a, const La
 }
 template <typename TX, typename TY, bool GENERAL>
 static betty_status backward_shape(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
-  constexpr int CH = backward_chunks(GENERAL), GR = sizeof(TY) == 4 ? 1 : 2;
-  if (!l.ahead)
-    return l.granule == 8 ? launch_backward<TX, TY, 8, false, 4, GENERAL>(stream, a, l, dparams)
-                          : launch_backward<TX, TY, 1, false, 4, GENERAL>(stream, a, l, dparams);
-  if (l.granule == 8)
-    return l.wide ? launch_backward<TX, TY, 8, true, CH, GENERAL>(stream, a, l, dparams) : launch_backward<TX, TY, 8, true, 1, GENERAL>(stream, a, l, dparams);
-  return l.wide ? launch_backward<TX, TY, GR, true, CH, GENERAL>(stream, a, l, dparams) : launch_backward<TX, TY, GR, true, 1, GENERAL>(stream, a, l, dparams);
+  if (!l.vec) return launch_backward<TX, TY, false, 4, GENERAL>(stream, a, l, dparams);
+  return l.wide ? launch_backward<TX, TY, true, backward_chunks(GENERAL), GENERAL>(stream, a, l, dparams)
+                : launch_backward<TX, TY, true, 1, GENERAL>(stream, a, l, dparams);
 }
 template <typename TX, typename TY>
 static betty_status backward_typed(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
