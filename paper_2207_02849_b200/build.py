@@ -36,6 +36,11 @@ def _stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _older(path: str, deps) -> bool:
+    """Whether `path` is missing or older than any of `deps`."""
+    return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu of the package into libbetty.so; returns its path."""
     if not force and not _stale():
@@ -45,15 +50,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
     build_dir = os.path.join(PKG_DIR, "_build")
     os.makedirs(build_dir, exist_ok=True)
     procs = []
+    headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")]
+    headers += [os.path.join(ROOT, "include", "betty.h"), os.path.abspath(__file__)]
     # the MLP family sources are compiled twice: bfloat16 operands (default) and IEEE half operands
     units = [(src, "", []) for src in SOURCES] + [(src, "_f16", ["-DBETTY_FP16_OPERANDS"]) for src in FAMILY_SOURCES]
     for src, suffix, extra in units:
         obj = os.path.join(build_dir, src.replace(".cu", suffix + ".o"))
+        objs.append(obj)
+        if not force and not _older(obj, [os.path.join(CSRC, src)] + headers):
+            continue
         cmd = [nvcc, "-c", os.path.join(CSRC, src), "-o", obj] + NVCC_FLAGS + extra
         if verbose:
             cmd += ["-Xptxas", "-v"]
         procs.append((src + suffix, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-        objs.append(obj)
     for src, p in procs:
         out, _ = p.communicate()
         if p.returncode != 0:
