@@ -23,7 +23,6 @@ enum Mode { FORWARD = 0, BACKWARD_DATA = 1, BACKWARD_WEIGHT = 2 };
 static constexpr int BM = 128;                // accumulator lanes of one CTA
 static constexpr int BK = 64;                 // contraction chunk: 64 operand values = one 128-byte swizzle row
 static constexpr int A_BYTES = BM * BK * 2;
-static constexpr int B_BOX = 32;              // rows of the batch per TMA box where a tile is not full
 static constexpr int MAX_GROUPS = 1024;
 static constexpr int THREADS = 320;           // warp 0: TMA, warp 1: MMA, warps 2-9: epilogue
 static constexpr int EPI_WARPS = 8;
@@ -31,6 +30,7 @@ static constexpr uint32_t SPIN = 1u << 24;
 
 template <int CG, int NT> struct Cfg {
   static constexpr int B_BYTES = NT / CG * BK * 2;          // each CTA of a pair stages half of the columns
+  static_assert(NT / CG == 128, "the boxes of B hold up to 128 columns of a CTA");
   static constexpr int STAGE = A_BYTES + B_BYTES;
   static constexpr int STAGES = (192 * 1024) / STAGE < 8 ? (192 * 1024) / STAGE : 8;
   static constexpr int TMEM_COLS = 2 * NT;                  // two accumulators: a tile drains while the next is multiplied
@@ -45,6 +45,7 @@ struct Args {
   int depth;               // contraction extent (not BACKWARD_WEIGHT)
   void* out; int64_t ldo, group_stride;
   uint32_t type_bits;      // operand format bits of the instruction descriptor
+  int a_blocked, b_blocked;// MN-major operands: maps with 64-value blocks as a dimension of their own (see make_blocked_map)
   const CUtensorMap* maps; // BACKWARD_WEIGHT: [groups][2]
   StatusBlock* sb;
 };
@@ -94,6 +95,15 @@ __device__ __forceinline__ void load_3d(void* dst, const CUtensorMap* tm, int x,
   else
     asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(s_u32(dst)), "l"(tm), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void load_4d(void* dst, const CUtensorMap* tm, int x, int y, int z, int w, uint32_t bar) {
+  if (CG == 1)
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(s_u32(dst)), "l"(tm), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+  else
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(s_u32(dst)), "l"(tm), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
 // shared-memory matrix descriptor, 128-byte swizzle: start address, leading and stride byte offsets in 16-byte units
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
@@ -230,7 +240,7 @@ template <> __device__ __forceinline__ __half from_f(float v) { return __float2h
 // CG = 2: a pair of CTAs (a cluster of two) shares a tile of 256 lanes; each stages its own lanes of A and half of the
 // columns of B, the even CTA issues the products, both hold the accumulator rows of their own lanes.
 template <int CG, int NT, int MODE, typename TO>
-__device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmBfull, const Args& a) {
+__device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& tmB32, const CUtensorMap& tmB64, const CUtensorMap& tmB128, const Args& a) {
   using C = Cfg<CG, NT>;
   constexpr int S = C::STAGES;
   constexpr bool A_MN = MODE != FORWARD, B_MN = MODE == BACKWARD_WEIGHT;
@@ -284,19 +294,20 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
       const Tile r = tile_at<CG, NT, MODE>(a, off, before, t, group);
       const int l = r.l0 + (int)rank * BM, half = r.width / CG, c = r.c0 + (int)rank * half;
       const CUtensorMap* ma = &tmA;
-      const CUtensorMap* mb = &tmB;
+      // one box that covers this CTA's columns; rows of it past the tile's are not used
+      const CUtensorMap* mb = half <= 32 ? &tmB32 : (half <= 64 ? &tmB64 : &tmB128);
+      uint32_t b_bytes = (half <= 32 ? 32 : (half <= 64 ? 64 : 128)) * BK * 2;
       if (MODE == BACKWARD_WEIGHT) {
         ma = a.maps + 2 * r.group;
         mb = ma + 1;
+        b_bytes = C::B_BYTES;
         if (mapped != r.group && r.chunks) {
           asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(ma) : "memory");
           asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(mb) : "memory");
           mapped = r.group;
         }
       }
-      const bool whole = !B_MN && r.width == NT;
-      const int boxes = B_MN ? half / 64 : (half + B_BOX - 1) / B_BOX;
-      const uint32_t bytes = CG * (A_BYTES + (uint32_t)boxes * (B_MN ? 64 * BK * 2 : B_BOX * BK * 2));
+      const uint32_t bytes = CG * (A_BYTES + b_bytes);
       for (int it = 0; it < r.chunks; ++it) {
         if (round && !wait(&empty[s], (round - 1) & 1u, abort_flag)) { ok = false; break; }
         unsigned char* sa = smem + s * C::STAGE;
@@ -307,18 +318,25 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
         if (MODE == FORWARD) {
           load_3d<CG>(sa, ma, k, l, r.group, bar);
         } else if (MODE == BACKWARD_DATA) {
-          load_3d<CG>(sa, ma, l, k, r.group, bar);
-          load_3d<CG>(sa + 8192, ma, l + 64, k, r.group, bar);
+          if (a.a_blocked) {
+            load_4d<CG>(sa, ma, 0, k, l / 64, r.group, bar);
+          } else {
+            load_3d<CG>(sa, ma, l, k, r.group, bar);
+            load_3d<CG>(sa + 8192, ma, l + 64, k, r.group, bar);
+          }
+        } else if (a.a_blocked) {
+          load_3d<CG>(sa, ma, 0, k, l / 64, bar);
         } else {
           load_2d<CG>(sa, ma, l, k, bar);
           load_2d<CG>(sa + 8192, ma, l + 64, k, bar);
         }
-        if (B_MN) {
-          for (int j = 0; j < boxes; ++j) load_2d<CG>(sb + j * 8192, mb, c + 64 * j, k, bar);
-        } else if (whole) {
-          load_2d<CG>(sb, &tmBfull, k, c, bar);
+        if (!B_MN) {
+          load_2d<CG>(sb, mb, k, c, bar);
+        } else if (a.b_blocked) {
+          load_3d<CG>(sb, mb, 0, k, c / 64, bar);
         } else {
-          for (int j = 0; j < boxes; ++j) load_2d<CG>(sb + j * (B_BOX * BK * 2), mb, k, c + B_BOX * j, bar);
+          load_2d<CG>(sb, mb, c, k, bar);
+          load_2d<CG>(sb + 8192, mb, c + 64, k, bar);
         }
         if (++s == S) { s = 0; ++round; }
       }
@@ -424,15 +442,15 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
 
 template <int NT, int MODE, typename TO>
 __global__ void __launch_bounds__(THREADS, 1)
-k_grouped(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmBfull,
-          const Args a) {
-  body<1, NT, MODE, TO>(tmA, tmB, tmBfull, a);
+k_grouped(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB32, const __grid_constant__ CUtensorMap tmB64,
+          const __grid_constant__ CUtensorMap tmB128, const Args a) {
+  body<1, NT, MODE, TO>(tmA, tmB32, tmB64, tmB128, a);
 }
 template <int NT, int MODE, typename TO>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
-k_grouped_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmBfull,
-               const Args a) {
-  body<2, NT, MODE, TO>(tmA, tmB, tmBfull, a);
+k_grouped_pair(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB32, const __grid_constant__ CUtensorMap tmB64,
+               const __grid_constant__ CUtensorMap tmB128, const Args a) {
+  body<2, NT, MODE, TO>(tmA, tmB32, tmB64, tmB128, a);
 }
 
 // Writes group e's tensor maps of the weight gradient's operands: the given maps with the row extent cut at the group's end.
@@ -498,15 +516,27 @@ static EncodeTiledFn encode_fn() {
 // an operand as the kernels read it: [groups][rows][cols], 16-bit values
 struct Operand { const void* p; int64_t cols, rows, groups, ld, group_stride; };
 
-static bool make_map(CUtensorMap* tm, int dtype, const Operand& o, bool three, int box_cols, int box_rows) {
+static bool encode(CUtensorMap* tm, int dtype, int rank, const Operand& o, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
   EncodeTiledFn fn = encode_fn();
-  if (!fn) return false;
-  cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.groups};
-  cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)o.group_stride * 2};
-  cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1}, ones[3] = {1, 1, 1};
-  return fn(tm, dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, three ? 3 : 2, (void*)o.p, dims, strides,
-            box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  return fn && fn(tm, dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, (void*)o.p, dims, strides, box,
+                  ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+static bool make_map(CUtensorMap* tm, int dtype, const Operand& o, bool three, int box_cols, int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.groups};
+  const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)o.group_stride * 2};
+  const cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
+  return encode(tm, dtype, three ? 3 : 2, o, dims, strides, box);
+}
+// The same operand with its columns cut into blocks of 64 (their number a dimension of its own), so that one copy brings two
+// blocks of 64 rows in the order that an MN-major operand wants: the issuing thread, not the bytes, bounds the loads
+// otherwise.  Needs a multiple of 64 columns: a short last block would be read past its row.
+static bool make_blocked_map(CUtensorMap* tm, int dtype, const Operand& o, bool three) {
+  const cuuint64_t dims[4] = {64, (cuuint64_t)o.rows, (cuuint64_t)o.cols / 64, (cuuint64_t)o.groups};
+  const cuuint64_t strides[3] = {(cuuint64_t)o.ld * 2, 128, (cuuint64_t)o.group_stride * 2};
+  const cuuint32_t box[4] = {64, 64, 2, 1};
+  return encode(tm, dtype, three ? 4 : 3, o, dims, strides, box);
 }
 
 static inline int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
@@ -528,7 +558,7 @@ static betty_status align_operand(cudaStream_t stream, Arena& arena, Operand& o)
 }
 
 template <int CG, int NT, int MODE, typename TO>
-static betty_status launch_kernel(cudaStream_t stream, const CUtensorMap (&tm)[3], const Args& a, int64_t tiles) {
+static betty_status launch_kernel(cudaStream_t stream, const CUtensorMap (&tm)[4], const Args& a, int64_t tiles) {
   const size_t smem = (size_t)Cfg<CG, NT>::smem(a.groups);
   static SmemLimit limit = {};
   auto kernel = [] {
@@ -538,21 +568,27 @@ static betty_status launch_kernel(cudaStream_t stream, const CUtensorMap (&tm)[3
   BETTY_TRY(ensure_dynamic_smem(kernel, limit, smem));
   const int64_t most = current_sm_count() / CG;
   const int workers = (int)(tiles < 1 ? 1 : (tiles < most ? tiles : most));
-  launch_pdl(kernel, dim3((unsigned)(workers * CG)), dim3(THREADS), smem, stream, tm[0], tm[1], tm[2], a);
+  launch_pdl(kernel, dim3((unsigned)(workers * CG)), dim3(THREADS), smem, stream, tm[0], tm[1], tm[2], tm[3], a);
   BETTY_LAUNCH_CHECK();
   return BETTY_OK;
 }
 
 template <int CG, int NT, int MODE>
 static betty_status run(cudaStream_t stream, Arena& arena, int dtype, int out_dtype, const Operand& A, const Operand& B, Args a) {
-  CUtensorMap tm[3];
-  constexpr bool three = MODE != BACKWARD_WEIGHT;
-  bool ok = make_map(&tm[0], dtype, A, three, 64, MODE == FORWARD ? BM : 64);
-  if (MODE == BACKWARD_WEIGHT) {
-    ok = ok && make_map(&tm[1], dtype, B, false, 64, 64);
-    tm[2] = tm[1];
+  CUtensorMap tm[4];
+  bool ok;
+  if (MODE == FORWARD) {
+    ok = make_map(&tm[0], dtype, A, true, BK, BM);
   } else {
-    ok = ok && make_map(&tm[1], dtype, B, false, BK, B_BOX) && make_map(&tm[2], dtype, B, false, BK, NT / CG);
+    a.a_blocked = A.cols % 64 == 0;
+    ok = a.a_blocked ? make_blocked_map(&tm[0], dtype, A, MODE == BACKWARD_DATA) : make_map(&tm[0], dtype, A, MODE == BACKWARD_DATA, 64, BK);
+  }
+  if (MODE == BACKWARD_WEIGHT) {
+    a.b_blocked = B.cols % 64 == 0;
+    ok = ok && (a.b_blocked ? make_blocked_map(&tm[1], dtype, B, false) : make_map(&tm[1], dtype, B, false, 64, BK));
+    tm[2] = tm[3] = tm[1];
+  } else {
+    ok = ok && make_map(&tm[1], dtype, B, false, BK, 32) && make_map(&tm[2], dtype, B, false, BK, 64) && make_map(&tm[3], dtype, B, false, BK, 128);
   }
   if (!ok) return BETTY_ERR_CUDA;
   const int64_t lane_tiles = (a.lanes + BM * CG - 1) / (BM * CG);
