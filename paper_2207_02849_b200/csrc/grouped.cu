@@ -30,11 +30,13 @@ static constexpr uint32_t SPIN = 1u << 24;
 
 template <int CG, int NT> struct Cfg {
   static constexpr int B_BYTES = NT / CG * BK * 2;          // each CTA of a pair stages half of the columns
-  static_assert(NT / CG == 128, "the boxes of B hold up to 128 columns of a CTA");
+  static_assert(NT / CG <= 128, "the boxes of B hold up to 128 columns of a CTA");
   static constexpr int STAGE = A_BYTES + B_BYTES;
-  static constexpr int STAGES = (192 * 1024) / STAGE < 8 ? (192 * 1024) / STAGE : 8;
+  // narrow tiles leave room for the partial sums of a split contraction (SPLIT_BYTES for each CTA but the first)
+  static constexpr int SPLIT_BYTES = NT <= 64 ? BM * NT * 4 : 0, MAX_SPLIT = NT <= 32 ? 4 : (NT <= 64 ? 2 : 1);
+  static constexpr int STAGES = ((NT <= 64 ? 160 : 192) * 1024) / STAGE;
   static constexpr int TMEM_COLS = 2 * NT;                  // two accumulators: a tile drains while the next is multiplied
-  static constexpr int smem(int groups) { return STAGES * STAGE + 1024 + 256 + 2 * (groups + 1) * 4; }
+  static constexpr int smem(int groups, int split) { return STAGES * STAGE + 1024 + 256 + (split - 1) * SPLIT_BYTES + 2 * (groups + 1) * 4; }
 };
 
 struct Args {
@@ -47,6 +49,7 @@ struct Args {
   uint32_t type_bits;      // operand format bits of the instruction descriptor
   int a_blocked, b_blocked;// MN-major operands: maps with 64-value blocks as a dimension of their own (see make_blocked_map)
   const CUtensorMap* maps; // BACKWARD_WEIGHT: [groups][2]
+  int split;               // CTAs of a cluster that share a tile's contraction (single-SM tiles; then a cluster has one tile at most)
   StatusBlock* sb;
 };
 
@@ -78,6 +81,7 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t smem_addr, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr), "r"(rank));
   return r;
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(tm) : "memory"); }
 template <int CG>
 __device__ __forceinline__ void load_2d(void* dst, const CUtensorMap* tm, int x, int y, uint32_t bar) {
   if (CG == 1)
@@ -144,6 +148,15 @@ __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+
+// One lane of a converged warp, the same each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(p));
+  return p != 0;
+}
+// a value all lanes have, in a form the compiler knows to be the same for all
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 // ------------------------------------------------------------------ tiles
 // Columns per tile of a group with n rows: the tiles of a group are of equal width, so that a few rows over a multiple of
@@ -252,19 +265,25 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
   uint64_t* acc_empty = acc_full + 2;
   uint32_t* tmem_slot = (uint32_t*)(acc_empty + 2);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
-  int* off = (int*)(smem + S * C::STAGE + 256);
+  float* parts = (float*)(smem + S * C::STAGE + 256);        // split contraction: [CTA - 1][column][lane]
+  int* off = (int*)((unsigned char*)parts + (a.split - 1) * C::SPLIT_BYTES);
   int* before = off + a.groups + 1;
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   uint32_t rank = 0;
-  if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+  const bool clustered = CG == 2 || a.split > 1;
+  if (clustered) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  // a pair's rank is its half of the lanes; a split's rank is its part of the contraction
+  const uint32_t half_rank = CG == 2 ? rank : 0;
+  const int part_rank = CG == 1 ? (int)rank : 0;
+  const int worker = blockIdx.x / (CG * a.split), workers = gridDim.x / (CG * a.split);
 
   if (tid == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
     for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], CG * EPI_WARPS); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_map(&tmA); prefetch_map(&tmB32); prefetch_map(&tmB64); prefetch_map(&tmB128);
   }
   if (warp == 0) {
     if (CG == 1) {
@@ -279,103 +298,124 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
   if (warp == 1) list_tiles<CG, NT, MODE>(a, off, before, blockIdx.x == 0);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  if (CG == 2) cluster_sync_all();     // the peer's barriers exist before anything is signalled across the pair
+  if (clustered) cluster_sync_all();   // the others' barriers exist before anything is signalled across the cluster
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
   const int tiles = before[a.groups];
+  Tile mine = {};          // epilogue warps of a split: the cluster's tile
+  int mine_l = 0;
+  bool have_mine = false;
 
-  if (warp == 0 && lane == 0) {
+  // The loading and the multiplying warp run their loops with all lanes, and one lane issues: copies and products take their
+  // descriptors and coordinates from uniform registers, and a loop that the compiler cannot see to be the same for the warp
+  // moves each of them there one by one (measured: 400 ns per chunk of four products in a loop of lane 0 alone, whatever
+  // their width, which was the pace of the whole kernel).
+  if (warp == 0) {
     // ---------------- producer
+    const bool leader = elect_one();
     const uint32_t full0 = CG == 2 ? in_cta(s_u32(full), 0) : s_u32(full);
     int s = 0, group = 0, mapped = -1;
     uint32_t round = 0;
     bool ok = true;
     for (int t = worker; t < tiles && ok; t += workers) {
       const Tile r = tile_at<CG, NT, MODE>(a, off, before, t, group);
-      const int l = r.l0 + (int)rank * BM, half = r.width / CG, c = r.c0 + (int)rank * half;
+      const int g = uniform(r.group), half = uniform(r.width) / CG;
+      const int l = uniform(r.l0) + (int)half_rank * BM, c = uniform(r.c0) + (int)half_rank * half, k0 = uniform(r.k0), chunks = uniform(r.chunks);
       const CUtensorMap* ma = &tmA;
       // one box that covers this CTA's columns; rows of it past the tile's are not used
       const CUtensorMap* mb = half <= 32 ? &tmB32 : (half <= 64 ? &tmB64 : &tmB128);
       uint32_t b_bytes = (half <= 32 ? 32 : (half <= 64 ? 64 : 128)) * BK * 2;
       if (MODE == BACKWARD_WEIGHT) {
-        ma = a.maps + 2 * r.group;
+        ma = a.maps + 2 * g;
         mb = ma + 1;
         b_bytes = C::B_BYTES;
-        if (mapped != r.group && r.chunks) {
-          asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(ma) : "memory");
-          asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(mb) : "memory");
-          mapped = r.group;
+        if (mapped != g && chunks) {
+          if (leader) {
+            asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(ma) : "memory");
+            asm volatile("fence.proxy.tensormap::generic.acquire.gpu [%0], 128;" ::"l"(mb) : "memory");
+          }
+          mapped = g;
         }
       }
       const uint32_t bytes = CG * (A_BYTES + b_bytes);
-      for (int it = 0; it < r.chunks; ++it) {
-        if (round && !wait(&empty[s], (round - 1) & 1u, abort_flag)) { ok = false; break; }
+      const int it1 = (part_rank + 1) * chunks / a.split;
+      for (int it = part_rank * chunks / a.split; it < it1; ++it) {
+        if (round && !__all_sync(0xffffffffu, wait(&empty[s], (round - 1) & 1u, abort_flag))) { ok = false; break; }
         unsigned char* sa = smem + s * C::STAGE;
         unsigned char* sb = sa + A_BYTES;
         const uint32_t bar = full0 + 8u * (uint32_t)s;
-        const int k = r.k0 + it * BK;
-        if (rank == 0) expect_tx(&full[s], bytes);
-        if (MODE == FORWARD) {
-          load_3d<CG>(sa, ma, k, l, r.group, bar);
-        } else if (MODE == BACKWARD_DATA) {
-          if (a.a_blocked) {
-            load_4d<CG>(sa, ma, 0, k, l / 64, r.group, bar);
+        const int k = k0 + it * BK;
+        if (leader) {
+          if (half_rank == 0) expect_tx(&full[s], bytes);
+          if (MODE == FORWARD) {
+            load_3d<CG>(sa, ma, k, l, g, bar);
+          } else if (MODE == BACKWARD_DATA) {
+            if (a.a_blocked) {
+              load_4d<CG>(sa, ma, 0, k, l / 64, g, bar);
+            } else {
+              load_3d<CG>(sa, ma, l, k, g, bar);
+              load_3d<CG>(sa + 8192, ma, l + 64, k, g, bar);
+            }
+          } else if (a.a_blocked) {
+            load_3d<CG>(sa, ma, 0, k, l / 64, bar);
           } else {
-            load_3d<CG>(sa, ma, l, k, r.group, bar);
-            load_3d<CG>(sa + 8192, ma, l + 64, k, r.group, bar);
+            load_2d<CG>(sa, ma, l, k, bar);
+            load_2d<CG>(sa + 8192, ma, l + 64, k, bar);
           }
-        } else if (a.a_blocked) {
-          load_3d<CG>(sa, ma, 0, k, l / 64, bar);
-        } else {
-          load_2d<CG>(sa, ma, l, k, bar);
-          load_2d<CG>(sa + 8192, ma, l + 64, k, bar);
+          if (!B_MN) {
+            load_2d<CG>(sb, mb, k, c, bar);
+          } else if (a.b_blocked) {
+            load_3d<CG>(sb, mb, 0, k, c / 64, bar);
+          } else {
+            load_2d<CG>(sb, mb, c, k, bar);
+            load_2d<CG>(sb + 8192, mb, c + 64, k, bar);
+          }
         }
-        if (!B_MN) {
-          load_2d<CG>(sb, mb, k, c, bar);
-        } else if (a.b_blocked) {
-          load_3d<CG>(sb, mb, 0, k, c / 64, bar);
-        } else {
-          load_2d<CG>(sb, mb, c, k, bar);
-          load_2d<CG>(sb + 8192, mb, c + 64, k, bar);
-        }
+        __syncwarp();
         if (++s == S) { s = 0; ++round; }
       }
     }
     if (*abort_flag)       // copies already issued land in a few microseconds; shared memory must outlive them
       for (int i = 0; i < 64; ++i) __nanosleep(20000);
-  } else if (warp == 1 && lane == 0 && rank == 0) {
+  } else if (warp == 1 && half_rank == 0) {
     // ---------------- MMA issuer (of a pair: the even CTA)
     // K-major: 16 values are 32 bytes further along the swizzled row; 8-row groups 1024 bytes apart.  MN-major: 16
     // contraction rows are 2048 bytes further; 64-value blocks along the other dimension 8192 bytes apart.
+    const bool leader = elect_one();
     const uint32_t sa0 = s_u32(smem), sb0 = sa0 + A_BYTES;
     const uint64_t a0 = A_MN ? smem_desc(sa0, 8192, 1024) : smem_desc(sa0, 16, 1024);
     const uint64_t b0 = B_MN ? smem_desc(sb0, 8192, 1024) : smem_desc(sb0, 16, 1024);
     constexpr uint32_t a_step = A_MN ? 2048 >> 4 : 32 >> 4, b_step = B_MN ? 2048 >> 4 : 32 >> 4;
     const uint32_t fixed = 1u << 4 | a.type_bits | (A_MN ? 1u << 15 : 0u) | (B_MN ? 1u << 16 : 0u) | (uint32_t)(BM * CG / 16) << 24;
+    const uint32_t tmem_u = (uint32_t)uniform((int)tmem_base);
     int s = 0, j = 0, group = 0;
     uint32_t round = 0, stage_off = 0;
     bool ok = true;
     for (int t = worker; t < tiles && ok; t += workers) {
       const Tile r = tile_at<CG, NT, MODE>(a, off, before, t, group);
-      if (!r.chunks) continue;
+      const int chunks = uniform(r.chunks);
+      if (!chunks) continue;
       const int as = j & 1;
-      if (j >= 2 && !wait(&acc_empty[as], (uint32_t)(((j >> 1) - 1) & 1), abort_flag)) break;
+      if (j >= 2 && !__all_sync(0xffffffffu, wait(&acc_empty[as], (uint32_t)(((j >> 1) - 1) & 1), abort_flag))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t acc = tmem_base + (uint32_t)(as * NT), idesc = fixed | (uint32_t)(r.width >> 3) << 17;
-      for (int it = 0; it < r.chunks; ++it) {
-        if (!wait(&full[s], round & 1u, abort_flag)) { ok = false; break; }
+      const uint32_t acc = tmem_u + (uint32_t)(as * NT), idesc = fixed | (uint32_t)(uniform(r.width) >> 3) << 17;
+      const int it0 = part_rank * chunks / a.split, it1 = (part_rank + 1) * chunks / a.split;
+      for (int it = it0; it < it1; ++it) {
+        if (!__all_sync(0xffffffffu, wait(&full[s], round & 1u, abort_flag))) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        uint64_t da = a0 + stage_off, db = b0 + stage_off;
-        mma<CG>(acc, da, db, idesc, it > 0 ? 1u : 0u);
+        const uint64_t da = a0 + stage_off, db = b0 + stage_off;
+        const uint32_t done = s_u32(&empty[s]);
+        if (leader) {
+          mma<CG>(acc, da, db, idesc, it > it0 ? 1u : 0u);
 #pragma unroll
-        for (int kk = 1; kk < BK / 16; ++kk) {
-          da += a_step; db += b_step;
-          mma<CG>(acc, da, db, idesc, 1u);
+          for (int kk = 1; kk < BK / 16; ++kk) mma<CG>(acc, da + kk * a_step, db + kk * b_step, idesc, 1u);
+          commit<CG>(done);
         }
-        commit<CG>(s_u32(&empty[s]));
+        __syncwarp();
         if (++s == S) { s = 0; ++round; stage_off = 0; } else stage_off += C::STAGE >> 4;
       }
-      if (ok) commit<CG>(s_u32(&acc_full[as]));
+      if (ok && leader) commit<CG>(s_u32(&acc_full[as]));
+      __syncwarp();
       ++j;
     }
   } else if (warp >= 2) {
@@ -384,7 +424,7 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
     int j = 0, group = 0;
     for (int t = worker; t < tiles; t += workers) {
       const Tile r = tile_at<CG, NT, MODE>(a, off, before, t, group);
-      const int l = r.l0 + (int)rank * BM + q * 32 + lane;
+      const int l = r.l0 + (int)half_rank * BM + q * 32 + lane;
       TO* out = (TO*)a.out + (MODE == BACKWARD_WEIGHT ? r.group * a.group_stride : 0) + (int64_t)r.c0 * a.ldo + l;
       const int chunks = (r.width + 31) / 32, c_begin = part ? (chunks + 1) / 2 : 0, c_end = part ? chunks : (chunks + 1) / 2;
       if (!r.chunks) {     // a group without rows: its gradient is zero
@@ -397,6 +437,21 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
       have = __all_sync(0xffffffffu, have);
       if (!have) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      if (CG == 1 && a.split > 1) {      // this CTA's part of the sum to the first CTA, which stores the tile below
+        mine = r; mine_l = l;
+        if (part_rank > 0) {
+          const uint32_t to = in_cta(s_u32(parts), 0) + (uint32_t)((part_rank - 1) * C::SPLIT_BYTES + (q * 32 + lane) * 4);
+#pragma unroll 1
+          for (int c = c_begin; c < c_end; ++c) {
+            uint32_t v[32];
+            tmem_load32(v, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(c * 32));
+#pragma unroll
+            for (int k = 0; k < 32; ++k) asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(to + (c * 32 + k) * BM * 4), "r"(v[k]) : "memory");
+          }
+        }
+        have_mine = true;
+        break;
+      }
 #pragma unroll 1
       for (int c = c_begin; c < c_end; ++c) {
         if (c * 32 >= r.cols) break;
@@ -430,6 +485,27 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
     }
   }
   __syncwarp();
+  if (CG == 1 && a.split > 1) {
+    cluster_sync_all();                  // the parts are in the first CTA's shared memory
+    if (have_mine && part_rank == 0) {
+      const int q = warp & 3, part = (warp - 2) >> 2, chunks = (mine.width + 31) / 32;
+      TO* out = (TO*)a.out + (MODE == BACKWARD_WEIGHT ? mine.group * a.group_stride : 0) + (int64_t)mine.c0 * a.ldo + mine_l;
+#pragma unroll 1
+      for (int c = part ? (chunks + 1) / 2 : 0; c < (part ? chunks : (chunks + 1) / 2); ++c) {
+        if (c * 32 >= mine.cols) break;
+        uint32_t v[32];
+        tmem_load32(v, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(c * 32));
+        const int n = min(32, mine.cols - c * 32);
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+          if (k < n) {
+            float x = __uint_as_float(v[k]);
+            for (int p = 0; p + 1 < a.split; ++p) x += parts[(size_t)p * BM * NT + (c * 32 + k) * BM + q * 32 + lane];
+            if (mine_l < a.lanes) out[(int64_t)(c * 32 + k) * a.ldo] = from_f<TO>(x);
+          }
+      }
+    }
+  }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (CG == 2) cluster_sync_all();       // neither CTA leaves while the other may still signal its barriers
@@ -559,16 +635,28 @@ static betty_status align_operand(cudaStream_t stream, Arena& arena, Operand& o)
 
 template <int CG, int NT, int MODE, typename TO>
 static betty_status launch_kernel(cudaStream_t stream, const CUtensorMap (&tm)[4], const Args& a, int64_t tiles) {
-  const size_t smem = (size_t)Cfg<CG, NT>::smem(a.groups);
+  const size_t smem = (size_t)Cfg<CG, NT>::smem(a.groups, a.split);
   static SmemLimit limit = {};
   auto kernel = [] {
     if constexpr (CG == 2) return k_grouped_pair<NT, MODE, TO>;
     else return k_grouped<NT, MODE, TO>;
   }();
   BETTY_TRY(ensure_dynamic_smem(kernel, limit, smem));
-  const int64_t most = current_sm_count() / CG;
+  const int64_t most = current_sm_count() / (CG * a.split);
   const int workers = (int)(tiles < 1 ? 1 : (tiles < most ? tiles : most));
-  launch_pdl(kernel, dim3((unsigned)(workers * CG)), dim3(THREADS), smem, stream, tm[0], tm[1], tm[2], tm[3], a);
+  if (a.split == 1) {
+    launch_pdl(kernel, dim3((unsigned)(workers * CG)), dim3(THREADS), smem, stream, tm[0], tm[1], tm[2], tm[3], a);
+  } else {                 // as launch_pdl, with a cluster per tile
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(workers * a.split)); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    (void)cudaLaunchKernelEx(&cfg, kernel, tm[0], tm[1], tm[2], tm[3], a);
+  }
   BETTY_LAUNCH_CHECK();
   return BETTY_OK;
 }
@@ -601,7 +689,11 @@ static betty_status run(cudaStream_t stream, Arena& arena, int dtype, int out_dt
     BETTY_LAUNCH_CHECK();
     tiles = lane_tiles * ((a.cols + NT - 1) / NT) * a.groups;
   } else {
-    tiles = lane_tiles * (a.rows / NT + a.groups);
+    tiles = lane_tiles * (a.rows / NT + (a.rows < a.groups ? a.rows : a.groups));
+    // few tiles: the CTAs of a cluster share each tile's contraction, at least four chunks each
+    const int chunks = (a.depth + BK - 1) / BK;
+    if (CG == 1)
+      while (a.split < Cfg<CG, NT>::MAX_SPLIT && tiles * a.split * 2 <= current_sm_count() && chunks >= 8 * a.split) a.split *= 2;
   }
   if (out_dtype == BETTY_F32) return launch_kernel<CG, NT, MODE, float>(stream, tm, a, tiles);
   if (dtype == BETTY_BF16) return launch_kernel<CG, NT, MODE, __nv_bfloat16>(stream, tm, a, tiles);
@@ -617,10 +709,16 @@ static betty_status product(const betty_grouped_cfg* c, int64_t rows, const int3
   a.type_bits = c->dtype == BETTY_BF16 ? (1u << 7 | 1u << 10) : 0u;
   BETTY_TRY(align_operand(s, arena, A));
   BETTY_TRY(align_operand(s, arena, B));
-  bool pair;
-  if (MODE == BACKWARD_WEIGHT) pair = a.lanes > BM && a.cols > 128;
-  else pair = a.lanes > BM && rows >= (int64_t)96 * c->n_groups;
-  if (pair) return run<2, 256, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
+  a.split = 1;
+  if (MODE == BACKWARD_WEIGHT)
+    return a.lanes > BM && a.cols > 128 ? run<2, 256, MODE>(s, arena, c->dtype, out_dtype, A, B, a) : run<1, 128, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
+  const int64_t used = rows < c->n_groups ? rows : c->n_groups, mean = (rows + used - 1) / used;
+  // Pairs of SMs with wide tiles where the batch fills them; a wide stage that is mostly empty would leave too few copies in
+  // flight for the memory's latency (~2 us from HBM), so a few rows per expert take narrow stages, eight or ten deep.
+  if (mean <= 32) return run<1, 32, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
+  const int64_t pair_tiles = (a.lanes + 2 * BM - 1) / (2 * BM) * ((mean + 255) / 256) * used;
+  if (mean <= 64 || (mean <= 128 && pair_tiles * 2 < current_sm_count() / 2)) return run<1, 64, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
+  if (a.lanes > BM) return run<2, 256, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
   return run<1, 128, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
 }
 

@@ -79,6 +79,16 @@ def test_products(counts, n_in, n_out, dtype):
         _check(bt, counts, 4, n_in, n_out, dtype)
 
 
+@pytest.mark.parametrize("counts", [[1], [5, 0, 30], [64], [40, 55, 0, 61], [100, 90]], ids=lambda c: "-".join(map(str, c)))
+@pytest.mark.parametrize("n_in,n_out", [(4096, 200), (2056, 1032), (520, 130)])
+def test_few_rows_and_long_contractions(counts, n_in, n_out):
+    """Tiles whose contraction is shared by several CTAs."""
+    import paper_2207_02849_b200 as bt
+    for dtype in (BF, HF):
+        _check(bt, counts, 1, n_in, n_out, dtype, seed=n_in + sum(counts))
+        _check(bt, counts, 0, n_out, n_in, dtype, out=F, seed=n_in + sum(counts))
+
+
 @pytest.mark.parametrize("n_in,n_out", [(1, 1), (7, 64), (64, 7), (129, 257), (1001, 33)])
 @pytest.mark.parametrize("counts", [[3, 0, 70], [300, 161]])
 def test_odd_widths(counts, n_in, n_out):
