@@ -9,10 +9,11 @@ namespace blocknorm {
 // barrier, values, sum, barrier) is several times longer than the memory needs for it, and the rows of a batch share it.
 template <typename TX, typename TY, bool VEC, int CH, int R, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
-  __shared__ float red[2 * RED_VALUES * 16];
+  __shared__ __align__(16) float red[2 * RED_VALUES * 16];
   extern __shared__ __align__(16) char slots[];
+  row_sums_init(red);
   pdl_enter();
-  const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G, subs = blockDim.x / G;
+  const int G = a.G, d = a.d, t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0, subs = G == 32 ? blockDim.x >> 5 : 1;
   // thread group `g` takes rows kind, kind + classes, ... : batches g / classes, g / classes + step, ... of R of them
   const int g_id = blockIdx.x * subs + sub, kind = g_id % a.classes;
   const int64_t n_rows = (a.rows - kind + a.classes - 1) / a.classes, step = (int64_t)(gridDim.x * subs / a.classes) * R;
@@ -198,8 +199,8 @@ static constexpr int forward_batch(bool general) { return general ? 1 : 2; }
 template <typename TX, typename TY, bool GENERAL>
 static betty_status forward_layout(cudaStream_t stream, const Args& a, const Layout& l) {
   if (!l.vec) return launch_forward<TX, TY, false, 4, 1, GENERAL>(stream, a, l);
-  return l.wide ? launch_forward<TX, TY, true, FWD_CHUNKS, forward_batch(GENERAL), GENERAL>(stream, a, l)
-                : launch_forward<TX, TY, true, 1, 1, GENERAL>(stream, a, l);
+  if (l.wide) return launch_forward<TX, TY, true, FWD_CHUNKS, forward_batch(GENERAL), GENERAL>(stream, a, l);
+  return l.chunks == 1 ? launch_forward<TX, TY, true, 1, 1, GENERAL>(stream, a, l) : launch_forward<TX, TY, true, 2, 1, GENERAL>(stream, a, l);
 }
 template <typename TX, typename TY>
 static betty_status forward_typed(cudaStream_t stream, const Args& a, const Layout& l) {
@@ -222,19 +223,19 @@ betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int classes) 
 
 // Many rows take the wide kernel (several chunks per thread: a row's fixed cost, its sums and addresses, is shared by more
 // values); rows that would leave thread groups idle take one chunk per thread.  Rows that cannot be fetched ahead (no common
-// shift; rows so wide that two batches do not fit the shared memory) are read where they are used, four chunks per thread.
+// shift; rows so wide that two do not fit the shared memory) are read where they are used, four chunks per thread.
 Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int classes, const Needs& n) {
   const int bx = xd == BETTY_F32 ? 4 : 2, by = yd == BETTY_F32 ? 4 : 2, sms = current_sm_count();
   const int64_t span = classes > 1 ? d + 7 : d;              // columns with the head of a shifted row
-  for (int attempt = classes > 0 ? 0 : 2; ; ++attempt) {     // wide, one chunk per thread, not fetched ahead
+  for (int attempt = classes > 0 ? 0 : 3; ; ++attempt) {     // wide, one chunk per thread, two, not fetched ahead
     Layout l = {};
-    l.vec = attempt < 2;
+    l.vec = attempt < 3;
     l.wide = attempt == 0;
-    l.chunks = attempt == 0 ? n.wide_chunks : (attempt == 1 ? 1 : MAX_CH);
+    l.chunks = attempt == 0 ? n.wide_chunks : (attempt == 3 ? MAX_CH : attempt);
     const int batch = attempt == 0 ? n.batch : 1;
     const int64_t need = l.vec ? span : d;
     l.G = 32;
-    while (l.G < MAX_G && (int64_t)l.G * 8 * l.chunks < need) l.G *= 2;
+    while (l.G < MAX_G && (int64_t)l.G * 8 * l.chunks < need) l.G += 32;
     if ((int64_t)l.G * 8 * l.chunks < need) continue;
     l.threads = l.G == 32 ? SMALL_THREADS : l.G;
     const int groups = l.threads / l.G;

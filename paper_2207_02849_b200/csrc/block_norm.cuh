@@ -11,7 +11,8 @@
 namespace betty {
 namespace blocknorm {
 
-// A row is held by G threads (a power of two, 32 .. MAX_G), CH * 8 values each.  VEC: chunk c of thread t is the eight
+// A row is held by G threads (a multiple of 32 up to MAX_G; a block's eight warps hold eight rows where G is 32, otherwise
+// a block holds one), CH * 8 values each.  VEC: chunk c of thread t is the eight
 // values from (c * G + t) * 8 - shift, one or two 16-byte accesses, where shift is how far the row starts behind a 16-byte
 // boundary (counted modulo 8 values).  Rows of an odd width start at every shift in turn; the rows that one thread group
 // takes all have the same one ("class": rows of equal number modulo `classes`), so that a thread's columns, and with them
@@ -188,26 +189,24 @@ __device__ __forceinline__ void row_sums(float (&v)[NV], float* red, int& half, 
   const int warps = G >> 5;
   if (lane % (32 / P) == 0) r[lane / (32 / P) * 16 + (t >> 5)] = u[0];
   __syncthreads();
-  const float2* r2 = (const float2*)r;              // at least two warps; every thread adds them in the same order
+  // every thread adds them in the same order, four at a time (the places of absent warps hold zeros)
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const float2 w = r2[i * 8];
-    v[i] = w.x + w.y;
+    const float4 w = *(const float4*)(r + i * 16);
+    v[i] = (w.x + w.y) + (w.z + w.w);
   }
-  if (warps > 2) {
+  for (int j = 4; j < warps; j += 4) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const float2 w = r2[i * 8 + 1];
-      v[i] += w.x + w.y;
-    }
-    for (int j = 4; j < warps; j += 4) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const float4 w = *(const float4*)(r + i * 16 + j);
-        v[i] += (w.x + w.y) + (w.z + w.w);
-      }
+      const float4 w = *(const float4*)(r + i * 16 + j);
+      v[i] += (w.x + w.y) + (w.z + w.w);
     }
   }
+}
+// once, before the first sum
+__device__ __forceinline__ void row_sums_init(float* red) {
+  for (int i = threadIdx.x; i < 2 * RED_VALUES * 16; i += blockDim.x) red[i] = 0.f;
+  __syncthreads();
 }
 
 __device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }

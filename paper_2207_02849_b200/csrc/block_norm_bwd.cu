@@ -47,10 +47,11 @@ __device__ __forceinline__ int64_t gate_slot(const Args& a, int kind, int64_t sh
 // leaves the gate, so A waits in shared memory.
 template <typename TX, typename TY, bool VEC, int CH, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
-  __shared__ float red[2 * RED_VALUES * 16];
+  __shared__ __align__(16) float red[2 * RED_VALUES * 16];
   extern __shared__ __align__(16) char slots[];      // fetched rows; G = 32: at the end the warps' column sums
+  row_sums_init(red);
   pdl_enter();
-  const int G = a.G, d = a.d, t = threadIdx.x & (G - 1), sub = threadIdx.x / G, subs = blockDim.x / G;
+  const int G = a.G, d = a.d, t = G == 32 ? threadIdx.x & 31 : threadIdx.x, sub = G == 32 ? threadIdx.x >> 5 : 0, subs = G == 32 ? blockDim.x >> 5 : 1;
   // walker: share `share` of the rows kind, kind + classes, ...; `at` and `last` count those
   const int walker = blockIdx.x * subs + sub, kind = walker % a.classes, share = walker / a.classes;
   const int64_t n_rows = class_rows(a, kind);
@@ -639,8 +640,7 @@ static betty_status launch_backward(cudaStream_t stream, const Args& a, const La
 template <typename TX, typename TY, bool GENERAL>
 static betty_status backward_shape(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
   if (!l.vec) return launch_backward<TX, TY, false, 4, GENERAL>(stream, a, l, dparams);
-  return l.wide ? launch_backward<TX, TY, true, backward_chunks(GENERAL), GENERAL>(stream, a, l, dparams)
-                : launch_backward<TX, TY, true, 1, GENERAL>(stream, a, l, dparams);
+  return l.chunks == 1 ? launch_backward<TX, TY, true, 1, GENERAL>(stream, a, l, dparams) : launch_backward<TX, TY, true, 2, GENERAL>(stream, a, l, dparams);
 }
 template <typename TX, typename TY>
 static betty_status backward_typed(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {

@@ -250,6 +250,19 @@ template <> __device__ __forceinline__ float from_f(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
 
+// the first n of 32 accumulator columns of this thread's lane
+template <typename TO>
+__device__ __forceinline__ void store_columns(TO* o, int64_t ldo, const uint32_t (&v)[32], int n) {
+  if (n >= 32) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) o[k * ldo] = from_f<TO>(__uint_as_float(v[k]));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (k < n) o[k * ldo] = from_f<TO>(__uint_as_float(v[k]));
+  }
+}
+
 // CG = 2: a pair of CTAs (a cluster of two) shares a tile of 256 lanes; each stages its own lanes of A and half of the
 // columns of B, the even CTA issues the products, both hold the accumulator rows of their own lanes.
 template <int CG, int NT, int MODE, typename TO>
@@ -457,18 +470,7 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
         if (c * 32 >= r.cols) break;
         uint32_t v[32];
         tmem_load32(v, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(as * NT + c * 32));
-        if (l < a.lanes) {
-          TO* o = out + (int64_t)(c * 32) * a.ldo;
-          const int n = r.cols - c * 32;
-          if (n >= 32) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) o[(int64_t)k * a.ldo] = from_f<TO>(__uint_as_float(v[k]));
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (k < n) o[(int64_t)k * a.ldo] = from_f<TO>(__uint_as_float(v[k]));
-          }
-        }
+        if (l < a.lanes) store_columns<TO>(out + (int64_t)(c * 32) * a.ldo, a.ldo, v, r.cols - c * 32);
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
@@ -479,9 +481,8 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
       ++j;
     }
     if (MODE != BACKWARD_WEIGHT) {       // rows beyond the last group: zeros
-      const int64_t n = (int64_t)(a.rows - off[a.groups]) * a.lanes, step = (int64_t)gridDim.x * EPI_WARPS * 32;
-      for (int64_t i = (int64_t)blockIdx.x * EPI_WARPS * 32 + tid - 64; i < n; i += step)
-        ((TO*)a.out)[(off[a.groups] + i / a.lanes) * a.ldo + i % a.lanes] = from_f<TO>(0.f);
+      for (int row = off[a.groups] + blockIdx.x * EPI_WARPS + warp - 2; row < a.rows; row += gridDim.x * EPI_WARPS)
+        for (int l = lane; l < a.lanes; l += 32) ((TO*)a.out)[row * a.ldo + l] = from_f<TO>(0.f);
     }
   }
   __syncwarp();
@@ -495,14 +496,15 @@ __device__ __forceinline__ void body(const CUtensorMap& tmA, const CUtensorMap& 
         if (c * 32 >= mine.cols) break;
         uint32_t v[32];
         tmem_load32(v, tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(c * 32));
-        const int n = min(32, mine.cols - c * 32);
+        const uint32_t from = s_u32(parts) + (uint32_t)((c * 32 * BM + q * 32 + lane) * 4);
+        for (int p = 0; p + 1 < a.split; ++p) {          // in the parts' order
+          float w[32];
 #pragma unroll
-        for (int k = 0; k < 32; ++k)
-          if (k < n) {
-            float x = __uint_as_float(v[k]);
-            for (int p = 0; p + 1 < a.split; ++p) x += parts[(size_t)p * BM * NT + (c * 32 + k) * BM + q * 32 + lane];
-            if (mine_l < a.lanes) out[(int64_t)(c * 32 + k) * a.ldo] = from_f<TO>(x);
-          }
+          for (int k = 0; k < 32; ++k) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(w[k]) : "r"(from + (uint32_t)(p * C::SPLIT_BYTES + k * BM * 4)));
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + w[k]);
+        }
+        if (mine_l < a.lanes) store_columns<TO>(out + (int64_t)(c * 32) * a.ldo, a.ldo, v, mine.cols - c * 32);
       }
     }
   }
@@ -690,10 +692,10 @@ static betty_status run(cudaStream_t stream, Arena& arena, int dtype, int out_dt
     tiles = lane_tiles * ((a.cols + NT - 1) / NT) * a.groups;
   } else {
     tiles = lane_tiles * (a.rows / NT + (a.rows < a.groups ? a.rows : a.groups));
-    // few tiles: the CTAs of a cluster share each tile's contraction, at least four chunks each
+    // few tiles: the CTAs of a cluster share each tile's contraction, eight chunks each or more
     const int chunks = (a.depth + BK - 1) / BK;
     if (CG == 1)
-      while (a.split < Cfg<CG, NT>::MAX_SPLIT && tiles * a.split * 2 <= current_sm_count() && chunks >= 8 * a.split) a.split *= 2;
+      while (a.split < Cfg<CG, NT>::MAX_SPLIT && tiles * a.split * 2 <= current_sm_count() && chunks >= 16 * a.split) a.split *= 2;
   }
   if (out_dtype == BETTY_F32) return launch_kernel<CG, NT, MODE, float>(stream, tm, a, tiles);
   if (dtype == BETTY_BF16) return launch_kernel<CG, NT, MODE, __nv_bfloat16>(stream, tm, a, tiles);
@@ -713,12 +715,14 @@ static betty_status product(const betty_grouped_cfg* c, int64_t rows, const int3
   if (MODE == BACKWARD_WEIGHT)
     return a.lanes > BM && a.cols > 128 ? run<2, 256, MODE>(s, arena, c->dtype, out_dtype, A, B, a) : run<1, 128, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
   const int64_t used = rows < c->n_groups ? rows : c->n_groups, mean = (rows + used - 1) / used;
-  // Pairs of SMs with wide tiles where the batch fills them; a wide stage that is mostly empty would leave too few copies in
-  // flight for the memory's latency (~2 us from HBM), so a few rows per expert take narrow stages, eight or ten deep.
-  if (mean <= 32) return run<1, 32, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
   const int64_t pair_tiles = (a.lanes + 2 * BM - 1) / (2 * BM) * ((mean + 255) / 256) * used;
+  // Measured (bf16, us; pairs 256 wide / single SM 128 / 64 / 32): 24 rows, 8 experts, 1024 x 1024: 12.1 / 11.1 / 9.7 / 10.2; 1 row,
+  // 4096 x 4096: 19.4 / 18.4 / 13.6 / 11.7 (the last two with split contractions); 200 rows, 8 experts, 4096 x 4096: 51.5 / 50.4 /
+  // 50.3 / 61.7; 300 rows, 4 experts, 4096 -> 1024: 20.5 / 19.3 / 14.8 / 17.9; 800 rows, 4 experts, 1024 -> 2048: 11.7 / 9.3 /
+  // 12.7 / 15.7; 5001 rows, 16 experts, 2048 -> 1024: 27.7 / 31.1 / 43.2 / 70.6.
+  if (rows <= 32) return run<1, 32, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
   if (mean <= 64 || (mean <= 128 && pair_tiles * 2 < current_sm_count() / 2)) return run<1, 64, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
-  if (a.lanes > BM) return run<2, 256, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
+  if (a.lanes > BM && pair_tiles * 4 > current_sm_count()) return run<2, 256, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
   return run<1, 128, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
 }
 
