@@ -44,7 +44,7 @@ def batch(g, teacher, block, d, dtype, device="cuda"):
     return offsets, x, target.clone()
 
 
-def main(steps=60, n_experts=4, d=256, hidden=256, rows=1024, groups=8, lr=0.5, lr_upper=20.0, eps0=0.05, alpha=1.0, seed=0, out=print):
+def main(steps=60, n_experts=4, d=256, hidden=256, rows=1024, groups=8, lr=1.0, lr_upper=200.0, eps0=0.05, alpha=1.0, seed=0, out=print):
     g = torch.Generator(device="cuda").manual_seed(seed)
     dtype = torch.bfloat16
     block = ExpertBlock(n_experts, d, hidden, rows, dtype)
