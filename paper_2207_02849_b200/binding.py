@@ -470,6 +470,8 @@ def _mat(t: Optional[torch.Tensor], rows: int, cols: int, dtype: torch.dtype, na
     """Address and leading dimension of a [rows, cols] matrix with consecutive values in a row."""
     if t is None:
         return None, 0
+    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols) and t.is_contiguous():
+        return t.data_ptr(), cols
     if t.dtype is not dtype or not t.is_cuda:
         raise ValueError(f"{name} must be a {dtype} CUDA tensor, got {t.dtype} on {t.device}")
     if t.shape != (rows, cols):

@@ -68,13 +68,14 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   const float* b_post = a.params + 4 * (int64_t)d;
   const int bx = CH * 8 * G * (int)sizeof(TX), by = CH * 8 * G * (int)sizeof(TY);
   const int at_o = bx, at_y = 2 * bx, at_u = 2 * bx + by, at_g = 2 * bx + 2 * by;
-  // shared memory: the walkers' slots; then for each walker w_pre and e of its columns, [half chunk][thread]; then A (and B)
+  // shared memory: the walkers' slots; then for each walker w_pre, e (and b_post s) of its columns, [half chunk][thread]; then A (and B)
   // of walkers whose gates are shared, where a warp holds a row (several walkers to a block), [value][thread] (elsewhere A
   // and B wait in the block's row of the column sums)
   const uint32_t base_s = shared_address(slots), slots_end = base_s + subs * (a.ahead + 1) * a.slot_bytes;
   const uint32_t ring = base_s + sub * (a.ahead + 1) * a.slot_bytes;
-  const uint32_t w_s = slots_end + (sub * 4 * CH * G + t) * 16, e_s = w_s + 2 * CH * G * 16;
-  const uint32_t acc_s = slots_end + subs * 4 * CH * G * 16 + (sub * (GENERAL ? 2 : 1) * CH * 8 * G + t) * 4;
+  constexpr int KEPT = GENERAL ? 6 : 4;      // half chunks of w_pre, e (and b_post s) for each chunk
+  const uint32_t w_s = slots_end + (sub * KEPT * CH * G + t) * 16, e_s = w_s + 2 * CH * G * 16, b_s = e_s + 2 * CH * G * 16;
+  const uint32_t acc_s = slots_end + subs * KEPT * CH * G * 16 + (sub * (GENERAL ? 2 : 1) * CH * 8 * G + t) * 4;
   float* const partials = a.col_partials + (int64_t)blockIdx.x * (a.bias ? 4 : 2) * d;
   const TX* const xs = (const TX*)a.x;
   const TX* const os = (const TX*)a.dxo;
@@ -165,6 +166,13 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       load8<VEC>(w, w_pre, c, pl);
       sts16f(w_s + (2 * c) * G * 16, w[0], w[1], w[2], w[3]);
       sts16f(w_s + (2 * c + 1) * G * 16, w[4], w[5], w[6], w[7]);
+      if (bias) {
+        float s[8];
+        load8<VEC>(w, b_post, c, pl);
+        load8<VEC>(s, s_res, c, pl);
+        sts16f(b_s + (2 * c) * G * 16, w[0] * s[0], w[1] * s[1], w[2] * s[2], w[3] * s[3]);
+        sts16f(b_s + (2 * c + 1) * G * 16, w[4] * s[4], w[5] * s[5], w[6] * s[6], w[7] * s[7]);
+      }
       keep_e(c);
     }
 #pragma unroll
@@ -344,11 +352,19 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) z[k] = mul2(m[k], e[k]);
         if (bias) {
-          f2 b[4], s[4];
-          param(b_post, c, b);
-          param(s_res, c, s);
+          f2 b[4];
+          if constexpr (KEEP) {
+            const float4 b0 = lds16f(b_s + (2 * c) * G * 16), b1 = lds16f(b_s + (2 * c + 1) * G * 16);
+            b[0] = f2{b0.x, b0.y}; b[1] = f2{b0.z, b0.w}; b[2] = f2{b1.x, b1.y}; b[3] = f2{b1.z, b1.w};
+          } else {
+            f2 s[4];
+            param(b_post, c, b);
+            param(s_res, c, s);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) z[k] = fma2(b[k], s[k], z[k]);
+            for (int k = 0; k < 4; ++k) b[k] = mul2(b[k], s[k]);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) z[k] = add2(b[k], z[k]);
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) z[k] = mul2(z[k], dX[k]);
@@ -506,7 +522,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
 
 // Adds the blocks' column sums and forms the parameter gradients (the first param_blocks blocks: 32 columns each, SLICES
 // slices of the list added in a fixed order), then the gates whose rows lie in several walkers' shares.
-static constexpr int SLICES = 16, GATE_COLUMNS = 128;
+static constexpr int SLICES = 32, GATE_COLUMNS = 128;
 template <typename TY>
 __global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int blocks, int param_blocks, float* __restrict__ dparams) {
   __shared__ float part[4][SLICES][32];
@@ -529,13 +545,17 @@ __global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) part[i][slice][threadIdx.x & 31] = v[i];
     __syncthreads();
+    if (slice < 4) {                 // one warp per quantity
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < SLICES; ++i) s += part[slice][i][threadIdx.x & 31];
+      __syncwarp();
+      part[slice][0][threadIdx.x & 31] = s;
+    }
+    __syncthreads();
     if (slice == 0 && j < d) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = 0.f;
-#pragma unroll
-        for (int s = 0; s < SLICES; ++s) v[i] += part[i][s][threadIdx.x];
-      }
+      for (int i = 0; i < 4; ++i) v[i] = part[i][0][threadIdx.x];
       const float w = a.params[d + j], s = a.params[2 * (int64_t)d + j];
       dparams[j] = v[0];
       dparams[d + j] = s * v[1];
@@ -610,7 +630,7 @@ Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int xd, int 
   const bool gated = c->gate != BETTY_GATE_NONE, general = is_general(c->bias, c->pre, c->post);
   const bool row_gate = gated && c->rows_per_gate == 1;             // a gate shared by rows stays in L1
   Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, 0};
-  n.acc_arrays = gated && !row_gate && c->d <= 32 * 8 * MAX_CH ? 2 + (general ? 2 : 1) : 2;      // w_pre, e; A (and B) where a warp holds a row
+  n.acc_arrays = gated && !row_gate && c->d <= 32 * 8 * MAX_CH ? (general ? 5 : 3) : (general ? 3 : 2);      // w_pre, e (, b s); A (, B) where a warp holds a row
   Layout l = layout_of(c->d, rows, xd, yd, classes, n);
   const size_t combine = l.G == 32 ? (size_t)(l.threads / 32) * l.chunks * 256 * sizeof(float) : 0;
   if (l.smem < combine) l.smem = combine;

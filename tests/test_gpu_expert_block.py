@@ -56,6 +56,36 @@ def test_block_gradients(gated, act, kind, gate, per_gate):
         assert _rel(grads[k], w) < TOL, (k, _rel(grads[k], w))
 
 
+def test_block_replays_from_a_graph():
+    """A captured forward and backward pass gives the bits of the direct calls."""
+    from paper_2207_02849_b200.expert_block import ExpertBlock
+    E, d, hidden, rows = 3, 128, 192, 90
+    g = torch.Generator().manual_seed(7)
+    r = lambda *s, scale=1.0: (torch.randn(*s, generator=g) * scale).cuda()  # noqa: E731
+    p = {"entry": 1 + r(3, d, scale=0.1), "exit": 1 + r(3, d, scale=0.1), "up": r(E, 2 * hidden, d, scale=0.1).bfloat16(),
+         "down": r(E, d, hidden, scale=0.1).bfloat16()}
+    block = ExpertBlock(E, d, hidden, rows)
+    offsets = torch.tensor([0, 31, 31, 85], dtype=torch.int32, device="cuda")
+    x, dx_out = r(rows, d), r(rows, d)
+
+    def step():
+        x_out, u_out, kept = block.forward(p, offsets, x)
+        return [x_out, u_out] + [v for v in block.backward(p, offsets, kept, dx_out, None).values() if v is not None]
+
+    direct = [t.clone() for t in step()]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for t in captured:
+        t.fill_(float("nan"))
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(direct, captured):
+        assert torch.equal(a, b)
+
+
 def test_reweighting_example_separates_the_groups():
     spec = importlib.util.spec_from_file_location("example", os.path.join(ROOT, "examples", "reweight_expert_block.py"))
     m = importlib.util.module_from_spec(spec)
