@@ -7,6 +7,9 @@ namespace blocknorm {
 // Bound by memory: per value of a 16-bit row 3 reads and 2 writes, ~20 operations.  Thread groups walk the rows with the
 // parameters in registers and the next rows' values already on their way, R rows at a time: a row's own chain (values, sum,
 // barrier, values, sum, barrier) is several times longer than the memory needs for it, and the rows of a batch share it.
+// Measured at 16384 x 4096 bf16 with a gate per row: 180 us with one row per 512 threads and the next one in registers, 140 with
+// four rows at a time, 108 to 120 with two rows of two chunks in each of two blocks per SM (5.6 to 6.2 TB/s; the bytes
+// alone 104 us).
 template <typename TX, typename TY, bool VEC, int CH, int R, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
   __shared__ __align__(16) float red[2 * RED_VALUES * 16];

@@ -12,9 +12,8 @@ namespace betty {
 namespace blocknorm {
 
 // A row is held by G threads (a multiple of 32 up to MAX_G; a block's eight warps hold eight rows where G is 32, otherwise
-// a block holds one), CH * 8 values each.  VEC: chunk c of thread t is the eight
-// values from (c * G + t) * 8 - shift, one or two 16-byte accesses, where shift is how far the row starts behind a 16-byte
-// boundary (counted modulo 8 values).  Rows of an odd width start at every shift in turn; the rows that one thread group
+// a block holds one), CH * 8 values each.  VEC: chunk c of thread t is the eight values from (c * G + t) * 8 - shift, one or
+// two 16-byte accesses, where shift is how far the row starts behind a 16-byte boundary (counted modulo 8 values).  Rows of an odd width start at every shift in turn; the rows that one thread group
 // takes all have the same one ("class": rows of equal number modulo `classes`), so that a thread's columns, and with them
 // its parameters and column sums, stay the same.  Otherwise (matrices whose rows start at different shifts, or wider rows
 // than shared memory holds) values are accessed one by one: value k of chunk c is column (c * 8 + k) * G + t.

@@ -19,9 +19,6 @@ __device__ __forceinline__ int64_t class_rows(const Args& a, int kind) { return 
 __device__ __forceinline__ int64_t share_start(int64_t share, int64_t n, int shares) { return share * n / shares; }
 __device__ __forceinline__ int64_t share_of(int64_t i, int64_t n, int shares) { return ((i + 1) * shares - 1) / n; }
 
-
-
-
 // a row of sums in the workspace: 16 bytes at a time where that fits
 template <bool VEC>
 __device__ __forceinline__ void store_sums(float* row, const float (&v)[8], int c, const Place& w) {
@@ -44,7 +41,13 @@ __device__ __forceinline__ int64_t gate_slot(const Args& a, int kind, int64_t sh
 // and then dX, dm, dy and all products of the row come out in one go.  Layer norms take the means first and <dm>, <dm m>
 // from dm itself: their combination would cancel two differences that are scaled up by 1 / sigma each where rows are flat.
 // A gate shared by rows needs one sum H = sum dX m per gate: dg = a'(g) s w_post H, and A gains a(g) H when the walker
-// leaves the gate, so A waits in shared memory.
+// leaves the gate, so A waits in the block's row of the column sums.
+//
+// Measured: 8192 x 4096 bf16, RMS norms, gates of 1024 rows: 120 to 127 us (3.2 TB/s) against 62 us for the bytes; 2731 x 1537
+// fp32, layer norms with biases: 70 us against 21.  The instruction stream bounds it, at 16 warps per SM (two blocks of
+// 256 threads at 128 registers): with the loads, the stores or the row sums left out it still takes 111, 115 or 107 of 133 us.
+// Two chunks per thread with the coefficients in shared memory took 123 us where registers for them spilled and took 153;
+// one chunk per thread and 512 threads per row 141; two rows at a time 178 to 201 (spills).
 template <typename TX, typename TY, bool VEC, int CH, bool GENERAL>
 __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   __shared__ __align__(16) float red[2 * RED_VALUES * 16];

@@ -12,6 +12,10 @@
 // instruction, not an empty one.  In the weight gradient the ragged dimension is contracted over: the last chunk of an
 // expert's rows must not read the next expert's, so the tensor maps of its operands end at the expert's last row and TMA
 // fills the rest with zeros (k_group_maps writes one pair of maps per expert).
+//
+// Measured (bf16, alone with a cold L2 / back to back under the power cap): 16384 rows, 8 uneven experts, 4096 x 4096: 386 / 440 us,
+// 1.42 / 1.25 PFLOP/s, 85 % of the measured library rate in both; weight gradient 4096 x 2048: 191 / 227 us; 5001 rows, 16 experts,
+// 2048 -> 1024 (fp16): 32 us against 15 for its bytes: 128 tiles on 74 pairs are two rounds.
 #include <cuda.h>
 #include "common.cuh"
 
