@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
 
 // Adds the blocks' column sums and forms the parameter gradients (the first param_blocks blocks: 32 columns each, SLICES
 // slices of the list added in a fixed order), then the gates whose rows lie in several walkers' shares.
-static constexpr int SLICES = 32, GATE_COLUMNS = 128;
+static constexpr int SLICES = 32, GATE_COLUMNS = 256;
 template <typename TY>
 __global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int blocks, int param_blocks, float* __restrict__ dparams) {
   __shared__ float part[4][SLICES][32];
