@@ -226,7 +226,9 @@ betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int classes) 
 
 // Many rows take the wide kernel (several chunks per thread: a row's fixed cost, its sums and addresses, is shared by more
 // values); rows that would leave thread groups idle take one chunk per thread.  Rows that cannot be fetched ahead (no common
-// shift; rows so wide that two do not fit the shared memory) are read where they are used, four chunks per thread.
+// shift; rows so wide that one does not fit the shared memory) are read where they are used, four chunks per thread.  Wide rows
+// of which only one fits are fetched when it is their turn (backward, a gate to each row, 4096 rows: 8192 bf16 values 166 us,
+// read where they are used 536; 6144 fp32 values 274 and 534).
 Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int classes, const Needs& n) {
   const int bx = xd == BETTY_F32 ? 4 : 2, by = yd == BETTY_F32 ? 4 : 2, sms = current_sm_count();
   const int64_t span = classes > 1 ? d + 7 : d;              // columns with the head of a shifted row
@@ -251,9 +253,12 @@ Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int classes, const Nee
       return l;
     }
     if (l.wide && span <= (int64_t)MAX_G * 8 && rows < (int64_t)2 * batch * groups * l.blocks_per_sm * sms) continue;
-    const int64_t slot = (int64_t)l.slot_bytes * groups * batch, budget = (int64_t)(222 * 1024) / l.blocks_per_sm - 2048 - (int64_t)acc;
+    // the last 5 KB only where a row would not fit without them: as L1 they serve the kernels better than one row more in
+    // flight would (2731 x 1537 fp32 backward 70 us, 77 with them; 16384 x 4096 bf16 forward 115, 122)
+    const int64_t most = (attempt == 2 ? 227 : 222) * 1024;
+    const int64_t slot = (int64_t)l.slot_bytes * groups * batch, budget = most / l.blocks_per_sm - 2048 - (int64_t)acc;
     l.ahead = (int)(budget / slot) - 1;
-    if (l.ahead < 1) continue;
+    if (l.ahead < (attempt == 2 ? 0 : 1)) continue;
     if (l.ahead > MAX_AHEAD) l.ahead = MAX_AHEAD;
     l.smem = acc + (size_t)(l.ahead + 1) * slot;
     return l;

@@ -215,7 +215,7 @@ struct Args {
   int d, G;
   int classes;              // 1, 2, 4 or 8: row r starts at the shift of row r % classes,
   int ld8;                  // which is (r * ld8) modulo 8
-  int ahead;                // batches of rows fetched ahead of the present one, 1 .. MAX_AHEAD (kernels that fetch ahead)
+  int ahead;                // batches of rows fetched ahead of the present one, up to MAX_AHEAD (kernels that fetch ahead)
   int slot_bytes;           // of one row, all streams
   int pre, post, gate, bias;
   unsigned per_gate;
@@ -245,7 +245,7 @@ struct Layout {
   int threads;              // of a block
   int blocks_per_sm;        // that the grid counts on
   bool wide;                // two chunks and several rows at a time: many rows; else the shortest way for a few
-  int ahead, slot_bytes;    // batches fetched ahead; 0: rows are read from global memory where they are used
+  int ahead, slot_bytes;    // batches fetched ahead; 0 with vec: a row is fetched when it is its turn
   size_t smem;
 };
 

@@ -99,6 +99,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         if (row_gate) copy_row<CH>(p + at_g, row_at<TY>(gs, r, a.ldg), pl);
       }
       copies_commit();
+      if (CH == 2 && a.ahead == 0) copies_commit();      // an empty group behind the present row's: copies_wait leaves one in flight
     }
   };
   // one chunk of a stream of the present row

@@ -356,3 +356,23 @@ def test_refusals_of_the_binding():
     with pytest.raises(bt.BettyError) as e:
         bt.betty_block_norm_backward(cfg, p, t, t, gate, t, t, o, o.clone(), gate.clone(), p.clone(), small)
     assert e.value.status == bt.BETTY_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("rows", [1, 7, 8, 9, 15, 17, 85, 150, 1300])
+@pytest.mark.parametrize("d,per_gate", [(515, 7), (515, 20), (1538, 7), (1540, 5), (4101, 9)])
+def test_gates_shared_by_a_few_rows_of_an_odd_width(rows, d, per_gate):
+    """Rows whose starts repeat every 2, 4 or 8 rows are walked by class, so a gate's rows lie in several walkers' shares; with
+    few rows the classes differ in length and a share can be empty."""
+    import paper_2207_02849_b200 as bt
+    q = _problem(rows + d, rows, d, F, F, "sigmoid", per_gate, False)
+    _check_backward(bt, q, (d, "rms", "rms", "sigmoid", per_gate, False, 1e-5))
+
+
+@pytest.mark.parametrize("d", [5200, 8192])
+@pytest.mark.parametrize("kind,bias", [("rms", False), ("layer", True)])
+@pytest.mark.parametrize("rows", [3, 500])
+def test_rows_too_wide_for_two_to_be_fetched(rows, d, kind, bias):
+    import paper_2207_02849_b200 as bt
+    for tx, ty in ((F, F), (BF, BF), (F, BF)):
+        q = _problem(rows + d, rows, d, tx, ty, "sigmoid", 1, bias)
+        _check_backward(bt, q, (d, kind, kind, "sigmoid", 1, bias, 1e-5))
