@@ -253,8 +253,8 @@ Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int classes, const Nee
       return l;
     }
     if (l.wide && span <= (int64_t)MAX_G * 8 && rows < (int64_t)2 * batch * groups * l.blocks_per_sm * sms) continue;
-    // the last 5 KB only where a row would not fit without them: as L1 they serve the kernels better than one row more in
-    // flight would (2731 x 1537 fp32 backward 70 us, 77 with them; 16384 x 4096 bf16 forward 115, 122)
+    // the last 5 KB (left to L1 elsewhere) where a row would not fit without them: 4096 x 8192 fp32 backward 356 us, read
+    // where it is used 637
     const int64_t most = (attempt == 2 ? 227 : 222) * 1024;
     const int64_t slot = (int64_t)l.slot_bytes * groups * batch, budget = most / l.blocks_per_sm - 2048 - (int64_t)acc;
     l.ahead = (int)(budget / slot) - 1;
