@@ -371,7 +371,7 @@ extern "C" betty_status betty_block_norm_backward(const betty_block_norm_cfg* cf
   if (!aligned16(params) || !aligned16(dparams)) return BETTY_ERR_ALIGNMENT;
   if (!ws || ws_bytes < sizeof(StatusBlock) || (((uintptr_t)ws) & 255u)) return BETTY_ERR_WORKSPACE;
   const int64_t d = cfg->d;
-  const bool gated = y && cfg->gate != BETTY_GATE_NONE;
+  const bool gated = rows > 0 && y && cfg->gate != BETTY_GATE_NONE;      // without rows there is no gate row to read either
   Args a = {};
   Rows r = {-1, 1};
   if (rows > 0) {
