@@ -92,6 +92,13 @@ __device__ __forceinline__ float max_nan(float a, float b) {       // NaN if eit
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+// 127 * (1 / t), both operations rounded to fp32 with subnormal results kept: 1 / t is one from t = 2^126 on (the library is
+// compiled with subnormals flushed, which would make the whole group zeros), the product never is
+__device__ __forceinline__ float steps_per_unit(float t) {
+  float r;
+  asm("{\n\t.reg .f32 a;\n\trcp.rn.f32 a, %1;\n\tmul.rn.f32 %0, a, 0f42FE0000;\n\t}" : "=f"(r) : "f"(t));
+  return r;
+}
 // z -> q (its fp32 holder's low byte) and the group's scale; lane l of a group's STORE_LANES lanes has its values 8l .. 8l+7 and
 // 64 + 8l .. (aligned rows; otherwise every STORE_LANES-th of each half)
 template <bool ALIGNED>
@@ -104,7 +111,7 @@ __device__ __forceinline__ void quantise(const f2 (&z)[2][4], int8_t* q, float* 
 #pragma unroll
   for (int o = STORE_LANES / 2; o; o >>= 1) t = max_nan(t, __shfl_xor_sync(0xffffffffu, t, o));
   const bool bad = !(t <= 3.4028235e38f), some = t >= TINY && !bad;
-  const float inv = some ? __fmul_rn(__frcp_rn(t), 127.f) : 0.f;
+  const float inv = some ? steps_per_unit(t) : 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t b[8];
