@@ -301,18 +301,20 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       for (int i = 0; i < NS; ++i) S[i] = s2[i].x + s2[i].y;
       row_sums<NS>(S, red, half, G, t);
     }
-    float r = 1.f, q = 1.f, cx = 0.f, mean_dn = 0.f;      // dX = dx' + r (dn0 - <dn>) + cx (x - mean)
+    // dX = dx' + r (dn0 - <dn>) + cn n with n = r (x - mean) and cn = -r <dn n>.  Every factor here is of the size of n, dn, x or
+    // 1 / x: a coefficient of x itself would have r^3 in it, which leaves the fp32 range for rows beyond 1e-12 .. 1e12.
+    float r = 1.f, q = 1.f, cn = 0.f, mean_dn = 0.f;
     if (a.pre != BETTY_NORM_NONE && has_u) {
       r = rsqrtf(fmaf(S[0], a.inv_d, a.eps));
-      cx = -r * r * r * S[1] * a.inv_d;
+      cn = -(r * (S[1] * a.inv_d)) * r;
       if (pre_layer) mean_dn = S[3] * a.inv_d;
     }
     float pm = 0.f;
     if (a.post != BETTY_NORM_NONE && has_y) {
       q = rsqrtf(fmaf(S[2], a.inv_d, a.eps));
-      if constexpr (!GENERAL) pm = q * fmaf(r, S[NS - 2], fmaf(cx, S[NS - 1], S[3])) * a.inv_d;
+      if constexpr (!GENERAL) pm = q * fmaf(r, S[NS - 2], fmaf(cn, r * S[NS - 1], S[3])) * a.inv_d;
     }
-    const f2 r2 = both(r), cx2 = both(cx), q2 = both(q), pq2 = both(-pm * q), dn2 = both(-mean_dn);
+    const f2 r2 = both(r), cn2 = both(cn), q2 = both(q), pq2 = both(-pm * q), dn2 = both(-mean_dn);
     f2 dm[GENERAL ? CH : 1][4], sm = both(0.f), sd = both(0.f);       // layer norms: dm, sum dm m, sum dm
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -330,14 +332,15 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           if (GENERAL) x[k] = fma2(both(-mx), mask[c][k], x[k]);
-          dX[k] = fma2(x[k], cx2, dX[k]);
+          const f2 n = mul2(x[k], r2);
+          dX[k] = fma2(n, cn2, dX[k]);
           f2 dn = mul2(u[k], w[k]);
           if (GENERAL) dn = add2(dn, dn2);          // subtracted before the scaling: r can be large where a row is flat
           dX[k] = fma2(dn, r2, dX[k]);
           if (GENERAL) {
             accD[c][k] = add2(accD[c][k], u[k]);
           }
-          accC[c][k] = fma2(u[k], mul2(x[k], r2), accC[c][k]);
+          accC[c][k] = fma2(u[k], n, accC[c][k]);
         }
       }
       singles(out, dX);

@@ -2,6 +2,9 @@
 import pytest
 import torch
 
+from tests import block_reference as ref
+from tests.test_gpu_block_norm import SLACK, _cfg, _gradients, _problem
+
 pytestmark = pytest.mark.gpu
 BF, HF, F = torch.bfloat16, torch.float16, torch.float32
 
@@ -19,3 +22,36 @@ def test_no_rows_and_no_gate_rows():
                                                 torch.cuda.current_stream().cuda_stream)
     assert status == bt.BETTY_OK and bt.betty_poll_status(ws)[0] == bt.BETTY_OK
     assert float(dparams.abs().max()) == 0.0 and float((y - 1).abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("size", [1e-17, 1e-13, 1e13, 1e17])
+@pytest.mark.parametrize("which", ["x", "y"])
+@pytest.mark.parametrize("kind,act", [("rms", "none"), ("rms", "linear"), ("layer", "none")])
+@pytest.mark.parametrize("d", [256, 515])
+def test_rows_of_any_size(size, which, kind, act, d):
+    """A norm takes out its row's size: with eps = 0 the gradients of rows scaled by c are those of the rows divided by c.  What
+    is added to them from elsewhere has the same size here, so that the same tolerances hold: every intermediate result is in
+    range as long as the squares of the row are (1e-19 to 1e19)."""
+    import paper_2207_02849_b200 as bt
+    q = _problem(17, 12, d, F, F, act, 1, False)
+    q[which] *= size
+    if which == "x":
+        q["dxo"] *= 1.0 / size
+        q["y"] *= size                                # keeps u's own input at one size; eps is 0
+    args = (d, kind, kind, act, 1, False, 0.0)
+    cfg = _cfg(bt, *args)
+    ws = bt.Workspace.of_bytes(bt.betty_block_norm_workspace_size(cfg, 12))
+    dx, dy, dp = torch.empty_like(q["x"]), torch.empty_like(q["y"]), torch.empty_like(q["params"])
+    dg = torch.empty_like(q["gate"]) if act != "none" else None
+    bt.betty_block_norm_backward(cfg, q["params"], q["x"], q["y"], q["gate"], q["du"], q["dxo"], dx, dy, dg, dp, ws)
+    want = _gradients(q, args)
+    rms = lambda t: t.pow(2).mean(-1, keepdim=True).sqrt()  # noqa: E731
+    n = rms(ref.d64(q["x"]) - (ref.d64(q["x"]).mean(1, keepdim=True) if kind == "layer" else 0.0))
+    m = rms(ref.d64(q["y"]) - (ref.d64(q["y"]).mean(1, keepdim=True) if kind == "layer" else 0.0))
+    p = ref.d64(q["params"]).abs().amax(1)
+    big = rms(want["dx"]) + rms(ref.d64(q["dxo"])) + p[0] * rms(ref.d64(q["du"])) / n      # the terms that make dX
+    amp = float(p[1] * p[2]) * (4.0 if act == "linear" else 1.0)
+    assert float(((dx.double().cpu() - want["dx"]).abs() / big).max()) <= SLACK
+    assert float(((dy.double().cpu() - want["dy"]).abs() / (rms(want["dy"]) + amp * big / m)).max()) <= SLACK
+    if dg is not None:
+        assert float(((dg.double().cpu() - want["dgate"]).abs() / (4.0 * amp * big)).max()) <= SLACK
