@@ -369,8 +369,12 @@ betty_status betty_block_norm(const betty_block_norm_cfg* cfg, const float* para
                               const void* y, int64_t ldy, const void* gate, int64_t ldg, void* x_out, int64_t ldxo, void* u,
                               int64_t ldu, void* stream);
 
-/* Workspace of the backward call on up to `rows` rows (on the current device). */
+/* Workspace of the backward call on up to `rows` rows (on the current device), whatever the matrices' leading dimensions. */
 betty_status betty_block_norm_workspace_size(const betty_block_norm_cfg* cfg, int64_t rows, size_t* bytes);
+/* The same; any_layout == 0: not for matrices that all share a leading dimension that differs from d modulo 8 (contiguous
+ * matrices and slices of them next to contiguous ones are served; others may return BETTY_ERR_WORKSPACE).  With a gate shared
+ * by a few rows the difference is up to an fp32 copy of one matrix, since rows of an odd leading dimension are summed apart. */
+betty_status betty_block_norm_workspace_size_for(const betty_block_norm_cfg* cfg, int64_t rows, int32_t any_layout, size_t* bytes);
 
 /* Gradients of betty_block_norm from its stored x' and its inputs y and gate (no statistics are kept):
  * du (NULL: u was not used) and dx_out (the gradient that reaches x' from elsewhere; NULL: none), not both NULL, give

@@ -124,6 +124,7 @@ def lib():
     mat = [VP, I64]
     sig["betty_block_norm"] = [BN, VP, I64] + 5 * mat + [VP]
     sig["betty_block_norm_workspace_size"] = [BN, I64, C.POINTER(SZ)]
+    sig["betty_block_norm_workspace_size_for"] = [BN, I64, I32, C.POINTER(SZ)]
     sig["betty_block_norm_backward"] = [BN, VP, I64] + 8 * mat + [VP, VP, SZ, VP]
     sig["betty_act8_store"] = [A8, I64] + 4 * mat + [VP]
     sig["betty_act8_restore"] = [A8, I64] + 3 * mat + [VP]
@@ -532,9 +533,11 @@ def betty_block_norm(cfg: BlockNorm, params: torch.Tensor, x: torch.Tensor, y: O
                                   _stream(stream)), "betty_block_norm")
 
 
-def betty_block_norm_workspace_size(cfg: BlockNorm, rows: int) -> int:
+def betty_block_norm_workspace_size(cfg: BlockNorm, rows: int, any_layout: bool = True) -> int:
+    """any_layout False: for contiguous matrices (and slices of wider ones next to contiguous ones)."""
     out = C.c_size_t(0)
-    _check(lib().betty_block_norm_workspace_size(cfg._ref(torch.float32, torch.float32), int(rows), C.byref(out)), "betty_block_norm_workspace_size")
+    _check(lib().betty_block_norm_workspace_size_for(cfg._ref(torch.float32, torch.float32), int(rows), int(any_layout), C.byref(out)),
+           "betty_block_norm_workspace_size")
     return int(out.value)
 
 

@@ -283,6 +283,7 @@ static betty_status check_cfg(const betty_block_norm_cfg* c, int64_t rows) {
 // The matrices of a call: `classes` becomes 0 when their rows do not all start at the same shift (see block_norm.cuh), else
 // the period of the shifts.
 struct Rows { int64_t ld; int classes; };      // ld: modulo 8, or -1 before the first matrix
+static inline int classes_of(int64_t ld8) { return ld8 == 0 ? 1 : (ld8 == 4 ? 2 : (ld8 % 2 == 0 ? 4 : 8)); }
 static betty_status check_matrix(const void* p, int64_t ld, int64_t rows, int64_t d, int dtype, Rows& r) {
   if (!p) return BETTY_OK;
   if (rows > 1 && ld < d) return BETTY_ERR_SHAPE;
@@ -292,7 +293,7 @@ static betty_status check_matrix(const void* p, int64_t ld, int64_t rows, int64_
   if (rows > 1) {
     if (r.ld >= 0 && r.ld != (ld & 7)) r.classes = 0;
     r.ld = ld & 7;
-    if (r.classes) r.classes = r.ld == 0 ? 1 : (r.ld == 4 ? 2 : (r.ld % 2 == 0 ? 4 : 8));
+    if (r.classes) r.classes = classes_of(r.ld);
   }
   return BETTY_OK;
 }
@@ -340,25 +341,31 @@ extern "C" betty_status betty_block_norm(const betty_block_norm_cfg* cfg, const 
   return forward((cudaStream_t)stream, a, cfg->x_dtype, cfg->y_dtype, r.classes);
 }
 
-extern "C" betty_status betty_block_norm_workspace_size(const betty_block_norm_cfg* cfg, int64_t rows, size_t* bytes) {
+extern "C" betty_status betty_block_norm_workspace_size_for(const betty_block_norm_cfg* cfg, int64_t rows, int32_t any_layout, size_t* bytes) {
   if (!bytes) return BETTY_ERR_INVALID_ARG;
   BETTY_TRY(check_cfg(cfg, rows));
-  const int64_t gates = (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate;
   const bool shared = cfg->gate != BETTY_GATE_NONE && cfg->rows_per_gate > 1;
   int64_t floats = 0;
-  // whatever the matrices' types and addresses will be
-  for (int classes : {0, 1, 2, 4, 8})
+  // whatever the matrices' types will be, and their addresses: none (0: not at one shift, 1: one row) or those of their own width
+  for (int classes : {0, 1, 2, 4, 8}) {
+    if (!any_layout && classes > 1 && classes != classes_of(cfg->d & 7)) continue;
     for (int xd : {BETTY_F32, BETTY_BF16})
-      for (int yd : {BETTY_F32, BETTY_BF16}) {
-        const Layout l = backward_layout(cfg, rows, xd, yd, classes);
-        int blocks, shares;
-        const int used = l.vec ? classes : 1;
-        backward_grid(rows, l, used, blocks, shares);
-        const int64_t n = ((int64_t)blocks * quantities(cfg) + (shared ? used * (shares + gates) : 0)) * cfg->d;
-        if (n > floats) floats = n;
-      }
+      for (int yd : {BETTY_F32, BETTY_BF16})
+        for (int64_t r : {rows, (int64_t)0}) {       // fewer rows may take the other layout, of more and smaller blocks
+          const Layout l = backward_layout(cfg, r, xd, yd, classes);
+          int blocks, shares;
+          const int used = l.vec ? classes : 1;
+          backward_grid(rows, l, used, blocks, shares);
+          const int64_t sums = shared ? used * gate_sums_of(rows, cfg->rows_per_gate, used, shares).rows : 0;
+          const int64_t n = ((int64_t)blocks * quantities(cfg) + sums) * cfg->d;
+          if (n > floats) floats = n;
+        }
+  }
   *bytes = sizeof(StatusBlock) + 2 * 256 + (size_t)floats * sizeof(float);
   return BETTY_OK;
+}
+extern "C" betty_status betty_block_norm_workspace_size(const betty_block_norm_cfg* cfg, int64_t rows, size_t* bytes) {
+  return betty_block_norm_workspace_size_for(cfg, rows, 1, bytes);
 }
 
 extern "C" betty_status betty_block_norm_backward(const betty_block_norm_cfg* cfg, const float* params, int64_t rows,
@@ -400,8 +407,10 @@ extern "C" betty_status betty_block_norm_backward(const betty_block_norm_cfg* cf
   a.ld8 = r.ld > 0 ? (int)r.ld : 0;
   backward_grid(rows, l, a.classes, blocks, a.shares);
   a.col_partials = arena.alloc<float>((size_t)blocks * quantities(cfg) * d);
-  if (gated && cfg->rows_per_gate > 1)
-    a.gate_partials = arena.alloc<float>((size_t)(a.classes * (a.shares + (rows + cfg->rows_per_gate - 1) / cfg->rows_per_gate)) * d);
+  if (gated && cfg->rows_per_gate > 1) {
+    a.gate_sums = gate_sums_of(rows, cfg->rows_per_gate, a.classes, a.shares);
+    a.gate_partials = arena.alloc<float>((size_t)(a.classes * a.gate_sums.rows) * d);
+  }
   if (arena.overflow) return BETTY_ERR_WORKSPACE;
   return backward((cudaStream_t)stream, a, l, cfg->x_dtype, cfg->y_dtype, dparams);
 }

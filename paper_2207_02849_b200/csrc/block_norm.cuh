@@ -210,6 +210,9 @@ __device__ __forceinline__ void row_sums_init(float* red) {
 
 __device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
 
+// places of the walkers' sums for gates of several rows (see gate_slot)
+struct GateSums { int64_t rows; unsigned per_share, per_gate, per_row, begins; };
+
 struct Args {
   int64_t rows;
   int d, G;
@@ -233,7 +236,8 @@ struct Args {
   void* dx; uint32_t lddx;
   void* dy; uint32_t lddy;
   void* dg; uint32_t lddg;
-  float* gate_partials;                // [classes][shares + gates][d] (gates of several rows)
+  float* gate_partials;                // [classes][gate_sums.rows][d] (gates of several rows)
+  GateSums gate_sums;
   float* col_partials;                 // [blocks, quantities, d]
   int shares;                          // backward: contiguous shares that the rows of a class are cut into
 };
@@ -259,6 +263,7 @@ Layout layout_of(int64_t d, int64_t rows, int x_dtype, int y_dtype, int classes,
 betty_status forward(cudaStream_t stream, Args& a, int x_dtype, int y_dtype, int classes);
 Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int x_dtype, int y_dtype, int classes);
 void backward_grid(int64_t rows, const Layout& l, int classes, int& blocks, int& shares);
+GateSums gate_sums_of(int64_t rows, int64_t per_gate, int classes, int shares);
 betty_status backward(cudaStream_t stream, Args& a, const Layout& l, int x_dtype, int y_dtype, float* dparams);
 
 }  // namespace blocknorm

@@ -25,10 +25,15 @@ __device__ __forceinline__ void store_sums(float* row, const float (&v)[8], int 
   if (VEC && w.shift == 0 && w.d % 4 == 0) store8<VEC>(row, v, c, w);
   else store_each<VEC>(row, v, c, w);
 }
-// a walker's sum for a gate of several rows: shares and gates both grow along the rows, so no two pairs of a class meet
-__device__ __forceinline__ int64_t gate_slot(const Args& a, int kind, int64_t share, int64_t gate) {
-  const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
-  return kind * (a.shares + gates) + share + gate;
+// Where a walker's sum for a gate of several rows waits to be added to the other walkers'.  One class: a share has at most two
+// gates that are not all its own, one that began before it and one that `begins` in it and goes on behind it.  Several
+// classes: shares and gates both grow along the rows, so no two pairs of a class meet at share + gate; where that is more
+// places than the class has rows (gates of few rows), a pair's place is its last row.
+__device__ __forceinline__ unsigned first_slot(const Args& a, int kind, unsigned share) {
+  return (unsigned)kind * (unsigned)a.gate_sums.rows + a.gate_sums.per_share * share;
+}
+__device__ __forceinline__ unsigned gate_slot(const Args& a, unsigned first, unsigned gate, bool begins, unsigned last_row) {
+  return first + a.gate_sums.per_gate * gate + a.gate_sums.per_row * last_row + (begins ? a.gate_sums.begins : 0u);
 }
 
 // Each walker (thread group) takes a contiguous share of the rows, so that the column sums stay in its registers; it writes
@@ -48,7 +53,7 @@ __device__ __forceinline__ int64_t gate_slot(const Args& a, int kind, int64_t sh
 // 256 threads at 128 registers): with the loads, the stores or the row sums left out it still takes 111, 115 or 107 of 133 us.
 // Two chunks per thread with the coefficients in shared memory took 123 us where registers for them spilled and took 153;
 // one chunk per thread and 512 threads per row 141; two rows at a time 178 to 201 (spills).
-template <typename TX, typename TY, bool VEC, int CH, bool GENERAL>
+template <typename TX, typename TY, bool VEC, int CH, bool GENERAL, bool SHARED>
 __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   __shared__ __align__(16) float red[2 * RED_VALUES * 16];
   extern __shared__ __align__(16) char slots[];      // fetched rows; G = 32: at the end the warps' column sums
@@ -58,13 +63,14 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   // walker: share `share` of the rows kind, kind + classes, ...; `at` and `last` count those
   const int walker = blockIdx.x * subs + sub, kind = walker % a.classes, share = walker / a.classes;
   const int64_t n_rows = class_rows(a, kind);
-  const int64_t first = share < a.shares ? share_start(share, n_rows, a.shares) : n_rows;
-  const int64_t last = share < a.shares ? share_start(share + 1, n_rows, a.shares) : n_rows;
+  // (row numbers and what is added to them stay below 2^32: a call has at most 2^31 - 1 rows, and so has a gate)
+  const unsigned first = share < a.shares ? (unsigned)share_start(share, n_rows, a.shares) : (unsigned)n_rows;
+  const unsigned last = share < a.shares ? (unsigned)share_start(share + 1, n_rows, a.shares) : (unsigned)n_rows;
   const Place pl = {t, G, d, VEC ? (int)((kind * a.ld8) & 7) : 0};
-  auto row_of = [&](int64_t i) { return kind + i * a.classes; };
+  auto row_of = [&](unsigned i) { return (unsigned)kind + i * (unsigned)a.classes; };
   const bool has_y = a.y != nullptr, has_g = a.gate != BETTY_GATE_NONE, has_u = a.du != nullptr, has_o = a.dxo != nullptr;
   const bool pre_layer = GENERAL && a.pre == BETTY_NORM_LAYER && has_u, post_layer = GENERAL && a.post == BETTY_NORM_LAYER && has_y;
-  const bool shared_gate = has_g && a.per_gate > 1, row_gate = has_g && !shared_gate, bias = GENERAL && a.bias;
+  const bool shared_gate = SHARED, row_gate = has_g && !SHARED, bias = GENERAL && a.bias;
   const float* w_pre = a.params;
   const float* w_post = a.params + d;
   const float* s_res = a.params + 2 * (int64_t)d;
@@ -85,10 +91,10 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   const TY* const ys = (const TY*)a.y;
   const TY* const us = (const TY*)a.du;
   const TY* const gs = (const TY*)a.g;
-  auto fetch = [&](int64_t i, int slot) {
+  auto fetch = [&](unsigned i, int slot) {
     if constexpr (VEC) {
       if (i < last) {
-        const int64_t r = row_of(i);
+        const unsigned r = row_of(i);
         const uint32_t p = ring + slot * a.slot_bytes;
         if (has_u) {
           copy_row<CH>(p, row_at<TX>(xs, r, a.ldx), pl);
@@ -104,7 +110,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   };
   // one chunk of a stream of the present row
   uint32_t p = 0;
-  int64_t row = 0;
+  unsigned row = 0;
   auto get = [&](auto* base, uint32_t ld, int at, int c, f2 (&o)[4]) {
     typedef typename std::remove_const<typename std::remove_pointer<decltype(base)>::type>::type T;
     float v[8];
@@ -121,9 +127,10 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   if (VEC)
     for (int i = 0; i < a.ahead; ++i) fetch(first + i, i);
 
-  int64_t gate = 0, gate_end = 0;          // of a shared gate: the present row's, and the row after its last
+  const unsigned slot0 = first_slot(a, kind, (unsigned)share);
+  unsigned gate = 0, gate_end = 0;         // of a shared gate: the present row's, and the row after its last
   if (shared_gate && first < last) {
-    gate = (unsigned)row_of(first) / a.per_gate;
+    gate = row_of(first) / a.per_gate;
     gate_end = (gate + 1) * a.per_gate;
   }
   // w_pre and e = w_post s, times a(g) of a shared gate: in shared memory; wide rows form them where they are used
@@ -203,7 +210,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       }
     }
   }
-  for (int64_t at = first; at < last; ++at) {
+  for (unsigned at = first; at < last; ++at) {
     row = row_of(at);
     if constexpr (VEC) {
       fetch(at + a.ahead, slot == 0 ? a.ahead : slot - 1);
@@ -428,8 +435,8 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         }
       }
     }
-    if (has_y && shared_gate && (at + 1 == last || row + a.classes >= gate_end)) {           // the walker leaves the gate
-      const int64_t g0 = gate * a.per_gate, g1 = gate_end < a.rows ? gate_end : a.rows;
+    if (has_y && shared_gate && (at + 1 == last || row + (unsigned)a.classes >= gate_end)) {           // the walker leaves the gate
+      const unsigned g0 = gate * a.per_gate, g1 = min(gate_end, (unsigned)a.rows);
       const bool whole = a.classes == 1 && g0 >= first && g1 <= last;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
@@ -469,10 +476,10 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
           }
         }
         if (whole) store_each<VEC>(row_at<TY>(a.dg, gate, a.lddg), dg, c, pl);
-        else store_sums<VEC>(a.gate_partials + gate_slot(a, kind, share, gate) * d, dg, c, pl);
+        else store_sums<VEC>(a.gate_partials + (int64_t)gate_slot(a, slot0, gate, g0 >= first, at) * d, dg, c, pl);
       }
       if (at + 1 < last) {
-        gate = (unsigned)row_of(at + 1) / a.per_gate;
+        gate = row_of(at + 1) / a.per_gate;
         gate_end = (gate + 1) * a.per_gate;
       }
 #pragma unroll
@@ -530,24 +537,35 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
 // Adds the blocks' column sums and forms the parameter gradients (the first param_blocks blocks: 32 columns each, SLICES
 // slices of the list added in a fixed order), then the gates whose rows lie in several walkers' shares.
 static constexpr int SLICES = 32, GATE_COLUMNS = 256;
-template <typename TY>
+// Every SLICES-th block's sums from block `slice` on, in order, U at a time: all of a batch's loads are on their way before the
+// first is added, the last batch's too (left to the compiler that one became a load at a time: 2731 x 1537 fp32 6 us slower).
+template <int NQ, int U>
+__device__ __forceinline__ void add_blocks(float (&v)[4], const float* sums, int64_t d, int slice, int blocks) {
+  for (int b = slice; b < blocks; b += U * SLICES) {
+    float t[U][NQ];
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) t[i][k] = b + i * SLICES < blocks ? sums[((int64_t)(b + i * SLICES) * NQ + k) * d] : 0.f;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int k = 0; k < NQ; ++k) v[k] += t[i][k];
+  }
+}
+// SHARED: there are such gates (a kernel of its own, so that the others' sums keep their registers).
+struct GateRows { int64_t n, i1, lo, hi; };       // of a class: its rows, the row after the gate's last, the shares that hold the gate's
+template <typename TY, bool SHARED>
 __global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int blocks, int param_blocks, float* __restrict__ dparams) {
   __shared__ float part[4][SLICES][32];
   pdl_enter();
   const int d = a.d;
-  if ((int)blockIdx.x < param_blocks) {
+  if (!SHARED || (int)blockIdx.x < param_blocks) {
     const int j = blockIdx.x * 32 + (threadIdx.x & 31), slice = threadIdx.x >> 5, nq = a.bias ? 4 : 2;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (j < d) {
-      const float* p = a.col_partials + (int64_t)slice * nq * d + j;
-      const int64_t step = (int64_t)SLICES * nq * d;
-      if (nq == 2) {
-#pragma unroll 10
-        for (int b = slice; b < blocks; b += SLICES, p += step) { v[0] += p[0]; v[1] += p[d]; }
-      } else {
-#pragma unroll 5
-        for (int b = slice; b < blocks; b += SLICES, p += step) { v[0] += p[0]; v[1] += p[d]; v[2] += p[2 * (int64_t)d]; v[3] += p[3 * (int64_t)d]; }
-      }
+      if (nq == 2) add_blocks<2, 10>(v, a.col_partials + j, d, slice, blocks);
+      else add_blocks<4, 5>(v, a.col_partials + j, d, slice, blocks);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) part[i][slice][threadIdx.x & 31] = v[i];
@@ -589,22 +607,36 @@ __global__ void __launch_bounds__(32 * SLICES) k_backward_sums(const Args a, int
   }
   const int64_t g0 = gate * a.per_gate, g1 = g0 + a.per_gate < a.rows ? g0 + a.per_gate : a.rows;
   constexpr int GS = 32 * SLICES / GATE_COLUMNS;
-  float s = 0.f;
-  for (int kind = 0; kind < a.classes; ++kind) {
-    // the class's rows of the gate, and the shares that hold them
+  __shared__ GateRows of_class[8];
+  if ((int)threadIdx.x < a.classes) {             // once for the block: these are 64-bit divisions
+    const int kind = threadIdx.x;
     const int64_t n = class_rows(a, kind), i0 = g0 > kind ? (g0 - kind + a.classes - 1) / a.classes : 0;
     const int64_t i1 = g1 > kind ? (g1 - kind + a.classes - 1) / a.classes : 0;
-    if (i0 >= i1) continue;
-    const int64_t lo = share_of(i0, n, a.shares), hi = share_of(i1 - 1, n, a.shares);
+    of_class[kind] = i0 < i1 ? GateRows{n, i1, share_of(i0, n, a.shares), share_of(i1 - 1, n, a.shares)} : GateRows{0, 0, 0, -1};
+  }
+  __syncthreads();
+  float s = 0.f;
+  for (int kind = 0; kind < a.classes; ++kind) {
+    const int64_t n = of_class[kind].n, i1 = of_class[kind].i1, lo = of_class[kind].lo, hi = of_class[kind].hi;
+    if (hi < lo) continue;                        // the class has none of the gate's rows
     if (a.classes == 1 && lo == hi) return;       // one walker had all of the gate's rows and has written dg
     if (j < d) {
-      const float* p = a.gate_partials + gate_slot(a, kind, lo + slice, gate) * d + j;
-      if (n >= a.shares) {
+      int64_t w = lo + slice;
+      if (slice == 0 && a.classes == 1) {         // the share that the gate begins in
+        s = a.gate_partials[(int64_t)gate_slot(a, first_slot(a, kind, (unsigned)lo), (unsigned)gate, true, 0u) * d + j];
+        w += GS;
+      }
+      if (n >= a.shares && !a.gate_sums.per_row) {
+        const float* p = a.gate_partials + (int64_t)gate_slot(a, first_slot(a, kind, (unsigned)w), (unsigned)gate, false, 0u) * d + j;
+        const int64_t step = (int64_t)GS * d * (a.classes == 1 ? 2 : 1);
 #pragma unroll 8
-        for (int64_t w = lo + slice; w <= hi; w += GS, p += (int64_t)GS * d) s += *p;
-      } else {                                    // some shares of the class may be empty: their slots hold nothing
-        for (int64_t w = lo + slice; w <= hi; w += GS, p += (int64_t)GS * d)
-          if (share_start(w, n, a.shares) < share_start(w + 1, n, a.shares)) s += *p;
+        for (; w <= hi; w += GS, p += step) s += *p;
+      } else {
+        for (; w <= hi; w += GS) {
+          const int64_t to = w == hi ? i1 : share_start(w + 1, n, a.shares);
+          if (n < a.shares && share_start(w, n, a.shares) >= to) continue;       // an empty share: its place holds nothing
+          s += a.gate_partials[(int64_t)gate_slot(a, first_slot(a, kind, (unsigned)w), (unsigned)gate, false, (unsigned)(to - 1)) * d + j];
+        }
       }
     }
   }
@@ -630,6 +662,12 @@ void backward_grid(int64_t rows, const Layout& l, int classes, int& blocks, int&
   shares = (int)n;
   blocks = (int)((n * classes + groups - 1) / groups);
 }
+GateSums gate_sums_of(int64_t rows, int64_t per_gate, int classes, int shares) {
+  if (classes == 1) return {2 * (int64_t)shares, 2, 0, 0, 1};
+  const int64_t pairs = shares + (rows + per_gate - 1) / per_gate, most = (rows + classes - 1) / classes;
+  if (most < pairs) return {most, 0, 0, 1, 0};
+  return {pairs, 1, 1, 0, 0};
+}
 static inline bool is_general(int bias, int pre, int post) { return bias || pre == BETTY_NORM_LAYER || post == BETTY_NORM_LAYER; }
 // chunks per thread of the wide kernel: the layer norms' and biases' sums leave registers for one
 static constexpr int backward_chunks(bool general) { return general ? 1 : 2; }
@@ -644,34 +682,40 @@ Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int xd, int 
   return l;
 }
 
-template <typename TX, typename TY, bool VEC, int CH, bool GENERAL>
+template <typename TX, typename TY, bool VEC, int CH, bool GENERAL, bool SHARED>
 static betty_status launch_backward(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
   static SmemLimit limit = {};
-  if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_backward<TX, TY, VEC, CH, GENERAL>, limit, l.smem));
+  if (l.smem > 40 * 1024) BETTY_TRY(ensure_dynamic_smem(k_backward<TX, TY, VEC, CH, GENERAL, SHARED>, limit, l.smem));
   int blocks, shares;
   backward_grid(a.rows, l, a.classes, blocks, shares);
-  launch_pdl(k_backward<TX, TY, VEC, CH, GENERAL>, dim3(blocks), dim3(l.threads), l.smem, stream, a);
+  launch_pdl(k_backward<TX, TY, VEC, CH, GENERAL, SHARED>, dim3(blocks), dim3(l.threads), l.smem, stream, a);
   BETTY_LAUNCH_CHECK();
   const int param_blocks = (a.d + 31) / 32;
   int64_t items = 0;
-  if (a.gate_partials && a.rows > 0) {
+  if (SHARED) {
     const int64_t gates = (a.rows + a.per_gate - 1) / a.per_gate;
     items = a.classes > 1 || gates < a.shares ? gates : a.shares - 1;
   }
-  launch_pdl(k_backward_sums<TY>, dim3((unsigned)(param_blocks + items * ((a.d + GATE_COLUMNS - 1) / GATE_COLUMNS))), dim3(32 * SLICES), 0, stream, a,
+  launch_pdl(k_backward_sums<TY, SHARED>, dim3((unsigned)(param_blocks + items * ((a.d + GATE_COLUMNS - 1) / GATE_COLUMNS))), dim3(32 * SLICES), 0, stream, a,
              blocks, param_blocks,
              dparams);
   BETTY_LAUNCH_CHECK();
   return BETTY_OK;
 }
-template <typename TX, typename TY, bool GENERAL>
+template <typename TX, typename TY, bool GENERAL, bool SHARED>
 static betty_status backward_shape(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
-  if (!l.vec) return launch_backward<TX, TY, false, 4, GENERAL>(stream, a, l, dparams);
-  return l.chunks == 1 ? launch_backward<TX, TY, true, 1, GENERAL>(stream, a, l, dparams) : launch_backward<TX, TY, true, 2, GENERAL>(stream, a, l, dparams);
+  if (!l.vec) return launch_backward<TX, TY, false, 4, GENERAL, SHARED>(stream, a, l, dparams);
+  return l.chunks == 1 ? launch_backward<TX, TY, true, 1, GENERAL, SHARED>(stream, a, l, dparams)
+                       : launch_backward<TX, TY, true, 2, GENERAL, SHARED>(stream, a, l, dparams);
+}
+template <typename TX, typename TY, bool GENERAL>
+static betty_status backward_gated(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
+  const bool shared = a.gate != BETTY_GATE_NONE && a.per_gate > 1;
+  return shared ? backward_shape<TX, TY, GENERAL, true>(stream, a, l, dparams) : backward_shape<TX, TY, GENERAL, false>(stream, a, l, dparams);
 }
 template <typename TX, typename TY>
 static betty_status backward_typed(cudaStream_t stream, const Args& a, const Layout& l, float* dparams) {
-  return is_general(a.bias, a.pre, a.post) ? backward_shape<TX, TY, true>(stream, a, l, dparams) : backward_shape<TX, TY, false>(stream, a, l, dparams);
+  return is_general(a.bias, a.pre, a.post) ? backward_gated<TX, TY, true>(stream, a, l, dparams) : backward_gated<TX, TY, false>(stream, a, l, dparams);
 }
 betty_status backward(cudaStream_t stream, Args& a, const Layout& l, int xd, int yd, float* dparams) {
   a.G = l.G; a.ahead = l.ahead; a.slot_bytes = l.slot_bytes;

@@ -32,7 +32,8 @@ class ExpertBlock:
         self.exit = bt.BlockNorm(d, pre=norm, post=norm, gate=gate, rows_per_gate=rows_per_gate, eps=eps, bias=bias)
         self.up = bt.Grouped(n_experts, d, self.act8.width, code)
         self.down = bt.Grouped(n_experts, hidden, d, code)
-        need = max(bt.betty_block_norm_workspace_size(self.entry, rows), bt.betty_block_norm_workspace_size(self.exit, rows),
+        # the block's own matrices are contiguous: only x, its gradient and the gate can be the caller's slices
+        need = max(bt.betty_block_norm_workspace_size(self.entry, rows, False), bt.betty_block_norm_workspace_size(self.exit, rows, False),
                    bt.betty_grouped_workspace_size(self.up, rows), bt.betty_grouped_workspace_size(self.down, rows))
         self.ws = bt.Workspace.of_bytes(need, device)
 

@@ -55,3 +55,30 @@ def test_rows_of_any_size(size, which, kind, act, d):
     assert float(((dy.double().cpu() - want["dy"]).abs() / (rms(want["dy"]) + amp * big / m)).max()) <= SLACK
     if dg is not None:
         assert float(((dg.double().cpu() - want["dgate"]).abs() / (4.0 * amp * big)).max()) <= SLACK
+
+
+@pytest.mark.parametrize("rows", [1, 9, 300, 3000])
+@pytest.mark.parametrize("d,per_gate", [(96, 3), (515, 2), (515, 40), (1538, 3), (1540, 2), (2048, 2), (2048, 11), (2048, 700)])
+def test_gate_sums_stay_in_the_workspace(rows, d, per_gate):
+    """A workspace of exactly the size that contiguous matrices need: the gradients of the call with room for every layout, bit
+    for bit, and nothing written behind it."""
+    import paper_2207_02849_b200 as bt
+    args = (d, "rms", "rms", "sigmoid", per_gate, False, 1e-5)
+    q, cfg = _problem(rows + d, rows, d, F, BF, "sigmoid", per_gate, False), _cfg(bt, *args)
+    need = bt.betty_block_norm_workspace_size(cfg, rows, any_layout=False)
+    exact, room = bt.Workspace.of_bytes(need + 4096), bt.Workspace.of_bytes(bt.betty_block_norm_workspace_size(cfg, rows))
+    exact.nbytes = need
+    behind = exact.buf[need + exact.ptr - exact.buf.data_ptr():]
+    behind.fill_(77)
+    runs = []
+    for ws in (exact, room):
+        outs = [torch.full_like(q[k], float("nan")) for k in ("x", "y", "gate", "params")]
+        bt.betty_block_norm_backward(cfg, q["params"], q["x"], q["y"], q["gate"], q["du"], q["dxo"], *outs, ws)
+        runs.append(outs)
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+    assert bool((behind == 77).all())
+    want = _gradients(q, args)
+    for got, k, t in zip(runs[0][:3], ("dx", "dy", "dgate"), (F, BF, BF)):
+        scale = want[k].pow(2).mean(-1, keepdim=True).sqrt() + 30.0 * min(rows, per_gate)
+        assert ref.close(got, want[k], t, SLACK, scale=scale) <= 0, k
