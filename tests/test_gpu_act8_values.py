@@ -52,3 +52,39 @@ def test_activations_at_the_ends_of_the_range(kind, dtype):
     a = a[:, 0].float().cpu()
     assert float(a[0]) == most and float(a[1]) == 0.0 and float(a[2]) == float("inf") and bool(torch.isnan(a[3]))
     assert float(a[4]) == 0.0 and float(a[5]) == 0.0
+
+
+def _every_value(dtype, low, high):
+    """All numbers of a 16-bit type in [low, high]."""
+    v = torch.arange(-(1 << 15), 1 << 15, dtype=torch.int32).to(torch.int16).view(dtype)
+    v = v[torch.isfinite(v)]
+    return v[(v.float() >= low) & (v.float() <= high)]
+
+
+@pytest.mark.parametrize("dtype,low", [(HF, -9.0), (BF, -13.0)])
+def test_gelu_of_16_bit_types_is_exact_in_relative_terms(dtype, low):
+    """Every number of the type.  The distribution function is within 5e-6 of itself by its approximation and, its exponential
+    being taken of v^2 / 2 as fp32 has it, within 7.5e-8 v^2 more (two and a half roundings) and ~1e-6 by ex2, the Horner steps and the
+    reciprocal: 2e-5 for |v| <= 13.  The activation is that and one rounding, the slope (store and backward agree on v where the
+    checkpoint holds v itself) that much of the sum of its two terms' magnitudes."""
+    import paper_2207_02849_b200 as bt
+    v = _every_value(dtype, low, 40.0)
+    z = v[:, None].cuda()                                  # a group of one value: q = +-127, restored to itself within 2^-22
+    cfg = bt.Act8(1, act=bt.ACT_GELU)
+    q, scales = cfg.empty(len(v))
+    a = torch.empty_like(z)
+    bt.betty_act8_store(cfg, z, a, q, scales)
+    v64 = v.double()[:, None]
+    cdf = 0.5 * torch.special.erfc(-v64 / 2.0 ** 0.5)
+    tiny = 2.0 ** -25 if dtype == HF else 2.0 ** -126
+    bound = lambda want, size: (ref.UNIT[dtype] * want.abs() + 2e-5 * size) * 1.001 + tiny  # noqa: E731
+    want = v64 * cdf
+    assert float(((a.double().cpu() - want).abs() - bound(want, want.abs())).max()) <= 0
+    dz, a8 = torch.empty_like(z), torch.empty_like(z)
+    bt.betty_act8_backward(cfg, q, scales, torch.ones_like(z), dz, a8)
+    r = ref.restored(q.cpu(), scales.cpu(), 1)
+    cdf, pdf = 0.5 * torch.special.erfc(-r / 2.0 ** 0.5), torch.exp(-0.5 * r * r) / (2.0 * torch.pi) ** 0.5
+    # q * scale is rounded to fp32 before its use: v^2 2^-23 more
+    assert float(((a8.double().cpu() - r * cdf).abs() - bound(r * cdf, 2.0 * (r * cdf).abs())).max()) <= 0
+    want = cdf + r * pdf
+    assert float(((dz.double().cpu() - want).abs() - bound(want, 2.0 * (cdf + r.abs() * pdf))).max()) <= 0
