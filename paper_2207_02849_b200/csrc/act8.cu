@@ -170,16 +170,6 @@ template <bool ALIGNED> struct Held {
   }
 };
 
-__device__ __forceinline__ float reciprocal(float v) {        // 1 ulp; 0 for an overflowed power
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ float exp2_f(float v) {            // within 2^-22 of itself
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-  return r;
-}
 // Activation and its slope (each used where the caller uses it).  fp32 values take erff, whose 1 + erf has 6e-8 absolute error.
 // For 16-bit types the distribution function of -|v| is exp(-v^2 / 2) t (c0 + c1 t + .. + c5 t^5), t = 1 / (1 + 0.31 |v|): its ratio
 // to the density is smooth and of order t, and the six coefficients are the ones of smallest largest RELATIVE error on 0 <= |v| <= 16
@@ -192,9 +182,16 @@ __device__ __forceinline__ void act_and_slope(f2 v, f2& f, f2& s) {
     f = f2{v.x != v.x ? v.x : fmaxf(v.x, 0.f), v.y != v.y ? v.y : fmaxf(v.y, 0.f)};
     s = f2{v.x != v.x ? v.x : (v.x > 0.f ? 1.f : 0.f), v.y != v.y ? v.y : (v.y > 0.f ? 1.f : 0.f)};
   } else if (ACT == BETTY_ACT_SILU) {
-    const f2 e = {__fdividef(1.f, 1.f + __expf(-v.x)), __fdividef(1.f, 1.f + __expf(-v.y))};
+    f2 e, rest;              // the sigmoid and 1 - it
+    if constexpr (sizeof(T) == 4) {
+      sigmoid_parts(v.x, e.x, rest.x);
+      sigmoid_parts(v.y, e.y, rest.y);
+    } else {                 // within 2^-22 (2 + |v|) of itself, against 2^-12 and 2^-9 of the rounding
+      e = f2{__fdividef(1.f, 1.f + __expf(-v.x)), __fdividef(1.f, 1.f + __expf(-v.y))};
+      rest = fma2(e, both(-1.f), both(1.f));
+    }
     f = mul2(v, e);
-    s = mul2(e, fma2(v, fma2(e, both(-1.f), both(1.f)), both(1.f)));
+    s = mul2(e, fma2(v, rest, both(1.f)));
   } else {
     f2 c, density;
     if constexpr (sizeof(T) == 4) {

@@ -43,6 +43,28 @@ __device__ __forceinline__ T* row_at(void* base, int64_t row, uint32_t ld_bytes)
   return (T*)((char*)base + (uint64_t)(uint32_t)row * ld_bytes);
 }
 
+__device__ __forceinline__ float reciprocal(float v) {        // 1 ulp; 0 for an overflowed power
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float exp2_f(float v) {            // within 2^-22 of itself
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+  return r;
+}
+// s = 1 / (1 + e^-v) and n = 1 - s = 1 / (1 + e^v), each within 7e-7 of itself, for results in fp32.  From e = exp(-|v|), which does
+// not overflow and leaves nothing to cancel; the product with log2 e is taken in two parts (a single one, rounded, is off by
+// 2^-24 of itself, which the power multiplies by |v|).  Beyond 104 the smaller one is below every fp32 number.
+__device__ __forceinline__ void sigmoid_parts(float v, float& s, float& n) {
+  const float a = fabsf(v) > 104.f ? 104.f : fabsf(v);        // NaN stays
+  const float hi = a * -1.4426950408889634f;
+  const float lo = fmaf(a, -1.925962989e-8f, fmaf(a, -1.4426950408889634f, -hi));
+  const float e0 = exp2_f(hi), e = fmaf(e0, lo * 0.6931471805599453f, e0), d = reciprocal(1.f + e);
+  s = v < 0.f ? e * d : d;
+  n = v < 0.f ? d : e * d;
+}
+
 // ---- pairs of fp32 values: one instruction for two products or sums ----
 struct alignas(8) f2 { float x, y; };
 __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {

@@ -88,3 +88,26 @@ def test_gelu_of_16_bit_types_is_exact_in_relative_terms(dtype, low):
     assert float(((a8.double().cpu() - r * cdf).abs() - bound(r * cdf, 2.0 * (r * cdf).abs())).max()) <= 0
     want = cdf + r * pdf
     assert float(((dz.double().cpu() - want).abs() - bound(want, 2.0 * (cdf + r.abs() * pdf))).max()) <= 0
+
+
+def test_silu_of_fp32_values_is_exact_in_relative_terms():
+    """sigmoid(v) from e = exp(-|v|): ex2 within 2^-22, its argument's rounding made good, the reciprocal and three roundings
+    2^-24 to 2^-23 each: below 8e-7 of the result; the slope s (1 + v (1 - s)) below 1e-6 of the sum of its terms' magnitudes."""
+    import paper_2207_02849_b200 as bt
+    g = torch.Generator().manual_seed(2)
+    z = torch.cat((torch.linspace(-80, 80, 20001), torch.randn(20000, generator=g) * 5.0))[:, None].cuda()
+    cfg = bt.Act8(1, act=bt.ACT_SILU)
+    q, scales = cfg.empty(z.shape[0])
+    a = torch.empty_like(z)
+    bt.betty_act8_store(cfg, z, a, q, scales)
+    v = z.double().cpu()
+    want = v / (1.0 + torch.exp(-v))
+    assert float(((a.double().cpu() - want).abs() - 8e-7 * want.abs()).max()) <= 0
+    back = torch.empty_like(z)
+    bt.betty_act8_restore(cfg, q, scales, back)            # the fp32 numbers that the backward pass takes
+    dz, a8 = torch.empty_like(z), torch.empty_like(z)
+    bt.betty_act8_backward(cfg, q, scales, torch.ones_like(z), dz, a8)
+    v = back.double().cpu()
+    s, n = 1.0 / (1.0 + torch.exp(-v)), 1.0 / (1.0 + torch.exp(v))
+    assert float(((a8.double().cpu() - v * s).abs() - 8e-7 * (v * s).abs()).max()) <= 0
+    assert float(((dz.double().cpu() - s * (1.0 + v * n)).abs() - 1e-6 * s * (1.0 + v.abs() * n)).max()) <= 0
