@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_forward(const Args a) {
             else load8<VEC>(g, gate_row(row), c, w);
             if (a.gate == BETTY_GATE_SIGMOID)
 #pragma unroll
-              for (int k = 0; k < 8; ++k) g[k] = sigmoid_f(g[k]);
+              for (int k = 0; k < 8; ++k) g[k] = sigmoid_gate<TX>(g[k]);
           }
 #pragma unroll
           for (int k = 0; k < 8; ++k) {

@@ -208,7 +208,23 @@ __device__ __forceinline__ void row_sums_init(float* red) {
   __syncthreads();
 }
 
-__device__ __forceinline__ float sigmoid_f(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
+// A sigmoid gate and 1 - it.  A residual stream in fp32 takes them to 7e-7 of themselves; where all results are rounded to 16 bits the
+// fast forms do, 2^-22 (2 + |v|) of the gate (for its complement, of 1).
+template <typename TX>
+__device__ __forceinline__ void sigmoid_gate(float v, float& s, float& n) {
+  if constexpr (sizeof(TX) == 4) {
+    sigmoid_parts(v, s, n);
+  } else {
+    s = __fdividef(1.f, 1.f + __expf(-v));
+    n = 1.f - s;
+  }
+}
+template <typename TX>
+__device__ __forceinline__ float sigmoid_gate(float v) {
+  float s, n;
+  sigmoid_gate<TX>(v, s, n);
+  return s;
+}
 
 // places of the walkers' sums for gates of several rows (see gate_slot)
 struct GateSums { int64_t rows; unsigned per_share, per_gate, per_row, begins; };

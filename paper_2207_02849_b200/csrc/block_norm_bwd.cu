@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
       load8<VEC>(g, row_at<TY>(gs, gate, a.ldg), c, pl);
       if (a.gate == BETTY_GATE_SIGMOID)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) g[k] = sigmoid_f(g[k]);
+        for (int k = 0; k < 8; ++k) g[k] = sigmoid_gate<TX>(g[k]);
       pairs(s, g);
 #pragma unroll
       for (int k = 0; k < 4; ++k) e[k] = mul2(e[k], s[k]);
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
               get(gs, a.ldg, at_g, c, g);
               if (a.gate == BETTY_GATE_SIGMOID)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) g[k] = f2{sigmoid_f(g[k].x), sigmoid_f(g[k].y)};
+                for (int k = 0; k < 4; ++k) g[k] = f2{sigmoid_gate<TX>(g[k].x), sigmoid_gate<TX>(g[k].y)};
 #pragma unroll
               for (int k = 0; k < 4; ++k) e[k] = mul2(e[k], g[k]);
             }
@@ -385,8 +385,11 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
         if (a.gate == BETTY_GATE_SIGMOID)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            g[k] = f2{sigmoid_f(g[k].x), sigmoid_f(g[k].y)};
-            z[k] = mul2(z[k], fma2(mul2(g[k], both(-1.f)), g[k], g[k]));
+            f2 s, n;
+            sigmoid_gate<TX>(g[k].x, s.x, n.x);
+            sigmoid_gate<TX>(g[k].y, s.y, n.y);
+            g[k] = s;
+            z[k] = mul2(z[k], mul2(s, n));
           }
         singles(out, z);
         store8<VEC>(row_at<TY>(a.dg, row, a.lddg), out, c, pl);
@@ -450,8 +453,9 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
           const float H = k & 1 ? accA[c][k / 2].y : accA[c][k / 2].x, E = !GENERAL ? 0.f : (k & 1 ? accB[GENERAL ? c : 0][k / 2].y : accB[GENERAL ? c : 0][k / 2].x);
           dg[k] = s[k] * (bias ? fmaf(b[k], E, w[k] * H) : w[k] * H);
           if (a.gate == BETTY_GATE_SIGMOID) {
-            g[k] = sigmoid_f(g[k]);
-            dg[k] *= g[k] * (1.f - g[k]);
+            float n;
+            sigmoid_gate<TX>(g[k], g[k], n);
+            dg[k] *= g[k] * n;
           }
           if (G == 32) {
             const uint32_t at_a = acc_s + (c * 8 + k) * G * 4, at_b = at_a + CH * 8 * G * 4;

@@ -53,16 +53,20 @@ __device__ __forceinline__ float exp2_f(float v) {            // within 2^-22 of
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
   return r;
 }
-// s = 1 / (1 + e^-v) and n = 1 - s = 1 / (1 + e^v), each within 7e-7 of itself, for results in fp32.  From e = exp(-|v|), which does
-// not overflow and leaves nothing to cancel; the product with log2 e is taken in two parts (a single one, rounded, is off by
-// 2^-24 of itself, which the power multiplies by |v|).  Beyond 104 the smaller one is below every fp32 number.
+__device__ __forceinline__ float between(float v, float low, float high) {        // NaN stays
+  float r;
+  asm("{\n\t.reg .f32 a;\n\tmax.NaN.f32 a, %1, %2;\n\tmin.NaN.f32 %0, a, %3;\n\t}" : "=f"(r) : "f"(v), "f"(low), "f"(high));
+  return r;
+}
+// s = 1 / (1 + e^-v) and n = 1 - s, each within 7e-7 of itself, for results in fp32.  The power of two is taken of the rounded product
+// with log2 e, and what that lacks of -v (2^-24 of it, which alone would be |v| 2^-24 of the power) is made good as a factor.
+// From -87.3 down s is below the normal numbers and 0; the bounds keep e finite and an infinite v from leaving a NaN.
 __device__ __forceinline__ void sigmoid_parts(float v, float& s, float& n) {
-  const float a = fabsf(v) > 104.f ? 104.f : fabsf(v);        // NaN stays
-  const float hi = a * -1.4426950408889634f;
-  const float lo = fmaf(a, -1.925962989e-8f, fmaf(a, -1.4426950408889634f, -hi));
-  const float e0 = exp2_f(hi), e = fmaf(e0, lo * 0.6931471805599453f, e0), d = reciprocal(1.f + e);
-  s = v < 0.f ? e * d : d;
-  n = v < 0.f ? d : e * d;
+  const float a = between(v, -88.7f, 104.f), p = a * -1.4426950408889634f;
+  const float lack = fmaf(p, 1.9046542e-9f, fmaf(p, -0.693147182f, -a));        // -a - p ln 2, ln 2 in two parts
+  const float e0 = exp2_f(p), e = fmaf(e0, lack, e0);
+  s = reciprocal(1.f + e);
+  n = v < 0.f ? 1.f - s : e * s;
 }
 
 // ---- pairs of fp32 values: one instruction for two products or sums ----

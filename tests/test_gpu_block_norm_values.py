@@ -82,3 +82,29 @@ def test_gate_sums_stay_in_the_workspace(rows, d, per_gate):
     for got, k, t in zip(runs[0][:3], ("dx", "dy", "dgate"), (F, BF, BF)):
         scale = want[k].pow(2).mean(-1, keepdim=True).sqrt() + 30.0 * min(rows, per_gate)
         assert ref.close(got, want[k], t, SLACK, scale=scale) <= 0, k
+
+
+@pytest.mark.parametrize("tx,ty", [(F, F), (F, BF)])
+def test_sigmoid_gate_of_fp32_results_is_exact_in_relative_terms(tx, ty):
+    """x' = a(g) with x = 0, y = 1, s = w_post = 1 and no norm.  From e = exp(-|g|): ex2 within 2^-22, the reciprocal and three
+    roundings: below 8e-7 of the result; infinite gates are shut or open."""
+    import paper_2207_02849_b200 as bt
+    d = 512
+    gate = torch.linspace(-80, 80, 40 * d).view(40, d).to(ty).cuda()
+    gate[0, 0], gate[0, 1] = -float("inf"), float("inf")
+    params = torch.ones(3, d, device="cuda")
+    x, y = torch.zeros(40, d, dtype=tx, device="cuda"), torch.ones(40, d, dtype=ty, device="cuda")
+    cfg = bt.BlockNorm(d, pre=bt.NORM_NONE, post=bt.NORM_NONE, gate=bt.GATE_SIGMOID)
+    x_out = torch.empty_like(x)
+    bt.betty_block_norm(cfg, params, x, y, gate, x_out, None)
+    g = gate.double().cpu()
+    want = 1.0 / (1.0 + torch.exp(-g))
+    assert float(((x_out.double().cpu() - want).abs() - 8e-7 * want).max()) <= 0
+    # dg = dx' s z a'(g), a' = a (1 - a): both factors to 8e-7
+    ws = bt.Workspace.of_bytes(bt.betty_block_norm_workspace_size(cfg, 40))
+    one, dx, dy, dg, dp = torch.ones_like(x), torch.empty_like(x), torch.empty_like(y), torch.empty_like(gate), torch.empty_like(params)
+    bt.betty_block_norm_backward(cfg, params, None, y, gate, None, one, dx, dy, dg, dp, ws)
+    slope = want / (1.0 + torch.exp(g))
+    unit = 0.0 if ty == F else ref.UNIT[ty] * 1.001
+    assert float(((dy.double().cpu() - want).abs() - (8e-7 + unit) * want).max()) <= 0
+    assert float(((dg.double().cpu() - slope).abs() - (1.6e-6 + unit) * slope).max()) <= 0
