@@ -41,6 +41,25 @@ def _older(path: str, deps) -> bool:
     return not os.path.exists(path) or any(os.path.getmtime(d) > os.path.getmtime(path) for d in deps)
 
 
+def _unfinished(path: str) -> str:
+    """Where the compiler writes: a file takes its place, and with it a date to be taken as fresh, only once it is whole."""
+    return os.path.join(PKG_DIR, "_build", f"{os.path.basename(path)}.{os.getpid()}.part")
+
+
+def _command(cmd, out: str):
+    return subprocess.Popen(cmd + ["-o", _unfinished(out)], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def _finish(p, out: str):
+    """Waits for the command; moves what it made into place.  Returns whether it succeeded, and its messages."""
+    text, _ = p.communicate()
+    if p.returncode == 0:
+        os.replace(_unfinished(out), out)
+    elif os.path.exists(_unfinished(out)):
+        os.remove(_unfinished(out))
+    return p.returncode == 0, text
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu of the package into libbetty.so; returns its path."""
     if not force and not _stale():
@@ -59,20 +78,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
         objs.append(obj)
         if not force and not _older(obj, [os.path.join(CSRC, src)] + headers):
             continue
-        cmd = [nvcc, "-c", os.path.join(CSRC, src), "-o", obj] + NVCC_FLAGS + extra
+        cmd = [nvcc, "-c", os.path.join(CSRC, src)] + NVCC_FLAGS + extra
         if verbose:
             cmd += ["-Xptxas", "-v"]
-        procs.append((src + suffix, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
-    for src, p in procs:
-        out, _ = p.communicate()
-        if p.returncode != 0:
-            raise RuntimeError(f"nvcc failed on {src}:\n{out}")
-        if verbose:
+        procs.append((src + suffix, obj, _command(cmd, obj)))
+    failed = []
+    for src, obj, p in procs:
+        ok, out = _finish(p, obj)
+        if not ok:
+            failed.append(f"nvcc failed on {src}:\n{out}")
+        elif verbose:
             print(out)
-    link = [nvcc, "-shared", "-o", LIB_PATH] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"]
-    r = subprocess.run(link, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}")
+    if failed:
+        raise RuntimeError("\n".join(failed))
+    ok, out = _finish(_command([nvcc, "-shared"] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"], LIB_PATH), LIB_PATH)
+    if not ok:
+        raise RuntimeError(f"link failed:\n{out}")
     return LIB_PATH
 
 
