@@ -215,7 +215,7 @@ betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int classes) 
   a.gate_ahead = a.per_gate == 1 || (classes == 1 && a.ld8 == 0 && a.ldg % 16 == 0 && aligned16(a.g));
   const int ys = (a.y ? 1 : 0) + (a.y && a.gate != BETTY_GATE_NONE ? 1 : 0);
   const bool general = a.bias || a.pre == BETTY_NORM_LAYER || a.post == BETTY_NORM_LAYER;
-  const Layout l = layout_of(a.d, a.rows, xd, yd, classes, {1, ys, FWD_CHUNKS, forward_batch(general), 0});
+  const Layout l = layout_of(a.d, a.rows, xd, yd, classes, {1, ys, FWD_CHUNKS, forward_batch(general), 0, 0});
   a.G = l.G; a.ahead = l.ahead; a.slot_bytes = l.slot_bytes; a.classes = l.vec ? classes : 1;
   if (xd == BETTY_F32 && yd == BETTY_F32) return forward_typed<float, float>(stream, a, l);
   if (xd == BETTY_F32 && yd == BETTY_BF16) return forward_typed<float, __nv_bfloat16>(stream, a, l);
@@ -246,7 +246,7 @@ Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int classes, const Nee
     const int groups = l.threads / l.G;
     l.blocks_per_sm = MAX_G / l.threads;
     l.slot_bytes = l.chunks * 8 * l.G * (n.streams_x * bx + n.streams_y * by);
-    const size_t acc = (size_t)n.acc_arrays * groups * l.chunks * 8 * l.G * sizeof(float);
+    const size_t acc = (size_t)((l.vec ? n.kept_arrays : 0) + n.sum_arrays) * groups * l.chunks * 8 * l.G * sizeof(float);
     if (!l.vec) {
       l.smem = acc;
       l.slot_bytes = 0;

@@ -272,7 +272,8 @@ struct Layout {
 struct Needs {
   int streams_x, streams_y; // rows fetched of the residual stream's and of the block's type
   int wide_chunks, batch;   // of the wide kernel
-  int acc_arrays;           // fp32 values of a row that each thread group keeps in shared memory
+  int kept_arrays;          // fp32 values of a row that each thread group keeps in shared memory beside fetched rows (coefficients)
+  int sum_arrays;           // and beside any rows (sums)
 };
 // classes: 0 where the matrices' rows do not start at one shift
 Layout layout_of(int64_t d, int64_t rows, int x_dtype, int y_dtype, int classes, const Needs& n);

@@ -84,7 +84,8 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   const uint32_t ring = base_s + sub * (a.ahead + 1) * a.slot_bytes;
   constexpr int KEPT = GENERAL ? 6 : 4;      // half chunks of w_pre, e (and b_post s) for each chunk
   const uint32_t w_s = slots_end + (sub * KEPT * CH * G + t) * 16, e_s = w_s + 2 * CH * G * 16, b_s = e_s + 2 * CH * G * 16;
-  const uint32_t acc_s = slots_end + subs * KEPT * CH * G * 16 + (sub * (GENERAL ? 2 : 1) * CH * 8 * G + t) * 4;
+  constexpr bool KEEP = CH <= 2;             // wide rows form w_pre and e where they are used
+  const uint32_t acc_s = slots_end + (KEEP ? subs * KEPT * CH * G * 16 : 0) + (sub * (GENERAL ? 2 : 1) * CH * 8 * G + t) * 4;
   float* const partials = a.col_partials + (int64_t)blockIdx.x * (a.bias ? 4 : 2) * d;
   const TX* const xs = (const TX*)a.x;
   const TX* const os = (const TX*)a.dxo;
@@ -133,8 +134,7 @@ __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
     gate = row_of(first) / a.per_gate;
     gate_end = (gate + 1) * a.per_gate;
   }
-  // w_pre and e = w_post s, times a(g) of a shared gate: in shared memory; wide rows form them where they are used
-  constexpr bool KEEP = CH <= 2;
+  // w_pre and e = w_post s, times a(g) of a shared gate
   auto make_e = [&](int c, f2 (&e)[4]) {
     f2 s[4];
     param(w_post, c, e);
@@ -678,8 +678,9 @@ static constexpr int backward_chunks(bool general) { return general ? 1 : 2; }
 Layout backward_layout(const betty_block_norm_cfg* c, int64_t rows, int xd, int yd, int classes) {
   const bool gated = c->gate != BETTY_GATE_NONE, general = is_general(c->bias, c->pre, c->post);
   const bool row_gate = gated && c->rows_per_gate == 1;             // a gate shared by rows stays in L1
-  Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, 0};
-  n.acc_arrays = gated && !row_gate && c->d <= 32 * 8 * MAX_CH ? (general ? 5 : 3) : (general ? 3 : 2);      // w_pre, e (, b s); A (, B) where a warp holds a row
+  Needs n = {2, row_gate ? 3 : 2, backward_chunks(general), 1, 0, 0};
+  n.kept_arrays = general ? 3 : 2;                                                                    // w_pre, e (, b s)
+  n.sum_arrays = gated && !row_gate && c->d <= 32 * 8 * MAX_CH ? (general ? 2 : 1) : 0;               // A (, B) where a warp holds a row
   Layout l = layout_of(c->d, rows, xd, yd, classes, n);
   const size_t combine = l.G == 32 ? (size_t)(l.threads / 32) * l.chunks * 256 * sizeof(float) : 0;
   if (l.smem < combine) l.smem = combine;

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from tests import block_reference as ref
-from tests.test_gpu_block_norm import SLACK, _cfg, _gradients, _problem
+from tests.test_gpu_block_norm import SLACK, _cfg, _check_backward, _check_forward, _gradients, _problem, _wide
 
 pytestmark = pytest.mark.gpu
 BF, HF, F = torch.bfloat16, torch.float16, torch.float32
@@ -108,3 +108,32 @@ def test_sigmoid_gate_of_fp32_results_is_exact_in_relative_terms(tx, ty):
     unit = 0.0 if ty == F else ref.UNIT[ty] * 1.001
     assert float(((dy.double().cpu() - want).abs() - (8e-7 + unit) * want).max()) <= 0
     assert float(((dg.double().cpu() - slope).abs() - (1.6e-6 + unit) * slope).max()) <= 0
+
+
+@pytest.mark.parametrize("d", [257, 264, 384, 500, 512, 7200, 8192])
+@pytest.mark.parametrize("per_gate", [1, 5])
+@pytest.mark.parametrize("kind,bias", [("layer", True), ("layer", False), ("rms", True)])
+def test_fp32_layer_norms_with_a_gate(d, per_gate, kind, bias):
+    """Widths whose two rows and coefficients do not fit a block's share of the shared memory."""
+    import paper_2207_02849_b200 as bt
+    for rows in (3, 5000 if d < 600 else 330):
+        q = _problem(rows + d, rows, d, F, F, "sigmoid", per_gate, bias)
+        args = (d, kind, kind, "sigmoid", per_gate, bias, 1e-5)
+        x_out, u = torch.full_like(q["x"], float("nan")), torch.full_like(q["y"], float("nan"))
+        bt.betty_block_norm(_cfg(bt, *args), q["params"], q["x"], q["y"], q["gate"], x_out, u)
+        _check_forward(q, args, x_out, u)
+        _check_backward(bt, q, args)
+
+
+@pytest.mark.parametrize("pad,shift", [(8, 8), (3, 0), (0, 1), (5, 2)])
+@pytest.mark.parametrize("d,per_gate", [(264, 1), (264, 4), (1030, 1), (2304, 3)])
+def test_layer_norms_with_biases_of_wider_buffers(pad, shift, d, per_gate):
+    import paper_2207_02849_b200 as bt
+    for tx, ty in ((F, F), (F, BF)):
+        q = _problem(9, 21, d, tx, ty, "sigmoid", per_gate, True)
+        args = (d, "layer", "layer", "sigmoid", per_gate, True, 1e-6)
+        wide = lambda t: _wide(t, pad, shift)  # noqa: E731
+        x_out, u = wide(torch.zeros_like(q["x"])), wide(torch.zeros_like(q["y"]))
+        bt.betty_block_norm(_cfg(bt, *args), q["params"], wide(q["x"]), wide(q["y"]), wide(q["gate"]), x_out, u)
+        _check_forward(q, args, x_out, u)
+        _check_backward(bt, q, args, tensors=wide)
