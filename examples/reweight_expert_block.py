@@ -40,7 +40,7 @@ def batch(g, teacher, block, d, dtype, device="cuda"):
     expert = torch.randint(0, block.up.n_groups, (n,), generator=g, device=device).sort()[0]
     offsets = torch.searchsorted(expert, torch.arange(block.up.n_groups + 1, device=device)).to(torch.int32)
     x = torch.randn(n, d, generator=g, device=device)
-    target, _, _ = block.forward(operands(teacher, dtype), offsets, x)
+    target, _, _ = block.forward(operands(teacher, dtype), offsets, x, next_norm=False)
     return offsets, x, target.clone()
 
 
@@ -57,7 +57,7 @@ def main(steps=60, n_experts=4, d=256, hidden=256, rows=1024, groups=8, lr=1.0, 
     per_group = torch.zeros(groups, device="cuda").index_add_(0, group, torch.ones(rows, device="cuda"))
 
     def residual(theta, data):
-        x_out, _, kept = block.forward(operands(theta, dtype), data[0], data[1])
+        x_out, _, kept = block.forward(operands(theta, dtype), data[0], data[1], next_norm=False)
         return x_out - data[2], kept
 
     def group_costs(theta):

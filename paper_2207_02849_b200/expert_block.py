@@ -3,8 +3,9 @@ checkpoint of their hidden layer, as one differentiable step.
 
     u = N(x) w + ...;  z = up_e u;  a = act(z)  (or act(z_gate) z_value);  y = down_e a;  x' = x + s a(g) N(y) w';  u' = N(x') w''
 
-for rows sorted by expert.  Between forward and backward a block keeps x, x', u, y and the checkpoint (q, scales) of z; the
-hidden activation is made again from the checkpoint.  Gradients are what the finite-difference approximation of a
+for rows sorted by expert.  Of blocks in a row, each makes the next one's u with its own exit norm.  Between forward and backward
+a block keeps x, x', u, y and the checkpoint (q, scales) of z (x only where it made its u itself); the hidden activation is made
+again from the checkpoint.  Gradients are what the finite-difference approximation of a
 best-response Jacobian needs: two gradients at displaced parameters (arXiv 2207.02849, Sec. 3.2)."""
 from __future__ import annotations
 
@@ -40,25 +41,31 @@ class ExpertBlock:
     def _rows(self, width: int, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
         return torch.empty(self.rows, width, dtype=dtype or self.dtype, device=self.device)
 
-    def forward(self, p: dict, offsets: torch.Tensor, x: torch.Tensor, gate: Optional[torch.Tensor] = None):
-        """(x', u', kept): the residual stream, the next block's normed input and what `backward` needs."""
-        u, z, a, y = self._rows(self.d), self._rows(self.act8.width), self._rows(self.hidden), self._rows(self.d)
+    def forward(self, p: dict, offsets: torch.Tensor, x: torch.Tensor, gate: Optional[torch.Tensor] = None,
+                u: Optional[torch.Tensor] = None, next_norm: bool = True):
+        """(x', u', kept): the residual stream, the next block's normed input and what `backward` needs.  `u`: the normed input
+        that the block before has made (its u', with its `exit` w_pre); None: it is made here, with `entry`.  next_norm False:
+        no block follows, u' is None."""
+        z, a, y = self._rows(self.act8.width), self._rows(self.hidden), self._rows(self.d)
         q, scales = self.act8.empty(self.rows, self.device)
-        x_out, u_out = torch.empty_like(x), self._rows(self.d)
-        bt.betty_block_norm(self.entry, p["entry"], x, None, None, None, u)
+        x_out, u_out, own_norm = torch.empty_like(x), self._rows(self.d) if next_norm else None, u is None
+        if own_norm:
+            u = self._rows(self.d)
+            bt.betty_block_norm(self.entry, p["entry"], x, None, None, None, u)
         bt.betty_grouped_forward(self.up, offsets, u, p["up"], z, self.ws)
         bt.betty_act8_store(self.act8, z, a, q, scales)
         bt.betty_grouped_forward(self.down, offsets, a, p["down"], y, self.ws)
         bt.betty_block_norm(self.exit, p["exit"], x, y, gate, x_out, u_out)
-        return x_out, u_out, {"x": x, "x_out": x_out, "u": u, "y": y, "q": q, "scales": scales, "gate": gate}
+        return x_out, u_out, {"x": x if own_norm else None, "x_out": x_out, "u": u, "y": y, "q": q, "scales": scales, "gate": gate}
 
     def backward(self, p: dict, offsets: torch.Tensor, kept: dict, dx_out: Optional[torch.Tensor], du_out: Optional[torch.Tensor],
                  weight_dtype: torch.dtype = torch.float32) -> dict:
-        """Gradients of x, gate and the parameters from those of x' and u' (either may be None)."""
+        """Gradients of x, gate and the parameters from those of x' and u' (either may be None).  Where `forward` was given u: its
+        gradient under "u", "x" without what goes through u, and no "entry": the block before takes them as du_out and dx_out."""
         x, gate = kept["x"], kept["gate"]
-        dx, dy, da, dz, a, du = (torch.empty_like(x), self._rows(self.d), self._rows(self.hidden), self._rows(self.act8.width),
+        dx, dy, da, dz, a, du = (torch.empty_like(kept["x_out"]), self._rows(self.d), self._rows(self.hidden), self._rows(self.act8.width),
                                  self._rows(self.hidden), self._rows(self.d))
-        grads = {"entry": torch.empty_like(p["entry"]), "exit": torch.empty_like(p["exit"]),
+        grads = {"exit": torch.empty_like(p["exit"]),
                  "up": torch.empty(p["up"].shape, dtype=weight_dtype, device=self.device),
                  "down": torch.empty(p["down"].shape, dtype=weight_dtype, device=self.device),
                  "gate": torch.empty_like(gate) if gate is not None else None, "x": dx}
@@ -69,5 +76,9 @@ class ExpertBlock:
         bt.betty_grouped_backward_weight(self.down, offsets, dy, a, grads["down"], self.ws)
         bt.betty_grouped_backward_weight(self.up, offsets, dz, kept["u"], grads["up"], self.ws)
         bt.betty_grouped_backward_data(self.up, offsets, dz, p["up"], du, self.ws)
-        bt.betty_block_norm_backward(self.entry, p["entry"], x, None, None, du, dx, dx, None, None, grads["entry"], self.ws)
+        if x is None:
+            grads["u"] = du
+        else:
+            grads["entry"] = torch.empty_like(p["entry"])
+            bt.betty_block_norm_backward(self.entry, p["entry"], x, None, None, du, dx, dx, None, None, grads["entry"], self.ws)
         return grads
