@@ -137,3 +137,32 @@ def test_layer_norms_with_biases_of_wider_buffers(pad, shift, d, per_gate):
         bt.betty_block_norm(_cfg(bt, *args), q["params"], wide(q["x"]), wide(q["y"]), wide(q["gate"]), x_out, u)
         _check_forward(q, args, x_out, u)
         _check_backward(bt, q, args, tensors=wide)
+
+
+@pytest.mark.parametrize("rows,d", [(5000, 96), (2500, 1002), (700, 2051), (320, 4096)])
+@pytest.mark.parametrize("kind,act,bias", [("rms", "linear", False), ("layer", "sigmoid", True)])
+def test_parameter_gradients_element_by_element(rows, d, kind, act, bias):
+    """Each is a sum over the rows, taken by walkers of at most 34 rows, at most eight warps of a block and 32 slices of at most ten
+    blocks: no more than 34 + 8 + 10 + 32 roundings of a running sum whose size is at most the sum of the magnitudes: 84 * 2^-24 =
+    5e-6 of it (roundings that all fall to one side, which they do not).  Each term besides carries the error of its own factors:
+    SLACK of du n, and for the others SLACK of the row's size of dX (the tolerance that dx itself is held to) times the
+    other factor."""
+    import paper_2207_02849_b200 as bt
+    q = _problem(rows, rows, d, F, F, act, 1, bias)
+    args = (d, kind, kind, act, 1, bias, 1e-5)
+    got = _check_backward(bt, q, args)[3].double().cpu()
+    p, x, y, du = (ref.d64(q[k]) for k in ("params", "x", "y", "du"))
+    g = ref.d64(q["gate"])
+    a = g if act == "linear" else torch.sigmoid(g)
+    want = _gradients(q, args)
+    n, m, dX = ref.unit(x, kind, 1e-5), ref.unit(y, kind, 1e-5), want["dx"]
+    rms = lambda t: t.pow(2).mean(-1, keepdim=True).sqrt()  # noqa: E731
+    big = rms(dX) + rms(ref.d64(q["dxo"])) + rms(du)
+    sums = lambda term, other: 5e-6 * term.abs().sum(0) + SLACK * (term.abs() + big * other.abs()).sum(0)  # noqa: E731
+    post, flat = sums(dX * a * m, a * (m.abs() + 1.0)), sums(dX * a, a)
+    bound = [5e-6 * (du * n).abs().sum(0) + SLACK * (du.abs() * (n.abs() + 1.0)).sum(0), p[2].abs() * post, p[1].abs() * post]
+    if bias:
+        bound[2] = bound[2] + p[4].abs() * flat
+        bound += [5e-6 * du.abs().sum(0), p[2].abs() * flat]
+    excess = (got - want["dparams"]).abs() / torch.stack(bound)
+    assert float(excess.max()) <= 1.0, excess.amax(1)
