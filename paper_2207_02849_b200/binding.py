@@ -517,7 +517,7 @@ class BlockNorm:
         return t.data_ptr()
 
     def _gate(self, t, rows: int, dtype, name: str):
-        return _mat(t, -(-rows // self.rows_per_gate), self.d, dtype, name)
+        return _mat(t, -(-rows // max(self.rows_per_gate, 1)), self.d, dtype, name)
 
 
 def betty_block_norm(cfg: BlockNorm, params: torch.Tensor, x: torch.Tensor, y: Optional[torch.Tensor], gate: Optional[torch.Tensor],

@@ -26,7 +26,9 @@ class ExpertBlock:
     def __init__(self, n_experts: int, d: int, hidden: int, rows: int, dtype: torch.dtype = torch.bfloat16, act: int = bt.ACT_SILU,
                  gated: bool = True, norm: int = bt.NORM_RMS, gate: int = bt.GATE_NONE, rows_per_gate: int = 1, eps: float = 1e-6,
                  bias: bool = False, device="cuda"):
-        code = {torch.bfloat16: bt.BETTY_BF16, torch.float16: bt.BETTY_F16}[dtype]
+        code = {torch.bfloat16: bt.BETTY_BF16, torch.float16: bt.BETTY_F16}.get(dtype)
+        if code is None:
+            raise ValueError(f"an expert block's operands are bf16 or fp16, got {dtype}")
         self.d, self.hidden, self.rows, self.dtype, self.device = int(d), int(hidden), int(rows), dtype, device
         self.act8 = bt.Act8(hidden, act=act, gated=gated)
         self.entry = bt.BlockNorm(d, pre=norm, post=bt.NORM_NONE, eps=eps, bias=bias)
