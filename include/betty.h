@@ -332,12 +332,14 @@ betty_status betty_gemm_bf16(int32_t M, int32_t N, int32_t n_pairs, const betty_
 
 /* ---- Operators of a trained residual block ----
  * For problems whose network is not one of the cost families above: a block  u = N(x),  y = experts(u),
- * x' = x + s a(g) N(y)  of a language model, forward and backward, next to the optimisers and the finite-difference
- * products of gradients that the caller takes with them.  All matrices are row-major DEVICE memory with a leading
+ * x' = x + s a(g) N(y)  of a language model, forward and backward.  A level (betty_level) cannot hold such a network: the
+ * caller strings the operators together and takes the gradient steps and finite differences of the gradients itself
+ * (examples/reweight_expert_block.py).  All matrices are row-major DEVICE memory with a leading
  * dimension in values (rows may be padded or be slices of wider rows); addresses need only their type's own alignment, 16-byte
  * aligned addresses and leading dimensions (and widths that are multiples of 8) take the faster accesses.  Parameter
  * blocks and their gradients are fp32 and 16-byte aligned, as above.  Outputs are overwritten, sums are fp32 in a
- * fixed order: the same call gives the same bits.  Zero rows are valid.  In-place use is possible where it is said. */
+ * fixed order: the same call gives the same bits.  Zero rows are valid.  In-place use is possible where it is said.
+ * Subnormal fp32 values and results may count as zero, as everywhere in the library. */
 
 typedef enum {
   BETTY_NORM_NONE = 0,   /* N(v) = v */

@@ -5,8 +5,8 @@
 //
 //   top = max |z|,   q = rint(z * (127 * (1 / top))),   scale = top * (1 / 127),   z~ = q * scale
 //
-// every operation rounded to fp32 on its own (no contraction), so that q is the same whoever computes it.  A group whose
-// top is below 1e-30 is held as zeros; one that holds an infinity or a NaN gets the scale NaN, so that it stays visible.
+// every operation rounded to fp32 on its own (no contraction, a subnormal 1 / top kept), so that q is the same whoever computes it.
+// A group whose top is below 1e-30 is held as zeros; one that holds an infinity or a NaN gets the scale NaN, so that it stays visible.
 //
 //   store:     a = act(z)                 or  act(z_gate) * z_value;  z -> q, scale
 //   backward:  dz = da * act'(z~)         or  [da * z~_value * act'(z~_gate) | da * act(z~_gate)];   a from z~ for the

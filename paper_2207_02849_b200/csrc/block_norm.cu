@@ -225,10 +225,12 @@ betty_status forward(cudaStream_t stream, Args& a, int xd, int yd, int classes) 
 }
 
 // Many rows take the wide kernel (several chunks per thread: a row's fixed cost, its sums and addresses, is shared by more
-// values); rows that would leave thread groups idle take one chunk per thread.  Rows that cannot be fetched ahead (no common
-// shift; rows so wide that one does not fit the shared memory) are read where they are used, four chunks per thread.  Wide rows
-// of which only one fits are fetched when it is their turn (backward, a gate to each row, 4096 rows: 8192 bf16 values 166 us,
-// read where they are used 536; 6144 fp32 values 274 and 534).
+// values); rows that would leave thread groups idle take one chunk per thread.  Rows that cannot be fetched ahead are read where they
+// are used, four chunks per thread: those without a common shift, those of which one does not fit the shared memory, and, backward,
+// fp32 rows of 257 to 512 values with a gate and layer norms or biases (with a gate to each row of 7169 to 8192, too): the blocks
+// that the group size gives an SM leave no room for two rows and the coefficients.  Wide rows of which only one fits are fetched
+// when it is their turn (backward, a gate to each row, 4096 rows, single launches: 8192 bf16 values 116 us, read where they are used
+// 501; 6144 fp32 values 282 and 490).
 Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int classes, const Needs& n) {
   const int bx = xd == BETTY_F32 ? 4 : 2, by = yd == BETTY_F32 ? 4 : 2, sms = current_sm_count();
   const int64_t span = classes > 1 ? d + 7 : d;              // columns with the head of a shifted row
@@ -253,8 +255,8 @@ Layout layout_of(int64_t d, int64_t rows, int xd, int yd, int classes, const Nee
       return l;
     }
     if (l.wide && span <= (int64_t)MAX_G * 8 && rows < (int64_t)2 * batch * groups * l.blocks_per_sm * sms) continue;
-    // the last 5 KB (left to L1 elsewhere) where a row would not fit without them: 4096 x 8192 fp32 backward 356 us, read
-    // where it is used 637
+    // the last 5 KB (left to L1 elsewhere) where a row would not fit without them: 4096 x 8192 fp32 RMS backward 364 us, read
+    // where it is used 595
     const int64_t most = (attempt == 2 ? 227 : 222) * 1024;
     const int64_t slot = (int64_t)l.slot_bytes * groups * batch, budget = most / l.blocks_per_sm - 2048 - (int64_t)acc;
     l.ahead = (int)(budget / slot) - 1;

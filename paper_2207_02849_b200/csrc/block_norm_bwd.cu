@@ -48,11 +48,13 @@ __device__ __forceinline__ unsigned gate_slot(const Args& a, unsigned first, uns
 // A gate shared by rows needs one sum H = sum dX m per gate: dg = a'(g) s w_post H, and A gains a(g) H when the walker
 // leaves the gate, so A waits in the block's row of the column sums.
 //
-// Measured: 8192 x 4096 bf16, RMS norms, gates of 1024 rows: 120 to 127 us (3.2 TB/s) against 62 us for the bytes; 2731 x 1537
-// fp32, layer norms with biases: 70 us against 21.  The instruction stream bounds it, at 16 warps per SM (two blocks of
-// 256 threads at 128 registers): with the loads, the stores or the row sums left out it still takes 111, 115 or 107 of 133 us.
-// Two chunks per thread with the coefficients in shared memory took 123 us where registers for them spilled and took 153;
-// one chunk per thread and 512 threads per row 141; two rows at a time 178 to 201 (spills).
+// Measured: 8192 x 4096 bf16, RMS norms, gates of 1024 rows: 99 us (4.1 TB/s) against 62 us for the bytes; 2731 x 1537 fp32, layer
+// norms with biases: 68 us against 21.  Neither pipe is full: the first issues 53 % of the time and uses 48 % of the memory, the
+// second 34 and 18 %, with 16 warps per SM (two blocks of 256 threads at 128 registers): what is exposed is a row's own chain,
+// from its values over two walks with the sums and a barrier between them.  SHARED (gates of several rows) is a template parameter
+// because what such a gate needs took registers from every row: 130 -> 105 us with one, 115 -> 93 without any gate (single launches,
+// cold).  Before that, two chunks per thread with the coefficients in shared memory took 123 us where registers for them spilled and
+// took 153; one chunk per thread and 512 threads per row 141; two rows at a time 178 to 201 (spills).
 template <typename TX, typename TY, bool VEC, int CH, bool GENERAL, bool SHARED>
 __global__ void __launch_bounds__(MAX_G, 1) k_backward(const Args a) {
   __shared__ __align__(16) float red[2 * RED_VALUES * 16];

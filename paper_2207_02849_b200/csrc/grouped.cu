@@ -14,8 +14,10 @@
 // fills the rest with zeros (k_group_maps writes one pair of maps per expert).
 //
 // Measured (bf16, alone with a cold L2 / back to back under the power cap): 16384 rows, 8 uneven experts, 4096 x 4096: 386 / 440 us,
-// 1.42 / 1.25 PFLOP/s, 85 % of the measured library rate in both; weight gradient 4096 x 2048: 191 / 227 us; 5001 rows, 16 experts,
-// 2048 -> 1024 (fp16): 32 us against 15 for its bytes: 128 tiles on 74 pairs are two rounds.
+// 1.42 / 1.25 PFLOP/s, 85 % of the measured library rate in both; weight gradient 4096 x 2048: 185 / 199 to 231 us (fp32 result 204 /
+// 215).  5001 rows, 16 experts, 2048 -> 1024 (fp16): 29 us in a row, 33 among other passes, 39 alone with a cold L2, against 15 for its
+// bytes.  Of that, 128 tiles on 74 pairs (two rounds, 1.73 would do) explain a sixth; the rest is the pace of about 320 ns per
+// contraction chunk where one of 160 columns needs 230, the first loads and the last tiles' drain.
 #include <cuda.h>
 #include "common.cuh"
 
@@ -738,7 +740,7 @@ static betty_status product(const betty_grouped_cfg* c, int64_t rows, const int3
     return a.lanes > BM && a.cols > 128 ? run<2, 256, MODE>(s, arena, c->dtype, out_dtype, A, B, a) : run<1, 128, MODE>(s, arena, c->dtype, out_dtype, A, B, a);
   const int64_t used = rows < c->n_groups ? rows : c->n_groups, mean = (rows + used - 1) / used;
   const int64_t pair_tiles = (a.lanes + 2 * BM - 1) / (2 * BM) * ((mean + 255) / 256) * used;
-  // Measured (bf16, us; pairs 256 wide / single SM 128 / 64 / 32): 24 rows, 8 experts, 1024 x 1024: 12.1 / 11.1 / 9.7 / 10.2; 1 row,
+  // Measured (bf16, us, launches in a row; pairs 256 wide / single SM 128 / 64 / 32): 24 rows, 8 experts, 1024 x 1024: 12.1 / 11.1 / 9.7 / 10.2; 1 row,
   // 4096 x 4096: 19.4 / 18.4 / 13.6 / 11.7 (the last two with split contractions); 200 rows, 8 experts, 4096 x 4096: 51.5 / 50.4 /
   // 50.3 / 61.7; 300 rows, 4 experts, 4096 -> 1024: 20.5 / 19.3 / 14.8 / 17.9; 800 rows, 4 experts, 1024 -> 2048: 11.7 / 9.3 /
   // 12.7 / 15.7; 5001 rows, 16 experts, 2048 -> 1024: 27.7 / 31.1 / 43.2 / 70.6.
@@ -752,7 +754,7 @@ static betty_status check(const betty_grouped_cfg* c, int64_t rows, const int32_
   if (!c || rows < 0) return BETTY_ERR_INVALID_ARG;
   if (c->dtype != BETTY_BF16 && c->dtype != BETTY_F16) return BETTY_ERR_DTYPE;
   if (c->n_groups < 1 || c->in < 1 || c->out < 1) return BETTY_ERR_SHAPE;
-  // 32-bit tile counts and coordinates: at most 2^31 rows, 2^24 columns, 1024 groups
+  // 32-bit tile counts and coordinates: at most 2^30 rows, 2^24 columns, 1024 groups
   if (c->n_groups > MAX_GROUPS || rows > (1 << 30) || c->in > (1 << 24) || c->out > (1 << 24)) return BETTY_ERR_UNSUPPORTED;
   if (((rows + 127) / 128 + c->n_groups) * ((c->out > c->in ? c->out : c->in) / 128 + 1) > (1 << 30) ||
       (int64_t)c->n_groups * (c->out / 128 + 1) * (c->in / 128 + 1) > (1 << 30))
