@@ -116,7 +116,7 @@ typedef enum {
   BETTY_ACT_GELU = 1,  /* erf form */
   BETTY_ACT_SILU = 2   /* z sigmoid(z); the betty_act8 calls only, not the levels' hidden layers */
 } betty_activation;
-typedef enum { BETTY_F32 = 0, BETTY_BF16 = 1, BETTY_I32 = 2, BETTY_F16 = 3 } betty_dtype;
+typedef enum { BETTY_F32 = 0, BETTY_BF16 = 1, BETTY_I32 = 2, BETTY_F16 = 3, BETTY_I64 = 4 /* token numbers only */ } betty_dtype;
 
 /* How a problem's gradient step is taken (the paper lets each problem bring its own optimiser: SGD with
  * momentum and weight decay for the classifiers, Adam for the weight net, App. C).
@@ -446,6 +446,58 @@ betty_status betty_grouped_backward_weight(const betty_grouped_cfg* cfg, int64_t
  * which the calls make of operands that do not start on 16-byte boundaries or whose leading dimensions (group strides)
  * are not multiples of 8; without that room such operands return BETTY_ERR_WORKSPACE. */
 betty_status betty_grouped_workspace_size(const betty_grouped_cfg* cfg, int64_t rows, int32_t any_layout, size_t* bytes);
+
+/* ---- losses over a vocabulary ----
+ * The losses of a language model whose logits are products of its last hidden rows with a matrix of the vocabulary, forward
+ * and backward, without the logits being kept: they are made again for the gradients, a piece of the vocabulary at a time.
+ * Conventions as for the residual block's operators above; the losses are one number per row, so that a problem
+ * above can weigh the rows (the row losses are then the gradient by the weights, and dloss the weights). */
+typedef struct {
+  int64_t vocab, d;      /* W is [vocab, d]; 1 .. 2^22 and 1 .. 2^16 */
+  int32_t dtype;         /* X and W: BETTY_BF16 or BETTY_F16; fp32 accumulation */
+  float temperature;     /* T in [1e-30, 1e30] */
+  float smoothing;       /* e in [0, 1]: share of the label that is spread over the whole vocabulary (cross entropy only) */
+  float z_loss;          /* zeta in [0, 1e30]: weight of the squared logarithm of the normaliser (cross entropy only) */
+} betty_vocab_cfg;
+
+/* Cross entropy of z_iv = x_i . w_v / T with the tokens target[rows] (BETTY_I32 or BETTY_I64):
+ *   lse_i = log sum_v exp z_iv,   loss_i = (1 - e) (lse_i - z_it) + e (lse_i - mean_v z_iv) + zeta lse_i^2.
+ * A row whose target is outside [0, vocab) is left out: loss_i = lse_i = 0, whatever X holds there. */
+betty_status betty_vocab_ce(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                            const void* target, int32_t target_dtype, float* loss, float* lse, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/* Gradients of sum_i dloss_i loss_i, with lse from the forward call:
+ *   dX_i = (dloss_i / T) sum_v dz_iv w_v,   dW_v = sum_i (dloss_i / T) dz_iv x_i,
+ *   dz_iv = (1 + 2 zeta lse_i) exp(z_iv - lse_i) - (1 - e) [v = target_i] - e / vocab.
+ * dX or dW may be NULL (not both).  Result types: BETTY_F32 or the operands' type.  dz is rounded to the operands' type before
+ * the two products.  A row that is left out, or whose dloss is 0, has a zero row in dX and no part in dW, whatever X holds there.
+ * fp16: rows whose weights are less than 2^-20 of the largest lose accuracy in dW. */
+betty_status betty_vocab_ce_backward(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                     const void* target, int32_t target_dtype, const float* lse, const float* dloss, void* dX,
+                                     int64_t lddx, int32_t dx_dtype, void* dW, int64_t lddw, int32_t dw_dtype, void* ws,
+                                     size_t ws_bytes, void* stream);
+
+/* Distillation from a teacher's top logits: ids and teacher are [rows, top] (1 <= top <= 1024; ids BETTY_I32 or BETTY_I64, teacher
+ * BETTY_F32, BETTY_BF16 or BETTY_F16), in any order.  With p_i the softmax of the row's teacher logits / T over its entries,
+ *   loss_i = sum_j p_ij (log p_ij - z_i,ids(i,j) + lse_i),   dz_iv = exp(z_iv - lse_i) - sum of p_ij over j with ids(i,j) = v.
+ * An entry whose id is outside [0, vocab) or whose logit is -inf is none (what else the logit of the former is is not looked at);
+ * a row without entries is left out as above.  An id that a row holds twice is two entries.  smoothing and z_loss have to be
+ * 0 (else BETTY_ERR_UNSUPPORTED). */
+betty_status betty_vocab_distill(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                 int32_t top, const void* ids, int64_t ldi, int32_t id_dtype, const void* teacher, int64_t ldt,
+                                 int32_t teacher_dtype, float* loss, float* lse, void* ws, size_t ws_bytes, void* stream);
+betty_status betty_vocab_distill_backward(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W,
+                                          int64_t ldw, int32_t top, const void* ids, int64_t ldi, int32_t id_dtype,
+                                          const void* teacher, int64_t ldt, int32_t teacher_dtype, const float* lse,
+                                          const float* dloss, void* dX, int64_t lddx, int32_t dx_dtype, void* dW, int64_t lddw,
+                                          int32_t dw_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace of the calls above on up to `rows` rows (at most 2^22) and `top` entries a row (0: cross entropy only), on the
+ * current device.  any_layout != 0: room for an aligned copy of W too, which the calls make of a W that does not start on a
+ * 16-byte boundary or whose leading dimension is not a multiple of 8; without that room such a W returns
+ * BETTY_ERR_WORKSPACE.  Other matrices need no room for their layout. */
+betty_status betty_vocab_workspace_size(const betty_vocab_cfg* cfg, int64_t rows, int32_t top, int32_t any_layout, size_t* bytes);
 
 /* The dataflow graph of Sec. 3.1: directed edges between problem indices.  An upper-to-lower edge
  * (from > to in the paper's ordering) says that theta_from constrains problem `to`; a lower-to-upper

@@ -22,7 +22,7 @@ BETTY_NEUMANN, BETTY_CG, BETTY_FD = range(3)
 ACT_RELU, ACT_GELU, ACT_SILU = range(3)
 NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
 GATE_NONE, GATE_LINEAR, GATE_SIGMOID = range(3)
-BETTY_F32, BETTY_BF16, BETTY_I32, BETTY_F16 = range(4)
+BETTY_F32, BETTY_BF16, BETTY_I32, BETTY_F16, BETTY_I64 = range(5)
 BETTY_OPT_GD, BETTY_OPT_MOMENTUM, BETTY_OPT_ADAM = range(3)
 BETTY_LR_CONSTANT, BETTY_LR_MULTISTEP, BETTY_LR_COSINE = range(3)
 
@@ -84,6 +84,11 @@ class _Act8Cfg(C.Structure):
     _fields_ = [("cols", C.c_int64), ("dtype", C.c_int32), ("act", C.c_int32), ("gated", C.c_int32)]
 
 
+class _VocabCfg(C.Structure):
+    _fields_ = [("vocab", C.c_int64), ("d", C.c_int64), ("dtype", C.c_int32), ("temperature", C.c_float), ("smoothing", C.c_float),
+                ("z_loss", C.c_float)]
+
+
 _lib = None
 
 
@@ -133,6 +138,13 @@ def lib():
     sig["betty_grouped_workspace_size"] = [GC, I64, I32, C.POINTER(SZ)]
     sig["betty_grouped_forward"] = sig["betty_grouped_backward_data"] = [GC, I64, VP] + 2 * mat + [I64] + mat + [I32, VP, SZ, VP]
     sig["betty_grouped_backward_weight"] = [GC, I64, VP] + 3 * mat + [I64, I32, VP, SZ, VP]
+    VC = C.POINTER(_VocabCfg)
+    sig["betty_vocab_workspace_size"] = [VC, I64, I32, I32, C.POINTER(SZ)]
+    head, top, results = [VC, I64] + 2 * mat, [I32] + mat + [I32] + mat + [I32], mat + [I32] + mat + [I32]
+    sig["betty_vocab_ce"] = head + [VP, I32, VP, VP, VP, SZ, VP]
+    sig["betty_vocab_ce_backward"] = head + [VP, I32, VP, VP] + results + [VP, SZ, VP]
+    sig["betty_vocab_distill"] = head + top + [VP, VP, VP, SZ, VP]
+    sig["betty_vocab_distill_backward"] = head + top + [VP, VP] + results + [VP, SZ, VP]
     EP, IP = C.POINTER(_Edge), C.POINTER(I32)
     sig["betty_find_paths"] = [I32, EP, I32, EP, I32, I32, IP, I32, IP, I32, IP, IP]
     sig["betty_selftest_wait_timeout"] = [VP, SZ, VP]
@@ -669,6 +681,102 @@ def betty_grouped_backward_weight(cfg: Grouped, offsets: torch.Tensor, dy: torch
     _check(lib().betty_grouped_backward_weight(cfg._ref, rows, cfg._offsets(offsets), *_mat(dy, rows, cfg.n_out, t, "dy"),
                                                *_mat(x, rows, cfg.n_in, t, "x"), *cfg._matrices(dw, dw.dtype, "dw"), _DT.get(dw.dtype, -1),
                                                ws.ptr, ws.nbytes, _stream(stream)), "betty_grouped_backward_weight")
+
+
+# ---- losses over a vocabulary ----
+_ID = {torch.int32: BETTY_I32, torch.int64: BETTY_I64}
+
+
+class VocabLoss:
+    """Configuration of the betty_vocab calls (betty.h): logits x . w / temperature over `vocab` tokens, operands of `dtype`
+    (BETTY_BF16 or BETTY_F16); smoothing and z_loss belong to the cross entropy."""
+
+    def __init__(self, vocab: int, d: int, dtype: int = BETTY_BF16, temperature: float = 1.0, smoothing: float = 0.0, z_loss: float = 0.0):
+        self.vocab, self.d = int(vocab), int(d)
+        self.torch_dtype = {BETTY_BF16: torch.bfloat16, BETTY_F16: torch.float16}.get(int(dtype))
+        self._ref = C.byref(_VocabCfg(self.vocab, self.d, int(dtype), float(temperature), float(smoothing), float(z_loss)))
+
+    def _operands(self, x: torch.Tensor, w: torch.Tensor):
+        t = self.torch_dtype
+        if t is None:
+            raise ValueError("the operands of a vocabulary loss are bf16 or fp16")
+        return (self._ref, x.shape[0], *_mat(x, x.shape[0], self.d, t, "x"), *_mat(w, self.vocab, self.d, t, "w"))
+
+    def _entries(self, ids: torch.Tensor, teacher: torch.Tensor, rows: int):
+        if ids.dtype not in _ID:
+            raise ValueError(f"ids must be int32 or int64, got {ids.dtype}")
+        if ids.dim() != 2:
+            raise ValueError(f"ids must have the shape ({rows}, entries), got {tuple(ids.shape)}")
+        top = ids.shape[1]
+        return (top, *_mat(ids, rows, top, ids.dtype, "ids"), _ID[ids.dtype], *_mat(teacher, rows, top, teacher.dtype, "teacher"),
+                _float_dtype(teacher.dtype))
+
+    def _results(self, dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], rows: int):
+        out = []
+        for t, n, name in ((dx, rows, "dx"), (dw, self.vocab, "dw")):
+            out += [None, 0, BETTY_F32] if t is None else [*_mat(t, n, self.d, t.dtype, name), _DT.get(t.dtype, -1)]
+        return out
+
+
+def _row_values(t: torch.Tensor, rows: int, dtypes, name: str) -> int:
+    if t.dtype not in dtypes or not t.is_cuda or t.shape != (rows,) or not (t.is_contiguous() or rows == 0):
+        raise ValueError(f"{name} must be {rows} contiguous values ({' or '.join(map(str, dtypes))}) on the GPU")
+    return t.data_ptr()
+
+
+def _on_current_device(*tensors) -> None:
+    """Kernels run on the current device: operands of another one are refused before anything is launched."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != here:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def betty_vocab_workspace_size(cfg: VocabLoss, rows: int, top: int = 0, any_layout: Optional[bool] = None) -> int:
+    """Workspace of any of the calls below on up to `rows` rows with `top` entries each (0: cross entropy only).  any_layout: room for
+    an aligned copy of w; default: where a contiguous one would need it."""
+    out = C.c_size_t(0)
+    _check(lib().betty_vocab_workspace_size(cfg._ref, int(rows), int(top), int(cfg.d % 8 != 0 if any_layout is None else any_layout), C.byref(out)),
+           "betty_vocab_workspace_size")
+    return int(out.value)
+
+
+def betty_vocab_ce(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                   ws: Workspace, stream=None) -> None:
+    """loss, lse [rows] fp32: the rows' cross entropy with `target` (int32 or int64) and the logarithm of its normaliser."""
+    rows, f = x.shape[0], (torch.float32,)
+    _on_current_device(x, w, target, loss, lse)
+    _check(lib().betty_vocab_ce(*cfg._operands(x, w), _row_values(target, rows, tuple(_ID), "target"), _ID[target.dtype], _row_values(loss, rows, f, "loss"),
+                                _row_values(lse, rows, f, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_ce")
+
+
+def betty_vocab_ce_backward(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
+                            dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], ws: Workspace, stream=None) -> None:
+    """dx, dw (None: not wanted) = the gradients of sum(dloss * loss)."""
+    rows, f = x.shape[0], (torch.float32,)
+    _on_current_device(x, w, target, lse, dloss, dx, dw)
+    _check(lib().betty_vocab_ce_backward(*cfg._operands(x, w), _row_values(target, rows, tuple(_ID), "target"), _ID[target.dtype],
+                                         _row_values(lse, rows, f, "lse"), _row_values(dloss, rows, f, "dloss"), *cfg._results(dx, dw, rows), ws.ptr,
+                                         ws.nbytes, _stream(stream)), "betty_vocab_ce_backward")
+
+
+def betty_vocab_distill(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, loss: torch.Tensor,
+                        lse: torch.Tensor, ws: Workspace, stream=None) -> None:
+    """loss [rows] = KL(teacher || student) with the teacher's distribution over its entries (ids, teacher) [rows, top]."""
+    rows, f = x.shape[0], (torch.float32,)
+    _on_current_device(x, w, ids, teacher, loss, lse)
+    _check(lib().betty_vocab_distill(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(loss, rows, f, "loss"),
+                                     _row_values(lse, rows, f, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_distill")
+
+
+def betty_vocab_distill_backward(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor,
+                                 dloss: torch.Tensor, dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], ws: Workspace, stream=None) -> None:
+    """dx, dw (None: not wanted) = the gradients of sum(dloss * loss)."""
+    rows, f = x.shape[0], (torch.float32,)
+    _on_current_device(x, w, ids, teacher, lse, dloss, dx, dw)
+    _check(lib().betty_vocab_distill_backward(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(lse, rows, f, "lse"),
+                                              _row_values(dloss, rows, f, "dloss"), *cfg._results(dx, dw, rows), ws.ptr, ws.nbytes, _stream(stream)),
+           "betty_vocab_distill_backward")
 
 
 def betty_selftest_wait_timeout(ws: Workspace, stream=None) -> None:

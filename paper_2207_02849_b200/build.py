@@ -12,7 +12,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libbetty.so")
 SOURCES = ["api.cu", "vec.cu", "logreg.cu", "logreg_small.cu", "mlp.cu", "gemm.cu", "gemm_tc.cu", "block_norm.cu",
-           "block_norm_bwd.cu", "act8.cu", "grouped.cu"]
+           "block_norm_bwd.cu", "act8.cu", "align.cu", "grouped.cu",
+           "vocab_loss.cu", "vocab_products.cu"]
 FAMILY_SOURCES = ["mlp.cu", "gemm.cu", "gemm_tc.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -1,0 +1,572 @@
+// Losses over a vocabulary: the rows that count and their entries, the losses from the statistics of the logits' tiles, and the
+// C entries (see vocab_loss.cuh for the mathematics).
+//
+// What surrounds the products is bound by memory and small beside them: a copy of x in, fp32 sums of dX out.
+#include "vocab_loss.cuh"
+
+namespace betty {
+namespace vocab {
+using namespace tc;
+
+static constexpr int ROW_THREADS = 256;
+
+// ------------------------------------------------------------------ values of the caller's types
+__device__ __forceinline__ int64_t whole(const void* p, int is64, int64_t i) { return is64 ? ((const int64_t*)p)[i] : ((const int32_t*)p)[i]; }
+__device__ __forceinline__ float real(const void* p, int dtype, int64_t i) {
+  if (dtype == BETTY_F32) return ((const float*)p)[i];
+  return dtype == BETTY_BF16 ? __bfloat162float(((const __nv_bfloat16*)p)[i]) : __half2float(((const __half*)p)[i]);
+}
+
+// ------------------------------------------------------------------ a teacher's entries
+// One block per row: the softmax of the row's logits over T, and its entries in ascending order of (id, place): a bitonic sort of
+// 64-bit keys in shared memory.  An entry without an id of the vocabulary or with a logit of -inf is none: what else its logit
+// is is not looked at.  The same id twice stays two entries; their shares add up where they are used.
+__global__ void k_entries(const void* ids, int64_t ldi, int id64, const void* logits, int64_t ldt, int dtype, int top, int padded, float inv_t, int64_t vocab,
+                          int32_t* id_out, float* p_out, uint8_t* some) {
+  extern __shared__ unsigned char raw[];
+  uint64_t* key = (uint64_t*)raw;
+  float* e = (float*)(key + padded);
+  __shared__ float red[32];
+  pdl_enter();
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x, warps = blockDim.x >> 5;
+  float m = -INFINITY;
+  for (int j = tid; j < padded; j += blockDim.x) {
+    uint64_t k = ~0ull;
+    float t = -INFINITY;
+    if (j < top) {
+      const int64_t id = whole(ids, id64, row * ldi + j);
+      if (id >= 0 && id < vocab) {
+        t = real(logits, dtype, row * ldt + j);
+        if (t != -INFINITY) k = (uint64_t)id << 32 | (uint32_t)j;
+        t *= inv_t;
+      }
+    }
+    key[j] = k;
+    e[j] = t;
+    m = fmaxf(m, t);
+  }
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if ((tid & 31) == 0) red[tid >> 5] = m;
+  __syncthreads();
+  m = red[0];
+  for (int i = 1; i < warps; ++i) m = fmaxf(m, red[i]);
+  __syncthreads();
+  const float base = m == -INFINITY ? 0.f : m;
+  float s = 0.f;
+  for (int j = tid; j < padded; j += blockDim.x) {
+    const float x = exp2f((e[j] - base) * LOG2E);
+    e[j] = x;
+    s += x;
+  }
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((tid & 31) == 0) red[tid >> 5] = s;
+  __syncthreads();
+  s = 0.f;
+  for (int i = 0; i < warps; ++i) s += red[i];
+  for (int size = 2; size <= padded; size <<= 1)
+    for (int stride = size >> 1; stride; stride >>= 1) {
+      __syncthreads();
+      for (int i = tid; i < padded / 2; i += blockDim.x) {
+        const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
+        const uint64_t x = key[lo], y = key[hi];
+        if ((x > y) == ((lo & size) == 0)) { key[lo] = y; key[hi] = x; }
+      }
+    }
+  __syncthreads();
+  const float inv = 1.f / s;
+  for (int j = tid; j < top; j += blockDim.x) {
+    const uint64_t k = key[j];
+    const bool there = k != ~0ull;
+    id_out[row * top + j] = there ? (int32_t)(k >> 32) : NO_ID;
+    p_out[row * top + j] = there ? e[(uint32_t)k] * inv : 0.f;
+  }
+  if (tid == 0) some[row] = key[0] != ~0ull;
+}
+
+// ------------------------------------------------------------------ the rows that count
+struct RowArgs {
+  int64_t rows, vocab;
+  int d;
+  int64_t dp, ldx;
+  const uint16_t* x_in;
+  const void* target; int id64; float share;   // cross entropy: an entry (target, share) per row
+  const uint8_t* some;                         // distillation: whether a row has an entry
+  int32_t* id; float* p;                       // cross entropy: the entries, written here
+  Meta* meta; int32_t* src; int32_t* pos; uint16_t* x; uint16_t* x_dw;
+  float* loss; float* lse_out;                 // forward: zeros for rows left out
+  const float* lse; const float* dloss;        // backward
+  RowCoef* coef; float* row_scale;
+  float inv_t, z_loss, smoothing;
+  int fp16;
+};
+
+__device__ __forceinline__ bool counts(const RowArgs& a, int64_t i) {
+  bool live;
+  if (a.some) {
+    live = a.some[i] != 0;
+  } else {
+    const int64_t t = whole(a.target, a.id64, i);
+    live = t >= 0 && t < a.vocab;
+  }
+  return live && !(a.dloss && a.dloss[i] == 0.f);
+}
+// bound of a row's |dz|
+__device__ __forceinline__ float bound_of(const RowArgs& a, int64_t i) { return fabsf(a.dloss[i] * a.inv_t) * (1.f + 2.f * a.z_loss * fabsf(a.lse[i])); }
+// exponent that brings a bound to [2^13, 2^14) (of bounds at the ends of the fp32 range: near it); of a bound that is zero or not
+// finite: none
+__device__ __forceinline__ int lift(float bound) {
+  return bound > 0.f && bound < INFINITY ? min(max(13 - ilogbf(bound), -100), 100) : 0;
+}
+static constexpr int NO_LIFT = 1 << 20;
+// Half precision: a row's coefficients are stored as dz 2^h, with h from the row's own bound, so that none of a row with a small
+// weight is lost; the sums dX take 2^-h back.  dW sums over rows of different h: with H the smallest, x is scaled by
+// 2^(H - h) for it.  Rows within 2^6 of the largest bound share H, so that their x is not scaled at all: 2^13 / 2^6 / 128 Ki
+// is still a normal number of the type.
+__device__ __forceinline__ int row_lift(float bound, int least) {
+  const int h = lift(bound);
+  return h <= least + 6 ? least : h - 6;
+}
+
+// Copies a row to a 16-byte boundary, zeros behind it; a warp.  scale: 1, or a power of two for the second copy
+__device__ __forceinline__ void copy_row(const RowArgs& a, int64_t from, int64_t to, float scale) {
+  const int lane = threadIdx.x & 31;
+  const uint16_t* in = a.x_in + from * a.ldx;
+  uint16_t* out = a.x + to * a.dp;
+  uint16_t* out2 = a.x_dw != a.x ? a.x_dw + to * a.dp : nullptr;
+  const bool aligned = ((uintptr_t)in & 15) == 0;
+  for (int c = lane * 8; c < a.dp; c += 256) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (aligned && c + 8 <= a.d) {
+      v = *(const uint4*)(in + c);
+    } else {
+      uint32_t w[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < a.d) w[k >> 1] |= (uint32_t)in[c + k] << (16 * (k & 1));
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    *(uint4*)(out + c) = v;
+    if (out2) {
+      uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 f = __half22float2(*(__half2*)&w[k]);
+        const __half2 h = __floats2half2_rn(f.x * scale, f.y * scale);
+        w[k] = *(const uint32_t*)&h;
+      }
+      *(uint4*)(out2 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+// Each block takes a range of rows and counts those before it itself: one launch, and the order is kept.
+__global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
+  __shared__ int counted[8], least_of[8];
+  __shared__ int list[ROW_THREADS];
+  pdl_enter();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t r0 = a.rows * blockIdx.x / gridDim.x, r1 = a.rows * (blockIdx.x + 1) / gridDim.x;
+  int before = 0, least = NO_LIFT;
+  const int64_t seen = a.fp16 && a.dloss ? a.rows : r0;
+  for (int64_t i = tid; i < seen; i += ROW_THREADS)
+    if (counts(a, i)) {
+      before += i < r0;
+      if (a.fp16 && a.dloss) {
+        const float b = bound_of(a, i);
+        if (b > 0.f && b < INFINITY) least = min(least, lift(b));
+      }
+    }
+  before = __reduce_add_sync(0xffffffffu, before);
+  least = __reduce_min_sync(0xffffffffu, least);
+  if (lane == 0) { counted[warp] = before; least_of[warp] = least; }
+  __syncthreads();
+  before = 0;
+  for (int i = 0; i < 8; ++i) { before += counted[i]; least = min(least, least_of[i]); }
+  if (least == NO_LIFT) least = 0;
+  for (int64_t base = r0; base < r1; base += ROW_THREADS) {
+    __syncthreads();                   // counted and list are free again
+    const int64_t i = base + tid;
+    const bool live = i < r1 && counts(a, i);
+    const uint32_t votes = __ballot_sync(0xffffffffu, live);
+    if (lane == 0) counted[warp] = __popc(votes);
+    __syncthreads();
+    int at = 0, all = 0;
+    for (int k = 0; k < 8; ++k) { if (k < warp) at += counted[k]; all += counted[k]; }
+    at += __popc(votes & ((1u << lane) - 1u));
+    if (i < r1) {
+      a.pos[i] = live ? before + at : -1;
+      if (live) {
+        const int64_t to = before + at;
+        list[at] = (int)(i - base);
+        a.src[to] = (int32_t)i;
+        if (!a.some) { a.id[i] = (int32_t)whole(a.target, a.id64, i); a.p[i] = a.share; }
+        if (a.dloss) {
+          const int h = a.fp16 ? row_lift(bound_of(a, i), least) : 0;
+          const float g = ldexpf(a.dloss[i] * a.inv_t, h), lse = a.lse[i];
+          a.coef[to] = {lse * LOG2E, g * (1.f + 2.f * a.z_loss * lse), -g * a.smoothing / (float)a.vocab, g};
+          a.row_scale[to] = ldexpf(1.f, -h);
+        }
+      } else if (a.loss) {
+        a.loss[i] = 0.f;
+        a.lse_out[i] = 0.f;
+      }
+    }
+    __syncthreads();
+    for (int k = warp; k < all; k += 8) {
+      const int64_t from = base + list[k];
+      const float scale = a.fp16 && a.dloss ? ldexpf(1.f, least - row_lift(bound_of(a, from), least)) : 1.f;
+      copy_row(a, from, before + k, scale);
+    }
+    before += all;
+  }
+  if (r1 == a.rows && blockIdx.x == gridDim.x - 1) {
+    if (tid == 0) { a.meta->n = before; a.meta->dw_scale = a.fp16 && a.dloss ? ldexpf(1.f, -least) : 1.f; }
+    if (a.dloss)                       // a contraction over the rows takes them 64 at a time
+      for (int64_t r = before + warp; r < (before + BK - 1) / BK * BK; r += 8)
+        for (int c = lane * 8; c < a.dp; c += 256) {
+          *(uint4*)(a.x + r * a.dp + c) = make_uint4(0u, 0u, 0u, 0u);
+          if (a.x_dw != a.x) *(uint4*)(a.x_dw + r * a.dp + c) = make_uint4(0u, 0u, 0u, 0u);
+        }
+  }
+}
+
+// ------------------------------------------------------------------ losses
+struct LossArgs {
+  const Meta* meta; const int32_t* src;
+  const float2* part; const float* part_y; int parts; int64_t rpad;
+  const float* p; const float* y_entry; int top;
+  int distill;
+  float smoothing, z_loss; int64_t vocab;
+  float* loss; float* lse;
+};
+// 32 rows a block, a lane each; the warps share a row's parts and entries
+__global__ void __launch_bounds__(512) k_losses(const LossArgs a) {
+  __shared__ float sm[16][32], ss[16][32], sy[16][32], se[16][32];
+  pdl_enter();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane, n = a.meta->n;
+  if (blockIdx.x * 32 >= n) return;
+  const bool live = row < n;
+  float m = -INFINITY, s = 0.f, y = 0.f, e = 0.f;
+  int64_t src = 0;
+  if (live) {
+    src = a.src[row];
+#pragma unroll 4
+    for (int i = warp; i < a.parts; i += 16) {
+      const float2 q = a.part[(int64_t)i * a.rpad + row];
+      const float most = fmaxf(m, q.x), base = most == -INFINITY ? 0.f : most;
+      s = s * exp2f(m - base) + q.y * exp2f(q.x - base);
+      m = most;
+      if (a.part_y) y += a.part_y[(int64_t)i * a.rpad + row];
+    }
+  }
+  sm[warp][lane] = m; ss[warp][lane] = s; sy[warp][lane] = y;
+  __syncthreads();
+  float most = -INFINITY;
+  for (int i = 0; i < 16; ++i) most = fmaxf(most, sm[i][lane]);
+  const float base = most == -INFINITY ? 0.f : most;
+  s = y = 0.f;
+  for (int i = 0; i < 16; ++i) { s += ss[i][lane] * exp2f(sm[i][lane] - base); y += sy[i][lane]; }
+  const float lse2 = base + log2f(s);
+  if (live)
+    for (int i = warp; i < a.top; i += 16) {
+      const float p = a.p[src * a.top + i];
+      // log p - (y - lse2): close to each other where the student has learnt its teacher
+      if (p > 0.f) e += p * ((a.distill ? log2f(p) : 0.f) - (a.y_entry[src * a.top + i] - lse2));
+      else if (!(p == 0.f)) e = p;
+    }
+  se[warp][lane] = e;
+  __syncthreads();
+  if (warp == 0 && live) {
+    e = 0.f;
+    for (int i = 0; i < 16; ++i) e += se[i][lane];
+    const float lse = lse2 * LN2;
+    if (a.smoothing != 0.f) e += a.smoothing * (lse2 - y / (float)a.vocab);
+    a.loss[src] = e * LN2 + a.z_loss * lse * lse;
+    a.lse[src] = lse;
+  }
+}
+
+// ------------------------------------------------------------------ dX
+// Row i of dX from the sums of its copy, or zeros; a warp per row, four columns a lane.
+template <typename T>
+__global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int64_t rpad, int split, const int32_t* pos, const float* row_scale, const float* sums,
+                                            T* dx, int64_t ld) {
+  pdl_enter();
+  const int lane = threadIdx.x & 31;
+  const bool wide = ((uintptr_t)dx % (4 * sizeof(T))) == 0 && ld % 4 == 0;
+  for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += (int64_t)gridDim.x * 8) {
+    const int at = pos[row];
+    const float f = at >= 0 ? row_scale[at] : 0.f;
+    const float* in = sums + (int64_t)(at >= 0 ? at : 0) * dp;
+    T* out = dx + row * ld;
+    for (int c = lane * 4; c < d; c += 128) {
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (at >= 0) {
+        v = *(const float4*)(in + c);
+        for (int s = 1; s < split; ++s) {
+          const float4 w = *(const float4*)(in + (int64_t)s * rpad * dp + c);
+          v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
+        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+      }
+      if (wide && c + 4 <= d) {
+        alignas(16) T o[4] = {from_f<T>(v.x), from_f<T>(v.y), from_f<T>(v.z), from_f<T>(v.w)};
+        if constexpr (sizeof(T) == 4) *(float4*)(out + c) = *(const float4*)o;
+        else *(uint2*)(out + c) = *(const uint2*)o;
+      } else {
+        const float o[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (c + k < d) out[c + k] = from_f<T>(o[k]);
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) k_zero_rows(int64_t rows, int d, unsigned char* p, int64_t ld, int bytes) {
+  pdl_enter();
+  for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += (int64_t)gridDim.x * 8)
+    for (int64_t c = threadIdx.x & 31; c < d; c += 32) {
+      if (bytes == 4) ((float*)p)[row * ld + c] = 0.f;
+      else ((uint16_t*)p)[row * ld + c] = 0;
+    }
+}
+
+// ------------------------------------------------------------------ host side
+static int64_t round_up(int64_t v, int64_t m) { return (v + m - 1) / m * m; }
+
+struct Call {
+  const betty_vocab_cfg* cfg;
+  int64_t rows;
+  const void* X; int64_t ldx;
+  const void* W; int64_t ldw;
+  const void* target; int32_t id_dtype;
+  int top; int64_t ldi;                        // distillation: top >= 1, else 0
+  const void* teacher; int64_t ldt; int32_t teacher_dtype;
+  float* loss; float* lse_out;                 // forward
+  const float* lse; const float* dloss;        // backward
+  void* dX; int64_t lddx; int32_t dx_dtype;
+  void* dW; int64_t lddw; int32_t dw_dtype;
+  bool backward;
+};
+
+static betty_status check_cfg(const betty_vocab_cfg* c, int64_t rows, int64_t top) {
+  if (!c || rows < 0) return BETTY_ERR_INVALID_ARG;
+  if (c->dtype != BETTY_BF16 && c->dtype != BETTY_F16) return BETTY_ERR_DTYPE;
+  if (c->vocab < 1 || c->d < 1 || top < 0) return BETTY_ERR_SHAPE;
+  // 32-bit tile counts and coordinates
+  if (c->vocab > (1 << 22) || c->d > (1 << 16) || rows > (1 << 22) || top > MAX_TOP) return BETTY_ERR_UNSUPPORTED;
+  if (!(c->temperature > 0.f) || !(c->temperature <= 1e30f) || !(c->temperature >= 1e-30f)) return BETTY_ERR_INVALID_ARG;
+  if (!(c->smoothing >= 0.f) || !(c->smoothing <= 1.f) || !(c->z_loss >= 0.f) || !(c->z_loss <= 1e30f)) return BETTY_ERR_INVALID_ARG;
+  return BETTY_OK;
+}
+static betty_status check_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols, int64_t bytes) {
+  if (!p) return BETTY_ERR_INVALID_ARG;
+  if (rows > 1 && ld < cols) return BETTY_ERR_SHAPE;
+  if (ld > ((int64_t)1 << 32)) return BETTY_ERR_UNSUPPORTED;      // 40-bit strides of tensor maps
+  return (uintptr_t)p % bytes ? BETTY_ERR_ALIGNMENT : BETTY_OK;
+}
+static int64_t float_bytes(int dtype) { return dtype == BETTY_F32 ? 4 : (dtype == BETTY_BF16 || dtype == BETTY_F16 ? 2 : 0); }
+
+static betty_status check(const Call& c, void* ws, size_t ws_bytes) {
+  BETTY_TRY(check_cfg(c.cfg, c.rows, c.top));
+  const bool distill = c.teacher_dtype >= 0;
+  if (distill && c.top < 1) return BETTY_ERR_SHAPE;
+  if (distill && (c.cfg->smoothing != 0.f || c.cfg->z_loss != 0.f)) return BETTY_ERR_UNSUPPORTED;
+  if (c.id_dtype != BETTY_I32 && c.id_dtype != BETTY_I64) return BETTY_ERR_DTYPE;
+  if (distill && !float_bytes(c.teacher_dtype)) return BETTY_ERR_DTYPE;
+  if (c.backward) {
+    if (!c.dX && !c.dW) return BETTY_ERR_INVALID_ARG;
+    if (c.dX && c.dx_dtype != BETTY_F32 && c.dx_dtype != c.cfg->dtype) return BETTY_ERR_DTYPE;
+    if (c.dW && c.dw_dtype != BETTY_F32 && c.dw_dtype != c.cfg->dtype) return BETTY_ERR_DTYPE;
+  }
+  if (!ws || ws_bytes < sizeof(StatusBlock) || (((uintptr_t)ws) & 255u)) return BETTY_ERR_WORKSPACE;
+  if (c.dW) BETTY_TRY(check_matrix(c.dW, c.lddw, c.cfg->vocab, c.cfg->d, float_bytes(c.dw_dtype)));
+  if (c.rows == 0) return BETTY_OK;
+  BETTY_TRY(check_matrix(c.X, c.ldx, c.rows, c.cfg->d, 2));
+  BETTY_TRY(check_matrix(c.W, c.ldw, c.cfg->vocab, c.cfg->d, 2));
+  if (c.dX) BETTY_TRY(check_matrix(c.dX, c.lddx, c.rows, c.cfg->d, float_bytes(c.dx_dtype)));
+  const int64_t ib = c.id_dtype == BETTY_I64 ? 8 : 4;
+  if (distill) {
+    BETTY_TRY(check_matrix(c.target, c.ldi, c.rows, c.top, ib));
+    BETTY_TRY(check_matrix(c.teacher, c.ldt, c.rows, c.top, float_bytes(c.teacher_dtype)));
+  } else {
+    BETTY_TRY(check_matrix(c.target, 1, 1, 1, ib));
+  }
+  const float* vectors[4] = {c.backward ? c.lse : c.loss, c.backward ? c.dloss : c.lse_out, nullptr, nullptr};
+  for (int i = 0; i < 2; ++i) BETTY_TRY(check_matrix(vectors[i], 1, 1, 1, 4));
+  return BETTY_OK;
+}
+
+static Shape shape_of(const betty_vocab_cfg* c, int64_t rows, int top, bool backward, bool dx, bool dw) {
+  Shape s = {};
+  s.dtype = c->dtype; s.rows = (int)rows; s.rpad = round_up(rows < 1 ? 1 : rows, 256);
+  s.vocab = (int)c->vocab; s.d = (int)c->d; s.dp = round_up(c->d, 64);
+  s.c2 = LOG2E / c->temperature;
+  s.top = top < 1 ? 1 : top;
+  choose_shape(s, backward, dx, dw);
+  return s;
+}
+
+// The call's arrays; with an empty arena: only their size.
+static betty_status lay_out(Arena& arena, const Shape& s, const Call& c, Buffers& b, uint8_t*& some) {
+  const bool distill = c.teacher_dtype >= 0;
+  b.sb = arena.status();
+  b.meta = arena.alloc<Meta>(1);
+  b.src = arena.alloc<int32_t>((size_t)s.rpad);
+  b.pos = arena.alloc<int32_t>((size_t)c.rows);
+  b.id = arena.alloc<int32_t>((size_t)(c.rows * s.top));
+  b.p = arena.alloc<float>((size_t)(c.rows * s.top));
+  some = distill ? arena.alloc<uint8_t>((size_t)c.rows) : nullptr;
+  b.x = b.x_dw = arena.alloc<uint16_t>((size_t)(s.rpad * s.dp));
+  b.part = nullptr; b.part_y = b.y_entry = nullptr; b.coef = nullptr; b.row_scale = nullptr; b.dz = nullptr; b.dx = nullptr;
+  if (!c.backward) {
+    const int64_t parts = logits_parts(s);
+    b.part = arena.alloc<float2>((size_t)(parts * s.rpad));
+    if (c.cfg->smoothing != 0.f) b.part_y = arena.alloc<float>((size_t)(parts * s.rpad));
+    b.y_entry = arena.alloc<float>((size_t)(c.rows * s.top));
+  } else {
+    b.coef = arena.alloc<RowCoef>((size_t)s.rpad);
+    b.row_scale = arena.alloc<float>((size_t)s.rpad);
+    b.dz = arena.alloc<uint16_t>((size_t)(s.rpad * s.piece));
+    if (c.dX) b.dx = arena.alloc<float>((size_t)(s.split * s.rpad * s.dp));
+    if (c.dW && s.dtype == BETTY_F16) b.x_dw = arena.alloc<uint16_t>((size_t)(s.rpad * s.dp));
+  }
+  return arena.overflow ? BETTY_ERR_WORKSPACE : BETTY_OK;
+}
+
+static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* stream_) {
+  BETTY_TRY(check(c, ws, ws_bytes));
+  const cudaStream_t stream = (cudaStream_t)stream_;
+  const betty_vocab_cfg* cfg = c.cfg;
+  const int64_t most = (int64_t)current_sm_count() * 4;
+  if (c.rows == 0) {
+    if (!c.dW) return BETTY_OK;
+    launch_pdl(k_zero_rows, dim3((unsigned)most), dim3(256), 0, stream, cfg->vocab, (int)cfg->d, (unsigned char*)c.dW, c.lddw, c.dw_dtype == BETTY_F32 ? 4 : 2);
+    BETTY_LAUNCH_CHECK();
+    return BETTY_OK;
+  }
+  const bool distill = c.teacher_dtype >= 0;
+  const Shape s = shape_of(cfg, c.rows, c.top, c.backward, c.dX != nullptr, c.dW != nullptr);
+  Arena arena(ws, ws_bytes);
+  Buffers b = {};
+  uint8_t* some;
+  BETTY_TRY(lay_out(arena, s, c, b, some));
+  Operand w = {c.W, cfg->d, cfg->vocab, 1, c.ldw, 0};
+  BETTY_TRY(align_operand(stream, arena, w));
+
+  if (distill) {
+    int padded = 2;
+    while (padded < c.top) padded *= 2;
+    const int threads = padded / 2 < 32 ? 32 : padded / 2;
+    launch_pdl(k_entries, dim3((unsigned)c.rows), dim3((unsigned)threads), (size_t)padded * 12, stream, c.target, c.ldi, (int)(c.id_dtype == BETTY_I64), c.teacher, c.ldt,
+               (int)c.teacher_dtype, c.top, padded, 1.f / cfg->temperature, cfg->vocab, (int32_t*)b.id, (float*)b.p, some);
+    BETTY_LAUNCH_CHECK();
+  }
+  RowArgs r = {};
+  r.rows = c.rows; r.vocab = cfg->vocab; r.d = (int)cfg->d; r.dp = s.dp; r.ldx = c.ldx; r.x_in = (const uint16_t*)c.X;
+  r.target = distill ? nullptr : c.target; r.id64 = c.id_dtype == BETTY_I64; r.share = 1.f - cfg->smoothing; r.some = some;
+  r.id = (int32_t*)b.id; r.p = (float*)b.p;
+  r.meta = b.meta; r.src = b.src; r.pos = b.pos; r.x = b.x; r.x_dw = b.x_dw;
+  r.loss = c.backward ? nullptr : c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.backward ? c.dloss : nullptr;
+  r.coef = b.coef; r.row_scale = b.row_scale;
+  r.inv_t = 1.f / cfg->temperature; r.z_loss = cfg->z_loss; r.smoothing = cfg->smoothing; r.fp16 = cfg->dtype == BETTY_F16;
+  const int64_t blocks = (c.rows + 7) / 8;
+  launch_pdl(k_rows, dim3((unsigned)(blocks < most ? blocks : most)), dim3(ROW_THREADS), 0, stream, r);
+  BETTY_LAUNCH_CHECK();
+
+  if (!c.backward) {
+    BETTY_TRY(logits_statistics(stream, s, b, w));
+    LossArgs l = {};
+    l.meta = b.meta; l.src = b.src; l.part = b.part; l.part_y = b.part_y; l.parts = logits_parts(s); l.rpad = s.rpad;
+    l.p = b.p; l.y_entry = b.y_entry; l.top = s.top; l.distill = distill;
+    l.smoothing = cfg->smoothing; l.z_loss = cfg->z_loss; l.vocab = cfg->vocab; l.loss = c.loss; l.lse = c.lse_out;
+    launch_pdl(k_losses, dim3((unsigned)((c.rows + 31) / 32)), dim3(512), 0, stream, l);
+    BETTY_LAUNCH_CHECK();
+    return BETTY_OK;
+  }
+  BETTY_TRY(logits_gradients(stream, s, b, w, c.dX != nullptr, c.dW, c.lddw, c.dw_dtype));
+  if (c.dX) {
+    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    if (c.dx_dtype == BETTY_F32)
+      launch_pdl(k_dx<float>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, s.rpad, s.split, b.pos, b.row_scale, b.dx, (float*)c.dX, c.lddx);
+    else if (c.dx_dtype == BETTY_BF16)
+      launch_pdl(k_dx<__nv_bfloat16>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, s.rpad, s.split, b.pos, b.row_scale, b.dx, (__nv_bfloat16*)c.dX, c.lddx);
+    else
+      launch_pdl(k_dx<__half>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, s.rpad, s.split, b.pos, b.row_scale, b.dx, (__half*)c.dX, c.lddx);
+    BETTY_LAUNCH_CHECK();
+  }
+  return BETTY_OK;
+}
+
+// What any call on up to `rows` rows needs.  The tiles go by the number of 128-row tiles: a call on fewer rows can need more than one
+// on all of them.
+static size_t workspace_bytes(const betty_vocab_cfg* cfg, int64_t rows, int top, bool any_layout) {
+  size_t most = 0;
+  for (int64_t tiles = 1; tiles <= (rows < 1 ? 1 : (rows + 127) / 128); ++tiles)
+    for (int form = 0; form < 4; ++form) {       // forward; gradients of x and W, of x, of W
+      Call c = {};
+      c.cfg = cfg; c.rows = rows < tiles * 128 ? rows : tiles * 128; c.top = top; c.teacher_dtype = top > 0 ? BETTY_F32 : -1;
+      c.backward = form > 0;
+      c.dX = form == 1 || form == 2 ? &c : nullptr;
+      c.dW = form == 1 || form == 3 ? &c : nullptr;
+      Arena arena((void*)256, SIZE_MAX / 2);
+      Buffers b = {};
+      uint8_t* some;
+      (void)lay_out(arena, shape_of(cfg, c.rows, top, c.backward, c.dX != nullptr, c.dW != nullptr), c, b, some);
+      if (arena.off > most) most = arena.off;
+    }
+  return most + (any_layout ? 256 + (size_t)(cfg->vocab * pad8(cfg->d)) * 2 : 0);
+}
+
+}  // namespace vocab
+}  // namespace betty
+
+using namespace betty;
+
+extern "C" betty_status betty_vocab_workspace_size(const betty_vocab_cfg* cfg, int64_t rows, int32_t top, int32_t any_layout, size_t* bytes) {
+  if (!bytes) return BETTY_ERR_INVALID_ARG;
+  BETTY_TRY(vocab::check_cfg(cfg, rows, top));
+  *bytes = vocab::workspace_bytes(cfg, rows, top, any_layout != 0);
+  return BETTY_OK;
+}
+
+extern "C" betty_status betty_vocab_ce(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw, const void* target,
+                                       int32_t target_dtype, float* loss, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  vocab::Call c = {};
+  c.cfg = cfg; c.rows = rows; c.X = X; c.ldx = ldx; c.W = W; c.ldw = ldw; c.target = target; c.id_dtype = target_dtype; c.teacher_dtype = -1;
+  c.loss = loss; c.lse_out = lse;
+  return vocab::evaluate(c, ws, ws_bytes, stream);
+}
+
+extern "C" betty_status betty_vocab_ce_backward(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                                const void* target, int32_t target_dtype, const float* lse, const float* dloss, void* dX, int64_t lddx,
+                                                int32_t dx_dtype, void* dW, int64_t lddw, int32_t dw_dtype, void* ws, size_t ws_bytes, void* stream) {
+  vocab::Call c = {};
+  c.cfg = cfg; c.rows = rows; c.X = X; c.ldx = ldx; c.W = W; c.ldw = ldw; c.target = target; c.id_dtype = target_dtype; c.teacher_dtype = -1;
+  c.lse = lse; c.dloss = dloss; c.dX = dX; c.lddx = lddx; c.dx_dtype = dx_dtype; c.dW = dW; c.lddw = lddw; c.dw_dtype = dw_dtype; c.backward = true;
+  return vocab::evaluate(c, ws, ws_bytes, stream);
+}
+
+extern "C" betty_status betty_vocab_distill(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw, int32_t top,
+                                            const void* ids, int64_t ldi, int32_t id_dtype, const void* teacher, int64_t ldt, int32_t teacher_dtype,
+                                            float* loss, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  vocab::Call c = {};
+  if (teacher_dtype < 0) return BETTY_ERR_DTYPE;
+  c.cfg = cfg; c.rows = rows; c.X = X; c.ldx = ldx; c.W = W; c.ldw = ldw; c.target = ids; c.id_dtype = id_dtype; c.top = top; c.ldi = ldi;
+  c.teacher = teacher; c.ldt = ldt; c.teacher_dtype = teacher_dtype; c.loss = loss; c.lse_out = lse;
+  return vocab::evaluate(c, ws, ws_bytes, stream);
+}
+
+extern "C" betty_status betty_vocab_distill_backward(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                                     int32_t top, const void* ids, int64_t ldi, int32_t id_dtype, const void* teacher, int64_t ldt,
+                                                     int32_t teacher_dtype, const float* lse, const float* dloss, void* dX, int64_t lddx, int32_t dx_dtype,
+                                                     void* dW, int64_t lddw, int32_t dw_dtype, void* ws, size_t ws_bytes, void* stream) {
+  vocab::Call c = {};
+  if (teacher_dtype < 0) return BETTY_ERR_DTYPE;
+  c.cfg = cfg; c.rows = rows; c.X = X; c.ldx = ldx; c.W = W; c.ldw = ldw; c.target = ids; c.id_dtype = id_dtype; c.top = top; c.ldi = ldi;
+  c.teacher = teacher; c.ldt = ldt; c.teacher_dtype = teacher_dtype; c.lse = lse; c.dloss = dloss;
+  c.dX = dX; c.lddx = lddx; c.dx_dtype = dx_dtype; c.dW = dW; c.lddw = lddw; c.dw_dtype = dw_dtype; c.backward = true;
+  return vocab::evaluate(c, ws, ws_bytes, stream);
+}

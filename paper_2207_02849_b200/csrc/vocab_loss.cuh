@@ -1,0 +1,73 @@
+// Losses of a language model over its vocabulary (vocab_loss.cu: rows, statistics and the C entries; vocab_products.cu: the
+// matrix products).
+//
+//   z_iv = x_i . w_v / T,   lse_i = log sum_v exp z_iv,   q_iv = exp(z_iv - lse_i)
+//   cross entropy   l_i = (1 - e) (lse_i - z_it) + e (lse_i - mean_v z_iv) + zeta lse_i^2
+//   distillation    l_i = sum_j p_ij (log p_ij - z_i,id(j) + lse_i),   p_i = softmax of the teacher's entries / T
+//   both            dl_i/dz_iv = a q_iv + b - sum over the row's entries at v of p,   a = 1 + 2 zeta lse_i, b = -e / V
+//                   dx_i = (g_i / T) sum_v dz_iv w_v,   dw_v = sum_i (g_i / T) dz_iv x_i
+//
+// The entries of a row are (id, p) pairs in ascending order of id: one, (t, 1 - e), of a cross entropy.  Rows that do not
+// count (and, in a backward pass, rows with g = 0) are left out before the products: the others are copied one after the
+// other into the workspace, on 16-byte boundaries, so that what a row left out holds reaches nothing and costs nothing, and
+// the host needs no count.  Logarithms and exponentials are taken to the base 2: y = z log2(e), lse2 = lse log2(e).
+#pragma once
+#include "tensor_core.cuh"
+
+namespace betty {
+namespace vocab {
+
+static constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+static constexpr int MAX_TOP = 1024;
+static constexpr int NO_ID = 0x7FFFFFFF;       // an entry that is none
+
+struct RowCoef { float lse2, a, b, e; };       // dz = a 2^(y - lse2) + b - e p, as it is stored for the products
+struct Meta {
+  int32_t n;             // rows that count
+  float dw_scale;        // what a sum over the stored dz and x is multiplied by to give dW
+};
+
+// What the products need to know of one call.
+struct Shape {
+  int dtype;             // operands
+  int rows;              // upper bound of the rows that count
+  int64_t rpad;          // rows of the workspace's matrices, a multiple of 256
+  int vocab, d;
+  int64_t dp;            // d rounded up to a multiple of 64: leading dimension of the workspace's copies of x
+  float c2;              // log2(e) / T
+  int top;               // entries of a row
+  int pairs;             // logits: pairs of SMs take tiles of 256 x 256, else an SM takes 128 x width
+  int width;
+  int product_pairs;     // gradients: the same choice
+  int piece;             // columns of the vocabulary at a time (backward), a multiple of 256
+  int split;             // parts of the contraction of dX
+};
+
+struct Buffers {
+  Meta* meta;
+  int32_t* src;          // [rpad] row of the caller's that row i of the copies is
+  int32_t* pos;          // [rows] where a row went, -1: left out
+  uint16_t* x;           // [rpad, dp]
+  uint16_t* x_dw;        // [rpad, dp] as the gradient of W takes it (fp16: scaled, else x itself)
+  const int32_t* id;     // [rows, top] entries
+  const float* p;
+  float2* part;          // [parts][rpad] maximum and sum of 2^(y - maximum) of a part of a row
+  float* part_y;         // [parts][rpad] sum of y (smoothing only)
+  float* y_entry;        // [rows, top] y at the entries
+  RowCoef* coef;         // [rpad]
+  float* row_scale;      // [rpad] what a row of dX is multiplied by
+  uint16_t* dz;          // [rpad, piece]
+  float* dx;             // [split][rpad, dp]
+  StatusBlock* sb;
+};
+
+int logits_parts(const Shape& s);
+// part, part_y (if not null) and y_entry of all rows that count
+betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w);
+// dX's fp32 sums (want_dx) and dW (dw not null), piece by piece
+betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, bool want_dx, void* dw, int64_t lddw,
+                              int dw_dtype);
+void choose_shape(Shape& s, bool backward, bool want_dx, bool want_dw);
+
+}  // namespace vocab
+}  // namespace betty

@@ -1,0 +1,715 @@
+// The matrix products of the losses over a vocabulary: the logits, whose accumulators are turned into a row's statistics or
+// into its gradient's coefficients before they leave the SM, and the two products of the gradients.
+//
+//   statistics   z = X W^T tile by tile; per row and half tile: max y, sum 2^(y - max), y at the row's entries
+//   gradient     z again, dz = a 2^(y - lse2) + b - e p, rounded to the operands' type: a piece of the vocabulary at a time
+//   products     dX += dz W over the piece's columns, dW = dz^T X over the rows; one launch for both
+//
+// An accumulator holds rows of the batch in its lanes and columns of the vocabulary, so a thread owns a row and its softmax
+// statistics need no exchange.
+#include "vocab_loss.cuh"
+
+namespace betty {
+namespace vocab {
+using namespace tc;
+
+enum Mode { STATS = 0, GRAD = 1, PRODUCTS = 2 };
+
+static constexpr int THREADS = 320;           // warp 0: TMA, warp 1: MMA, warps 2-9: epilogue
+static constexpr int EPI_WARPS = 8;
+static constexpr int STAGING = EPI_WARPS * 4096;   // each epilogue warp: 32 rows of 128 bytes
+
+template <int CG, int NT, int MODE> struct Cfg {
+  static constexpr int STAGE = A_BYTES + NT / CG * BK * 2;
+  static constexpr int OUT = MODE == STATS || (MODE == GRAD && CG == 1) ? 0 : STAGING;
+  static constexpr int STAGES = (229376 - OUT) / STAGE;
+  static constexpr int SMEM = STAGES * STAGE + OUT + 256 + 1024;
+  static constexpr int TMEM_COLS = 2 * NT;    // two accumulators: a tile drains while the next is multiplied
+  static_assert(SMEM <= 227 * 1024 && NT / CG <= 128 && STAGES * 16 + 48 <= 256, "shared memory");
+};
+
+struct alignas(64) Maps { CUtensorMap m[6]; };
+// logits: operands by rows
+enum { M_X = 0, M_W = 1, M_DZ_OUT = 2 };
+// products: dz by rows and by blocks of columns, W and X by blocks of columns, the results
+enum { M_DZ = 0, M_DZ_T = 1, M_W_T = 2, M_X_T = 3, M_DX = 4, M_DW = 5 };
+
+struct Args {
+  const Meta* meta;
+  StatusBlock* sb;
+  uint32_t type_bits;      // operand format bits of the instruction descriptor
+  uint32_t a_bytes, b_bytes;   // bytes of the copies of A (by rows) and B of one CTA and chunk
+  int col0, cols;          // the piece of the vocabulary: first column, columns
+  int d;
+  int64_t rpad;
+  // logits
+  int width, band;         // columns of a tile; row tiles that are taken together
+  float c2;
+  int top;
+  const int32_t* src; const int32_t* id; const float* p;
+  float2* part; float* part_y; float* y_entry;
+  const RowCoef* coef;
+  uint16_t* dz; int64_t ldz;
+  // products
+  int want_dx, want_dw, split, add;   // add: dX's sums already hold the pieces before
+  int w_blocked, dw_tma;
+  void* dw; int64_t lddw;
+};
+
+// ------------------------------------------------------------------ tiles
+struct Tile {
+  int trans;               // A is dz^T
+  int l0, c0;              // first lane (row, or column of the piece), first column (of the piece, or of d)
+  int k0, chunks;          // contraction
+  int part;                // split of dX's contraction, or column tile of the logits
+};
+struct Counts { int row_tiles, col_tiles, d_tiles, dx_tiles, tiles; };
+
+template <int CG, int NT, int MODE>
+__device__ __forceinline__ Counts count_tiles(const Args& a, int n) {
+  Counts c;
+  c.row_tiles = (n + BM * CG - 1) / (BM * CG);
+  if (MODE != PRODUCTS) {
+    c.col_tiles = (a.cols + a.width - 1) / a.width;
+    c.d_tiles = c.dx_tiles = 0;
+    c.tiles = c.row_tiles * c.col_tiles;
+  } else {
+    c.col_tiles = (a.cols + BM * CG - 1) / (BM * CG);
+    c.d_tiles = (a.d + NT - 1) / NT;
+    c.dx_tiles = a.want_dx ? c.row_tiles * c.d_tiles * a.split : 0;
+    c.tiles = c.dx_tiles + (a.want_dw ? c.col_tiles * c.d_tiles : 0);
+  }
+  return c;
+}
+template <int CG, int NT, int MODE>
+__device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, int t) {
+  Tile r;
+  if (MODE != PRODUCTS) {
+    const int per = a.band * c.col_tiles, band = t / per, in = t - band * per, height = min(a.band, c.row_tiles - band * a.band);
+    r.trans = 0;
+    r.part = in / height;
+    r.l0 = (band * a.band + in - r.part * height) * (BM * CG);
+    r.c0 = r.part * a.width;
+    r.k0 = 0;
+    r.chunks = (a.d + BK - 1) / BK;
+  } else if (t < c.dx_tiles) {
+    const int rest = t / c.d_tiles, chunks = (a.cols + BK - 1) / BK;
+    r.trans = 0;
+    r.c0 = (t - rest * c.d_tiles) * NT;
+    r.part = rest % a.split;
+    r.l0 = rest / a.split * (BM * CG);
+    const int k = (int)((int64_t)r.part * chunks / a.split);
+    r.k0 = k * BK;
+    r.chunks = (int)((int64_t)(r.part + 1) * chunks / a.split) - k;
+  } else {
+    t -= c.dx_tiles;
+    const int rest = t / c.d_tiles;
+    r.trans = 1;
+    r.c0 = (t - rest * c.d_tiles) * NT;
+    r.part = 0;
+    r.l0 = rest * (BM * CG);
+    r.k0 = 0;
+    r.chunks = (n + BK - 1) / BK;
+  }
+  return r;
+}
+
+// ------------------------------------------------------------------ epilogues
+// A row's entries in ascending order of id, from the first at or behind a column.
+struct Walk {
+  const int32_t* id;
+  int at, end, next;
+  __device__ __forceinline__ void start(const int32_t* ids, int top, int column) {
+    id = ids; end = top;
+    int lo = 0, hi = top;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (id[mid] < column) lo = mid + 1; else hi = mid;
+    }
+    at = lo;
+    next = at < end ? id[at] : NO_ID;
+  }
+  __device__ __forceinline__ void none() { id = nullptr; at = end = 0; next = NO_ID; }
+  __device__ __forceinline__ void step() { ++at; next = at < end ? id[at] : NO_ID; }
+};
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *(const uint32_t*)&v;
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *(const uint32_t*)&v;
+}
+
+__device__ __forceinline__ void store_2d(const CUtensorMap* tm, uint32_t from, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(from), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void add_2d(const CUtensorMap* tm, uint32_t from, int x, int y) {
+  asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(from), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// 16 bytes of a row of 128 in the layout of a 128-byte swizzle
+__device__ __forceinline__ void stage16(uint32_t rows, int row, int j, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(rows + (uint32_t)(row * 128 + ((j ^ (row & 7)) << 4))), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// Columns [from, to) of a tile (its accumulator at `acc`, its first column of the vocabulary `c0`) to a row's statistics.
+__device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, int from, int to, int limit, int row, bool live, float2* part, float* part_y) {
+  Walk w;
+  const int64_t entries = live ? (int64_t)a.src[row] * a.top : 0;
+  if (live) w.start(a.id + entries, a.top, c0 + from); else w.none();
+  float m = -INFINITY, s = 0.f, sum = 0.f;
+#pragma unroll 1
+  for (int c = from; c < to; c += 32) {
+    uint32_t v[32];
+    tmem_load32(v, acc + (uint32_t)c);
+    const int cb = c0 + c, end = min(min(cb + 32, c0 + to), limit);     // columns that exist
+    if (end < cb + 32) {
+#pragma unroll
+      for (int k = 0; k < 32; ++k)
+        if (cb + k >= end) v[k] = __float_as_uint(-INFINITY);
+    }
+    float top[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top[k] = __uint_as_float(v[k]);
+#pragma unroll
+    for (int k = 4; k < 32; ++k) top[k & 3] = fmaxf(top[k & 3], __uint_as_float(v[k]));
+    const float most = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.c2);
+    const float base = most == -INFINITY ? 0.f : most;
+    float e[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 32; ++k) e[k & 3] += exp2f(fmaf(__uint_as_float(v[k]), a.c2, -base));
+    s = fmaf(s, exp2f(m - base), (e[0] + e[1]) + (e[2] + e[3]));
+    m = most;
+    if (part_y) {
+      float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 32; ++k) y[k & 3] += cb + k < end ? __uint_as_float(v[k]) : 0.f;
+      sum += (y[0] + y[1]) + (y[2] + y[3]);
+    }
+    while (__any_sync(0xffffffffu, w.next < end)) {
+      float z = 0.f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k)
+        if (w.next - cb == k) z = __uint_as_float(v[k]);
+      if (w.next < end) {
+        a.y_entry[entries + w.at] = z * a.c2;
+        w.step();
+      }
+    }
+  }
+  if (live) {
+    *part = make_float2(m, s);
+    if (part_y) *part_y = sum * a.c2;
+  }
+}
+
+// 32 columns of a tile as coefficients of a row's gradient, packed in pairs; rows that do not count and columns that do not exist: 0
+template <typename T>
+__device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb, int end, bool live, const RowCoef& rc, const float* p, Walk& w, uint32_t (&out)[16]) {
+  uint32_t v[32];
+  tmem_load32(v, acc);
+#pragma unroll
+  for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(fmaf(rc.a, exp2f(fmaf(__uint_as_float(v[k]), a.c2, -rc.lse2)), rc.b));
+  while (__any_sync(0xffffffffu, w.next < end)) {
+    float e = 0.f;
+    if (w.next < end) e = rc.e * p[w.at];
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (w.next - cb == k) v[k] = __float_as_uint(__uint_as_float(v[k]) - e);
+    if (w.next < end) w.step();
+  }
+  if (end < cb + 32 || !live) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (cb + k >= end || !live) v[k] = 0u;
+  }
+#pragma unroll
+  for (int k = 0; k < 16; ++k) out[k] = pack2<T>(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
+}
+
+template <typename T> struct IsF32 { static constexpr bool value = false; };
+template <> struct IsF32<float> { static constexpr bool value = true; };
+
+// CG = 2: a pair of CTAs (a cluster of two) shares a tile of 256 lanes; each stages its own lanes of A and half of the
+// columns of B, the even CTA issues the products, both hold the accumulator rows of their own lanes.
+// T: the operands' type (logits' coefficients); TO: dW's type (products)
+template <int CG, int NT, int MODE, typename T, typename TO>
+__device__ __forceinline__ void body(const Maps& tm, const Args& a) {
+  using C = Cfg<CG, NT, MODE>;
+  constexpr int S = C::STAGES;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char* staging = smem + S * C::STAGE;
+  uint64_t* full = (uint64_t*)(staging + C::OUT);
+  uint64_t* empty = full + S;
+  uint64_t* acc_full = empty + S;
+  uint64_t* acc_empty = acc_full + 2;
+  uint32_t* tmem_slot = (uint32_t*)(acc_empty + 2);
+  volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+
+  const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+  uint32_t rank = 0;
+  if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+
+  if (tid == 0) {
+    for (int s = 0; s < S; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_empty[s], CG * EPI_WARPS); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    for (int i = 0; i < (MODE == PRODUCTS ? 6 : 3); ++i) prefetch_map(&tm.m[i]);
+  }
+  if (warp == 0) {
+    if (CG == 1) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_u32(tmem_slot)), "r"(C::TMEM_COLS) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s_u32(tmem_slot)), "r"(C::TMEM_COLS) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+  }
+  pdl_enter();             // global memory is touched from here on
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();     // the other's barriers exist before anything is signalled across the cluster
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = *tmem_slot;
+  const int n = uniform(a.meta->n);
+  const Counts count = count_tiles<CG, NT, MODE>(a, n);
+
+  // The loading and the multiplying warp run their loops with all lanes, and one lane issues (see grouped.cu).
+  if (warp == 0) {
+    // ---------------- producer
+    const bool leader = elect_one();
+    const uint32_t full0 = CG == 2 ? in_cta(s_u32(full), 0) : s_u32(full);
+    int s = 0;
+    uint32_t round = 0;
+    bool ok = true;
+    for (int t = worker; t < count.tiles && ok; t += workers) {
+      const Tile r = tile_at<CG, NT, MODE>(a, count, n, t);
+      const int trans = uniform(r.trans), chunks = uniform(r.chunks), k0 = uniform(r.k0);
+      const int l = uniform(r.l0) + (int)rank * BM;
+      const int c = MODE == PRODUCTS ? uniform(r.c0) + (int)rank * (NT / CG) : a.col0 + uniform(r.c0) + (int)rank * (a.width / CG);
+      const uint32_t bytes = CG * ((trans ? (uint32_t)A_BYTES : a.a_bytes) + a.b_bytes);
+      for (int it = 0; it < chunks; ++it) {
+        if (round && !__all_sync(0xffffffffu, wait(&empty[s], (round - 1) & 1u, abort_flag))) { ok = false; break; }
+        unsigned char* sa = smem + s * C::STAGE;
+        unsigned char* sb = sa + A_BYTES;
+        const uint32_t bar = full0 + 8u * (uint32_t)s;
+        const int k = k0 + it * BK;
+        if (leader) {
+          if (rank == 0) expect_tx(&full[s], bytes);
+          if (MODE != PRODUCTS) {
+            load_2d<CG>(sa, &tm.m[M_X], k, l, bar);
+            load_2d<CG>(sb, &tm.m[M_W], k, c, bar);
+          } else if (trans) {
+            load_3d<CG>(sa, &tm.m[M_DZ_T], 0, k, l / 64, bar);
+            load_3d<CG>(sb, &tm.m[M_X_T], 0, k, c / 64, bar);
+          } else {
+            load_2d<CG>(sa, &tm.m[M_DZ], k, l, bar);
+            if (a.w_blocked) {
+              load_3d<CG>(sb, &tm.m[M_W_T], 0, a.col0 + k, c / 64, bar);
+            } else {
+              load_2d<CG>(sb, &tm.m[M_W_T], c, a.col0 + k, bar);
+              load_2d<CG>(sb + 8192, &tm.m[M_W_T], c + 64, a.col0 + k, bar);
+            }
+          }
+        }
+        __syncwarp();
+        if (++s == S) { s = 0; ++round; }
+      }
+    }
+    if (*abort_flag)       // copies already issued land in a few microseconds; shared memory must outlive them
+      for (int i = 0; i < 64; ++i) __nanosleep(20000);
+  } else if (warp == 1 && rank == 0) {
+    // ---------------- MMA issuer (of a pair: the even CTA)
+    // K-major: 16 values are 32 bytes further along the swizzled row; 8-row groups 1024 bytes apart.  MN-major: 16
+    // contraction rows are 2048 bytes further; 64-value blocks along the other dimension 8192 bytes apart.
+    const bool leader = elect_one();
+    const uint32_t sa0 = s_u32(smem), sb0 = sa0 + A_BYTES;
+    const uint64_t a_rows = smem_desc(sa0, 16, 1024), a_cols = smem_desc(sa0, 8192, 1024);
+    const uint64_t b0 = MODE == PRODUCTS ? smem_desc(sb0, 8192, 1024) : smem_desc(sb0, 16, 1024);
+    constexpr uint32_t b_step = MODE == PRODUCTS ? 2048 >> 4 : 32 >> 4;
+    const uint32_t fixed = 1u << 4 | a.type_bits | (MODE == PRODUCTS ? 1u << 16 : 0u) | (uint32_t)(BM * CG / 16) << 24 |
+                           (uint32_t)((MODE == PRODUCTS ? NT : a.width) >> 3) << 17;
+    const uint32_t tmem_u = (uint32_t)uniform((int)tmem_base);
+    int s = 0, j = 0;
+    uint32_t round = 0, stage_off = 0;
+    bool ok = true;
+    for (int t = worker; t < count.tiles && ok; t += workers) {
+      const Tile r = tile_at<CG, NT, MODE>(a, count, n, t);
+      const int chunks = uniform(r.chunks), trans = uniform(r.trans);
+      if (!chunks) continue;
+      const int as = j & 1;
+      if (j >= 2 && !__all_sync(0xffffffffu, wait(&acc_empty[as], (uint32_t)(((j >> 1) - 1) & 1), abort_flag))) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const uint32_t acc = tmem_u + (uint32_t)(as * NT), idesc = fixed | (uint32_t)trans << 15;
+      const uint64_t a0 = trans ? a_cols : a_rows;
+      const uint32_t a_step = trans ? 2048 >> 4 : 32 >> 4;
+      for (int it = 0; it < chunks; ++it) {
+        if (!__all_sync(0xffffffffu, wait(&full[s], round & 1u, abort_flag))) { ok = false; break; }
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t da = a0 + stage_off, db = b0 + stage_off;
+        const uint32_t done = s_u32(&empty[s]);
+        if (leader) {
+          mma<CG>(acc, da, db, idesc, it ? 1u : 0u);
+#pragma unroll
+          for (int kk = 1; kk < BK / 16; ++kk) mma<CG>(acc, da + kk * a_step, db + kk * b_step, idesc, 1u);
+          commit<CG>(done);
+        }
+        __syncwarp();
+        if (++s == S) { s = 0; ++round; stage_off = 0; } else stage_off += C::STAGE >> 4;
+      }
+      if (ok && leader) commit<CG>(s_u32(&acc_full[as]));
+      __syncwarp();
+      ++j;
+    }
+  } else if (warp >= 2) {
+    // ---------------- epilogue: warp w reads accumulator lanes 32 * (w % 4) .. + 31, half of the columns
+    const int q = warp & 3, part = (warp - 2) >> 2;
+    const uint32_t mine = s_u32(staging) + (uint32_t)(warp - 2) * 4096u;
+    const float dw_scale = MODE == PRODUCTS ? a.meta->dw_scale : 1.f;
+    const int padded = (n + BK - 1) / BK * BK;           // rows of dz that a contraction over the rows reads
+    int j = 0;
+    for (int t = worker; t < count.tiles; t += workers) {
+      const Tile r = tile_at<CG, NT, MODE>(a, count, n, t);
+      const int as = j & 1;
+      if (r.chunks) {
+        bool have = wait(&acc_full[as], (uint32_t)((j >> 1) & 1), abort_flag);
+        have = __all_sync(0xffffffffu, have);
+        if (!have) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      }
+      const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(as * NT);
+      const int first = r.l0 + (int)rank * BM + q * 32, row = first + lane;
+      if (MODE == STATS) {
+        const int half = ((a.width + 63) >> 6) << 5, from = part ? half : 0, to = part ? a.width : half;
+        if (first < n) {
+          const int64_t at = (int64_t)(r.part * 2 + part) * a.rpad + row;
+          statistics(a, acc, r.c0, from, to, a.cols, row, row < n, a.part + at, a.part_y ? a.part_y + at : nullptr);
+        }
+      } else if (MODE == GRAD) {
+        if (first < padded) {
+          const bool live = row < n;
+          RowCoef rc = {0.f, 0.f, 0.f, 0.f};
+          Walk w;
+          w.none();
+          const float* p = a.p;
+          const int half = CG == 2 ? NT / 2 : ((a.width + 63) >> 6) << 5, from = part ? half : 0, to = part ? a.width : half;
+          const int limit = min(a.cols, r.c0 + a.width), shift = a.col0;
+          if (live) {
+            rc = a.coef[row];
+            const int64_t entries = (int64_t)a.src[row] * a.top;
+            p += entries;
+            w.start(a.id + entries, a.top, shift + r.c0 + from);
+          }
+          if (CG == 2) {
+#pragma unroll 1
+            for (int c = from; c < to; c += 64) {
+              const int x = r.c0 + c;
+              if (x >= a.cols) break;
+              uint32_t lo[16], hi[16];
+              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(x + 32, limit), live, rc, p, w, lo);
+              coefficients<T>(a, acc + (uint32_t)(c + 32), shift + x + 32, shift + max(x + 32, min(x + 64, limit)), live, rc, p, w, hi);
+              if (lane == 0) bulk_wait_read();
+              __syncwarp();
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                stage16(mine, lane, k, lo[4 * k], lo[4 * k + 1], lo[4 * k + 2], lo[4 * k + 3]);
+                stage16(mine, lane, 4 + k, hi[4 * k], hi[4 * k + 1], hi[4 * k + 2], hi[4 * k + 3]);
+              }
+              to_async_proxy();
+              __syncwarp();
+              if (lane == 0) { store_2d(&tm.m[M_DZ_OUT], mine, x, first); bulk_commit(); }
+            }
+          } else {
+            uint16_t* out = a.dz + (int64_t)row * a.ldz + r.c0;
+#pragma unroll 1
+            for (int c = from; c < to; c += 32) {
+              const int x = r.c0 + c;
+              if (x >= a.cols) break;
+              uint32_t v[16];
+              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(min(x + 32, r.c0 + to), limit), live, rc, p, w, v);
+              if (row < padded) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  if (c + 8 * k < to && x + 8 * k < a.cols) *(uint4*)(out + c + 8 * k) = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+              }
+            }
+          }
+        }
+      } else {
+        const int x0 = r.c0 + part * (NT / 2);
+        if (!r.trans || IsF32<TO>::value) {
+          const float f = r.trans ? dw_scale : 1.f;
+          const bool wanted = r.trans ? first < a.cols : first < n;
+          if (wanted) {
+#pragma unroll 1
+            for (int c = 0; c < NT / 2; c += 32) {
+              if (x0 + c >= a.d) break;
+              uint32_t v[32];
+              if (r.chunks) tmem_load32(v, acc + (uint32_t)(part * (NT / 2) + c));
+              if (lane == 0) bulk_wait_read();
+              __syncwarp();
+              if (r.trans) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) v[k] = r.chunks ? __float_as_uint(__uint_as_float(v[k]) * f) : 0u;
+              }
+#pragma unroll
+              for (int k = 0; k < 8; ++k) stage16(mine, lane, k, v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+              if (!r.trans || a.dw_tma) {
+                to_async_proxy();
+                __syncwarp();
+                if (lane == 0) {
+                  if (r.trans) store_2d(&tm.m[M_DW], mine, x0 + c, a.col0 + first);
+                  else if (a.add) add_2d(&tm.m[M_DX], mine, x0 + c, (int)((int64_t)r.part * a.rpad) + first);
+                  else store_2d(&tm.m[M_DX], mine, x0 + c, (int)((int64_t)r.part * a.rpad) + first);
+                  bulk_commit();
+                }
+              } else {       // rows of dW that do not start on 16-byte boundaries
+                __syncwarp();
+                float* out = (float*)a.dw + (int64_t)(a.col0 + first) * a.lddw + x0 + c;
+                for (int i = 0; i < 32 && first + i < a.cols; ++i) {
+                  uint32_t u;
+                  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(u) : "r"(mine + (uint32_t)(i * 128 + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4)) : "memory");
+                  if (x0 + c + lane < a.d) out[(int64_t)i * a.lddw + lane] = __uint_as_float(u);
+                }
+                __syncwarp();
+              }
+            }
+          }
+        } else if (first < a.cols) {
+          if constexpr (!IsF32<TO>::value) {
+#pragma unroll 1
+            for (int c = 0; c < NT / 2; c += 64) {
+              if (x0 + c >= a.d) break;
+              if (lane == 0) bulk_wait_read();
+              __syncwarp();
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                uint32_t v[32];
+                if (r.chunks) {
+                  tmem_load32(v, acc + (uint32_t)(part * (NT / 2) + c + h * 32));
+                } else {
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) v[k] = 0u;
+                }
+                uint32_t u[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) u[k] = pack2<TO>(__uint_as_float(v[2 * k]) * dw_scale, __uint_as_float(v[2 * k + 1]) * dw_scale);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) stage16(mine, lane, h * 4 + k, u[4 * k], u[4 * k + 1], u[4 * k + 2], u[4 * k + 3]);
+              }
+              if (a.dw_tma) {
+                to_async_proxy();
+                __syncwarp();
+                if (lane == 0) { store_2d(&tm.m[M_DW], mine, x0 + c, a.col0 + first); bulk_commit(); }
+              } else {
+                __syncwarp();
+                uint16_t* out = (uint16_t*)a.dw + (int64_t)(a.col0 + first) * a.lddw + x0 + c;
+                for (int i = 0; i < 32 && first + i < a.cols; ++i) {
+#pragma unroll
+                  for (int h = 0; h < 2; ++h) {
+                    const int e = h * 32 + lane;
+                    uint16_t u;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(u) : "r"(mine + (uint32_t)(i * 128 + (((e >> 3) ^ (i & 7)) << 4) + (e & 7) * 2)) : "memory");
+                    if (x0 + c + e < a.d) out[(int64_t)i * a.lddw + e] = u;
+                  }
+                }
+                __syncwarp();
+              }
+            }
+          }
+        }
+      }
+      if (r.chunks) {
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          const uint32_t bar = CG == 2 ? in_cta(s_u32(&acc_empty[as]), 0) : s_u32(&acc_empty[as]);
+          asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+        }
+        ++j;
+      }
+    }
+    if (C::OUT && lane == 0) bulk_wait_all();
+  }
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (CG == 2) cluster_sync_all();       // neither CTA leaves while the other may still signal its barriers
+  if (*abort_flag && tid == 0) record_status(a.sb, BETTY_ERR_TIMEOUT);
+  if (warp == 0) {
+    if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::TMEM_COLS) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::TMEM_COLS) : "memory");
+  }
+}
+
+template <int NT, int MODE, typename T, typename TO>
+__global__ void __launch_bounds__(THREADS, 1) k_vocab(const __grid_constant__ Maps tm, const Args a) {
+  body<1, NT, MODE, T, TO>(tm, a);
+}
+template <int NT, int MODE, typename T, typename TO>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_vocab_pair(const __grid_constant__ Maps tm, const Args a) {
+  body<2, NT, MODE, T, TO>(tm, a);
+}
+
+// ------------------------------------------------------------------ host side
+template <int CG, int NT, int MODE, typename T, typename TO>
+static betty_status launch(cudaStream_t stream, const Maps& tm, const Args& a, int64_t tiles) {
+  static SmemLimit limit = {};
+  auto kernel = [] {
+    if constexpr (CG == 2) return k_vocab_pair<NT, MODE, T, TO>;
+    else return k_vocab<NT, MODE, T, TO>;
+  }();
+  BETTY_TRY(ensure_dynamic_smem(kernel, limit, (size_t)Cfg<CG, NT, MODE>::SMEM));
+  const int64_t most = current_sm_count() / CG;
+  const int workers = (int)(tiles < 1 ? 1 : (tiles < most ? tiles : most));
+  launch_pdl(kernel, dim3((unsigned)(workers * CG)), dim3(THREADS), (size_t)Cfg<CG, NT, MODE>::SMEM, stream, tm, a);
+  BETTY_LAUNCH_CHECK();
+  return BETTY_OK;
+}
+
+static int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// A matrix by rows: boxes of `box_cols` values of `box_rows` rows
+static bool map_rows(CUtensorMap* tm, CUtensorMapDataType type, int bytes, const void* p, int64_t cols, int64_t rows, int64_t ld, int box_cols, int box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * bytes};
+  const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, ones[2] = {1, 1};
+  return fn && fn(tm, type, 2, (void*)p, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+static int box_rows_of(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }
+
+int logits_parts(const Shape& s) { return 2 * (int)div_up(s.vocab, s.width); }
+
+static void common_args(Args& a, const Shape& s, const Buffers& b) {
+  a.meta = b.meta; a.sb = b.sb;
+  a.type_bits = s.dtype == BETTY_BF16 ? (1u << 7 | 1u << 10) : 0u;
+  a.d = s.d; a.rpad = s.rpad;
+  a.width = s.width; a.c2 = s.c2; a.top = s.top;
+  a.src = b.src; a.id = b.id; a.p = b.p;
+  // the row tiles whose copies of x are taken together stay in L2 while W streams past them: 32 MB of it
+  const int64_t tile_bytes = (s.pairs ? 256 : 128) * s.dp * 2;
+  a.band = (int)(tile_bytes >= (32 << 20) ? 1 : (32 << 20) / tile_bytes);
+}
+static betty_status logits_maps(Maps& tm, Args& a, const Shape& s, const Buffers& b, const Operand& w) {
+  const CUtensorMapDataType type = s.dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  const int a_box = s.pairs ? 128 : box_rows_of(s.rows), b_box = s.pairs ? 128 : s.width;
+  a.a_bytes = (uint32_t)a_box * BK * 2; a.b_bytes = (uint32_t)b_box * BK * 2;
+  if (!map_rows(&tm.m[M_X], type, 2, b.x, s.dp, s.rpad, s.dp, BK, a_box)) return BETTY_ERR_CUDA;
+  if (!map_rows(&tm.m[M_W], type, 2, w.p, w.cols, w.rows, w.ld, BK, b_box)) return BETTY_ERR_CUDA;
+  tm.m[M_DZ_OUT] = tm.m[M_X];
+  return BETTY_OK;
+}
+
+betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w) {
+  Maps tm;
+  Args a = {};
+  common_args(a, s, b);
+  a.cols = s.vocab;
+  a.part = b.part; a.part_y = b.part_y; a.y_entry = b.y_entry;
+  BETTY_TRY(logits_maps(tm, a, s, b, w));
+  const int64_t tiles = div_up(s.rows, s.pairs ? 256 : 128) * div_up(s.vocab, s.width);
+  // the operands' type is in the instruction descriptor: nothing else of the statistics depends on it
+  if (s.pairs) return launch<2, 256, STATS, __nv_bfloat16, float>(stream, tm, a, tiles);
+  return launch<1, 128, STATS, __nv_bfloat16, float>(stream, tm, a, tiles);
+}
+
+template <typename T>
+static betty_status launch_grad(cudaStream_t stream, const Shape& s, const Maps& tm, const Args& a) {
+  const int64_t tiles = div_up(s.rows, s.pairs ? 256 : 128) * div_up(a.cols, s.width);
+  if (s.pairs) return launch<2, 256, GRAD, T, float>(stream, tm, a, tiles);
+  return launch<1, 128, GRAD, T, float>(stream, tm, a, tiles);
+}
+template <typename TO>
+static betty_status launch_products(cudaStream_t stream, const Shape& s, const Maps& tm, const Args& a) {
+  const int lanes = s.product_pairs ? 256 : 128, nt = lanes;
+  const int64_t tiles = (a.want_dx ? div_up(s.rows, lanes) * s.split : 0) * div_up(s.d, nt) + (a.want_dw ? div_up(a.cols, lanes) * div_up(s.d, nt) : 0);
+  if (s.product_pairs) return launch<2, 256, PRODUCTS, __nv_bfloat16, TO>(stream, tm, a, tiles);
+  return launch<1, 128, PRODUCTS, __nv_bfloat16, TO>(stream, tm, a, tiles);
+}
+
+betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, bool want_dx, void* dw, int64_t lddw, int dw_dtype) {
+  const CUtensorMapDataType type = s.dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  Maps lm, pm;
+  Args la = {}, pa = {};
+  common_args(la, s, b);
+  BETTY_TRY(logits_maps(lm, la, s, b, w));
+  la.coef = b.coef; la.dz = b.dz; la.ldz = s.piece;
+  if (!map_rows(&lm.m[M_DZ_OUT], type, 2, b.dz, s.piece, s.rpad, s.piece, 64, 32)) return BETTY_ERR_CUDA;
+
+  common_args(pa, s, b);
+  pa.want_dx = want_dx; pa.want_dw = dw != nullptr; pa.split = s.split;
+  pa.w_blocked = w.cols % 64 == 0;
+  pa.dw = dw; pa.lddw = lddw;
+  const int a_box = s.product_pairs ? 128 : box_rows_of(s.rows);
+  pa.a_bytes = (uint32_t)a_box * BK * 2; pa.b_bytes = 128 * BK * 2;
+  const Operand dz = {b.dz, s.piece, s.rpad, 1, s.piece, 0}, x = {b.x_dw, s.dp, s.rpad, 1, s.dp, 0};
+  bool ok = make_blocked_map(&pm.m[M_DZ_T], s.dtype, dz, false) && make_blocked_map(&pm.m[M_X_T], s.dtype, x, false);
+  ok = ok && (pa.w_blocked ? make_blocked_map(&pm.m[M_W_T], s.dtype, w, false) : make_map(&pm.m[M_W_T], s.dtype, w, false, 64, BK));
+  pm.m[M_DX] = pm.m[M_DW] = pm.m[M_DZ_T];
+  if (want_dx) ok = ok && map_rows(&pm.m[M_DX], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, b.dx, s.dp, s.rpad * s.split, s.dp, 32, 32);
+  const int ob = dw_dtype == BETTY_F32 ? 4 : 2;
+  if (s.vocab == 1) lddw = pad8(s.d);            // a stride that is never used still has to be a valid one
+  if (dw && (aligned16(dw) && (lddw * ob) % 16 == 0)) {
+    pa.dw_tma = 1;
+    ok = ok && map_rows(&pm.m[M_DW], dw_dtype == BETTY_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type, ob, dw, s.d, s.vocab, lddw, 128 / ob, 32);
+  }
+  if (!ok) return BETTY_ERR_CUDA;
+
+  for (int c = 0; c < s.vocab; c += s.piece) {
+    la.col0 = pa.col0 = c;
+    la.cols = pa.cols = s.vocab - c < s.piece ? s.vocab - c : s.piece;
+    pa.add = c > 0;
+    // columns behind the vocabulary's last are not in the map: the contraction reads zeros there
+    if ((c == 0 || pa.cols < s.piece) && !map_rows(&pm.m[M_DZ], type, 2, b.dz, pa.cols, s.rpad, s.piece, BK, a_box)) return BETTY_ERR_CUDA;
+    BETTY_TRY(s.dtype == BETTY_BF16 ? launch_grad<__nv_bfloat16>(stream, s, lm, la) : launch_grad<__half>(stream, s, lm, la));
+    BETTY_TRY(dw_dtype == BETTY_F32 ? launch_products<float>(stream, s, pm, pa)
+                                    : (s.dtype == BETTY_BF16 ? launch_products<__nv_bfloat16>(stream, s, pm, pa) : launch_products<__half>(stream, s, pm, pa)));
+  }
+  return BETTY_OK;
+}
+
+// Which tiles, and how much of the vocabulary at a time.
+void choose_shape(Shape& s, bool backward, bool want_dx, bool want_dw) {
+  const int64_t sms = current_sm_count(), rows = s.rows < 1 ? 1 : s.rows;
+  s.piece = (int)(div_up(s.vocab, 256) * 256);
+  if (backward) {
+    const int64_t most = (int64_t)1 << 26, fits = most / s.rpad / 256 * 256, piece = fits < 1024 ? 1024 : fits;
+    const int64_t pieces = div_up(s.vocab, piece);
+    s.piece = (int)(div_up(div_up(s.vocab, pieces), 256) * 256);
+  }
+  const int64_t cols = backward ? (s.piece < s.vocab ? s.piece : s.vocab) : s.vocab;
+  // an SM's share of the columns for a tile of 128 rows, its rounds being of equal length: pairs take 256 at a time
+  s.pairs = rows > 128;
+  s.width = 256;
+  int64_t best = s.pairs ? div_up(div_up(rows, 256) * div_up(cols, 256), sms / 2) * 256 : INT64_MAX;
+  for (int w = 128; w >= 32; w -= 16) {
+    const int64_t cost = div_up(div_up(rows, 128) * div_up(cols, w), sms) * (w + 16) * (rows > 128 ? 5 : 4) / 4;
+    if (cost < best) { best = cost; s.pairs = 0; s.width = w; }
+  }
+  s.split = 1;
+  s.product_pairs = 0;
+  if (!backward) return;
+  const int64_t pair_tiles = div_up(s.d, 256) * ((want_dx ? div_up(rows, 256) : 0) + (want_dw ? div_up(s.piece, 256) : 0));
+  s.product_pairs = rows > 128 && pair_tiles * 2 >= sms / 2;
+  if (want_dx) {           // few tiles with long contractions: parts of them, of 8 chunks or more
+    const int lanes = s.product_pairs ? 256 : 128;
+    const int64_t tiles = div_up(rows, lanes) * div_up(s.d, lanes), workers = s.product_pairs ? sms / 2 : sms, chunks = div_up(cols, BK);
+    int64_t split = workers / tiles;
+    if (split > chunks / 8) split = chunks / 8;
+    s.split = (int)(split < 1 ? 1 : split);
+  }
+}
+
+}  // namespace vocab
+}  // namespace betty
