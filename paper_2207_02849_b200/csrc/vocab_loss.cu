@@ -22,7 +22,7 @@ __device__ __forceinline__ float real(const void* p, int dtype, int64_t i) {
 // 64-bit keys in shared memory.  An entry without an id of the vocabulary or with a logit of -inf is none: what else its logit
 // is is not looked at.  The same id twice stays two entries; their shares add up where they are used.
 __global__ void k_entries(const void* ids, int64_t ldi, int id64, const void* logits, int64_t ldt, int dtype, int top, int padded, float inv_t, int64_t vocab,
-                          int32_t* id_out, float* p_out, uint8_t* some) {
+                          int2* out, uint8_t* some) {
   extern __shared__ unsigned char raw[];
   uint64_t* key = (uint64_t*)raw;
   float* e = (float*)(key + padded);
@@ -78,8 +78,7 @@ __global__ void k_entries(const void* ids, int64_t ldi, int id64, const void* lo
   for (int j = tid; j < top; j += blockDim.x) {
     const uint64_t k = key[j];
     const bool there = k != ~0ull;
-    id_out[row * top + j] = there ? (int32_t)(k >> 32) : NO_ID;
-    p_out[row * top + j] = there ? e[(uint32_t)k] * inv : 0.f;
+    out[row * top + j] = there ? make_int2((int32_t)(k >> 32), __float_as_int(e[(uint32_t)k] * inv)) : make_int2(NO_ID, 0);
   }
   if (tid == 0) some[row] = key[0] != ~0ull;
 }
@@ -92,13 +91,15 @@ struct RowArgs {
   const uint16_t* x_in;
   const void* target; int id64; float share;   // cross entropy: an entry (target, share) per row
   const uint8_t* some;                         // distillation: whether a row has an entry
-  int32_t* id; float* p;                       // cross entropy: the entries, written here
+  int2* entry;                                 // cross entropy: the entries, written here
   Meta* meta; int32_t* src; int32_t* pos; uint16_t* x; uint16_t* x_dw;
   float* loss; float* lse_out;                 // forward: zeros for rows left out
   const float* lse; const float* dloss;        // backward
   RowCoef* coef; float* row_scale;
   float inv_t, z_loss, smoothing;
   int fp16;
+  int lanes, workers, cols, want_dx, want_dw;  // the gradients' products
+  int64_t sum_rows;
 };
 
 __device__ __forceinline__ bool counts(const RowArgs& a, int64_t i) {
@@ -135,29 +136,58 @@ __device__ __forceinline__ void copy_row(const RowArgs& a, int64_t from, int64_t
   uint16_t* out = a.x + to * a.dp;
   uint16_t* out2 = a.x_dw != a.x ? a.x_dw + to * a.dp : nullptr;
   const bool aligned = ((uintptr_t)in & 15) == 0;
-  for (int c = lane * 8; c < a.dp; c += 256) {
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (aligned && c + 8 <= a.d) {
-      v = *(const uint4*)(in + c);
-    } else {
-      uint32_t w[4] = {0u, 0u, 0u, 0u};
+  constexpr int U = 4;                 // accesses in flight
+  for (int c0 = lane * 8; c0 < a.dp; c0 += 256 * U) {
+    uint4 v[U];
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (c + k < a.d) w[k >> 1] |= (uint32_t)in[c + k] << (16 * (k & 1));
-      v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    *(uint4*)(out + c) = v;
-    if (out2) {
-      uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + 256 * u;
+      v[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (aligned && c + 8 <= a.d) {
+        v[u] = *(const uint4*)(in + c);
+      } else if (c < a.d) {
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 f = __half22float2(*(__half2*)&w[k]);
-        const __half2 h = __floats2half2_rn(f.x * scale, f.y * scale);
-        w[k] = *(const uint32_t*)&h;
+        for (int k = 0; k < 8; ++k)
+          if (c + k < a.d) w[k >> 1] |= (uint32_t)in[c + k] << (16 * (k & 1));
+        v[u] = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      *(uint4*)(out2 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int c = c0 + 256 * u;
+      if (c >= a.dp) break;
+      *(uint4*)(out + c) = v[u];
+      if (out2) {
+        uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 f = __half22float2(*(__half2*)&w[k]);
+          const __half2 h = __floats2half2_rn(f.x * scale, f.y * scale);
+          w[k] = *(const uint32_t*)&h;
+        }
+        *(uint4*)(out2 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
     }
   }
+}
+
+// Parts of dX's contraction, for which there is room: the number with which the workers finish soonest, where dX's tiles come
+// first and dW's fill up.  Times in chunks of a contraction; a part's sums are written and read again.
+__device__ int choose_split(const RowArgs& a, int n) {
+  const Products p = products_of(n, a.d, a.cols, a.lanes);
+  const int most = min((int)(a.sum_rows / max(1, p.row_tiles * a.lanes)), max(1, p.dx_chunks / 8));
+  const int tiles = p.row_tiles * p.d_tiles;
+  const float second = a.want_dw ? (float)p.col_tiles * p.d_tiles * dw_cost(p) : 0.f;
+  const float part = (float)n * a.dp * (a.lanes == 256 ? 3.6e-6f : 7e-6f);      // 8 bytes a value at 6 TB/s, chunks of 0.37 (0.19) us
+  int best = 1;
+  float least = INFINITY;
+  for (int s = 1; s <= most; ++s) {
+    const float first = (float)((tiles * s + a.workers - 1) / a.workers) * dx_cost(p, s);
+    const float time = fmaxf(first, ((float)tiles * s * dx_cost(p, s) + second) / a.workers) + s * part;
+    if (time < least) { least = time; best = s; }
+  }
+  return best;
 }
 
 // Each block takes a range of rows and counts those before it itself: one launch, and the order is kept.
@@ -200,7 +230,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
         const int64_t to = before + at;
         list[at] = (int)(i - base);
         a.src[to] = (int32_t)i;
-        if (!a.some) { a.id[i] = (int32_t)whole(a.target, a.id64, i); a.p[i] = a.share; }
+        if (!a.some) a.entry[i] = make_int2((int32_t)whole(a.target, a.id64, i), __float_as_int(a.share));
         if (a.dloss) {
           const int h = a.fp16 ? row_lift(bound_of(a, i), least) : 0;
           const float g = ldexpf(a.dloss[i] * a.inv_t, h), lse = a.lse[i];
@@ -221,7 +251,11 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
     before += all;
   }
   if (r1 == a.rows && blockIdx.x == gridDim.x - 1) {
-    if (tid == 0) { a.meta->n = before; a.meta->dw_scale = a.fp16 && a.dloss ? ldexpf(1.f, -least) : 1.f; }
+    if (tid == 0) {
+      a.meta->n = before;
+      a.meta->split = a.dloss && a.want_dx ? choose_split(a, before) : 1;
+      a.meta->dw_scale = a.fp16 && a.dloss ? ldexpf(1.f, -least) : 1.f;
+    }
     if (a.dloss)                       // a contraction over the rows takes them 64 at a time
       for (int64_t r = before + warp; r < (before + BK - 1) / BK * BK; r += 8)
         for (int c = lane * 8; c < a.dp; c += 256) {
@@ -235,51 +269,67 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
 struct LossArgs {
   const Meta* meta; const int32_t* src;
   const float2* part; const float* part_y; int parts; int64_t rpad;
-  const float* p; const float* y_entry; int top;
+  const int2* entry; const float* y_entry; int top;
   int distill;
   float smoothing, z_loss; int64_t vocab;
   float* loss; float* lse;
 };
-// 32 rows a block, a lane each; the warps share a row's parts and entries
-__global__ void __launch_bounds__(512) k_losses(const LossArgs a) {
-  __shared__ float sm[16][32], ss[16][32], sy[16][32], se[16][32];
+// 8 rows a block; 64 threads share a row's parts and entries
+static constexpr int LOSS_ROWS = 8, LOSS_SLICES = 64;
+__global__ void __launch_bounds__(LOSS_ROWS * LOSS_SLICES) k_losses(const LossArgs a) {
+  __shared__ float sm[LOSS_SLICES][LOSS_ROWS], ss[LOSS_SLICES][LOSS_ROWS], sy[LOSS_SLICES][LOSS_ROWS];
   pdl_enter();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = blockIdx.x * 32 + lane, n = a.meta->n;
-  if (blockIdx.x * 32 >= n) return;
+  const int col = threadIdx.x % LOSS_ROWS, slice = threadIdx.x / LOSS_ROWS, row = blockIdx.x * LOSS_ROWS + col, n = a.meta->n;
+  if (blockIdx.x * LOSS_ROWS >= n) return;
   const bool live = row < n;
-  float m = -INFINITY, s = 0.f, y = 0.f, e = 0.f;
-  int64_t src = 0;
+  float m = -INFINITY, s = 0.f, y = 0.f;
+  const int64_t src = live ? a.src[row] : 0;
   if (live) {
-    src = a.src[row];
-#pragma unroll 4
-    for (int i = warp; i < a.parts; i += 16) {
-      const float2 q = a.part[(int64_t)i * a.rpad + row];
-      const float most = fmaxf(m, q.x), base = most == -INFINITY ? 0.f : most;
-      s = s * exp2f(m - base) + q.y * exp2f(q.x - base);
+    constexpr int U = 8;               // parts in flight
+    for (int i0 = slice; i0 < a.parts; i0 += LOSS_SLICES * U) {
+      float2 q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * LOSS_SLICES;
+        q[u] = i < a.parts ? a.part[(int64_t)i * a.rpad + row] : make_float2(-INFINITY, 0.f);
+      }
+      float most = m;
+#pragma unroll
+      for (int u = 0; u < U; ++u) most = fmaxf(most, q[u].x);
+      const float base = most == -INFINITY ? 0.f : most;
+      s *= exp2f(m - base);
+#pragma unroll
+      for (int u = 0; u < U; ++u) s += q[u].y * exp2f(q[u].x - base);
       m = most;
-      if (a.part_y) y += a.part_y[(int64_t)i * a.rpad + row];
     }
+    if (a.part_y)
+      for (int i = slice; i < a.parts; i += LOSS_SLICES) y += a.part_y[(int64_t)i * a.rpad + row];
   }
-  sm[warp][lane] = m; ss[warp][lane] = s; sy[warp][lane] = y;
+  sm[slice][col] = m; ss[slice][col] = s; sy[slice][col] = y;
   __syncthreads();
   float most = -INFINITY;
-  for (int i = 0; i < 16; ++i) most = fmaxf(most, sm[i][lane]);
+#pragma unroll 8
+  for (int i = 0; i < LOSS_SLICES; ++i) most = fmaxf(most, sm[i][col]);
   const float base = most == -INFINITY ? 0.f : most;
   s = y = 0.f;
-  for (int i = 0; i < 16; ++i) { s += ss[i][lane] * exp2f(sm[i][lane] - base); y += sy[i][lane]; }
+#pragma unroll 8
+  for (int i = 0; i < LOSS_SLICES; ++i) { s += ss[i][col] * exp2f(sm[i][col] - base); y += sy[i][col]; }
   const float lse2 = base + log2f(s);
+  float e = 0.f;
   if (live)
-    for (int i = warp; i < a.top; i += 16) {
-      const float p = a.p[src * a.top + i];
+    for (int i = slice; i < a.top; i += LOSS_SLICES) {
+      const float p = __int_as_float(a.entry[src * a.top + i].y);
       // log p - (y - lse2): close to each other where the student has learnt its teacher
       if (p > 0.f) e += p * ((a.distill ? log2f(p) : 0.f) - (a.y_entry[src * a.top + i] - lse2));
       else if (!(p == 0.f)) e = p;
     }
-  se[warp][lane] = e;
+  __syncthreads();                     // the maxima have been read
+  sm[slice][col] = e;
   __syncthreads();
-  if (warp == 0 && live) {
+  if (slice == 0 && live) {
     e = 0.f;
-    for (int i = 0; i < 16; ++i) e += se[i][lane];
+#pragma unroll 8
+    for (int i = 0; i < LOSS_SLICES; ++i) e += sm[i][col];
     const float lse = lse2 * LN2;
     if (a.smoothing != 0.f) e += a.smoothing * (lse2 - y / (float)a.vocab);
     a.loss[src] = e * LN2 + a.z_loss * lse * lse;
@@ -288,38 +338,40 @@ __global__ void __launch_bounds__(512) k_losses(const LossArgs a) {
 }
 
 // ------------------------------------------------------------------ dX
-// Row i of dX from the sums of its copy, or zeros; a warp per row, four columns a lane.
+// Row i of dX from the parts' sums of its copy, or zeros: a block takes 1024 columns of a row, a thread four.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int64_t rpad, int split, const int32_t* pos, const float* row_scale, const float* sums,
+__global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int lanes, const Meta* meta, const int32_t* pos, const float* row_scale, const float* sums,
                                             T* dx, int64_t ld) {
   pdl_enter();
-  const int lane = threadIdx.x & 31;
   const bool wide = ((uintptr_t)dx % (4 * sizeof(T))) == 0 && ld % 4 == 0;
-  for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += (int64_t)gridDim.x * 8) {
+  const int blocks = (d + 1023) / 1024, split = meta->split;
+  const int64_t stride = (int64_t)((meta->n + lanes - 1) / lanes * lanes) * dp;
+  for (int64_t b = blockIdx.x; b < rows * blocks; b += gridDim.x) {
+    const int64_t row = b / blocks;
+    const int c = (int)(b - row * blocks) * 1024 + (int)threadIdx.x * 4;
+    if (c >= d) continue;
     const int at = pos[row];
-    const float f = at >= 0 ? row_scale[at] : 0.f;
-    const float* in = sums + (int64_t)(at >= 0 ? at : 0) * dp;
     T* out = dx + row * ld;
-    for (int c = lane * 4; c < d; c += 128) {
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (at >= 0) {
-        v = *(const float4*)(in + c);
-        for (int s = 1; s < split; ++s) {
-          const float4 w = *(const float4*)(in + (int64_t)s * rpad * dp + c);
-          v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-        }
-        v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (at >= 0) {
+      const float f = row_scale[at];
+      const float* in = sums + (int64_t)at * dp + c;
+#pragma unroll 4
+      for (int s = 0; s < split; ++s) {
+        const float4 w = *(const float4*)(in + s * stride);
+        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
       }
-      if (wide && c + 4 <= d) {
-        alignas(16) T o[4] = {from_f<T>(v.x), from_f<T>(v.y), from_f<T>(v.z), from_f<T>(v.w)};
-        if constexpr (sizeof(T) == 4) *(float4*)(out + c) = *(const float4*)o;
-        else *(uint2*)(out + c) = *(const uint2*)o;
-      } else {
-        const float o[4] = {v.x, v.y, v.z, v.w};
+      v.x *= f; v.y *= f; v.z *= f; v.w *= f;
+    }
+    if (wide && c + 4 <= d) {
+      alignas(16) T o[4] = {from_f<T>(v.x), from_f<T>(v.y), from_f<T>(v.z), from_f<T>(v.w)};
+      if constexpr (sizeof(T) == 4) *(float4*)(out + c) = *(const float4*)o;
+      else *(uint2*)(out + c) = *(const uint2*)o;
+    } else {
+      const float o[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (c + k < d) out[c + k] = from_f<T>(o[k]);
-      }
+      for (int k = 0; k < 4; ++k)
+        if (c + k < d) out[c + k] = from_f<T>(o[k]);
     }
   }
 }
@@ -405,7 +457,8 @@ static Shape shape_of(const betty_vocab_cfg* c, int64_t rows, int top, bool back
   s.vocab = (int)c->vocab; s.d = (int)c->d; s.dp = round_up(c->d, 64);
   s.c2 = LOG2E / c->temperature;
   s.top = top < 1 ? 1 : top;
-  choose_shape(s, backward, dx, dw);
+  s.want_dx = dx; s.want_dw = dw;
+  choose_shape(s, backward);
   return s;
 }
 
@@ -416,8 +469,7 @@ static betty_status lay_out(Arena& arena, const Shape& s, const Call& c, Buffers
   b.meta = arena.alloc<Meta>(1);
   b.src = arena.alloc<int32_t>((size_t)s.rpad);
   b.pos = arena.alloc<int32_t>((size_t)c.rows);
-  b.id = arena.alloc<int32_t>((size_t)(c.rows * s.top));
-  b.p = arena.alloc<float>((size_t)(c.rows * s.top));
+  b.entry = arena.alloc<int2>((size_t)(c.rows * s.top));
   some = distill ? arena.alloc<uint8_t>((size_t)c.rows) : nullptr;
   b.x = b.x_dw = arena.alloc<uint16_t>((size_t)(s.rpad * s.dp));
   b.part = nullptr; b.part_y = b.y_entry = nullptr; b.coef = nullptr; b.row_scale = nullptr; b.dz = nullptr; b.dx = nullptr;
@@ -430,7 +482,7 @@ static betty_status lay_out(Arena& arena, const Shape& s, const Call& c, Buffers
     b.coef = arena.alloc<RowCoef>((size_t)s.rpad);
     b.row_scale = arena.alloc<float>((size_t)s.rpad);
     b.dz = arena.alloc<uint16_t>((size_t)(s.rpad * s.piece));
-    if (c.dX) b.dx = arena.alloc<float>((size_t)(s.split * s.rpad * s.dp));
+    if (c.dX) b.dx = arena.alloc<float>((size_t)(s.sum_rows * s.dp));
     if (c.dW && s.dtype == BETTY_F16) b.x_dw = arena.alloc<uint16_t>((size_t)(s.rpad * s.dp));
   }
   return arena.overflow ? BETTY_ERR_WORKSPACE : BETTY_OK;
@@ -461,17 +513,19 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
     while (padded < c.top) padded *= 2;
     const int threads = padded / 2 < 32 ? 32 : padded / 2;
     launch_pdl(k_entries, dim3((unsigned)c.rows), dim3((unsigned)threads), (size_t)padded * 12, stream, c.target, c.ldi, (int)(c.id_dtype == BETTY_I64), c.teacher, c.ldt,
-               (int)c.teacher_dtype, c.top, padded, 1.f / cfg->temperature, cfg->vocab, (int32_t*)b.id, (float*)b.p, some);
+               (int)c.teacher_dtype, c.top, padded, 1.f / cfg->temperature, cfg->vocab, b.entry, some);
     BETTY_LAUNCH_CHECK();
   }
   RowArgs r = {};
   r.rows = c.rows; r.vocab = cfg->vocab; r.d = (int)cfg->d; r.dp = s.dp; r.ldx = c.ldx; r.x_in = (const uint16_t*)c.X;
   r.target = distill ? nullptr : c.target; r.id64 = c.id_dtype == BETTY_I64; r.share = 1.f - cfg->smoothing; r.some = some;
-  r.id = (int32_t*)b.id; r.p = (float*)b.p;
+  r.entry = b.entry;
   r.meta = b.meta; r.src = b.src; r.pos = b.pos; r.x = b.x; r.x_dw = b.x_dw;
   r.loss = c.backward ? nullptr : c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.backward ? c.dloss : nullptr;
   r.coef = b.coef; r.row_scale = b.row_scale;
   r.inv_t = 1.f / cfg->temperature; r.z_loss = cfg->z_loss; r.smoothing = cfg->smoothing; r.fp16 = cfg->dtype == BETTY_F16;
+  r.lanes = s.product_pairs ? 256 : 128; r.workers = current_sm_count() / (s.product_pairs ? 2 : 1);
+  r.cols = s.piece < s.vocab ? s.piece : s.vocab; r.want_dx = s.want_dx; r.want_dw = s.want_dw; r.sum_rows = s.sum_rows;
   const int64_t blocks = (c.rows + 7) / 8;
   launch_pdl(k_rows, dim3((unsigned)(blocks < most ? blocks : most)), dim3(ROW_THREADS), 0, stream, r);
   BETTY_LAUNCH_CHECK();
@@ -480,21 +534,22 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
     BETTY_TRY(logits_statistics(stream, s, b, w));
     LossArgs l = {};
     l.meta = b.meta; l.src = b.src; l.part = b.part; l.part_y = b.part_y; l.parts = logits_parts(s); l.rpad = s.rpad;
-    l.p = b.p; l.y_entry = b.y_entry; l.top = s.top; l.distill = distill;
+    l.entry = b.entry; l.y_entry = b.y_entry; l.top = s.top; l.distill = distill;
     l.smoothing = cfg->smoothing; l.z_loss = cfg->z_loss; l.vocab = cfg->vocab; l.loss = c.loss; l.lse = c.lse_out;
-    launch_pdl(k_losses, dim3((unsigned)((c.rows + 31) / 32)), dim3(512), 0, stream, l);
+    launch_pdl(k_losses, dim3((unsigned)((c.rows + LOSS_ROWS - 1) / LOSS_ROWS)), dim3(LOSS_ROWS * LOSS_SLICES), 0, stream, l);
     BETTY_LAUNCH_CHECK();
     return BETTY_OK;
   }
-  BETTY_TRY(logits_gradients(stream, s, b, w, c.dX != nullptr, c.dW, c.lddw, c.dw_dtype));
+  BETTY_TRY(logits_gradients(stream, s, b, w, c.dW, c.lddw, c.dw_dtype));
   if (c.dX) {
-    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    const int64_t strips = c.rows * ((cfg->d + 1023) / 1024);
+    const dim3 grid((unsigned)(strips < most * 2 ? strips : most * 2));
     if (c.dx_dtype == BETTY_F32)
-      launch_pdl(k_dx<float>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, s.rpad, s.split, b.pos, b.row_scale, b.dx, (float*)c.dX, c.lddx);
+      launch_pdl(k_dx<float>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, b.meta, b.pos, b.row_scale, b.dx, (float*)c.dX, c.lddx);
     else if (c.dx_dtype == BETTY_BF16)
-      launch_pdl(k_dx<__nv_bfloat16>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, s.rpad, s.split, b.pos, b.row_scale, b.dx, (__nv_bfloat16*)c.dX, c.lddx);
+      launch_pdl(k_dx<__nv_bfloat16>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, b.meta, b.pos, b.row_scale, b.dx, (__nv_bfloat16*)c.dX, c.lddx);
     else
-      launch_pdl(k_dx<__half>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, s.rpad, s.split, b.pos, b.row_scale, b.dx, (__half*)c.dX, c.lddx);
+      launch_pdl(k_dx<__half>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, b.meta, b.pos, b.row_scale, b.dx, (__half*)c.dX, c.lddx);
     BETTY_LAUNCH_CHECK();
   }
   return BETTY_OK;

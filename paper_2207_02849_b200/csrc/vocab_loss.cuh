@@ -24,6 +24,7 @@ static constexpr int NO_ID = 0x7FFFFFFF;       // an entry that is none
 struct RowCoef { float lse2, a, b, e; };       // dz = a 2^(y - lse2) + b - e p, as it is stored for the products
 struct Meta {
   int32_t n;             // rows that count
+  int32_t split;         // parts of the contraction of dX, each with its own sums
   float dw_scale;        // what a sum over the stored dz and x is multiplied by to give dW
 };
 
@@ -40,8 +41,23 @@ struct Shape {
   int width;
   int product_pairs;     // gradients: the same choice
   int piece;             // columns of the vocabulary at a time (backward), a multiple of 256
-  int split;             // parts of the contraction of dX
+  int64_t sum_rows;      // rows of dX's sums: room for `split` times the rows that count
+  int want_dx, want_dw;
 };
+
+// ---- how the tiles of the gradients' products are spread ----
+// dX's tiles contract over the piece's columns, dW's over the rows: their lengths differ, by much where there are few rows.
+struct Products {
+  int row_tiles, d_tiles, col_tiles;   // tiles along the rows, d and the piece's columns
+  int dx_chunks, dw_chunks;            // lengths of the contractions
+};
+__host__ __device__ inline Products products_of(int n, int d, int cols, int lanes) {
+  return {(n + lanes - 1) / lanes, (d + lanes - 1) / lanes, (cols + lanes - 1) / lanes, (cols + tc::BK - 1) / tc::BK, (n + tc::BK - 1) / tc::BK};
+}
+// A tile's time in contraction chunks: what a tile costs beside them, and the shortest time in which a tile of dW is stored.
+// Measured with rows of 700 to 1700 (see vocab_products.cu).
+__host__ __device__ inline int dx_cost(const Products& p, int split) { return (p.dx_chunks + split - 1) / split + 4; }
+__host__ __device__ inline int dw_cost(const Products& p) { return (p.dw_chunks > 4 ? p.dw_chunks : 4) + 1; }
 
 struct Buffers {
   Meta* meta;
@@ -49,15 +65,14 @@ struct Buffers {
   int32_t* pos;          // [rows] where a row went, -1: left out
   uint16_t* x;           // [rpad, dp]
   uint16_t* x_dw;        // [rpad, dp] as the gradient of W takes it (fp16: scaled, else x itself)
-  const int32_t* id;     // [rows, top] entries
-  const float* p;
+  int2* entry;           // [rows, top] entries: id, and the bits of p
   float2* part;          // [parts][rpad] maximum and sum of 2^(y - maximum) of a part of a row
   float* part_y;         // [parts][rpad] sum of y (smoothing only)
   float* y_entry;        // [rows, top] y at the entries
   RowCoef* coef;         // [rpad]
   float* row_scale;      // [rpad] what a row of dX is multiplied by
   uint16_t* dz;          // [rpad, piece]
-  float* dx;             // [split][rpad, dp]
+  float* dx;             // [split][rows that count, up to whole tiles; dp], sum_rows in all
   StatusBlock* sb;
 };
 
@@ -65,9 +80,8 @@ int logits_parts(const Shape& s);
 // part, part_y (if not null) and y_entry of all rows that count
 betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w);
 // dX's fp32 sums (want_dx) and dW (dw not null), piece by piece
-betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, bool want_dx, void* dw, int64_t lddw,
-                              int dw_dtype);
-void choose_shape(Shape& s, bool backward, bool want_dx, bool want_dw);
+betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, void* dw, int64_t lddw, int dw_dtype);
+void choose_shape(Shape& s, bool backward);
 
 }  // namespace vocab
 }  // namespace betty

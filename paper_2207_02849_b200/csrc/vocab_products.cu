@@ -46,12 +46,12 @@ struct Args {
   int width, band;         // columns of a tile; row tiles that are taken together
   float c2;
   int top;
-  const int32_t* src; const int32_t* id; const float* p;
+  const int32_t* src; const int2* entry;
   float2* part; float* part_y; float* y_entry;
   const RowCoef* coef;
   uint16_t* dz; int64_t ldz;
   // products
-  int want_dx, want_dw, split, add;   // add: dX's sums already hold the pieces before
+  int want_dx, want_dw, add;          // add: dX's sums already hold the pieces before
   int w_blocked, dw_tma;
   void* dw; int64_t lddw;
 };
@@ -63,23 +63,46 @@ struct Tile {
   int k0, chunks;          // contraction
   int part;                // split of dX's contraction, or column tile of the logits
 };
-struct Counts { int row_tiles, col_tiles, d_tiles, dx_tiles, tiles; };
+struct Counts {
+  int row_tiles, col_tiles, d_tiles, split;
+  int first, second;       // tiles that are taken first (logits, dX), and then (dW)
+  int lead;                // workers with one tile less of the first kind start this many tiles earlier with the second
+};
 
 template <int CG, int NT, int MODE>
-__device__ __forceinline__ Counts count_tiles(const Args& a, int n) {
+__device__ __forceinline__ Counts count_tiles(const Args& a, int n, int split, int workers) {
   Counts c;
-  c.row_tiles = (n + BM * CG - 1) / (BM * CG);
+  c.split = split;
+  c.second = c.lead = 0;
   if (MODE != PRODUCTS) {
+    c.row_tiles = (n + BM * CG - 1) / (BM * CG);
     c.col_tiles = (a.cols + a.width - 1) / a.width;
-    c.d_tiles = c.dx_tiles = 0;
-    c.tiles = c.row_tiles * c.col_tiles;
+    c.d_tiles = 0;
+    c.first = c.row_tiles * c.col_tiles;
   } else {
-    c.col_tiles = (a.cols + BM * CG - 1) / (BM * CG);
-    c.d_tiles = (a.d + NT - 1) / NT;
-    c.dx_tiles = a.want_dx ? c.row_tiles * c.d_tiles * a.split : 0;
-    c.tiles = c.dx_tiles + (a.want_dw ? c.col_tiles * c.d_tiles : 0);
+    const Products p = products_of(n, a.d, a.cols, NT);
+    c.row_tiles = p.row_tiles; c.col_tiles = p.col_tiles; c.d_tiles = p.d_tiles;
+    c.first = a.want_dx ? p.row_tiles * p.d_tiles * split : 0;
+    c.second = a.want_dw ? p.col_tiles * p.d_tiles : 0;
+    if (c.first % workers) c.lead = (dx_cost(p, split) + dw_cost(p) / 2) / dw_cost(p);
   }
   return c;
+}
+// The i-th tile of a worker, -1 behind its last: the first kind in turn; then the second, which those whose turn it was not begin
+// with `lead` tiles of, as long as a tile of the first kind takes, before all take turns again.
+__device__ __forceinline__ int nth_tile(const Counts& c, int worker, int workers, int i) {
+  const int rounds = c.first / workers, over = c.first - rounds * workers, mine = rounds + (worker < over);
+  if (i < mine) return i * workers + worker;
+  int j = i - mine;
+  const int idle = workers - over;
+  int t;
+  if (worker >= over && j < c.lead) {
+    t = j * idle + worker - over;
+  } else {
+    if (worker >= over) j -= c.lead;
+    t = c.lead * idle + j * workers + worker;
+  }
+  return t < c.second ? c.first + t : -1;
 }
 template <int CG, int NT, int MODE>
 __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, int t) {
@@ -92,17 +115,17 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
     r.c0 = r.part * a.width;
     r.k0 = 0;
     r.chunks = (a.d + BK - 1) / BK;
-  } else if (t < c.dx_tiles) {
+  } else if (t < c.first) {
     const int rest = t / c.d_tiles, chunks = (a.cols + BK - 1) / BK;
     r.trans = 0;
     r.c0 = (t - rest * c.d_tiles) * NT;
-    r.part = rest % a.split;
-    r.l0 = rest / a.split * (BM * CG);
-    const int k = (int)((int64_t)r.part * chunks / a.split);
+    r.part = rest % c.split;
+    r.l0 = rest / c.split * (BM * CG);
+    const int k = (int)((int64_t)r.part * chunks / c.split);
     r.k0 = k * BK;
-    r.chunks = (int)((int64_t)(r.part + 1) * chunks / a.split) - k;
+    r.chunks = (int)((int64_t)(r.part + 1) * chunks / c.split) - k;
   } else {
-    t -= c.dx_tiles;
+    t -= c.first;
     const int rest = t / c.d_tiles;
     r.trans = 1;
     r.c0 = (t - rest * c.d_tiles) * NT;
@@ -115,22 +138,38 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
 }
 
 // ------------------------------------------------------------------ epilogues
-// A row's entries in ascending order of id, from the first at or behind a column.
+// A row's entries in ascending order of id, from the first at or behind a column.  The next AHEAD of them are in registers: they are
+// asked for before the accumulator is waited for, and a step asks for the one that is needed AHEAD steps later.
 struct Walk {
-  const int32_t* id;
-  int at, end, next;
-  __device__ __forceinline__ void start(const int32_t* ids, int top, int column) {
-    id = ids; end = top;
+  static constexpr int AHEAD = 3;
+  const int2* entry;
+  int at, end;
+  int2 q[AHEAD];
+  __device__ __forceinline__ int2 get(int i) const { return i < end ? entry[i] : make_int2(NO_ID, 0); }
+  __device__ __forceinline__ void start(const int2* entries, int top, int column) {
+    entry = entries; end = top;
     int lo = 0, hi = top;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
-      if (id[mid] < column) lo = mid + 1; else hi = mid;
+      if (entry[mid].x < column) lo = mid + 1; else hi = mid;
     }
     at = lo;
-    next = at < end ? id[at] : NO_ID;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) q[i] = get(at + i);
   }
-  __device__ __forceinline__ void none() { id = nullptr; at = end = 0; next = NO_ID; }
-  __device__ __forceinline__ void step() { ++at; next = at < end ? id[at] : NO_ID; }
+  __device__ __forceinline__ void none() {
+    entry = nullptr; at = end = 0;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) q[i] = make_int2(NO_ID, 0);
+  }
+  __device__ __forceinline__ int next() const { return q[0].x; }
+  __device__ __forceinline__ float share() const { return __int_as_float(q[0].y); }
+  __device__ __forceinline__ void step() {
+#pragma unroll
+    for (int i = 0; i + 1 < AHEAD; ++i) q[i] = q[i + 1];
+    q[AHEAD - 1] = get(at + AHEAD);
+    ++at;
+  }
 };
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
@@ -159,10 +198,8 @@ __device__ __forceinline__ void stage16(uint32_t rows, int row, int j, uint32_t 
 }
 
 // Columns [from, to) of a tile (its accumulator at `acc`, its first column of the vocabulary `c0`) to a row's statistics.
-__device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, int from, int to, int limit, int row, bool live, float2* part, float* part_y) {
-  Walk w;
-  const int64_t entries = live ? (int64_t)a.src[row] * a.top : 0;
-  if (live) w.start(a.id + entries, a.top, c0 + from); else w.none();
+__device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, int from, int to, int limit, bool live, Walk& w, float* y_entry, float2* part,
+                                           float* part_y) {
   float m = -INFINITY, s = 0.f, sum = 0.f;
 #pragma unroll 1
   for (int c = from; c < to; c += 32) {
@@ -192,13 +229,13 @@ __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, 
       for (int k = 0; k < 32; ++k) y[k & 3] += cb + k < end ? __uint_as_float(v[k]) : 0.f;
       sum += (y[0] + y[1]) + (y[2] + y[3]);
     }
-    while (__any_sync(0xffffffffu, w.next < end)) {
+    while (__any_sync(0xffffffffu, w.next() < end)) {
       float z = 0.f;
 #pragma unroll
       for (int k = 0; k < 32; ++k)
-        if (w.next - cb == k) z = __uint_as_float(v[k]);
-      if (w.next < end) {
-        a.y_entry[entries + w.at] = z * a.c2;
+        if (w.next() - cb == k) z = __uint_as_float(v[k]);
+      if (w.next() < end) {
+        y_entry[w.at] = z * a.c2;
         w.step();
       }
     }
@@ -211,18 +248,17 @@ __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, 
 
 // 32 columns of a tile as coefficients of a row's gradient, packed in pairs; rows that do not count and columns that do not exist: 0
 template <typename T>
-__device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb, int end, bool live, const RowCoef& rc, const float* p, Walk& w, uint32_t (&out)[16]) {
+__device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb, int end, bool live, const RowCoef& rc, Walk& w, uint32_t (&out)[16]) {
   uint32_t v[32];
   tmem_load32(v, acc);
 #pragma unroll
   for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(fmaf(rc.a, exp2f(fmaf(__uint_as_float(v[k]), a.c2, -rc.lse2)), rc.b));
-  while (__any_sync(0xffffffffu, w.next < end)) {
-    float e = 0.f;
-    if (w.next < end) e = rc.e * p[w.at];
+  while (__any_sync(0xffffffffu, w.next() < end)) {
+    const float e = rc.e * w.share();
 #pragma unroll
     for (int k = 0; k < 32; ++k)
-      if (w.next - cb == k) v[k] = __float_as_uint(__uint_as_float(v[k]) - e);
-    if (w.next < end) w.step();
+      if (w.next() - cb == k) v[k] = __float_as_uint(__uint_as_float(v[k]) - e);
+    if (w.next() < end) w.step();
   }
   if (end < cb + 32 || !live) {
 #pragma unroll
@@ -281,7 +317,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
   const int n = uniform(a.meta->n);
-  const Counts count = count_tiles<CG, NT, MODE>(a, n);
+  const Counts count = count_tiles<CG, NT, MODE>(a, n, uniform(a.meta->split), workers);
 
   // The loading and the multiplying warp run their loops with all lanes, and one lane issues (see grouped.cu).
   if (warp == 0) {
@@ -291,7 +327,9 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     int s = 0;
     uint32_t round = 0;
     bool ok = true;
-    for (int t = worker; t < count.tiles && ok; t += workers) {
+    for (int i = 0; ok; ++i) {
+      const int t = uniform(nth_tile(count, worker, workers, i));
+      if (t < 0) break;
       const Tile r = tile_at<CG, NT, MODE>(a, count, n, t);
       const int trans = uniform(r.trans), chunks = uniform(r.chunks), k0 = uniform(r.k0);
       const int l = uniform(r.l0) + (int)rank * BM;
@@ -342,7 +380,9 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     int s = 0, j = 0;
     uint32_t round = 0, stage_off = 0;
     bool ok = true;
-    for (int t = worker; t < count.tiles && ok; t += workers) {
+    for (int i = 0; ok; ++i) {
+      const int t = uniform(nth_tile(count, worker, workers, i));
+      if (t < 0) break;
       const Tile r = tile_at<CG, NT, MODE>(a, count, n, t);
       const int chunks = uniform(r.chunks), trans = uniform(r.trans);
       if (!chunks) continue;
@@ -377,9 +417,27 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     const float dw_scale = MODE == PRODUCTS ? a.meta->dw_scale : 1.f;
     const int padded = (n + BK - 1) / BK * BK;           // rows of dz that a contraction over the rows reads
     int j = 0;
-    for (int t = worker; t < count.tiles; t += workers) {
+    const int split_rows = count.row_tiles * (BM * CG);  // rows of one part of dX's sums
+    for (int i = 0;; ++i) {
+      const int t = nth_tile(count, worker, workers, i);
+      if (t < 0) break;
       const Tile r = tile_at<CG, NT, MODE>(a, count, n, t);
       const int as = j & 1;
+      const int first = r.l0 + (int)rank * BM + q * 32, row = first + lane;
+      // logits: this warp's columns of the tile; the row's entries there and its coefficients, before the accumulator is waited for
+      const int half = MODE == PRODUCTS ? NT / 2 : ((a.width + 63) >> 6) << 5, from = part ? half : 0, to = MODE == PRODUCTS || !part ? half : a.width;
+      const bool live = row < n;
+      Walk w;
+      RowCoef rc = {0.f, 0.f, 0.f, 0.f};
+      int64_t entries = 0;
+      if (MODE != PRODUCTS) {
+        w.none();
+        if (live) {
+          if (MODE == GRAD) rc = a.coef[row];
+          entries = (int64_t)a.src[row] * a.top;
+          w.start(a.entry + entries, a.top, a.col0 + r.c0 + from);
+        }
+      }
       if (r.chunks) {
         bool have = wait(&acc_full[as], (uint32_t)((j >> 1) & 1), abort_flag);
         have = __all_sync(0xffffffffu, have);
@@ -387,36 +445,22 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
       const uint32_t acc = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(as * NT);
-      const int first = r.l0 + (int)rank * BM + q * 32, row = first + lane;
       if (MODE == STATS) {
-        const int half = ((a.width + 63) >> 6) << 5, from = part ? half : 0, to = part ? a.width : half;
         if (first < n) {
           const int64_t at = (int64_t)(r.part * 2 + part) * a.rpad + row;
-          statistics(a, acc, r.c0, from, to, a.cols, row, row < n, a.part + at, a.part_y ? a.part_y + at : nullptr);
+          statistics(a, acc, r.c0, from, to, a.cols, live, w, a.y_entry + entries, a.part + at, a.part_y ? a.part_y + at : nullptr);
         }
       } else if (MODE == GRAD) {
         if (first < padded) {
-          const bool live = row < n;
-          RowCoef rc = {0.f, 0.f, 0.f, 0.f};
-          Walk w;
-          w.none();
-          const float* p = a.p;
-          const int half = CG == 2 ? NT / 2 : ((a.width + 63) >> 6) << 5, from = part ? half : 0, to = part ? a.width : half;
           const int limit = min(a.cols, r.c0 + a.width), shift = a.col0;
-          if (live) {
-            rc = a.coef[row];
-            const int64_t entries = (int64_t)a.src[row] * a.top;
-            p += entries;
-            w.start(a.id + entries, a.top, shift + r.c0 + from);
-          }
           if (CG == 2) {
 #pragma unroll 1
             for (int c = from; c < to; c += 64) {
               const int x = r.c0 + c;
               if (x >= a.cols) break;
               uint32_t lo[16], hi[16];
-              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(x + 32, limit), live, rc, p, w, lo);
-              coefficients<T>(a, acc + (uint32_t)(c + 32), shift + x + 32, shift + max(x + 32, min(x + 64, limit)), live, rc, p, w, hi);
+              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(x + 32, limit), live, rc, w, lo);
+              coefficients<T>(a, acc + (uint32_t)(c + 32), shift + x + 32, shift + max(x + 32, min(x + 64, limit)), live, rc, w, hi);
               if (lane == 0) bulk_wait_read();
               __syncwarp();
 #pragma unroll
@@ -435,7 +479,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
               const int x = r.c0 + c;
               if (x >= a.cols) break;
               uint32_t v[16];
-              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(min(x + 32, r.c0 + to), limit), live, rc, p, w, v);
+              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(min(x + 32, r.c0 + to), limit), live, rc, w, v);
               if (row < padded) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -448,7 +492,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
         const int x0 = r.c0 + part * (NT / 2);
         if (!r.trans || IsF32<TO>::value) {
           const float f = r.trans ? dw_scale : 1.f;
-          const bool wanted = r.trans ? first < a.cols : first < n;
+          const bool wanted = r.trans ? first < a.cols : first < n && r.chunks;   // the last piece may be shorter than its parts are many
           if (wanted) {
 #pragma unroll 1
             for (int c = 0; c < NT / 2; c += 32) {
@@ -468,8 +512,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
                 __syncwarp();
                 if (lane == 0) {
                   if (r.trans) store_2d(&tm.m[M_DW], mine, x0 + c, a.col0 + first);
-                  else if (a.add) add_2d(&tm.m[M_DX], mine, x0 + c, (int)((int64_t)r.part * a.rpad) + first);
-                  else store_2d(&tm.m[M_DX], mine, x0 + c, (int)((int64_t)r.part * a.rpad) + first);
+                  else if (a.add) add_2d(&tm.m[M_DX], mine, x0 + c, r.part * split_rows + first);
+                  else store_2d(&tm.m[M_DX], mine, x0 + c, r.part * split_rows + first);
                   bulk_commit();
                 }
               } else {       // rows of dW that do not start on 16-byte boundaries
@@ -596,7 +640,7 @@ static void common_args(Args& a, const Shape& s, const Buffers& b) {
   a.type_bits = s.dtype == BETTY_BF16 ? (1u << 7 | 1u << 10) : 0u;
   a.d = s.d; a.rpad = s.rpad;
   a.width = s.width; a.c2 = s.c2; a.top = s.top;
-  a.src = b.src; a.id = b.id; a.p = b.p;
+  a.src = b.src; a.entry = b.entry;
   // the row tiles whose copies of x are taken together stay in L2 while W streams past them: 32 MB of it
   const int64_t tile_bytes = (s.pairs ? 256 : 128) * s.dp * 2;
   a.band = (int)(tile_bytes >= (32 << 20) ? 1 : (32 << 20) / tile_bytes);
@@ -633,12 +677,12 @@ static betty_status launch_grad(cudaStream_t stream, const Shape& s, const Maps&
 template <typename TO>
 static betty_status launch_products(cudaStream_t stream, const Shape& s, const Maps& tm, const Args& a) {
   const int lanes = s.product_pairs ? 256 : 128, nt = lanes;
-  const int64_t tiles = (a.want_dx ? div_up(s.rows, lanes) * s.split : 0) * div_up(s.d, nt) + (a.want_dw ? div_up(a.cols, lanes) * div_up(s.d, nt) : 0);
+  const int64_t tiles = ((a.want_dx ? s.sum_rows / lanes : 0) + (a.want_dw ? div_up(a.cols, lanes) : 0)) * div_up(s.d, nt);
   if (s.product_pairs) return launch<2, 256, PRODUCTS, __nv_bfloat16, TO>(stream, tm, a, tiles);
   return launch<1, 128, PRODUCTS, __nv_bfloat16, TO>(stream, tm, a, tiles);
 }
 
-betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, bool want_dx, void* dw, int64_t lddw, int dw_dtype) {
+betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, void* dw, int64_t lddw, int dw_dtype) {
   const CUtensorMapDataType type = s.dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   Maps lm, pm;
   Args la = {}, pa = {};
@@ -648,7 +692,7 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
   if (!map_rows(&lm.m[M_DZ_OUT], type, 2, b.dz, s.piece, s.rpad, s.piece, 64, 32)) return BETTY_ERR_CUDA;
 
   common_args(pa, s, b);
-  pa.want_dx = want_dx; pa.want_dw = dw != nullptr; pa.split = s.split;
+  pa.want_dx = s.want_dx; pa.want_dw = s.want_dw;
   pa.w_blocked = w.cols % 64 == 0;
   pa.dw = dw; pa.lddw = lddw;
   const int a_box = s.product_pairs ? 128 : box_rows_of(s.rows);
@@ -657,7 +701,7 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
   bool ok = make_blocked_map(&pm.m[M_DZ_T], s.dtype, dz, false) && make_blocked_map(&pm.m[M_X_T], s.dtype, x, false);
   ok = ok && (pa.w_blocked ? make_blocked_map(&pm.m[M_W_T], s.dtype, w, false) : make_map(&pm.m[M_W_T], s.dtype, w, false, 64, BK));
   pm.m[M_DX] = pm.m[M_DW] = pm.m[M_DZ_T];
-  if (want_dx) ok = ok && map_rows(&pm.m[M_DX], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, b.dx, s.dp, s.rpad * s.split, s.dp, 32, 32);
+  if (s.want_dx) ok = ok && map_rows(&pm.m[M_DX], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, b.dx, s.dp, s.sum_rows, s.dp, 32, 32);
   const int ob = dw_dtype == BETTY_F32 ? 4 : 2;
   if (s.vocab == 1) lddw = pad8(s.d);            // a stride that is never used still has to be a valid one
   if (dw && (aligned16(dw) && (lddw * ob) % 16 == 0)) {
@@ -680,7 +724,7 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
 }
 
 // Which tiles, and how much of the vocabulary at a time.
-void choose_shape(Shape& s, bool backward, bool want_dx, bool want_dw) {
+void choose_shape(Shape& s, bool backward) {
   const int64_t sms = current_sm_count(), rows = s.rows < 1 ? 1 : s.rows;
   s.piece = (int)(div_up(s.vocab, 256) * 256);
   if (backward) {
@@ -697,18 +741,18 @@ void choose_shape(Shape& s, bool backward, bool want_dx, bool want_dw) {
     const int64_t cost = div_up(div_up(rows, 128) * div_up(cols, w), sms) * (w + 16) * (rows > 128 ? 5 : 4) / 4;
     if (cost < best) { best = cost; s.pairs = 0; s.width = w; }
   }
-  s.split = 1;
   s.product_pairs = 0;
+  s.sum_rows = s.rpad;
   if (!backward) return;
-  const int64_t pair_tiles = div_up(s.d, 256) * ((want_dx ? div_up(rows, 256) : 0) + (want_dw ? div_up(s.piece, 256) : 0));
+  const int64_t pair_tiles = div_up(s.d, 256) * ((s.want_dx ? div_up(rows, 256) : 0) + (s.want_dw ? div_up(s.piece, 256) : 0));
   s.product_pairs = rows > 128 && pair_tiles * 2 >= sms / 2;
-  if (want_dx) {           // few tiles with long contractions: parts of them, of 8 chunks or more
-    const int lanes = s.product_pairs ? 256 : 128;
-    const int64_t tiles = div_up(rows, lanes) * div_up(s.d, lanes), workers = s.product_pairs ? sms / 2 : sms, chunks = div_up(cols, BK);
-    int64_t split = workers / tiles;
-    if (split > chunks / 8) split = chunks / 8;
-    s.split = (int)(split < 1 ? 1 : split);
-  }
+  // dX with few rows: room for parts of its contraction, of 8 chunks or more, that are up to two tiles for each worker (k_rows
+  // chooses their number once the rows are counted)
+  const int lanes = s.product_pairs ? 256 : 128;
+  const int64_t tiles = div_up(rows, lanes) * div_up(s.d, lanes), workers = s.product_pairs ? sms / 2 : sms;
+  int64_t parts = div_up(2 * workers, tiles);
+  if (parts > div_up(cols, BK) / 8) parts = div_up(cols, BK) / 8;
+  s.sum_rows = s.rpad * (parts < 1 ? 1 : parts);
 }
 
 }  // namespace vocab
