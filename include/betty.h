@@ -453,7 +453,7 @@ betty_status betty_grouped_workspace_size(const betty_grouped_cfg* cfg, int64_t 
  * Conventions as for the residual block's operators above; the losses are one number per row, so that a problem
  * above can weigh the rows (the row losses are then the gradient by the weights, and dloss the weights). */
 typedef struct {
-  int64_t vocab, d;      /* W is [vocab, d]; 1 .. 2^22 and 1 .. 2^16 */
+  int64_t vocab, d;      /* W is [vocab, d]; 1 .. 2^22 - 1 and 1 .. 2^16 */
   int32_t dtype;         /* X and W: BETTY_BF16 or BETTY_F16; fp32 accumulation */
   float temperature;     /* T in [1e-30, 1e30] */
   float smoothing;       /* e in [0, 1]: share of the label that is spread over the whole vocabulary (cross entropy only) */

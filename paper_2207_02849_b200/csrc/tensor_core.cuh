@@ -167,8 +167,51 @@ static inline bool make_blocked_map(CUtensorMap* tm, int dtype, const Operand& o
 
 static inline int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
 
+// Copies a [rows, cols] matrix of 16-bit values to rows of `ld` values (a multiple of 8, from a 16-byte boundary), which is
+// what TMA reads; used for operands whose own rows do not start on 16-byte boundaries.  A warp takes a row at a time and a lane
+// four values: as 32-bit words where the row starts on a 4-byte boundary, else as the words around them, shifted together
+// (never outside the row: its ends go value by value).  Blocks of 256 threads.
+struct AlignRows {
+  const uint16_t* src; int64_t ld_src, rows_per_group, group_stride, rows; int cols;
+  uint16_t* dst; int ld;
+};
+__device__ __forceinline__ void align_rows(const AlignRows& a, int64_t block, int64_t blocks) {
+  const int lane = threadIdx.x & 31, cols = a.cols, ld = a.ld;
+  constexpr int U = 4;
+  for (int64_t row = block * 8 + (threadIdx.x >> 5); row < a.rows; row += blocks * 8) {
+    const uint16_t* p = a.rows_per_group == a.rows ? a.src + row * a.ld_src
+                                                   : a.src + (row / a.rows_per_group) * a.group_stride + (row % a.rows_per_group) * a.ld_src;
+    uint16_t* q = a.dst + row * ld;
+    const bool odd = (uintptr_t)p & 2;
+    for (int c0 = lane * 4; c0 < ld; c0 += 128 * U) {
+      uint2 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + 128 * u;
+        v[u] = make_uint2(0u, 0u);
+        if (!odd && c + 4 <= cols) {
+          v[u] = make_uint2(*(const uint32_t*)(p + c), *(const uint32_t*)(p + c + 2));
+        } else if (odd && c > 0 && c + 5 <= cols) {
+          const uint32_t x = *(const uint32_t*)(p + c - 1), y = *(const uint32_t*)(p + c + 1), z = *(const uint32_t*)(p + c + 3);
+          v[u] = make_uint2(__funnelshift_r(x, y, 16), __funnelshift_r(y, z, 16));
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (c + k < cols) (k < 2 ? v[u].x : v[u].y) |= (uint32_t)p[c + k] << (16 * (k & 1));
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + 128 * u < ld) *(uint2*)(q + c0 + 128 * u) = v[u];
+    }
+  }
+}
+
 // The operand itself, or its rows copied to 16-byte boundaries in the workspace (align.cu).
 betty_status align_operand(cudaStream_t stream, Arena& arena, Operand& o);
+// The same without the launch: o becomes the copy that align_rows(a) still has to make (a.rows == 0: none).
+betty_status plan_alignment(Arena& arena, Operand& o, AlignRows& a);
+int64_t align_blocks(const AlignRows& a);
 
 }  // namespace tc
 }  // namespace betty

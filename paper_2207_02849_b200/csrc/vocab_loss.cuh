@@ -65,10 +65,11 @@ struct Buffers {
   int32_t* pos;          // [rows] where a row went, -1: left out
   uint16_t* x;           // [rpad, dp]
   uint16_t* x_dw;        // [rpad, dp] as the gradient of W takes it (fp16: scaled, else x itself)
-  int2* entry;           // [rows, top] entries: id, and the bits of p
+  int2* entry;           // [rpad, top] entries of the rows that count: id, and the bits of p
+  int2* entry_in;        // [rows, top] the same of all rows (distillation)
   float2* part;          // [parts][rpad] maximum and sum of 2^(y - maximum) of a part of a row
   float* part_y;         // [parts][rpad] sum of y (smoothing only)
-  float* y_entry;        // [rows, top] y at the entries
+  float* y_entry;        // [rpad, top] y at the entries
   RowCoef* coef;         // [rpad]
   float* row_scale;      // [rpad] what a row of dX is multiplied by
   uint16_t* dz;          // [rpad, piece]
@@ -77,10 +78,10 @@ struct Buffers {
 };
 
 int logits_parts(const Shape& s);
-// part, part_y (if not null) and y_entry of all rows that count
-betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w);
+// part, part_y (if not null) and y_entry of all rows that count; w_ahead: w is not written by the kernels of this call
+betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, bool w_ahead);
 // dX's fp32 sums (want_dx) and dW (dw not null), piece by piece
-betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, void* dw, int64_t lddw, int dw_dtype);
+betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, bool w_ahead, void* dw, int64_t lddw, int dw_dtype);
 void choose_shape(Shape& s, bool backward);
 
 }  // namespace vocab

@@ -44,9 +44,10 @@ struct Args {
   int64_t rpad;
   // logits
   int width, band;         // columns of a tile; row tiles that are taken together
+  int ahead;               // W may be asked for before the kernels before this one are done
   float c2;
   int top;
-  const int32_t* src; const int2* entry;
+  const int2* entry;
   float2* part; float* part_y; float* y_entry;
   const RowCoef* coef;
   uint16_t* dz; int64_t ldz;
@@ -138,37 +139,53 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
 }
 
 // ------------------------------------------------------------------ epilogues
-// A row's entries in ascending order of id, from the first at or behind a column.  The next AHEAD of them are in registers: they are
-// asked for before the accumulator is waited for, and a step asks for the one that is needed AHEAD steps later.
+// A row's entries in ascending order of id, from the first at or behind a column; the next AHEAD of them are in registers.  They are
+// asked for together, before the accumulator is waited for: an entry that is asked for when it is needed costs a warp its
+// latency (a list that was refilled at each step: 8192 rows, 128 entries, 32000 x 2048: 268 us instead of 181 for 8192 columns).
 struct Walk {
-  static constexpr int AHEAD = 3;
+  static constexpr int AHEAD = 4;
   const int2* entry;
-  int at, end;
+  int at, end, left;       // place of q[0]; entries in q
   int2 q[AHEAD];
-  __device__ __forceinline__ int2 get(int i) const { return i < end ? entry[i] : make_int2(NO_ID, 0); }
+  __device__ __forceinline__ void fill() {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) q[i] = at + i < end ? entry[at + i] : make_int2(NO_ID, 0);
+    left = AHEAD;
+  }
+  // the first entry at or behind the column: eight places are looked at at a time
   __device__ __forceinline__ void start(const int2* entries, int top, int column) {
     entry = entries; end = top;
-    int lo = 0, hi = top;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (entry[mid].x < column) lo = mid + 1; else hi = mid;
+    int lo = 0, len = top > 1 ? top : 0;
+    while (len > 0) {
+      const int step = (len + 7) >> 3;
+      int below = 0;
+#pragma unroll
+      for (int k = 1; k <= 8; ++k)
+        if (k * step <= len) below += entry[lo + k * step - 1].x < column;
+      const int stop = lo + len;
+      lo += below * step;
+      len = min(step - 1, stop - lo);
     }
     at = lo;
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) q[i] = get(at + i);
+    fill();
+    if (top == 1 && q[0].x < column) q[0].x = NO_ID;
   }
   __device__ __forceinline__ void none() {
-    entry = nullptr; at = end = 0;
+    entry = nullptr; at = end = 0; left = AHEAD;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) q[i] = make_int2(NO_ID, 0);
   }
   __device__ __forceinline__ int next() const { return q[0].x; }
   __device__ __forceinline__ float share() const { return __int_as_float(q[0].y); }
   __device__ __forceinline__ void step() {
-#pragma unroll
-    for (int i = 0; i + 1 < AHEAD; ++i) q[i] = q[i + 1];
-    q[AHEAD - 1] = get(at + AHEAD);
     ++at;
+    if (--left == 0) {
+      fill();
+    } else {
+#pragma unroll
+      for (int i = 0; i + 1 < AHEAD; ++i) q[i] = q[i + 1];
+      q[AHEAD - 1].x = NO_ID;
+    }
   }
 };
 
@@ -188,6 +205,9 @@ __device__ __forceinline__ void store_2d(const CUtensorMap* tm, uint32_t from, i
 __device__ __forceinline__ void add_2d(const CUtensorMap* tm, uint32_t from, int x, int y) {
   asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(from), "r"(x), "r"(y) : "memory");
 }
+__device__ __forceinline__ void prefetch_2d(const CUtensorMap* tm, int x, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global [%0, {%1, %2}];" ::"l"(tm), "r"(x), "r"(y) : "memory");
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
@@ -195,6 +215,20 @@ __device__ __forceinline__ void to_async_proxy() { asm volatile("fence.proxy.asy
 // 16 bytes of a row of 128 in the layout of a 128-byte swizzle
 __device__ __forceinline__ void stage16(uint32_t rows, int row, int j, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(rows + (uint32_t)(row * 128 + ((j ^ (row & 7)) << 4))), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// v[i] for an i of 0 .. 31 that differs by lane (any value for others): a tree of selections, since registers have no index and an
+// array in memory costs a store of all of it
+__device__ __forceinline__ float pick(const uint32_t (&v)[32], int i) {
+  uint32_t w[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) w[k] = i & 16 ? v[k + 16] : v[k];
+#pragma unroll
+  for (int half = 8; half; half >>= 1) {
+#pragma unroll
+    for (int k = 0; k < half; ++k) w[k] = i & half ? w[k + half] : w[k];
+  }
+  return __uint_as_float(w[0]);
 }
 
 // Columns [from, to) of a tile (its accumulator at `acc`, its first column of the vocabulary `c0`) to a row's statistics.
@@ -230,10 +264,7 @@ __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, 
       sum += (y[0] + y[1]) + (y[2] + y[3]);
     }
     while (__any_sync(0xffffffffu, w.next() < end)) {
-      float z = 0.f;
-#pragma unroll
-      for (int k = 0; k < 32; ++k)
-        if (w.next() - cb == k) z = __uint_as_float(v[k]);
+      const float z = pick(v, w.next() - cb);
       if (w.next() < end) {
         y_entry[w.at] = z * a.c2;
         w.step();
@@ -255,9 +286,9 @@ __device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb
   for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(fmaf(rc.a, exp2f(fmaf(__uint_as_float(v[k]), a.c2, -rc.lse2)), rc.b));
   while (__any_sync(0xffffffffu, w.next() < end)) {
     const float e = rc.e * w.share();
+    const int at = w.next() - cb;
 #pragma unroll
-    for (int k = 0; k < 32; ++k)
-      if (w.next() - cb == k) v[k] = __float_as_uint(__uint_as_float(v[k]) - e);
+    for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) - (at == k ? e : 0.f));
     if (w.next() < end) w.step();
   }
   if (end < cb + 32 || !live) {
@@ -310,7 +341,14 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
   }
-  pdl_enter();             // global memory is touched from here on
+  if (MODE != PRODUCTS && a.ahead && warp == 1 && elect_one()) {
+    // a single row tile: which columns this CTA begins with does not depend on the count of rows, and W is not written by the kernels
+    // before this one: its first tile is on the way to L2 while they run
+    const int c = worker * a.width;
+    if (c < a.cols)
+      for (int k = 0; k < a.d; k += BK) prefetch_2d(&tm.m[M_W], k, a.col0 + c + (int)rank * (a.width / CG));
+  }
+  pdl_enter();             // global memory is written, and read otherwise, from here on
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
   if (CG == 2) cluster_sync_all();     // the other's barriers exist before anything is signalled across the cluster
@@ -434,7 +472,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
         w.none();
         if (live) {
           if (MODE == GRAD) rc = a.coef[row];
-          entries = (int64_t)a.src[row] * a.top;
+          entries = (int64_t)row * a.top;
           w.start(a.entry + entries, a.top, a.col0 + r.c0 + from);
         }
       }
@@ -640,7 +678,7 @@ static void common_args(Args& a, const Shape& s, const Buffers& b) {
   a.type_bits = s.dtype == BETTY_BF16 ? (1u << 7 | 1u << 10) : 0u;
   a.d = s.d; a.rpad = s.rpad;
   a.width = s.width; a.c2 = s.c2; a.top = s.top;
-  a.src = b.src; a.entry = b.entry;
+  a.entry = b.entry;
   // the row tiles whose copies of x are taken together stay in L2 while W streams past them: 32 MB of it
   const int64_t tile_bytes = (s.pairs ? 256 : 128) * s.dp * 2;
   a.band = (int)(tile_bytes >= (32 << 20) ? 1 : (32 << 20) / tile_bytes);
@@ -655,13 +693,14 @@ static betty_status logits_maps(Maps& tm, Args& a, const Shape& s, const Buffers
   return BETTY_OK;
 }
 
-betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w) {
+betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, bool w_ahead) {
   Maps tm;
   Args a = {};
   common_args(a, s, b);
   a.cols = s.vocab;
   a.part = b.part; a.part_y = b.part_y; a.y_entry = b.y_entry;
   BETTY_TRY(logits_maps(tm, a, s, b, w));
+  a.ahead = w_ahead && s.rows <= 128;
   const int64_t tiles = div_up(s.rows, s.pairs ? 256 : 128) * div_up(s.vocab, s.width);
   // the operands' type is in the instruction descriptor: nothing else of the statistics depends on it
   if (s.pairs) return launch<2, 256, STATS, __nv_bfloat16, float>(stream, tm, a, tiles);
@@ -682,7 +721,7 @@ static betty_status launch_products(cudaStream_t stream, const Shape& s, const M
   return launch<1, 128, PRODUCTS, __nv_bfloat16, TO>(stream, tm, a, tiles);
 }
 
-betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, void* dw, int64_t lddw, int dw_dtype) {
+betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, bool w_ahead, void* dw, int64_t lddw, int dw_dtype) {
   const CUtensorMapDataType type = s.dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   Maps lm, pm;
   Args la = {}, pa = {};
@@ -714,6 +753,7 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
     la.col0 = pa.col0 = c;
     la.cols = pa.cols = s.vocab - c < s.piece ? s.vocab - c : s.piece;
     pa.add = c > 0;
+    la.ahead = w_ahead && s.rows <= 128 && c == 0;
     // columns behind the vocabulary's last are not in the map: the contraction reads zeros there
     if ((c == 0 || pa.cols < s.piece) && !map_rows(&pm.m[M_DZ], type, 2, b.dz, pa.cols, s.rpad, s.piece, BK, a_box)) return BETTY_ERR_CUDA;
     BETTY_TRY(s.dtype == BETTY_BF16 ? launch_grad<__nv_bfloat16>(stream, s, lm, la) : launch_grad<__half>(stream, s, lm, la));
