@@ -211,6 +211,9 @@ __device__ int choose_split(const RowArgs& a, int n) {
   const Products p = products_of(n, a.d, a.cols, a.lanes);
   const int most = min((int)(a.sum_rows / max(1, p.row_tiles * a.lanes)), max(1, p.dx_chunks / 8));
   const int tiles = p.row_tiles * p.d_tiles;
+  // one tile of rows: W streams past it once, and that is the time; all workers take part in it, in one round (24 rows, 32000 x 2048
+  // in 3 / 6 / 9 / 12 parts: 98.5 / 92.9 / 91.9 / 95.7 us; 8 rows, 128000 x 4096 in 3 / 4 / 6: 579 / 558 / 619)
+  if (p.row_tiles == 1) return min(most, max(1, a.workers / tiles));
   const float second = a.want_dw ? (float)p.col_tiles * p.d_tiles * dw_cost(p) : 0.f;
   const float part = (float)n * a.dp * (a.lanes == 256 ? 3.6e-6f : 7e-6f);      // 8 bytes a value at 6 TB/s, chunks of 0.37 (0.19) us
   int best = 1;

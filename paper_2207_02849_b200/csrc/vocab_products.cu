@@ -61,6 +61,7 @@ struct Args {
 struct Tile {
   int trans;               // A is dz^T
   int l0, c0;              // first lane (row, or column of the piece), first column (of the piece, or of d)
+  int width;               // columns of the instruction
   int k0, chunks;          // contraction
   int part;                // split of dX's contraction, or column tile of the logits
 };
@@ -114,12 +115,14 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
     r.part = in / height;
     r.l0 = (band * a.band + in - r.part * height) * (BM * CG);
     r.c0 = r.part * a.width;
+    r.width = a.width;
     r.k0 = 0;
     r.chunks = (a.d + BK - 1) / BK;
   } else if (t < c.first) {
     const int rest = t / c.d_tiles, chunks = (a.cols + BK - 1) / BK;
     r.trans = 0;
     r.c0 = (t - rest * c.d_tiles) * NT;
+    r.width = a.d - r.c0 > NT / 2 ? NT : NT / 2;         // blocks of 64 columns in each CTA
     r.part = rest % c.split;
     r.l0 = rest / c.split * (BM * CG);
     const int k = (int)((int64_t)r.part * chunks / c.split);
@@ -130,6 +133,7 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
     const int rest = t / c.d_tiles;
     r.trans = 1;
     r.c0 = (t - rest * c.d_tiles) * NT;
+    r.width = a.d - r.c0 > NT / 2 ? NT : NT / 2;
     r.part = 0;
     r.l0 = rest * (BM * CG);
     r.k0 = 0;
@@ -371,7 +375,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       const Tile r = tile_at<CG, NT, MODE>(a, count, n, t);
       const int trans = uniform(r.trans), chunks = uniform(r.chunks), k0 = uniform(r.k0);
       const int l = uniform(r.l0) + (int)rank * BM;
-      const int c = MODE == PRODUCTS ? uniform(r.c0) + (int)rank * (NT / CG) : a.col0 + uniform(r.c0) + (int)rank * (a.width / CG);
+      const int c = (MODE == PRODUCTS ? 0 : a.col0) + uniform(r.c0) + (int)rank * (uniform(r.width) / CG);
       const uint32_t bytes = CG * ((trans ? (uint32_t)A_BYTES : a.a_bytes) + a.b_bytes);
       for (int it = 0; it < chunks; ++it) {
         if (round && !__all_sync(0xffffffffu, wait(&empty[s], (round - 1) & 1u, abort_flag))) { ok = false; break; }
@@ -412,8 +416,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     const uint64_t a_rows = smem_desc(sa0, 16, 1024), a_cols = smem_desc(sa0, 8192, 1024);
     const uint64_t b0 = MODE == PRODUCTS ? smem_desc(sb0, 8192, 1024) : smem_desc(sb0, 16, 1024);
     constexpr uint32_t b_step = MODE == PRODUCTS ? 2048 >> 4 : 32 >> 4;
-    const uint32_t fixed = 1u << 4 | a.type_bits | (MODE == PRODUCTS ? 1u << 16 : 0u) | (uint32_t)(BM * CG / 16) << 24 |
-                           (uint32_t)((MODE == PRODUCTS ? NT : a.width) >> 3) << 17;
+    const uint32_t fixed = 1u << 4 | a.type_bits | (MODE == PRODUCTS ? 1u << 16 : 0u) | (uint32_t)(BM * CG / 16) << 24;
     const uint32_t tmem_u = (uint32_t)uniform((int)tmem_base);
     int s = 0, j = 0;
     uint32_t round = 0, stage_off = 0;
@@ -427,7 +430,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       const int as = j & 1;
       if (j >= 2 && !__all_sync(0xffffffffu, wait(&acc_empty[as], (uint32_t)(((j >> 1) - 1) & 1), abort_flag))) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t acc = tmem_u + (uint32_t)(as * NT), idesc = fixed | (uint32_t)trans << 15;
+      const uint32_t acc = tmem_u + (uint32_t)(as * NT), idesc = fixed | (uint32_t)trans << 15 | (uint32_t)(uniform(r.width) >> 3) << 17;
       const uint64_t a0 = trans ? a_cols : a_rows;
       const uint32_t a_step = trans ? 2048 >> 4 : 32 >> 4;
       for (int it = 0; it < chunks; ++it) {
@@ -768,7 +771,9 @@ void choose_shape(Shape& s, bool backward) {
   const int64_t sms = current_sm_count(), rows = s.rows < 1 ? 1 : s.rows;
   s.piece = (int)(div_up(s.vocab, 256) * 256);
   if (backward) {
-    const int64_t most = (int64_t)1 << 26, fits = most / s.rpad / 256 * 256, piece = fits < 1024 ? 1024 : fits;
+    // coefficients of 256 MB: fewer, longer pieces have fewer ends and fewer additions to dX's sums (8192 x 65536 x 4096 in 16 / 8 / 4
+    // pieces: 9.38 / 9.17 / 9.27 ms; 1640 of 4096 rows x 32000 x 2048 in 4 / 2 / 1: 535 / 500 / 488 us)
+    const int64_t most = (int64_t)1 << 27, fits = most / s.rpad / 256 * 256, piece = fits < 1024 ? 1024 : fits;
     const int64_t pieces = div_up(s.vocab, piece);
     s.piece = (int)(div_up(div_up(s.vocab, pieces), 256) * 256);
   }
