@@ -167,10 +167,38 @@ static inline bool make_blocked_map(CUtensorMap* tm, int dtype, const Operand& o
 
 static inline int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
 
+// The values c .. c + 7 of a row of 16-bit values, zeros behind its last: the two 16-byte words around them, shifted together (never
+// outside the row: its ends go value by value).
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int c, int cols) {
+  uint32_t w[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+  const int m = (int)((uintptr_t)(row + c) & 15) >> 1;       // values of the first word that lie before c
+  if (m == 0 && c + 8 <= cols) return *(const uint4*)(row + c);
+  if (c >= m && c - m + 16 <= cols) {
+    const uint4 x = *(const uint4*)(row + c - m), y = *(const uint4*)(row + c - m + 8);
+    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; w[4] = y.x; w[5] = y.y; w[6] = y.z; w[7] = y.w;
+    if (m & 4) {
+#pragma unroll
+      for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+    }
+    if (m & 2) {
+#pragma unroll
+      for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+    }
+    if (m & 1) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (c + k < cols) w[k >> 1] |= (uint32_t)row[c + k] << (16 * (k & 1));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Copies a [rows, cols] matrix of 16-bit values to rows of `ld` values (a multiple of 8, from a 16-byte boundary), which is
 // what TMA reads; used for operands whose own rows do not start on 16-byte boundaries.  A warp takes a row at a time and a lane
-// four values: as 32-bit words where the row starts on a 4-byte boundary, else as the words around them, shifted together
-// (never outside the row: its ends go value by value).  Blocks of 256 threads.
+// eight values.  Blocks of 256 threads.
 struct AlignRows {
   const uint16_t* src; int64_t ld_src, rows_per_group, group_stride, rows; int cols;
   uint16_t* dst; int ld;
@@ -182,27 +210,13 @@ __device__ __forceinline__ void align_rows(const AlignRows& a, int64_t block, in
     const uint16_t* p = a.rows_per_group == a.rows ? a.src + row * a.ld_src
                                                    : a.src + (row / a.rows_per_group) * a.group_stride + (row % a.rows_per_group) * a.ld_src;
     uint16_t* q = a.dst + row * ld;
-    const bool odd = (uintptr_t)p & 2;
-    for (int c0 = lane * 4; c0 < ld; c0 += 128 * U) {
-      uint2 v[U];
+    for (int c0 = lane * 8; c0 < ld; c0 += 256 * U) {
+      uint4 v[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = c0 + 128 * u;
-        v[u] = make_uint2(0u, 0u);
-        if (!odd && c + 4 <= cols) {
-          v[u] = make_uint2(*(const uint32_t*)(p + c), *(const uint32_t*)(p + c + 2));
-        } else if (odd && c > 0 && c + 5 <= cols) {
-          const uint32_t x = *(const uint32_t*)(p + c - 1), y = *(const uint32_t*)(p + c + 1), z = *(const uint32_t*)(p + c + 3);
-          v[u] = make_uint2(__funnelshift_r(x, y, 16), __funnelshift_r(y, z, 16));
-        } else {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (c + k < cols) (k < 2 ? v[u].x : v[u].y) |= (uint32_t)p[c + k] << (16 * (k & 1));
-        }
-      }
+      for (int u = 0; u < U; ++u) v[u] = load8(p, c0 + 256 * u, cols);
 #pragma unroll
       for (int u = 0; u < U; ++u)
-        if (c0 + 128 * u < ld) *(uint2*)(q + c0 + 128 * u) = v[u];
+        if (c0 + 256 * u < ld) *(uint4*)(q + c0 + 256 * u) = v[u];
     }
   }
 }

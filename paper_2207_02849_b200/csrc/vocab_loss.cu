@@ -162,30 +162,11 @@ __device__ __forceinline__ void copy_row(const RowArgs& a, int64_t from, int64_t
   const uint16_t* in = a.x_in + from * a.ldx;
   uint16_t* out = a.x + to * a.dp;
   uint16_t* out2 = a.x_dw != a.x ? a.x_dw + to * a.dp : nullptr;
-  const bool aligned = ((uintptr_t)in & 15) == 0, odd = (uintptr_t)in & 2;
   constexpr int U = 4;                 // accesses in flight
   for (int c0 = lane * 8; c0 < a.dp; c0 += 256 * U) {
     uint4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int c = c0 + 256 * u;
-      v[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (aligned && c + 8 <= a.d) {
-        v[u] = *(const uint4*)(in + c);
-      } else if (!odd && c + 8 <= a.d) {
-        const uint32_t* w = (const uint32_t*)(in + c);
-        v[u] = make_uint4(w[0], w[1], w[2], w[3]);
-      } else if (odd && c > 0 && c + 9 <= a.d) {       // the words around the values, shifted together
-        const uint32_t* w = (const uint32_t*)(in + c - 1);
-        v[u] = make_uint4(__funnelshift_r(w[0], w[1], 16), __funnelshift_r(w[1], w[2], 16), __funnelshift_r(w[2], w[3], 16), __funnelshift_r(w[3], w[4], 16));
-      } else if (c < a.d) {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (c + k < a.d) w[k >> 1] |= (uint32_t)in[c + k] << (16 * (k & 1));
-        v[u] = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
+    for (int u = 0; u < U; ++u) v[u] = load8(in, c0 + 256 * u, a.d);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + 256 * u;
@@ -207,21 +188,27 @@ __device__ __forceinline__ void copy_row(const RowArgs& a, int64_t from, int64_t
 
 // Parts of dX's contraction, for which there is room: the number with which the workers finish soonest, where dX's tiles come
 // first and dW's fill up.  Times in chunks of a contraction; a part's sums are written and read again.
-__device__ int choose_split(const RowArgs& a, int n) {
+__device__ int choose_split(const RowArgs& a, int n) {           // a warp
   const Products p = products_of(n, a.d, a.cols, a.lanes);
   const int most = min((int)(a.sum_rows / max(1, p.row_tiles * a.lanes)), max(1, p.dx_chunks / 8));
   const int tiles = p.row_tiles * p.d_tiles;
   // one tile of rows: W streams past it once, and that is the time; all workers take part in it, in one round (24 rows, 32000 x 2048
   // in 3 / 6 / 9 / 12 parts: 98.5 / 92.9 / 91.9 / 95.7 us; 8 rows, 128000 x 4096 in 3 / 4 / 6: 579 / 558 / 619)
-  if (p.row_tiles == 1) return min(most, max(1, a.workers / tiles));
+  if (p.row_tiles <= 1) return min(most, max(1, a.workers / max(1, tiles)));
   const float second = a.want_dw ? (float)p.col_tiles * p.d_tiles * dw_cost(p) : 0.f;
   const float part = (float)n * a.dp * (a.lanes == 256 ? 3.6e-6f : 7e-6f);      // 8 bytes a value at 6 TB/s, chunks of 0.37 (0.19) us
   int best = 1;
   float least = INFINITY;
-  for (int s = 1; s <= most; ++s) {
+  for (int s = 1 + (threadIdx.x & 31); s <= most; s += 32) {
     const float first = (float)((tiles * s + a.workers - 1) / a.workers) * dx_cost(p, s);
     const float time = fmaxf(first, ((float)tiles * s * dx_cost(p, s) + second) / a.workers) + s * part;
     if (time < least) { least = time; best = s; }
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const float t = __shfl_xor_sync(0xffffffffu, least, o);
+    const int s = __shfl_xor_sync(0xffffffffu, best, o);
+    if (t < least || (t == least && s < best)) { least = t; best = s; }
   }
   return best;
 }
@@ -293,13 +280,12 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
     before += all;
   }
   if ((int)blockIdx.x == a.row_blocks - 1) {
-    if (tid == 0) {
-      a.meta->n = before;
-      a.meta->split = a.dloss && a.want_dx ? choose_split(a, before) : 1;
-      a.meta->dw_scale = a.fp16 && a.dloss ? ldexpf(1.f, -least) : 1.f;
+    if (warp == 0) {
+      const int split = a.dloss && a.want_dx ? choose_split(a, before) : 1;
+      if (lane == 0) { a.meta->n = before; a.meta->split = split; a.meta->dw_scale = a.fp16 && a.dloss ? ldexpf(1.f, -least) : 1.f; }
     }
-    if (a.dloss)                       // a contraction over the rows takes them 64 at a time
-      for (int64_t r = before + warp; r < (before + BK - 1) / BK * BK; r += 8)
+    if (a.dloss)                       // a contraction over the rows takes them 16 at a time
+      for (int64_t r = before + warp; r < (before + 15) / 16 * 16; r += 8)
         for (int c = lane * 8; c < a.dp; c += 256) {
           *(uint4*)(a.x + r * a.dp + c) = make_uint4(0u, 0u, 0u, 0u);
           if (a.x_dw != a.x) *(uint4*)(a.x_dw + r * a.dp + c) = make_uint4(0u, 0u, 0u, 0u);

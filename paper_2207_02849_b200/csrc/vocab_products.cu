@@ -346,11 +346,11 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     }
   }
   if (MODE != PRODUCTS && a.ahead && warp == 1 && elect_one()) {
-    // a single row tile: which columns this CTA begins with does not depend on the count of rows, and W is not written by the kernels
-    // before this one: its first tile is on the way to L2 while they run
-    const int c = worker * a.width;
-    if (c < a.cols)
-      for (int k = 0; k < a.d; k += BK) prefetch_2d(&tm.m[M_W], k, a.col0 + c + (int)rank * (a.width / CG));
+    // a single row tile: which columns this CTA takes does not depend on the count of rows, and W is not written by the kernels before
+    // this one: the first 512 KB are on the way to L2 while they run
+    int left = (512 << 10) / (a.width / CG * BK * 2);
+    for (int c = worker * a.width; c < a.cols; c += workers * a.width)
+      for (int k = 0; k < a.d && left > 0; k += BK, --left) prefetch_2d(&tm.m[M_W], k, a.col0 + c + (int)rank * (a.width / CG));
   }
   pdl_enter();             // global memory is written, and read otherwise, from here on
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -433,6 +433,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       const uint32_t acc = tmem_u + (uint32_t)(as * NT), idesc = fixed | (uint32_t)trans << 15 | (uint32_t)(uniform(r.width) >> 3) << 17;
       const uint64_t a0 = trans ? a_cols : a_rows;
       const uint32_t a_step = trans ? 2048 >> 4 : 32 >> 4;
+      // a contraction over the rows ends with the 16 that hold the last of them: what the copies behind those hold is not looked at
+      const int last = trans ? (n + 15) / 16 - (chunks - 1) * (BK / 16) : BK / 16;
       for (int it = 0; it < chunks; ++it) {
         if (!__all_sync(0xffffffffu, wait(&full[s], round & 1u, abort_flag))) { ok = false; break; }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -441,7 +443,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
         if (leader) {
           mma<CG>(acc, da, db, idesc, it ? 1u : 0u);
 #pragma unroll
-          for (int kk = 1; kk < BK / 16; ++kk) mma<CG>(acc, da + kk * a_step, db + kk * b_step, idesc, 1u);
+          for (int kk = 1; kk < BK / 16; ++kk)
+            if (kk < last || it + 1 < chunks) mma<CG>(acc, da + kk * a_step, db + kk * b_step, idesc, 1u);
           commit<CG>(done);
         }
         __syncwarp();
@@ -456,7 +459,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     const int q = warp & 3, part = (warp - 2) >> 2;
     const uint32_t mine = s_u32(staging) + (uint32_t)(warp - 2) * 4096u;
     const float dw_scale = MODE == PRODUCTS ? a.meta->dw_scale : 1.f;
-    const int padded = (n + BK - 1) / BK * BK;           // rows of dz that a contraction over the rows reads
+    const int padded = (n + 15) / 16 * 16;               // rows of dz that a contraction over the rows takes
     int j = 0;
     const int split_rows = count.row_tiles * (BM * CG);  // rows of one part of dX's sums
     for (int i = 0;; ++i) {
