@@ -129,18 +129,16 @@ struct RowArgs {
   AlignRows align; int row_blocks;             // the blocks behind row_blocks copy W to 16-byte boundaries, where that is needed
 };
 
-__device__ __forceinline__ bool counts(const RowArgs& a, int64_t i) {
-  bool live;
-  if (a.some) {
-    live = a.some[i] != 0;
-  } else {
-    const int64_t t = whole(a.target, a.id64, i);
-    live = t >= 0 && t < a.vocab;
-  }
-  return live && !(a.dloss && a.dloss[i] == 0.f);
+// What says whether a row counts: its target, or whether it has an entry, and its weight
+struct Mark { int64_t t; float g; };
+__device__ __forceinline__ Mark mark(const RowArgs& a, int64_t i) {
+  return {a.some ? (a.some[i] ? 0 : -1) : whole(a.target, a.id64, i), a.dloss ? a.dloss[i] : 1.f};
 }
+__device__ __forceinline__ bool counts(const RowArgs& a, const Mark& m) { return m.t >= 0 && m.t < a.vocab && !(m.g == 0.f); }
 // bound of a row's |dz|
-__device__ __forceinline__ float bound_of(const RowArgs& a, int64_t i) { return fabsf(a.dloss[i] * a.inv_t) * (1.f + 2.f * a.z_loss * fabsf(a.lse[i])); }
+__device__ __forceinline__ float bound_of(const RowArgs& a, int64_t i, float g) {
+  return fabsf(g * a.inv_t) * (a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * fabsf(a.lse[i]) : 1.f);
+}
 // exponent that brings a bound to [2^13, 2^14) (of bounds at the ends of the fp32 range: near it); of a bound that is zero or not
 // finite: none
 __device__ __forceinline__ int lift(float bound) {
@@ -194,7 +192,7 @@ __device__ int choose_split(const RowArgs& a, int n) {           // a warp
   const int tiles = p.row_tiles * p.d_tiles;
   // one tile of rows: W streams past it once, and that is the time; all workers take part in it, in one round (24 rows, 32000 x 2048
   // in 3 / 6 / 9 / 12 parts: 98.5 / 92.9 / 91.9 / 95.7 us; 8 rows, 128000 x 4096 in 3 / 4 / 6: 579 / 558 / 619)
-  if (p.row_tiles <= 1) return min(most, max(1, a.workers / max(1, tiles)));
+  if (p.row_tiles <= 1) return min(min(most, 32), max(1, a.workers / max(1, tiles)));
   const float second = a.want_dw ? (float)p.col_tiles * p.d_tiles * dw_cost(p) : 0.f;
   const float part = (float)n * a.dp * (a.lanes == 256 ? 3.6e-6f : 7e-6f);      // 8 bytes a value at 6 TB/s, chunks of 0.37 (0.19) us
   int best = 1;
@@ -225,15 +223,24 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t r0 = a.rows * blockIdx.x / a.row_blocks, r1 = a.rows * (blockIdx.x + 1) / a.row_blocks;
   int before = 0, least = NO_LIFT;
-  const int64_t seen = a.fp16 && a.dloss ? a.rows : r0;
-  for (int64_t i = tid; i < seen; i += ROW_THREADS)
-    if (counts(a, i)) {
-      before += i < r0;
-      if (a.fp16 && a.dloss) {
-        const float b = bound_of(a, i);
-        if (b > 0.f && b < INFINITY) least = min(least, lift(b));
+  const bool lifted = a.fp16 && a.dloss;
+  const int64_t seen = lifted ? a.rows : r0;
+  constexpr int U = 8;                 // rows in flight
+  for (int64_t i0 = tid; i0 < seen; i0 += ROW_THREADS * U) {
+    Mark m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) m[u] = i0 + u * ROW_THREADS < seen ? mark(a, i0 + u * ROW_THREADS) : Mark{-1, 0.f};
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (counts(a, m[u])) {
+        const int64_t i = i0 + u * ROW_THREADS;
+        before += i < r0;
+        if (lifted) {
+          const float b = bound_of(a, i, m[u].g);
+          if (b > 0.f && b < INFINITY) least = min(least, lift(b));
+        }
       }
-    }
+  }
   before = __reduce_add_sync(0xffffffffu, before);
   least = __reduce_min_sync(0xffffffffu, least);
   if (lane == 0) { counted[warp] = before; least_of[warp] = least; }
@@ -244,7 +251,8 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
   for (int64_t base = r0; base < r1; base += ROW_THREADS) {
     __syncthreads();                   // counted and list are free again
     const int64_t i = base + tid;
-    const bool live = i < r1 && counts(a, i);
+    const Mark m = i < r1 ? mark(a, i) : Mark{-1, 0.f};
+    const bool live = counts(a, m);
     const uint32_t votes = __ballot_sync(0xffffffffu, live);
     if (lane == 0) counted[warp] = __popc(votes);
     __syncthreads();
@@ -257,10 +265,10 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
         const int64_t to = before + at;
         list[at] = (int)(i - base);
         a.src[to] = (int32_t)i;
-        if (!a.some) a.entry[to] = make_int2((int32_t)whole(a.target, a.id64, i), __float_as_int(a.share));
+        if (!a.some) a.entry[to] = make_int2((int32_t)m.t, __float_as_int(a.share));
         if (a.dloss) {
-          const int h = a.fp16 ? row_lift(bound_of(a, i), least) : 0;
-          const float g = ldexpf(a.dloss[i] * a.inv_t, h), lse = a.lse[i];
+          const int h = a.fp16 ? row_lift(bound_of(a, i, m.g), least) : 0;
+          const float g = ldexpf(m.g * a.inv_t, h), lse = a.lse[i];
           a.coef[to] = {lse * LOG2E, g * (1.f + 2.f * a.z_loss * lse), -g * a.smoothing / (float)a.vocab, g};
           a.row_scale[to] = ldexpf(1.f, -h);
         }
@@ -272,7 +280,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
     __syncthreads();
     for (int k = warp; k < all; k += 8) {
       const int64_t from = base + list[k];
-      const float scale = a.fp16 && a.dloss ? ldexpf(1.f, least - row_lift(bound_of(a, from), least)) : 1.f;
+      const float scale = lifted && a.x_dw != a.x ? ldexpf(1.f, least - row_lift(bound_of(a, from, a.dloss[from]), least)) : 1.f;
       if (a.some)
         for (int j = lane; j < a.top; j += 32) a.entry[(before + k) * (int64_t)a.top + j] = a.entry_in[from * a.top + j];
       copy_row(a, from, before + k, scale);
@@ -282,7 +290,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
   if ((int)blockIdx.x == a.row_blocks - 1) {
     if (warp == 0) {
       const int split = a.dloss && a.want_dx ? choose_split(a, before) : 1;
-      if (lane == 0) { a.meta->n = before; a.meta->split = split; a.meta->dw_scale = a.fp16 && a.dloss ? ldexpf(1.f, -least) : 1.f; }
+      if (lane == 0) { a.meta->n = before; a.meta->split = split; a.meta->dw_scale = lifted ? ldexpf(1.f, -least) : 1.f; }
     }
     if (a.dloss)                       // a contraction over the rows takes them 16 at a time
       for (int64_t r = before + warp; r < (before + 15) / 16 * 16; r += 8)
@@ -383,15 +391,16 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
 }
 
 // ------------------------------------------------------------------ dX
-// Row i of dX from the parts' sums of its copy, or zeros: a block takes `width` columns of a row, a thread four at a time.
+// Row i of dX from the parts' sums of its copy, or zeros: blockDim.x threads take `width` columns of a row, four at a time each,
+// blockDim.y of them in a block of 256.
 template <typename T>
 __global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int lanes, int width, const Meta* meta, const int32_t* pos, const float* row_scale,
                                             const float* sums, T* dx, int64_t ld) {
   pdl_enter();
   const bool wide = ((uintptr_t)dx % (4 * sizeof(T))) == 0 && ld % 4 == 0;
-  const int strips = (d + width - 1) / width, split = meta->split;
+  const int strips = (d + width - 1) / width, split = meta->split, step = (int)blockDim.x * 4;
   const int64_t stride = (int64_t)((meta->n + lanes - 1) / lanes * lanes) * dp;
-  for (int64_t b = blockIdx.x; b < rows * strips; b += gridDim.x) {
+  for (int64_t b = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; b < rows * strips; b += (int64_t)gridDim.x * blockDim.y) {
     const int64_t row = b / strips;
     const int c0 = (int)(b - row * strips) * width, end = min(d, c0 + width);
     const int at = pos[row];
@@ -399,11 +408,11 @@ __global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int
     const float* in = sums + (int64_t)max(at, 0) * dp;
     T* out = dx + row * ld;
 #pragma unroll 4
-    for (int c = c0 + (int)threadIdx.x * 4; c < end; c += 1024) {
+    for (int c = c0 + (int)threadIdx.x * 4; c < end; c += step) {
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (at >= 0) {
         v = *(const float4*)(in + c);
-#pragma unroll 4
+#pragma unroll 8
         for (int s = 1; s < split; ++s) {
           const float4 w = *(const float4*)(in + s * stride + c);
           v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
@@ -589,15 +598,18 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   }
   BETTY_TRY(logits_gradients(stream, s, b, w, !copied, c.dW, c.lddw, c.dw_dtype));
   if (c.dX) {
-    const int width = c.rows < most ? 1024 : (int)s.dp;           // few rows: more blocks than rows
-    const int64_t strips = c.rows * ((cfg->d + width - 1) / width);
-    const dim3 grid((unsigned)(strips < most * 2 ? strips : most * 2));
+    // a row's threads: enough for one access each up to 256; few rows: more blocks than rows
+    int across = 32;
+    while (across < 256 && across * 4 < cfg->d) across *= 2;
+    const int width = c.rows < most ? across * 4 : (int)s.dp;
+    const int64_t strips = (c.rows * ((cfg->d + width - 1) / width) + 256 / across - 1) / (256 / across);
+    const dim3 grid((unsigned)(strips < most * 2 ? strips : most * 2)), block((unsigned)across, (unsigned)(256 / across));
     if (c.dx_dtype == BETTY_F32)
-      launch_pdl(k_dx<float>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (float*)c.dX, c.lddx);
+      launch_pdl(k_dx<float>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (float*)c.dX, c.lddx);
     else if (c.dx_dtype == BETTY_BF16)
-      launch_pdl(k_dx<__nv_bfloat16>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (__nv_bfloat16*)c.dX, c.lddx);
+      launch_pdl(k_dx<__nv_bfloat16>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (__nv_bfloat16*)c.dX, c.lddx);
     else
-      launch_pdl(k_dx<__half>, grid, dim3(256), 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (__half*)c.dX, c.lddx);
+      launch_pdl(k_dx<__half>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (__half*)c.dX, c.lddx);
     BETTY_LAUNCH_CHECK();
   }
   return BETTY_OK;

@@ -17,13 +17,12 @@ enum Mode { STATS = 0, GRAD = 1, PRODUCTS = 2 };
 
 static constexpr int THREADS = 320;           // warp 0: TMA, warp 1: MMA, warps 2-9: epilogue
 static constexpr int EPI_WARPS = 8;
-static constexpr int STAGING = EPI_WARPS * 4096;   // each epilogue warp: 32 rows of 128 bytes
+static constexpr int STAGING = EPI_WARPS * 4096;   // each epilogue warp: 32 rows of 128 bytes, for its entries and its results
 
 template <int CG, int NT, int MODE> struct Cfg {
   static constexpr int STAGE = A_BYTES + NT / CG * BK * 2;
-  static constexpr int OUT = MODE == STATS || (MODE == GRAD && CG == 1) ? 0 : STAGING;
-  static constexpr int STAGES = (229376 - OUT) / STAGE;
-  static constexpr int SMEM = STAGES * STAGE + OUT + 256 + 1024;
+  static constexpr int STAGES = (229376 - STAGING) / STAGE;
+  static constexpr int SMEM = STAGES * STAGE + STAGING + 256 + 1024;
   static constexpr int TMEM_COLS = 2 * NT;    // two accumulators: a tile drains while the next is multiplied
   static_assert(SMEM <= 227 * 1024 && NT / CG <= 128 && STAGES * 16 + 48 <= 256, "shared memory");
 };
@@ -221,23 +220,20 @@ __device__ __forceinline__ void stage16(uint32_t rows, int row, int j, uint32_t 
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(rows + (uint32_t)(row * 128 + ((j ^ (row & 7)) << 4))), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-// v[i] for an i of 0 .. 31 that differs by lane (any value for others): a tree of selections, since registers have no index and an
-// array in memory costs a store of all of it
-__device__ __forceinline__ float pick(const uint32_t (&v)[32], int i) {
-  uint32_t w[16];
-#pragma unroll
-  for (int k = 0; k < 16; ++k) w[k] = i & 16 ? v[k + 16] : v[k];
-#pragma unroll
-  for (int half = 8; half; half >>= 1) {
-#pragma unroll
-    for (int k = 0; k < half; ++k) w[k] = i & half ? w[k + half] : w[k];
-  }
-  return __uint_as_float(w[0]);
+// Registers have no index.  The entries among 32 columns go through the warp's staging, a lane's row each: the columns' values are put
+// there for the entries to pick theirs, or the entries' shares for the columns to subtract.  (Selecting them in registers, 31 or 64
+// instructions for the entries that the lanes have next: a fifth of the columns being entries, 10799 rows x 715 x 192: 132 us.)
+__device__ __forceinline__ uint32_t staged_at(uint32_t rows, int row, int k) { return rows + (uint32_t)(row * 128 + (((k >> 2) ^ (row & 7)) << 4) + (k & 3) * 4); }
+__device__ __forceinline__ float staged(uint32_t at) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
 }
 
 // Columns [from, to) of a tile (its accumulator at `acc`, its first column of the vocabulary `c0`) to a row's statistics.
 __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, int from, int to, int limit, bool live, Walk& w, float* y_entry, float2* part,
-                                           float* part_y) {
+                                           float* part_y, uint32_t mine) {
+  const int lane = threadIdx.x & 31;
   float m = -INFINITY, s = 0.f, sum = 0.f;
 #pragma unroll 1
   for (int c = from; c < to; c += 32) {
@@ -267,12 +263,14 @@ __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, 
       for (int k = 0; k < 32; ++k) y[k & 3] += cb + k < end ? __uint_as_float(v[k]) : 0.f;
       sum += (y[0] + y[1]) + (y[2] + y[3]);
     }
-    while (__any_sync(0xffffffffu, w.next() < end)) {
-      const float z = pick(v, w.next() - cb);
-      if (w.next() < end) {
-        y_entry[w.at] = z * a.c2;
+    if (__any_sync(0xffffffffu, w.next() < end)) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) stage16(mine, lane, k, v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+      while (w.next() < end) {
+        y_entry[w.at] = staged(staged_at(mine, lane, w.next() - cb)) * a.c2;
         w.step();
       }
+      __syncwarp();
     }
   }
   if (live) {
@@ -283,17 +281,32 @@ __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, 
 
 // 32 columns of a tile as coefficients of a row's gradient, packed in pairs; rows that do not count and columns that do not exist: 0
 template <typename T>
-__device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb, int end, bool live, const RowCoef& rc, Walk& w, uint32_t (&out)[16]) {
+__device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb, int end, bool live, const RowCoef& rc, Walk& w, uint32_t mine, uint32_t (&out)[16]) {
+  const int lane = threadIdx.x & 31;
   uint32_t v[32];
   tmem_load32(v, acc);
 #pragma unroll
   for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(fmaf(rc.a, exp2f(fmaf(__uint_as_float(v[k]), a.c2, -rc.lse2)), rc.b));
-  while (__any_sync(0xffffffffu, w.next() < end)) {
-    const float e = rc.e * w.share();
-    const int at = w.next() - cb;
+  if (__any_sync(0xffffffffu, w.next() < end)) {
+    if (lane == 0) bulk_wait_read();             // of the results that were staged there before
+    __syncwarp();
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) - (at == k ? e : 0.f));
-    if (w.next() < end) w.step();
+    for (int k = 0; k < 8; ++k) stage16(mine, lane, k, 0u, 0u, 0u, 0u);
+    while (w.next() < end) {
+      const uint32_t at = staged_at(mine, lane, w.next() - cb);
+      const float e = fmaf(rc.e, w.share(), staged(at));
+      asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(e) : "memory");
+      w.step();
+    }
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      float e[4];
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(e[0]), "=f"(e[1]), "=f"(e[2]), "=f"(e[3]) : "r"(staged_at(mine, lane, 4 * k)) : "memory");
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * k + i] = __float_as_uint(__uint_as_float(v[4 * k + i]) - e[i]);
+    }
+    __syncwarp();
   }
   if (end < cb + 32 || !live) {
 #pragma unroll
@@ -317,7 +330,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char* staging = smem + S * C::STAGE;
-  uint64_t* full = (uint64_t*)(staging + C::OUT);
+  uint64_t* full = (uint64_t*)(staging + STAGING);
   uint64_t* empty = full + S;
   uint64_t* acc_full = empty + S;
   uint64_t* acc_empty = acc_full + 2;
@@ -492,7 +505,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       if (MODE == STATS) {
         if (first < n) {
           const int64_t at = (int64_t)(r.part * 2 + part) * a.rpad + row;
-          statistics(a, acc, r.c0, from, to, a.cols, live, w, a.y_entry + entries, a.part + at, a.part_y ? a.part_y + at : nullptr);
+          statistics(a, acc, r.c0, from, to, a.cols, live, w, a.y_entry + entries, a.part + at, a.part_y ? a.part_y + at : nullptr, mine);
         }
       } else if (MODE == GRAD) {
         if (first < padded) {
@@ -503,8 +516,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
               const int x = r.c0 + c;
               if (x >= a.cols) break;
               uint32_t lo[16], hi[16];
-              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(x + 32, limit), live, rc, w, lo);
-              coefficients<T>(a, acc + (uint32_t)(c + 32), shift + x + 32, shift + max(x + 32, min(x + 64, limit)), live, rc, w, hi);
+              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(x + 32, limit), live, rc, w, mine, lo);
+              coefficients<T>(a, acc + (uint32_t)(c + 32), shift + x + 32, shift + max(x + 32, min(x + 64, limit)), live, rc, w, mine, hi);
               if (lane == 0) bulk_wait_read();
               __syncwarp();
 #pragma unroll
@@ -523,7 +536,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
               const int x = r.c0 + c;
               if (x >= a.cols) break;
               uint32_t v[16];
-              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(min(x + 32, r.c0 + to), limit), live, rc, w, v);
+              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(min(x + 32, r.c0 + to), limit), live, rc, w, mine, v);
               if (row < padded) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -626,7 +639,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
         ++j;
       }
     }
-    if (C::OUT && lane == 0) bulk_wait_all();
+    if (lane == 0) bulk_wait_all();
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
