@@ -154,14 +154,16 @@ __device__ __forceinline__ int row_lift(float bound, int least) {
   return h <= least + 6 ? least : h - 6;
 }
 
-// Copies a row to a 16-byte boundary, zeros behind it; a warp.  scale: 1, or a power of two for the second copy
-__device__ __forceinline__ void copy_row(const RowArgs& a, int64_t from, int64_t to, float scale) {
+// Copies a segment of a row to a 16-byte boundary, zeros behind the row's end; a warp.  scale: 1, or a power of two for the second copy
+static constexpr int SEGMENT = 1024;
+__device__ __forceinline__ void copy_segment(const RowArgs& a, int64_t from, int64_t to, int segment, float scale) {
   const int lane = threadIdx.x & 31;
   const uint16_t* in = a.x_in + from * a.ldx;
   uint16_t* out = a.x + to * a.dp;
   uint16_t* out2 = a.x_dw != a.x ? a.x_dw + to * a.dp : nullptr;
-  constexpr int U = 4;                 // accesses in flight
-  for (int c0 = lane * 8; c0 < a.dp; c0 += 256 * U) {
+  constexpr int U = SEGMENT / 256;     // accesses in flight
+  const int c0 = segment * SEGMENT + lane * 8;
+  {
     uint4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = load8(in, c0 + 256 * u, a.d);
@@ -215,6 +217,7 @@ __device__ int choose_split(const RowArgs& a, int n) {           // a warp
 __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
   __shared__ int counted[8], least_of[8];
   __shared__ int list[ROW_THREADS];
+  __shared__ float scales[ROW_THREADS];
   pdl_enter();
   if ((int)blockIdx.x >= a.row_blocks) {
     align_rows(a.align, blockIdx.x - a.row_blocks, gridDim.x - a.row_blocks);
@@ -252,6 +255,7 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
     __syncthreads();                   // counted and list are free again
     const int64_t i = base + tid;
     const Mark m = i < r1 ? mark(a, i) : Mark{-1, 0.f};
+    const float lse = a.dloss && i < r1 ? a.lse[i] : 0.f;
     const bool live = counts(a, m);
     const uint32_t votes = __ballot_sync(0xffffffffu, live);
     if (lane == 0) counted[warp] = __popc(votes);
@@ -268,7 +272,8 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
         if (!a.some) a.entry[to] = make_int2((int32_t)m.t, __float_as_int(a.share));
         if (a.dloss) {
           const int h = a.fp16 ? row_lift(bound_of(a, i, m.g), least) : 0;
-          const float g = ldexpf(m.g * a.inv_t, h), lse = a.lse[i];
+          const float g = ldexpf(m.g * a.inv_t, h);
+          scales[at] = ldexpf(1.f, least - h);
           a.coef[to] = {lse * LOG2E, g * (1.f + 2.f * a.z_loss * lse), -g * a.smoothing / (float)a.vocab, g};
           a.row_scale[to] = ldexpf(1.f, -h);
         }
@@ -278,12 +283,15 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
       }
     }
     __syncthreads();
-    for (int k = warp; k < all; k += 8) {
-      const int64_t from = base + list[k];
-      const float scale = lifted && a.x_dw != a.x ? ldexpf(1.f, least - row_lift(bound_of(a, from, a.dloss[from]), least)) : 1.f;
-      if (a.some)
-        for (int j = lane; j < a.top; j += 32) a.entry[(before + k) * (int64_t)a.top + j] = a.entry_in[from * a.top + j];
-      copy_row(a, from, before + k, scale);
+    if (a.some)
+      for (int k = tid; k < all * a.top; k += ROW_THREADS) {
+        const int r = k / a.top;
+        a.entry[(before + r) * (int64_t)a.top + k - r * a.top] = a.entry_in[(base + list[r]) * a.top + k - r * a.top];
+      }
+    const int segments = (int)((a.dp + SEGMENT - 1) / SEGMENT);
+    for (int k = warp; k < all * segments; k += 8) {
+      const int r = k / segments;
+      copy_segment(a, base + list[r], before + r, k - r * segments, lifted ? scales[r] : 1.f);
     }
     before += all;
   }
@@ -320,16 +328,18 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
   pdl_enter();
   const int col = threadIdx.x % ROWS, slice = threadIdx.x / ROWS, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = blockIdx.x * ROWS + col, n = a.meta->n;
-  if (blockIdx.x * ROWS >= n) return;
-  const bool live = row < n;
+  // few rows: what may be needed is asked for before it is known which rows count (the arrays have room for all)
+  constexpr bool EARLY = ROWS == 8;
+  if (!EARLY && blockIdx.x * ROWS >= n) return;
+  const bool live = row < n, ask = EARLY || live;
   float m = -INFINITY, s = 0.f, y = 0.f;
   // the first of a thread's entries is asked for before the parts
-  const int64_t entries = (int64_t)(live ? row : 0) * a.top;
-  const int64_t src = live ? a.src[row] : 0;
+  const int64_t entries = (int64_t)(ask ? row : 0) * a.top;
+  const int64_t src = ask ? a.src[row] : 0;
   float p0 = 0.f, y0 = 0.f;
-  if (live && slice < a.top) { p0 = __int_as_float(a.entry[entries + slice].y); y0 = a.y_entry[entries + slice]; }
-  if (live) {
-    constexpr int U = 8;               // parts in flight
+  if (ask && slice < a.top) { p0 = __int_as_float(a.entry[entries + slice].y); y0 = a.y_entry[entries + slice]; }
+  if (ask) {
+    constexpr int U = EARLY ? 12 : 8;  // parts in flight
     for (int i0 = slice; i0 < a.parts; i0 += SLICES * U) {
       float2 q[U];
 #pragma unroll
@@ -579,7 +589,8 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   r.inv_t = 1.f / cfg->temperature; r.z_loss = cfg->z_loss; r.smoothing = cfg->smoothing; r.fp16 = cfg->dtype == BETTY_F16;
   r.lanes = s.product_pairs ? 256 : 128; r.workers = current_sm_count() / (s.product_pairs ? 2 : 1);
   r.cols = s.piece < s.vocab ? s.piece : s.vocab; r.want_dx = s.want_dx; r.want_dw = s.want_dw; r.sum_rows = s.sum_rows;
-  const int64_t blocks = (c.rows + 7) / 8;
+  // a block a row where there are few (the warps share it), about four rows a block up to four blocks an SM
+  const int64_t sms = current_sm_count(), fours = (c.rows + 3) / 4, blocks = fours < sms ? (c.rows < sms ? c.rows : sms) : fours;
   r.row_blocks = (int)(blocks < most ? blocks : most);
   launch_pdl(k_rows, dim3((unsigned)(r.row_blocks + (r.align.rows ? align_blocks(r.align) : 0))), dim3(ROW_THREADS), 0, stream, r);
   BETTY_LAUNCH_CHECK();
@@ -598,9 +609,10 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   }
   BETTY_TRY(logits_gradients(stream, s, b, w, !copied, c.dW, c.lddw, c.dw_dtype));
   if (c.dX) {
-    // a row's threads: enough for one access each up to 256; few rows: more blocks than rows
+    // a row's threads: four accesses of four columns each; few rows: one access, and more blocks than rows
+    const int accesses = c.rows < most ? 1 : 4;
     int across = 32;
-    while (across < 256 && across * 4 < cfg->d) across *= 2;
+    while (across < 256 && across * 4 * accesses < cfg->d) across *= 2;
     const int width = c.rows < most ? across * 4 : (int)s.dp;
     const int64_t strips = (c.rows * ((cfg->d + width - 1) / width) + 256 / across - 1) / (256 / across);
     const dim3 grid((unsigned)(strips < most * 2 ? strips : most * 2)), block((unsigned)across, (unsigned)(256 / across));

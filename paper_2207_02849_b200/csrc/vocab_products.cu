@@ -19,12 +19,12 @@ static constexpr int THREADS = 320;           // warp 0: TMA, warp 1: MMA, warps
 static constexpr int EPI_WARPS = 8;
 static constexpr int STAGING = EPI_WARPS * 4096;   // each epilogue warp: 32 rows of 128 bytes, for its entries and its results
 
-template <int CG, int NT, int MODE> struct Cfg {
-  static constexpr int STAGE = A_BYTES + NT / CG * BK * 2;
-  static constexpr int STAGES = (229376 - STAGING) / STAGE;
-  static constexpr int SMEM = STAGES * STAGE + STAGING + 256 + 1024;
+template <int CG, int NT> struct Cfg {
+  static constexpr int STAGES = 192 * 1024;   // bytes of operands in flight
+  static constexpr int MAX_STAGES = 16;
+  static constexpr int SMEM = STAGES + STAGING + 512 + 1024;
   static constexpr int TMEM_COLS = 2 * NT;    // two accumulators: a tile drains while the next is multiplied
-  static_assert(SMEM <= 227 * 1024 && NT / CG <= 128 && STAGES * 16 + 48 <= 256, "shared memory");
+  static_assert(SMEM <= 227 * 1024 && MAX_STAGES * 16 + 48 <= 512, "shared memory");
 };
 
 struct alignas(64) Maps { CUtensorMap m[6]; };
@@ -38,6 +38,8 @@ struct Args {
   StatusBlock* sb;
   uint32_t type_bits;      // operand format bits of the instruction descriptor
   uint32_t a_bytes, b_bytes;   // bytes of the copies of A (by rows) and B of one CTA and chunk
+  uint32_t a_room, stage;      // bytes between A and B of a stage, and of a stage
+  int stages;
   int col0, cols;          // the piece of the vocabulary: first column, columns
   int d;
   int64_t rpad;
@@ -325,14 +327,14 @@ template <> struct IsF32<float> { static constexpr bool value = true; };
 // T: the operands' type (logits' coefficients); TO: dW's type (products)
 template <int CG, int NT, int MODE, typename T, typename TO>
 __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
-  using C = Cfg<CG, NT, MODE>;
-  constexpr int S = C::STAGES;
+  using C = Cfg<CG, NT>;
+  const int S = a.stages;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  unsigned char* staging = smem + S * C::STAGE;
+  unsigned char* staging = smem + C::STAGES;
   uint64_t* full = (uint64_t*)(staging + STAGING);
-  uint64_t* empty = full + S;
-  uint64_t* acc_full = empty + S;
+  uint64_t* empty = full + C::MAX_STAGES;
+  uint64_t* acc_full = empty + C::MAX_STAGES;
   uint64_t* acc_empty = acc_full + 2;
   uint32_t* tmem_slot = (uint32_t*)(acc_empty + 2);
   volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
@@ -392,8 +394,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       const uint32_t bytes = CG * ((trans ? (uint32_t)A_BYTES : a.a_bytes) + a.b_bytes);
       for (int it = 0; it < chunks; ++it) {
         if (round && !__all_sync(0xffffffffu, wait(&empty[s], (round - 1) & 1u, abort_flag))) { ok = false; break; }
-        unsigned char* sa = smem + s * C::STAGE;
-        unsigned char* sb = sa + A_BYTES;
+        unsigned char* sa = smem + s * a.stage;
+        unsigned char* sb = sa + a.a_room;
         const uint32_t bar = full0 + 8u * (uint32_t)s;
         const int k = k0 + it * BK;
         if (leader) {
@@ -425,7 +427,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     // K-major: 16 values are 32 bytes further along the swizzled row; 8-row groups 1024 bytes apart.  MN-major: 16
     // contraction rows are 2048 bytes further; 64-value blocks along the other dimension 8192 bytes apart.
     const bool leader = elect_one();
-    const uint32_t sa0 = s_u32(smem), sb0 = sa0 + A_BYTES;
+    const uint32_t sa0 = s_u32(smem), sb0 = sa0 + a.a_room;
     const uint64_t a_rows = smem_desc(sa0, 16, 1024), a_cols = smem_desc(sa0, 8192, 1024);
     const uint64_t b0 = MODE == PRODUCTS ? smem_desc(sb0, 8192, 1024) : smem_desc(sb0, 16, 1024);
     constexpr uint32_t b_step = MODE == PRODUCTS ? 2048 >> 4 : 32 >> 4;
@@ -461,7 +463,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
           commit<CG>(done);
         }
         __syncwarp();
-        if (++s == S) { s = 0; ++round; stage_off = 0; } else stage_off += C::STAGE >> 4;
+        if (++s == S) { s = 0; ++round; stage_off = 0; } else stage_off += a.stage >> 4;
       }
       if (ok && leader) commit<CG>(s_u32(&acc_full[as]));
       __syncwarp();
@@ -669,10 +671,10 @@ static betty_status launch(cudaStream_t stream, const Maps& tm, const Args& a, i
     if constexpr (CG == 2) return k_vocab_pair<NT, MODE, T, TO>;
     else return k_vocab<NT, MODE, T, TO>;
   }();
-  BETTY_TRY(ensure_dynamic_smem(kernel, limit, (size_t)Cfg<CG, NT, MODE>::SMEM));
+  BETTY_TRY(ensure_dynamic_smem(kernel, limit, (size_t)Cfg<CG, NT>::SMEM));
   const int64_t most = current_sm_count() / CG;
   const int workers = (int)(tiles < 1 ? 1 : (tiles < most ? tiles : most));
-  launch_pdl(kernel, dim3((unsigned)(workers * CG)), dim3(THREADS), (size_t)Cfg<CG, NT, MODE>::SMEM, stream, tm, a);
+  launch_pdl(kernel, dim3((unsigned)(workers * CG)), dim3(THREADS), (size_t)Cfg<CG, NT>::SMEM, stream, tm, a);
   BETTY_LAUNCH_CHECK();
   return BETTY_OK;
 }
@@ -690,6 +692,17 @@ static bool map_rows(CUtensorMap* tm, CUtensorMapDataType type, int bytes, const
 
 static int box_rows_of(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }
 
+// Stages of the operands.  With few rows only those of A are copied and have room: the instruction's other rows are read from what
+// lies behind, whatever that is just then, and end in accumulator lanes that nothing looks at.  That leaves room for more stages, which
+// is what a tile of few rows waits for (a copy takes some 1.5 us: 8 rows, 16576 x 512 ran at 0.27 us a chunk with 6 stages, and as
+// fast with half of the columns).
+static void set_stages(Args& a, bool whole_a) {
+  a.a_room = whole_a ? A_BYTES : a.a_bytes;
+  a.stage = a.a_room + a.b_bytes;
+  const int fit = Cfg<1, 128>::STAGES / (int)a.stage;
+  a.stages = fit < Cfg<1, 128>::MAX_STAGES ? fit : Cfg<1, 128>::MAX_STAGES;
+}
+
 int logits_parts(const Shape& s) { return 2 * (int)div_up(s.vocab, s.width); }
 
 static void common_args(Args& a, const Shape& s, const Buffers& b) {
@@ -706,6 +719,7 @@ static betty_status logits_maps(Maps& tm, Args& a, const Shape& s, const Buffers
   const CUtensorMapDataType type = s.dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const int a_box = s.pairs ? 128 : box_rows_of(s.rows), b_box = s.pairs ? 128 : s.width;
   a.a_bytes = (uint32_t)a_box * BK * 2; a.b_bytes = (uint32_t)b_box * BK * 2;
+  set_stages(a, false);
   if (!map_rows(&tm.m[M_X], type, 2, b.x, s.dp, s.rpad, s.dp, BK, a_box)) return BETTY_ERR_CUDA;
   if (!map_rows(&tm.m[M_W], type, 2, w.p, w.cols, w.rows, w.ld, BK, b_box)) return BETTY_ERR_CUDA;
   tm.m[M_DZ_OUT] = tm.m[M_X];
@@ -723,14 +737,14 @@ betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffer
   const int64_t tiles = div_up(s.rows, s.pairs ? 256 : 128) * div_up(s.vocab, s.width);
   // the operands' type is in the instruction descriptor: nothing else of the statistics depends on it
   if (s.pairs) return launch<2, 256, STATS, __nv_bfloat16, float>(stream, tm, a, tiles);
-  return launch<1, 128, STATS, __nv_bfloat16, float>(stream, tm, a, tiles);
+  return launch<1, 256, STATS, __nv_bfloat16, float>(stream, tm, a, tiles);
 }
 
 template <typename T>
 static betty_status launch_grad(cudaStream_t stream, const Shape& s, const Maps& tm, const Args& a) {
   const int64_t tiles = div_up(s.rows, s.pairs ? 256 : 128) * div_up(a.cols, s.width);
   if (s.pairs) return launch<2, 256, GRAD, T, float>(stream, tm, a, tiles);
-  return launch<1, 128, GRAD, T, float>(stream, tm, a, tiles);
+  return launch<1, 256, GRAD, T, float>(stream, tm, a, tiles);
 }
 template <typename TO>
 static betty_status launch_products(cudaStream_t stream, const Shape& s, const Maps& tm, const Args& a) {
@@ -755,6 +769,7 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
   pa.dw = dw; pa.lddw = lddw;
   const int a_box = s.product_pairs ? 128 : box_rows_of(s.rows);
   pa.a_bytes = (uint32_t)a_box * BK * 2; pa.b_bytes = 128 * BK * 2;
+  set_stages(pa, s.want_dw);
   const Operand dz = {b.dz, s.piece, s.rpad, 1, s.piece, 0}, x = {b.x_dw, s.dp, s.rpad, 1, s.dp, 0};
   bool ok = make_blocked_map(&pm.m[M_DZ_T], s.dtype, dz, false) && make_blocked_map(&pm.m[M_X_T], s.dtype, x, false);
   ok = ok && (pa.w_blocked ? make_blocked_map(&pm.m[M_W_T], s.dtype, w, false) : make_map(&pm.m[M_W_T], s.dtype, w, false, 64, BK));
@@ -794,13 +809,19 @@ void choose_shape(Shape& s, bool backward) {
     s.piece = (int)(div_up(div_up(s.vocab, pieces), 256) * 256);
   }
   const int64_t cols = backward ? (s.piece < s.vocab ? s.piece : s.vocab) : s.vocab;
-  // an SM's share of the columns for a tile of 128 rows, its rounds being of equal length: pairs take 256 at a time
-  s.pairs = rows > 128;
-  s.width = 256;
-  int64_t best = s.pairs ? div_up(div_up(rows, 256) * div_up(cols, 256), sms / 2) * 256 : INT64_MAX;
-  for (int w = 128; w >= 32; w -= 16) {
-    const int64_t cost = div_up(div_up(rows, 128) * div_up(cols, w), sms) * (w + 16) * (rows > 128 ? 5 : 4) / 4;
-    if (cost < best) { best = cost; s.pairs = 0; s.width = w; }
+  // Tiles of the logits: pairs take 256 x 256, a single SM 128 rows x width.  Time of the rounds in us: a contraction chunk takes 0.34 in
+  // a pair; alone 0.27 for any width up to 112 and little more above with one tile of rows, but 0.53 for 256 columns with several
+  // (777 rows x 12345 x 1537: 44.7 us, pairs 27.9), and a tile is drained while the next is multiplied, 256 columns in 3 us in a
+  // pair, alone somewhat slower (1293 rows x 116984 x 128, gradients: 279 us, pairs 225).
+  const double chunks = (double)div_up(s.d, BK);
+  double best = 1e30;
+  for (int w = 32; w <= 272; w += 16) {
+    const bool pair = w > 256;
+    if (pair && rows <= 128) break;
+    const int64_t rounds = pair ? div_up(div_up(rows, 256) * div_up(cols, 256), sms / 2) : div_up(div_up(rows, 128) * div_up(cols, w), sms);
+    const double multiply = chunks * (pair ? 0.34 : 0.25 + (rows <= 128 ? 0.09 : 0.28) * w / 256), drain = pair ? 3.0 : 0.4 + (backward ? 4.4 : 3.0) * w / 256;
+    const double time = (double)rounds * (multiply > drain ? multiply : drain) + (multiply > drain ? drain : multiply);
+    if (time <= best) { best = time; s.pairs = pair; s.width = pair ? 256 : w; }
   }
   s.product_pairs = 0;
   s.sum_rows = s.rpad;
