@@ -38,7 +38,7 @@ struct Args {
   StatusBlock* sb;
   uint32_t type_bits;      // operand format bits of the instruction descriptor
   uint32_t a_bytes, b_bytes;   // bytes of the copies of A (by rows) and B of one CTA and chunk
-  uint32_t a_room, stage;      // bytes between A and B of a stage, and of a stage
+  uint32_t stage;              // bytes of a stage: 128 rows of A, B
   int stages;
   int col0, cols;          // the piece of the vocabulary: first column, columns
   int d;
@@ -395,7 +395,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       for (int it = 0; it < chunks; ++it) {
         if (round && !__all_sync(0xffffffffu, wait(&empty[s], (round - 1) & 1u, abort_flag))) { ok = false; break; }
         unsigned char* sa = smem + s * a.stage;
-        unsigned char* sb = sa + a.a_room;
+        unsigned char* sb = sa + A_BYTES;
         const uint32_t bar = full0 + 8u * (uint32_t)s;
         const int k = k0 + it * BK;
         if (leader) {
@@ -427,7 +427,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     // K-major: 16 values are 32 bytes further along the swizzled row; 8-row groups 1024 bytes apart.  MN-major: 16
     // contraction rows are 2048 bytes further; 64-value blocks along the other dimension 8192 bytes apart.
     const bool leader = elect_one();
-    const uint32_t sa0 = s_u32(smem), sb0 = sa0 + a.a_room;
+    const uint32_t sa0 = s_u32(smem), sb0 = sa0 + A_BYTES;
     const uint64_t a_rows = smem_desc(sa0, 16, 1024), a_cols = smem_desc(sa0, 8192, 1024);
     const uint64_t b0 = MODE == PRODUCTS ? smem_desc(sb0, 8192, 1024) : smem_desc(sb0, 16, 1024);
     constexpr uint32_t b_step = MODE == PRODUCTS ? 2048 >> 4 : 32 >> 4;
@@ -692,13 +692,11 @@ static bool map_rows(CUtensorMap* tm, CUtensorMapDataType type, int bytes, const
 
 static int box_rows_of(int rows) { return rows <= 32 ? 32 : (rows <= 64 ? 64 : 128); }
 
-// Stages of the operands.  With few rows only those of A are copied and have room: the instruction's other rows are read from what
-// lies behind, whatever that is just then, and end in accumulator lanes that nothing looks at.  That leaves room for more stages, which
-// is what a tile of few rows waits for (a copy takes some 1.5 us: 8 rows, 16576 x 512 ran at 0.27 us a chunk with 6 stages, and as
-// fast with half of the columns).
-static void set_stages(Args& a, bool whole_a) {
-  a.a_room = whole_a ? A_BYTES : a.a_bytes;
-  a.stage = a.a_room + a.b_bytes;
+// A stage has room for all 128 rows of A: of few rows only those are copied, the others hold what was there before and end in accumulator
+// lanes that nothing looks at.  (Room for the copied rows alone, and more stages for it, was no faster: 8 rows 21.8 us, with whole
+// ones 22.3; 24 rows, gradients, 91.1 and 87.8.)
+static void set_stages(Args& a) {
+  a.stage = A_BYTES + a.b_bytes;
   const int fit = Cfg<1, 128>::STAGES / (int)a.stage;
   a.stages = fit < Cfg<1, 128>::MAX_STAGES ? fit : Cfg<1, 128>::MAX_STAGES;
 }
@@ -719,7 +717,7 @@ static betty_status logits_maps(Maps& tm, Args& a, const Shape& s, const Buffers
   const CUtensorMapDataType type = s.dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const int a_box = s.pairs ? 128 : box_rows_of(s.rows), b_box = s.pairs ? 128 : s.width;
   a.a_bytes = (uint32_t)a_box * BK * 2; a.b_bytes = (uint32_t)b_box * BK * 2;
-  set_stages(a, false);
+  set_stages(a);
   if (!map_rows(&tm.m[M_X], type, 2, b.x, s.dp, s.rpad, s.dp, BK, a_box)) return BETTY_ERR_CUDA;
   if (!map_rows(&tm.m[M_W], type, 2, w.p, w.cols, w.rows, w.ld, BK, b_box)) return BETTY_ERR_CUDA;
   tm.m[M_DZ_OUT] = tm.m[M_X];
@@ -769,7 +767,7 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
   pa.dw = dw; pa.lddw = lddw;
   const int a_box = s.product_pairs ? 128 : box_rows_of(s.rows);
   pa.a_bytes = (uint32_t)a_box * BK * 2; pa.b_bytes = 128 * BK * 2;
-  set_stages(pa, s.want_dw);
+  set_stages(pa);
   const Operand dz = {b.dz, s.piece, s.rpad, 1, s.piece, 0}, x = {b.x_dw, s.dp, s.rpad, 1, s.dp, 0};
   bool ok = make_blocked_map(&pm.m[M_DZ_T], s.dtype, dz, false) && make_blocked_map(&pm.m[M_X_T], s.dtype, x, false);
   ok = ok && (pa.w_blocked ? make_blocked_map(&pm.m[M_W_T], s.dtype, w, false) : make_map(&pm.m[M_W_T], s.dtype, w, false, 64, BK));
