@@ -107,6 +107,13 @@ __device__ __forceinline__ int nth_tile(const Counts& c, int worker, int workers
   }
   return t < c.second ? c.first + t : -1;
 }
+// Tiles that run together are about as many along d as across it, so that they share what they read.
+__device__ __forceinline__ void raster(int rows, int cols, int t, int& row, int& col) {
+  constexpr int G = 8;
+  const int per = rows * G, group = t / per, in = t - group * per, width = min(G, cols - group * G);
+  row = in / width;
+  col = group * G + in - row * width;
+}
 template <int CG, int NT, int MODE>
 __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, int t) {
   Tile r;
@@ -120,9 +127,11 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
     r.k0 = 0;
     r.chunks = (a.d + BK - 1) / BK;
   } else if (t < c.first) {
-    const int rest = t / c.d_tiles, chunks = (a.cols + BK - 1) / BK;
+    int rest, dt;
+    raster(c.row_tiles * c.split, c.d_tiles, t, rest, dt);
+    const int chunks = (a.cols + BK - 1) / BK;
     r.trans = 0;
-    r.c0 = (t - rest * c.d_tiles) * NT;
+    r.c0 = dt * NT;
     r.width = a.d - r.c0 > NT / 2 ? NT : NT / 2;         // blocks of 64 columns in each CTA
     r.part = rest % c.split;
     r.l0 = rest / c.split * (BM * CG);
@@ -131,9 +140,10 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
     r.chunks = (int)((int64_t)(r.part + 1) * chunks / c.split) - k;
   } else {
     t -= c.first;
-    const int rest = t / c.d_tiles;
+    int rest, dt;
+    raster(c.col_tiles, c.d_tiles, t, rest, dt);
     r.trans = 1;
-    r.c0 = (t - rest * c.d_tiles) * NT;
+    r.c0 = dt * NT;
     r.width = a.d - r.c0 > NT / 2 ? NT : NT / 2;
     r.part = 0;
     r.l0 = rest * (BM * CG);
