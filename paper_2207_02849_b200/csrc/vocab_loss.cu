@@ -164,16 +164,17 @@ __device__ __forceinline__ void copy_segment(const RowArgs& a, int64_t from, int
   constexpr int U = SEGMENT / 256;     // accesses in flight
   const int c0 = segment * SEGMENT + lane * 8;
   {
-    uint4 v[U];
+    Words raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load8(in, c0 + 256 * u, a.d);
+    for (int u = 0; u < U; ++u) raw[u] = fetch8(in, c0 + 256 * u, a.d);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + 256 * u;
       if (c >= a.dp) break;
-      *(uint4*)(out + c) = v[u];
+      const uint4 v = shift8(raw[u], in, c, a.d);
+      *(uint4*)(out + c) = v;
       if (out2) {
-        uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float2 f = __half22float2(*(__half2*)&w[k]);
