@@ -195,7 +195,7 @@ __device__ int choose_split(const RowArgs& a, int n) {           // a warp
   const int tiles = p.row_tiles * p.d_tiles;
   // one tile of rows: W streams past it once, and that is the time; all workers take part in it, in one round (24 rows, 32000 x 2048
   // in 3 / 6 / 9 / 12 parts: 98.5 / 92.9 / 91.9 / 95.7 us; 8 rows, 128000 x 4096 in 3 / 4 / 6: 579 / 558 / 619)
-  if (p.row_tiles <= 1) return min(min(most, 32), max(1, a.workers / max(1, tiles)));
+  if (p.row_tiles <= 1) return min(most, max(1, a.workers / max(1, tiles)));
   const float second = a.want_dw ? (float)p.col_tiles * p.d_tiles * dw_cost(p) : 0.f;
   const float part = (float)n * a.dp * (a.lanes == 256 ? 3.6e-6f : 7e-6f);      // 8 bytes a value at 6 TB/s, chunks of 0.37 (0.19) us
   int best = 1;
@@ -575,12 +575,12 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   uint8_t* some;
   BETTY_TRY(lay_out(arena, s, c, b, some));
   Operand w = {c.W, cfg->d, cfg->vocab, 1, c.ldw, 0};
+  RowArgs r = {};
+  BETTY_TRY(plan_alignment(arena, w, r.align));
   if (distill) {
     const EntryArgs e = {c.rows, cfg->vocab, c.target, c.ldi, c.id_dtype == BETTY_I64, c.teacher, c.ldt, c.teacher_dtype, c.top, 1.f / cfg->temperature, b.entry_in, some};
     BETTY_TRY(sort_entries<1>(stream, e));
   }
-  RowArgs r = {};
-  BETTY_TRY(plan_alignment(arena, w, r.align));
   r.rows = c.rows; r.vocab = cfg->vocab; r.d = (int)cfg->d; r.dp = s.dp; r.ldx = c.ldx; r.x_in = (const uint16_t*)c.X;
   r.target = distill ? nullptr : c.target; r.id64 = c.id_dtype == BETTY_I64; r.share = 1.f - cfg->smoothing; r.some = some;
   r.entry = b.entry; r.entry_in = b.entry_in; r.top = s.top;

@@ -154,9 +154,8 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
 }
 
 // ------------------------------------------------------------------ epilogues
-// A row's entries in ascending order of id, from the first at or behind a column; the next AHEAD of them are in registers.  They are
-// asked for together, before the accumulator is waited for: an entry that is asked for when it is needed costs a warp its
-// latency (a list that was refilled at each step: 8192 rows, 128 entries, 32000 x 2048: 268 us instead of 181 for 8192 columns).
+// A row's entries in ascending order of id, from the first at or behind a column; the next AHEAD of them are in registers, asked for
+// together and before the accumulator is waited for, so that their latency is hidden behind the products.
 struct Walk {
   static constexpr int AHEAD = 4;
   const int2* entry;
@@ -233,8 +232,10 @@ __device__ __forceinline__ void stage16(uint32_t rows, int row, int j, uint32_t 
 }
 
 // Registers have no index.  The entries among 32 columns go through the warp's staging, a lane's row each: the columns' values are put
-// there for the entries to pick theirs, or the entries' shares for the columns to subtract.  (Selecting them in registers, 31 or 64
-// instructions for the entries that the lanes have next: a fifth of the columns being entries, 10799 rows x 715 x 192: 132 us.)
+// there for the entries to pick theirs, or the entries' shares for the columns to subtract.  A call of 10799 rows x 715 x 192 with 102
+// entries a row takes 96 us; selecting them in registers, 31 or 64 instructions for the entries that the lanes have next, it took 132.
+// Comparing an index with each of 32 registers by hand is no way out: the compiler makes an array in local memory of that, which is
+// stored for every 32 columns, entries or not (8192 x 65536 x 4096: 3.27 ms, now 3.02).
 __device__ __forceinline__ uint32_t staged_at(uint32_t rows, int row, int k) { return rows + (uint32_t)(row * 128 + (((k >> 2) ^ (row & 7)) << 4) + (k & 3) * 4); }
 __device__ __forceinline__ float staged(uint32_t at) {
   float v;
@@ -785,7 +786,8 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
   if (s.want_dx) ok = ok && map_rows(&pm.m[M_DX], CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, b.dx, s.dp, s.sum_rows, s.dp, 32, 32);
   const int ob = dw_dtype == BETTY_F32 ? 4 : 2;
   if (s.vocab == 1) lddw = pad8(s.d);            // a stride that is never used still has to be a valid one
-  if (dw && (aligned16(dw) && (lddw * ob) % 16 == 0)) {
+  // a TMA store writes whole 16-byte pieces: where a row does not end with one, what lies behind it would be overwritten
+  if (dw && aligned16(dw) && (lddw * ob) % 16 == 0 && ((int64_t)s.d * ob) % 16 == 0) {
     pa.dw_tma = 1;
     ok = ok && map_rows(&pm.m[M_DW], dw_dtype == BETTY_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type, ob, dw, s.d, s.vocab, lddw, 128 / ob, 32);
   }
@@ -836,13 +838,13 @@ void choose_shape(Shape& s, bool backward) {
   if (!backward) return;
   const int64_t pair_tiles = div_up(s.d, 256) * ((s.want_dx ? div_up(rows, 256) : 0) + (s.want_dw ? div_up(s.piece, 256) : 0));
   s.product_pairs = rows > 128 && pair_tiles * 2 >= sms / 2;
-  // dX with few rows: room for parts of its contraction, of 8 chunks or more, that are up to two tiles for each worker (k_rows
-  // chooses their number once the rows are counted)
+  // dX with few rows: room for parts of its contraction, of 8 chunks or more, that are up to two tiles for each worker, and 32 at most
+  // (8 rows x 56960 x 64 in 111 parts: 20 us to add them up, in 32: 6); k_rows chooses their number once the rows are counted
   const int lanes = s.product_pairs ? 256 : 128;
   const int64_t tiles = div_up(rows, lanes) * div_up(s.d, lanes), workers = s.product_pairs ? sms / 2 : sms;
   int64_t parts = div_up(2 * workers, tiles);
   if (parts > div_up(cols, BK) / 8) parts = div_up(cols, BK) / 8;
-  s.sum_rows = s.rpad * (parts < 1 ? 1 : parts);
+  s.sum_rows = s.rpad * (parts < 1 ? 1 : (parts < 32 ? parts : 32));
 }
 
 }  // namespace vocab

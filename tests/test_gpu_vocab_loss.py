@@ -190,7 +190,7 @@ def _wide(pad, shift):
     return wrap
 
 
-@pytest.mark.parametrize("pad,shift,d", [(8, 8, 128), (3, 0, 128), (0, 1, 136), (7, 2, 65), (1, 3, 64), (4, 4, 200)])
+@pytest.mark.parametrize("pad,shift,d", [(8, 8, 128), (3, 0, 128), (0, 1, 136), (7, 2, 65), (1, 3, 64), (4, 4, 200), (5, 0, 67), (7, 0, 129), (14, 8, 66)])
 @pytest.mark.parametrize("rows,vocab", [(20, 333), (260, 700)])
 def test_rows_of_wider_buffers(pad, shift, d, rows, vocab):
     """What lies beside the rows is NaN: nothing of it may reach a sum."""
@@ -425,3 +425,84 @@ def test_a_workspace_of_the_stated_size_is_enough(rows):
     torch.cuda.synchronize()
     assert bool((ws.buf[end:] == 77).all())
     _check_ce(bt, x, w, target, dloss, ws=ws)
+
+
+# ---- the ends of the ranges ----
+@pytest.mark.parametrize("rows,vocab,d", [(3, 40, 65536), (200, 300, 20000), (4, (1 << 22) - 1, 8), (150, 1 << 21, 8), (100000, 50, 16)])
+def test_largest_sizes(rows, vocab, d):
+    import paper_2207_02849_b200 as bt
+    _check_ce(bt, *_problem(1, rows, vocab, d, BF))
+
+
+def test_ids_at_the_end_of_the_largest_vocabulary():
+    import paper_2207_02849_b200 as bt
+    vocab = (1 << 22) - 1
+    x, w, _, dloss = _problem(1, 5, vocab, 8, HF, boost=0.0)
+    ids = torch.full((5, 1024), -1, device="cuda")
+    ids[:, -3:] = torch.tensor([vocab - 1, 0, vocab - 2], device="cuda")
+    ids[0, :] = vocab - 1
+    _check_distill(bt, x, w, ids, torch.randn(5, 1024, device="cuda"), dloss)
+
+
+def test_offsets_beyond_32_bits():
+    """Leading dimensions of 2^20: the last of 2500 rows begin behind 2^31 values."""
+    import paper_2207_02849_b200 as bt
+
+    def far(t):
+        v = torch.empty(t.shape[0], 1 << 20, dtype=t.dtype, device="cuda")[:, :t.shape[1]]
+        v.copy_(t)
+        return v
+    _check_ce(bt, *_problem(1, 2500, 2300, 64, BF), wrap=far)
+
+
+@pytest.mark.parametrize("d,pad", [(67, 5), (65, 7), (130, 6), (3, 5)])
+@pytest.mark.parametrize("out", [BF, F])
+def test_aligned_results_of_odd_widths_leave_their_neighbours(d, pad, out):
+    import paper_2207_02849_b200 as bt
+    x, w, target, dloss = _problem(6, 150, 401, d, BF)
+    cfg = _cfg(bt, 401, d, BF)
+    ws = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, 150))
+    lse = torch.logsumexp(x.float() @ w.float().t(), 1)
+    bx, bw = torch.full((150, d + pad), 7.0, dtype=out, device="cuda"), torch.full((401, d + pad), 7.0, dtype=out, device="cuda")
+    dx, dw = _nan(150, d, dtype=out), _nan(401, d, dtype=out)
+    bt.betty_vocab_ce_backward(cfg, x, w, target, lse, dloss, bx[:, :d], bw[:, :d], ws)
+    bt.betty_vocab_ce_backward(cfg, x, w, target, lse, dloss, dx, dw, ws)
+    for b, t in ((bx, dx), (bw, dw)):
+        assert bool((b[:, d:] == 7).all()) and torch.equal(b[:, :d], t)
+
+
+def test_a_matrix_that_cannot_be_read_in_place_needs_room():
+    """The refusal comes before anything is launched.  (Both gradients against a teacher take all of a workspace of the stated size;
+    other calls may find room in what they do not need themselves.)"""
+    import paper_2207_02849_b200 as bt
+    x, w, target, dloss = _problem(6, 30, 401, 64, BF)
+    w1 = _wide(3, 0)(w)
+    ids, logits = (t.cuda() for t in _entries(5, 30, 401, 7, F, "any"))
+    cfg = _cfg(bt, 401, 64, BF)
+    lse, dx, dw = torch.zeros(30, device="cuda"), _nan(30, 64, dtype=BF), _nan(401, 64, dtype=BF)
+    torch.cuda.synchronize()
+    for top, call in ((0, lambda ws: bt.betty_vocab_ce_backward(cfg, x, w1, target, lse, dloss, dx, dw, ws)),
+                      (7, lambda ws: bt.betty_vocab_distill_backward(cfg, x, w1, ids, logits, lse, dloss, dx, dw, ws))):
+        small = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, 30, top, any_layout=False))
+        before = bt.betty_kernel_launches()
+        with pytest.raises(bt.BettyError) as e:
+            call(small)
+        assert e.value.status == bt.BETTY_ERR_WORKSPACE and bt.betty_kernel_launches() == before
+        call(bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, 30, top, any_layout=True)))
+
+
+def test_a_matrix_changed_just_before_the_call():
+    """W is asked for while its rows are counted: what the stream has written to it before is what counts."""
+    import paper_2207_02849_b200 as bt
+    x, w, target, dloss = _problem(16, 16, 40000, 512, BF)
+    cfg = _cfg(bt, 40000, 512, BF)
+    ws = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, 16))
+    loss, lse = _nan(16), _nan(16)
+    for k in range(6):
+        other = torch.randn_like(w)
+        w.copy_(other * 0.05)
+        bt.betty_vocab_ce(cfg, x, w, target, loss, lse, ws)
+        w2 = w.clone()
+        w.zero_()
+        e = ref.Expected(x, w2, ref.entries_ce(target, 40000, 0.0))
+        e.check_forward(loss, lse)
