@@ -7,7 +7,7 @@ from tests import vocab_reference as ref
 pytestmark = pytest.mark.gpu
 BF, HF, F = torch.bfloat16, torch.float16, torch.float32
 SIZES = [(1, 8), (2, 64), (100, 1), (257, 72), (1000, 200), (4099, 515), (513, 1025), (20000, 64)]
-ROWS = [1, 7, 33, 128, 129, 300, 700]
+ROWS = [1, 7, 16, 17, 33, 128, 129, 300, 700]
 
 
 def _problem(seed, rows, vocab, d, dtype, ignored=0.2, boost=6.0):
@@ -333,9 +333,9 @@ def test_gradients_against_differences(distill):
 
 
 # ---- calls ----
-def test_repeated_and_captured_calls_give_the_same_bits():
+@pytest.mark.parametrize("rows,vocab,d", [(400, 5000, 200), (8, 5000, 200), (16, 30000, 64), (17, 30000, 64)])
+def test_repeated_and_captured_calls_give_the_same_bits(rows, vocab, d):
     import paper_2207_02849_b200 as bt
-    rows, vocab, d = 400, 5000, 200
     x, w, target, dloss = _problem(14, rows, vocab, d, BF)
     ids, logits = (t.cuda() for t in _entries(5, rows, vocab, 40, F, "dense"))
     cfg = _cfg(bt, vocab, d, BF)
