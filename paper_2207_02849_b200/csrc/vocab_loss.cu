@@ -1,7 +1,8 @@
 // Losses over a vocabulary: the rows that count and their entries, the losses from the statistics of the logits' tiles, and the
 // C entries (see vocab_loss.cuh for the mathematics).
 //
-// What surrounds the products is bound by memory and small beside them: a copy of x in, fp32 sums of dX out.
+// What surrounds the products is bound by memory and small beside them, with few rows by latency: a copy of x in (8192 x 4096: 134 MB in 22
+// to 26 us), 8 bytes of statistics per row and half tile (8192 rows of 128 parts: 8 us), fp32 sums of dX out (201 MB in 45 to 50 us).
 #include "vocab_loss.cuh"
 
 namespace betty {

@@ -6,7 +6,12 @@
 //   products     dX += dz W over the piece's columns, dW = dz^T X over the rows; one launch for both
 //
 // An accumulator holds rows of the batch in its lanes and columns of the vocabulary, so a thread owns a row and its softmax
-// statistics need no exchange.
+// statistics need no exchange.  Pairs of SMs take tiles of 256 x 256 (the widest instruction; each SM stages half of the operands, 64 KB
+// for 8.4 MFLOP of a chunk), and two accumulators let a tile drain, in about 3 us, while the next is multiplied: with d of 700
+// and more the products hide the epilogues.  A launch of the statistics, 8192 x 16384 x 4096: 656 us, 1.68 PFLOP/s; of the
+// coefficients: 661 to 674; of both products: 1421 us, 1.55 PFLOP/s; the tensor pipe is 94 % busy in all.  With few rows (one tile
+// of rows on single SMs) W's stream bounds all three: 24 x 32000 x 2048, 131 MB in 28 us; dX and dW 46 us (131 MB read again, 131
+// written).
 #include "vocab_loss.cuh"
 
 namespace betty {
