@@ -718,17 +718,25 @@ class VocabLoss:
         return out
 
 
-def _row_values(t: torch.Tensor, rows: int, dtypes, name: str) -> int:
-    if t.dtype not in dtypes or not t.is_cuda or t.shape != (rows,) or not (t.is_contiguous() or rows == 0):
-        raise ValueError(f"{name} must be {rows} contiguous values ({' or '.join(map(str, dtypes))}) on the GPU")
-    return t.data_ptr()
+def _row_values(t: torch.Tensor, rows: int, name: str, dtype: torch.dtype = torch.float32) -> int:
+    """Address of one value per row."""
+    if t.dtype is dtype and t.is_cuda and t.shape == (rows,) and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be {rows} contiguous {dtype} values on the GPU, got {t.dtype} of shape {tuple(t.shape)} on {t.device}")
+
+
+def _tokens(t: torch.Tensor, rows: int):
+    """Address and type of the rows' tokens."""
+    if t.dtype not in _ID:
+        raise ValueError(f"target must be int32 or int64, got {t.dtype}")
+    return _row_values(t, rows, "target", t.dtype), _ID[t.dtype]
 
 
 def _on_current_device(*tensors) -> None:
     """Kernels run on the current device: operands of another one are refused before anything is launched."""
-    here = torch.cuda.current_device()
+    here = _raw_device() if _raw_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != here:
+        if t is not None and t.get_device() not in (here, -1):             # -1: not on a GPU, which is refused where its type is
             raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
 
 
@@ -744,38 +752,38 @@ def betty_vocab_workspace_size(cfg: VocabLoss, rows: int, top: int = 0, any_layo
 def betty_vocab_ce(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
                    ws: Workspace, stream=None) -> None:
     """loss, lse [rows] fp32: the rows' cross entropy with `target` (int32 or int64) and the logarithm of its normaliser."""
-    rows, f = x.shape[0], (torch.float32,)
+    rows = x.shape[0]
     _on_current_device(x, w, target, loss, lse)
-    _check(lib().betty_vocab_ce(*cfg._operands(x, w), _row_values(target, rows, tuple(_ID), "target"), _ID[target.dtype], _row_values(loss, rows, f, "loss"),
-                                _row_values(lse, rows, f, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_ce")
+    _check(lib().betty_vocab_ce(*cfg._operands(x, w), *_tokens(target, rows), _row_values(loss, rows, "loss"),
+                                _row_values(lse, rows, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_ce")
 
 
 def betty_vocab_ce_backward(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, target: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor,
                             dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], ws: Workspace, stream=None) -> None:
     """dx, dw (None: not wanted) = the gradients of sum(dloss * loss)."""
-    rows, f = x.shape[0], (torch.float32,)
+    rows = x.shape[0]
     _on_current_device(x, w, target, lse, dloss, dx, dw)
-    _check(lib().betty_vocab_ce_backward(*cfg._operands(x, w), _row_values(target, rows, tuple(_ID), "target"), _ID[target.dtype],
-                                         _row_values(lse, rows, f, "lse"), _row_values(dloss, rows, f, "dloss"), *cfg._results(dx, dw, rows), ws.ptr,
+    _check(lib().betty_vocab_ce_backward(*cfg._operands(x, w), *_tokens(target, rows),
+                                         _row_values(lse, rows, "lse"), _row_values(dloss, rows, "dloss"), *cfg._results(dx, dw, rows), ws.ptr,
                                          ws.nbytes, _stream(stream)), "betty_vocab_ce_backward")
 
 
 def betty_vocab_distill(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, loss: torch.Tensor,
                         lse: torch.Tensor, ws: Workspace, stream=None) -> None:
     """loss [rows] = KL(teacher || student) with the teacher's distribution over its entries (ids, teacher) [rows, top]."""
-    rows, f = x.shape[0], (torch.float32,)
+    rows = x.shape[0]
     _on_current_device(x, w, ids, teacher, loss, lse)
-    _check(lib().betty_vocab_distill(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(loss, rows, f, "loss"),
-                                     _row_values(lse, rows, f, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_distill")
+    _check(lib().betty_vocab_distill(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(loss, rows, "loss"),
+                                     _row_values(lse, rows, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_distill")
 
 
 def betty_vocab_distill_backward(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, lse: torch.Tensor,
                                  dloss: torch.Tensor, dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], ws: Workspace, stream=None) -> None:
     """dx, dw (None: not wanted) = the gradients of sum(dloss * loss)."""
-    rows, f = x.shape[0], (torch.float32,)
+    rows = x.shape[0]
     _on_current_device(x, w, ids, teacher, lse, dloss, dx, dw)
-    _check(lib().betty_vocab_distill_backward(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(lse, rows, f, "lse"),
-                                              _row_values(dloss, rows, f, "dloss"), *cfg._results(dx, dw, rows), ws.ptr, ws.nbytes, _stream(stream)),
+    _check(lib().betty_vocab_distill_backward(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(lse, rows, "lse"),
+                                              _row_values(dloss, rows, "dloss"), *cfg._results(dx, dw, rows), ws.ptr, ws.nbytes, _stream(stream)),
            "betty_vocab_distill_backward")
 
 

@@ -775,7 +775,7 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
   common_args(la, s, b);
   BETTY_TRY(logits_maps(lm, la, s, b, w));
   la.coef = b.coef; la.dz = b.dz; la.ldz = s.piece;
-  if (!map_rows(&lm.m[M_DZ_OUT], type, 2, b.dz, s.piece, s.rpad, s.piece, 64, 32)) return BETTY_ERR_CUDA;
+  if (s.pairs && !map_rows(&lm.m[M_DZ_OUT], type, 2, b.dz, s.piece, s.rpad, s.piece, 64, 32)) return BETTY_ERR_CUDA;
 
   common_args(pa, s, b);
   pa.want_dx = s.want_dx; pa.want_dw = s.want_dw;
