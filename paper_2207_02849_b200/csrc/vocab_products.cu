@@ -165,11 +165,16 @@ struct Walk {
   static constexpr int AHEAD = 4;
   const int2* entry;
   int at, end, left;       // place of q[0]; entries in q
-  int2 q[AHEAD];
+  int2 q[AHEAD], then[AHEAD];
+  __device__ __forceinline__ void ask(int from) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) then[i] = from + i < end ? entry[from + i] : make_int2(NO_ID, 0);
+  }
   __device__ __forceinline__ void fill() {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) q[i] = at + i < end ? entry[at + i] : make_int2(NO_ID, 0);
+    for (int i = 0; i < AHEAD; ++i) q[i] = then[i];
     left = AHEAD;
+    ask(at + AHEAD);
   }
   // the first entry at or behind the column: eight places are looked at at a time
   __device__ __forceinline__ void start(const int2* entries, int top, int column) {
@@ -186,13 +191,14 @@ struct Walk {
       len = min(step - 1, stop - lo);
     }
     at = lo;
+    ask(at);
     fill();
     if (top == 1 && q[0].x < column) q[0].x = NO_ID;
   }
   __device__ __forceinline__ void none() {
     entry = nullptr; at = end = 0; left = AHEAD;
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) q[i] = make_int2(NO_ID, 0);
+    for (int i = 0; i < AHEAD; ++i) q[i] = then[i] = make_int2(NO_ID, 0);
   }
   __device__ __forceinline__ int next() const { return q[0].x; }
   __device__ __forceinline__ float share() const { return __int_as_float(q[0].y); }
