@@ -119,6 +119,7 @@ struct RowArgs {
   const void* target; int id64; float share;   // cross entropy: an entry (target, share) per row
   const uint8_t* some;                         // distillation: whether a row has an entry
   int2* entry; const int2* entry_in; int top;  // entries in the order of the copies (of entry_in's: distillation)
+  int64_t rpad;
   Meta* meta; int32_t* src; int32_t* pos; uint16_t* x; uint16_t* x_dw;
   float* loss; float* lse_out;                 // forward: zeros for rows left out
   const float* lse; const float* dloss;        // backward
@@ -287,8 +288,8 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
     __syncthreads();
     if (a.some)
       for (int k = tid; k < all * a.top; k += ROW_THREADS) {
-        const int r = k / a.top;
-        a.entry[(before + r) * (int64_t)a.top + k - r * a.top] = a.entry_in[(base + list[r]) * a.top + k - r * a.top];
+        const int j = k / all, r = k - j * all;
+        a.entry[j * a.rpad + before + r] = a.entry_in[(base + list[r]) * a.top + j];
       }
     const int segments = (int)((a.dp + SEGMENT - 1) / SEGMENT);
     for (int k = warp; k < all * segments; k += 8) {
@@ -336,10 +337,9 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
   const bool live = row < n, ask = EARLY || live;
   float m = -INFINITY, s = 0.f, y = 0.f;
   // the first of a thread's entries is asked for before the parts
-  const int64_t entries = (int64_t)(ask ? row : 0) * a.top;
   const int64_t src = ask ? a.src[row] : 0;
   float p0 = 0.f, y0 = 0.f;
-  if (ask && slice < a.top) { p0 = __int_as_float(a.entry[entries + slice].y); y0 = a.y_entry[entries + slice]; }
+  if (ask && slice < a.top) { p0 = __int_as_float(a.entry[slice * a.rpad + row].y); y0 = a.y_entry[slice * a.rpad + row]; }
   if (ask) {
     constexpr int U = EARLY ? 12 : 8;  // parts in flight
     for (int i0 = slice; i0 < a.parts; i0 += SLICES * U) {
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
   float e = 0.f;
   if (live)
     for (int i = slice; i < a.top; i += SLICES) {
-      const float p = i == slice ? p0 : __int_as_float(a.entry[entries + i].y), at = i == slice ? y0 : a.y_entry[entries + i];
+      const float p = i == slice ? p0 : __int_as_float(a.entry[i * a.rpad + row].y), at = i == slice ? y0 : a.y_entry[i * a.rpad + row];
       // log p - (y - lse2): close to each other where the student has learnt its teacher
       if (p > 0.f) e += p * ((a.distill ? log2f(p) : 0.f) - (at - lse2));
       else if (!(p == 0.f)) e = p;
@@ -584,7 +584,7 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   }
   r.rows = c.rows; r.vocab = cfg->vocab; r.d = (int)cfg->d; r.dp = s.dp; r.ldx = c.ldx; r.x_in = (const uint16_t*)c.X;
   r.target = distill ? nullptr : c.target; r.id64 = c.id_dtype == BETTY_I64; r.share = 1.f - cfg->smoothing; r.some = some;
-  r.entry = b.entry; r.entry_in = b.entry_in; r.top = s.top;
+  r.entry = b.entry; r.entry_in = b.entry_in; r.top = s.top; r.rpad = s.rpad;
   r.meta = b.meta; r.src = b.src; r.pos = b.pos; r.x = b.x; r.x_dw = b.x_dw;
   r.loss = c.backward ? nullptr : c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.backward ? c.dloss : nullptr;
   r.coef = b.coef; r.row_scale = b.row_scale;

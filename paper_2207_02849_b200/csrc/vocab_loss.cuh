@@ -65,11 +65,11 @@ struct Buffers {
   int32_t* pos;          // [rows] where a row went, -1: left out
   uint16_t* x;           // [rpad, dp]
   uint16_t* x_dw;        // [rpad, dp] as the gradient of W takes it (fp16: scaled, else x itself)
-  int2* entry;           // [rpad, top] entries of the rows that count: id, and the bits of p
+  int2* entry;           // [top][rpad] entries of the rows that count, the next row's beside a row's: id, and the bits of p
   int2* entry_in;        // [rows, top] the same of all rows (distillation)
   float2* part;          // [parts][rpad] maximum and sum of 2^(y - maximum) of a part of a row
   float* part_y;         // [parts][rpad] sum of y (smoothing only)
-  float* y_entry;        // [rpad, top] y at the entries
+  float* y_entry;        // [top][rpad] y at the entries
   RowCoef* coef;         // [rpad]
   float* row_scale;      // [rpad] what a row of dX is multiplied by
   uint16_t* dz;          // [rpad, piece]

@@ -163,12 +163,12 @@ __device__ __forceinline__ Tile tile_at(const Args& a, const Counts& c, int n, i
 // together and before the accumulator is waited for, so that their latency is hidden behind the products.
 struct Walk {
   static constexpr int AHEAD = 4;
-  const int2* entry;
+  const int2* entry; int64_t stride;   // the row's first; from one to the next
   int at, end, left;       // place of q[0]; entries in q
   int2 q[AHEAD], then[AHEAD];
   __device__ __forceinline__ void ask(int from) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) then[i] = from + i < end ? entry[from + i] : make_int2(NO_ID, 0);
+    for (int i = 0; i < AHEAD; ++i) then[i] = from + i < end ? entry[(from + i) * stride] : make_int2(NO_ID, 0);
   }
   __device__ __forceinline__ void fill() {
 #pragma unroll
@@ -177,15 +177,15 @@ struct Walk {
     ask(at + AHEAD);
   }
   // the first entry at or behind the column: eight places are looked at at a time
-  __device__ __forceinline__ void start(const int2* entries, int top, int column) {
-    entry = entries; end = top;
+  __device__ __forceinline__ void start(const int2* entries, int64_t apart, int top, int column) {
+    entry = entries; stride = apart; end = top;
     int lo = 0, len = top > 1 ? top : 0;
     while (len > 0) {
       const int step = (len + 7) >> 3;
       int below = 0;
 #pragma unroll
       for (int k = 1; k <= 8; ++k)
-        if (k * step <= len) below += entry[lo + k * step - 1].x < column;
+        if (k * step <= len) below += entry[(lo + k * step - 1) * stride].x < column;
       const int stop = lo + len;
       lo += below * step;
       len = min(step - 1, stop - lo);
@@ -196,7 +196,7 @@ struct Walk {
     if (top == 1 && q[0].x < column) q[0].x = NO_ID;
   }
   __device__ __forceinline__ void none() {
-    entry = nullptr; at = end = 0; left = AHEAD;
+    entry = nullptr; stride = 0; at = end = 0; left = AHEAD;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) q[i] = then[i] = make_int2(NO_ID, 0);
   }
@@ -291,7 +291,7 @@ __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, 
 #pragma unroll
       for (int k = 0; k < 8; ++k) stage16(mine, lane, k, v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
       while (w.next() < end) {
-        y_entry[w.at] = staged(staged_at(mine, lane, w.next() - cb)) * a.c2;
+        y_entry[w.at * a.rpad] = staged(staged_at(mine, lane, w.next() - cb)) * a.c2;
         w.step();
       }
       __syncwarp();
@@ -510,13 +510,11 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       const bool live = row < n;
       Walk w;
       RowCoef rc = {0.f, 0.f, 0.f, 0.f};
-      int64_t entries = 0;
       if (MODE != PRODUCTS) {
         w.none();
         if (live) {
           if (MODE == GRAD) rc = a.coef[row];
-          entries = (int64_t)row * a.top;
-          w.start(a.entry + entries, a.top, a.col0 + r.c0 + from);
+          w.start(a.entry + row, a.rpad, a.top, a.col0 + r.c0 + from);
         }
       }
       if (r.chunks) {
@@ -529,7 +527,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
       if (MODE == STATS) {
         if (first < n) {
           const int64_t at = (int64_t)(r.part * 2 + part) * a.rpad + row;
-          statistics(a, acc, r.c0, from, to, a.cols, live, w, a.y_entry + entries, a.part + at, a.part_y ? a.part_y + at : nullptr, mine);
+          statistics(a, acc, r.c0, from, to, a.cols, live, w, a.y_entry + row, a.part + at, a.part_y ? a.part_y + at : nullptr, mine);
         }
       } else if (MODE == GRAD) {
         if (first < padded) {
