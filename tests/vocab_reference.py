@@ -6,7 +6,9 @@ magnitudes, over T.  Taking it to the base 2, away from the maximum and to a pow
 (the power's own error); a sum of powers is a chain of fewer than 128 additions, and the logarithm of at most 2^22 is
 within 2^-21 of 24.  So lse is within the largest of its logits' errors and 2^-17, a relative error of q of the same size, and a loss
 within the errors of its logits and of lse, weighted as they are.
-A coefficient dz is rounded to the operands' type once (UNIT); sums over rows and over the vocabulary add as above."""
+A coefficient dz is rounded to the operands' type once (UNIT); sums over rows and over the vocabulary add as above.  In half precision
+it is stored times a power of two that brings its row's bound |g| (1 + 2 zeta |lse|) to 2^7 or more (2^13 or more for rows of
+nearly the largest bound), where half of the type's smallest step, 2^-25, is 2^-32 of the bound."""
 import math
 
 import torch
@@ -70,7 +72,8 @@ class Expected:
         # q from the logit and lse that are given in fp32, p to 2^-20 of itself, one rounding to the operands' type
         size = g.abs() * (q.abs() + smoothing / self.vocab + share)
         e = g.abs() * q.abs() * (ez + 2.0 ** -18 + 2.0 ** -22 * (z.abs() + self.lse[:, None].abs())) + size * 2.0 ** -20
-        e = torch.where(g != 0, e + UNIT[self.dtype] * 1.001 * (dz.abs() + e), 0.0)
+        step = 2.0 ** -32 * g.abs() * (1 + 2 * z_loss * self.lse[:, None].abs()) if self.dtype == torch.float16 else 0.0
+        e = torch.where(g != 0, e + UNIT[self.dtype] * 1.001 * (dz.abs() + e) + step, 0.0)
         m = dz.abs() + e
         ex = e @ wd.abs() + (self.vocab / 16 + 64) * 2.0 ** -23 * (m @ wd.abs())
         ew = e.t() @ xd.abs() + (self.rows / 16 + 8) * 2.0 ** -23 * (m.t() @ xd.abs())
