@@ -28,7 +28,8 @@ struct EntryArgs {
   const void* ids; int64_t ldi; int id64;
   const void* logits; int64_t ldt; int dtype;
   int top; float inv_t;
-  int2* out; uint8_t* some;
+  int2* out; int64_t out_row, out_place;       // from a row's entries to the next one's, from an entry to the next
+  uint8_t* some;
 };
 static constexpr uint32_t NO_KEY = 0xFFFFFFFFu;
 template <int R>
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(256) k_entries(const EntryArgs a) {
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int j = r * 32 + lane;
-    if (j < a.top) a.out[row * a.top + j] = key[r] != NO_KEY ? make_int2((int32_t)(key[r] >> 10), __float_as_int(shares[warp][key[r] & 1023u])) : make_int2(NO_ID, 0);
+    if (j < a.top) a.out[row * a.out_row + j * a.out_place] = key[r] != NO_KEY ? make_int2((int32_t)(key[r] >> 10), __float_as_int(shares[warp][key[r] & 1023u])) : make_int2(NO_ID, 0);
   }
   if (lane == 0) a.some[row] = key[0] != NO_KEY;
 }
@@ -320,6 +321,8 @@ struct LossArgs {
   int distill;
   float smoothing, z_loss; int64_t vocab;
   float* loss; float* lse;
+  // x in place: so many rows, each in its own place; which of them count
+  int rows; const void* target; int id64; const uint8_t* some; float share;
 };
 // ROWS rows a block of 512 threads, which share a row's parts and entries: 32 rows for whole cache lines, 8 where there are few.
 // Measured: 8192 rows of 512 parts: 14.5 us with 32, 29 with 8; 8 rows of 572: 14 with 32.
@@ -330,16 +333,26 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
   __shared__ float sm[WARPS][ROWS], ss[WARPS][ROWS], sy[WARPS][ROWS], se[WARPS][ROWS];
   pdl_enter();
   const int col = threadIdx.x % ROWS, slice = threadIdx.x / ROWS, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int row = blockIdx.x * ROWS + col, n = a.meta->n;
+  const int row = blockIdx.x * ROWS + col, n = a.rows ? a.rows : a.meta->n;
   // few rows: what may be needed is asked for before it is known which rows count (the arrays have room for all)
   constexpr bool EARLY = ROWS == 8;
   if (!EARLY && blockIdx.x * ROWS >= n) return;
-  const bool live = row < n, ask = EARLY || live;
+  bool live = row < n;
+  const bool ask = EARLY || live;
   float m = -INFINITY, s = 0.f, y = 0.f;
   // the first of a thread's entries is asked for before the parts
-  const int64_t src = ask ? a.src[row] : 0;
+  const int64_t src = a.rows ? row : (ask ? a.src[row] : 0);
   float p0 = 0.f, y0 = 0.f;
-  if (ask && slice < a.top) { p0 = __int_as_float(a.entry[slice * a.rpad + row].y); y0 = a.y_entry[slice * a.rpad + row]; }
+  if (ask && slice < a.top) {
+    p0 = a.rows && !a.distill ? a.share : __int_as_float(a.entry[slice * a.rpad + row].y);
+    y0 = a.y_entry[slice * a.rpad + row];
+  }
+  bool left_out = false;
+  if (a.rows && live) {
+    const int64_t t = a.distill ? (int64_t)a.some[row] - 1 : whole(a.target, a.id64, row);
+    left_out = t < 0 || t >= a.vocab;
+    live = !left_out;
+  }
   if (ask) {
     constexpr int U = EARLY ? 12 : 8;  // parts in flight
     for (int i0 = slice; i0 < a.parts; i0 += SLICES * U) {
@@ -399,6 +412,9 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
     if (a.smoothing != 0.f) e += a.smoothing * (lse2 - y / (float)a.vocab);
     a.loss[src] = e * LN2 + a.z_loss * lse * lse;
     a.lse[src] = lse;
+  } else if (slice == 0 && left_out) {
+    a.loss[src] = 0.f;
+    a.lse[src] = 0.f;
   }
 }
 
@@ -578,12 +594,31 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   Operand w = {c.W, cfg->d, cfg->vocab, 1, c.ldw, 0};
   RowArgs r = {};
   BETTY_TRY(plan_alignment(arena, w, r.align));
+  const int64_t ldx = c.rows == 1 ? pad8(cfg->d) : c.ldx;
+  const bool in_place = !c.backward && c.rows <= IN_PLACE_ROWS && aligned16(c.X) && ldx % 8 == 0 && !r.align.rows;
   if (distill) {
-    const EntryArgs e = {c.rows, cfg->vocab, c.target, c.ldi, c.id_dtype == BETTY_I64, c.teacher, c.ldt, c.teacher_dtype, c.top, 1.f / cfg->temperature, b.entry_in, some};
+    const EntryArgs e = {c.rows, cfg->vocab, c.target, c.ldi, c.id_dtype == BETTY_I64, c.teacher, c.ldt, c.teacher_dtype, c.top, 1.f / cfg->temperature, in_place ? b.entry : b.entry_in,
+                         in_place ? 1 : c.top, in_place ? s.rpad : 1, some};
     BETTY_TRY(sort_entries<1>(stream, e));
   }
+  LossArgs l = {};
+  if (!c.backward) {
+    l.meta = b.meta; l.src = b.src; l.part = b.part; l.part_y = b.part_y; l.parts = logits_parts(s); l.rpad = s.rpad;
+    l.entry = b.entry; l.y_entry = b.y_entry; l.top = s.top; l.distill = distill;
+    l.smoothing = cfg->smoothing; l.z_loss = cfg->z_loss; l.vocab = cfg->vocab; l.loss = c.loss; l.lse = c.lse_out;
+  }
+  const int id64 = c.id_dtype == BETTY_I64;
+  const float share = 1.f - cfg->smoothing;
+  if (in_place) {
+    const InPlace p = {c.X, ldx, distill ? nullptr : c.target, id64, share};
+    BETTY_TRY(logits_statistics(stream, s, b, w, true, &p));
+    l.rows = (int)c.rows; l.target = c.target; l.id64 = id64; l.some = some; l.share = share;
+    launch_pdl(k_losses<8>, dim3((unsigned)((c.rows + 7) / 8)), dim3(LOSS_THREADS), 0, stream, l);
+    BETTY_LAUNCH_CHECK();
+    return BETTY_OK;
+  }
   r.rows = c.rows; r.vocab = cfg->vocab; r.d = (int)cfg->d; r.dp = s.dp; r.ldx = c.ldx; r.x_in = (const uint16_t*)c.X;
-  r.target = distill ? nullptr : c.target; r.id64 = c.id_dtype == BETTY_I64; r.share = 1.f - cfg->smoothing; r.some = some;
+  r.target = distill ? nullptr : c.target; r.id64 = id64; r.share = share; r.some = some;
   r.entry = b.entry; r.entry_in = b.entry_in; r.top = s.top; r.rpad = s.rpad;
   r.meta = b.meta; r.src = b.src; r.pos = b.pos; r.x = b.x; r.x_dw = b.x_dw;
   r.loss = c.backward ? nullptr : c.loss; r.lse_out = c.lse_out; r.lse = c.lse; r.dloss = c.backward ? c.dloss : nullptr;
@@ -599,11 +634,7 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   const bool copied = r.align.rows != 0;
 
   if (!c.backward) {
-    BETTY_TRY(logits_statistics(stream, s, b, w, !copied));
-    LossArgs l = {};
-    l.meta = b.meta; l.src = b.src; l.part = b.part; l.part_y = b.part_y; l.parts = logits_parts(s); l.rpad = s.rpad;
-    l.entry = b.entry; l.y_entry = b.y_entry; l.top = s.top; l.distill = distill;
-    l.smoothing = cfg->smoothing; l.z_loss = cfg->z_loss; l.vocab = cfg->vocab; l.loss = c.loss; l.lse = c.lse_out;
+    BETTY_TRY(logits_statistics(stream, s, b, w, !copied, nullptr));
     if (c.rows <= 512) launch_pdl(k_losses<8>, dim3((unsigned)((c.rows + 7) / 8)), dim3(LOSS_THREADS), 0, stream, l);
     else launch_pdl(k_losses<32>, dim3((unsigned)((c.rows + 31) / 32)), dim3(LOSS_THREADS), 0, stream, l);
     BETTY_LAUNCH_CHECK();

@@ -77,9 +77,18 @@ struct Buffers {
   StatusBlock* sb;
 };
 
+// A forward pass over few rows that start on 16-byte boundaries: x is read in place, and which rows count is looked at where their losses
+// are made (rows left out make statistics that nothing reads).  8 rows x 32000 x 1024 21.7 -> 17.6 us.
+struct InPlace {
+  const void* x; int64_t ldx;
+  const void* target; int id64; float share;   // cross entropy: an entry (target, share) per row; else Buffers::entry, a row each
+};
+static constexpr int IN_PLACE_ROWS = 128;
+
 int logits_parts(const Shape& s);
-// part, part_y (if not null) and y_entry of all rows that count; w_ahead: w is not written by the kernels of this call
-betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, bool w_ahead);
+// part, part_y (if not null) and y_entry of all rows that count (in_place: of all rows); w_ahead: w is not written by the kernels of this
+// call
+betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, bool w_ahead, const InPlace* in_place);
 // dX's fp32 sums (want_dx) and dW (dw not null), piece by piece
 betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers& b, const tc::Operand& w, bool w_ahead, void* dw, int64_t lddw, int dw_dtype);
 void choose_shape(Shape& s, bool backward);

@@ -54,6 +54,8 @@ struct Args {
   float c2;
   int top;
   const int2* entry;
+  int rows;                // > 0: x is read in place, so many rows (statistics)
+  const void* target; int id64; float share;
   float2* part; float* part_y; float* y_entry;
   const RowCoef* coef;
   uint16_t* dz; int64_t ldz;
@@ -199,6 +201,11 @@ struct Walk {
     entry = nullptr; stride = 0; at = end = 0; left = AHEAD;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) q[i] = then[i] = make_int2(NO_ID, 0);
+  }
+  // a single entry
+  __device__ __forceinline__ void one(int id, float share, int column) {
+    none();
+    if (id >= column) q[0] = make_int2(id, __float_as_int(share));
   }
   __device__ __forceinline__ int next() const { return q[0].x; }
   __device__ __forceinline__ float share() const { return __int_as_float(q[0].y); }
@@ -383,8 +390,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     }
   }
   if (MODE != PRODUCTS && a.ahead && warp == 1 && elect_one()) {
-    // a single row tile: which columns this CTA takes does not depend on the count of rows, and W is not written by the kernels before
-    // this one: the first 512 KB are on the way to L2 while they run
+    // a single row tile: which columns this CTA takes does not depend on the count of rows.  The first 512 KB are on the way to L2 while the
+    // kernels before this one run (no read: what they still write to W, they write to L2 too)
     int left = (512 << 10) / (a.width / CG * BK * 2);
     for (int c = worker * a.width; c < a.cols; c += workers * a.width)
       for (int k = 0; k < a.d && left > 0; k += BK, --left) prefetch_2d(&tm.m[M_W], k, a.col0 + c + (int)rank * (a.width / CG));
@@ -395,8 +402,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
   if (CG == 2) cluster_sync_all();     // the other's barriers exist before anything is signalled across the cluster
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
-  const int n = uniform(a.meta->n);
-  const Counts count = count_tiles<CG, NT, MODE>(a, n, uniform(a.meta->split), workers);
+  const int n = MODE == STATS && a.rows ? a.rows : uniform(a.meta->n);
+  const Counts count = count_tiles<CG, NT, MODE>(a, n, MODE == PRODUCTS ? uniform(a.meta->split) : 1, workers);
 
   // The loading and the multiplying warp run their loops with all lanes, and one lane issues (see grouped.cu).
   if (warp == 0) {
@@ -514,7 +521,12 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
         w.none();
         if (live) {
           if (MODE == GRAD) rc = a.coef[row];
-          w.start(a.entry + row, a.rpad, a.top, a.col0 + r.c0 + from);
+          if (MODE == STATS && a.target) {
+            const int64_t id = a.id64 ? ((const int64_t*)a.target)[row] : ((const int32_t*)a.target)[row];
+            w.one(id >= 0 && id < a.cols ? (int)id : -1, a.share, r.c0 + from);
+          } else {
+            w.start(a.entry + row, a.rpad, a.top, a.col0 + r.c0 + from);
+          }
         }
       }
       if (r.chunks) {
@@ -744,7 +756,7 @@ static betty_status logits_maps(Maps& tm, Args& a, const Shape& s, const Buffers
   return BETTY_OK;
 }
 
-betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, bool w_ahead) {
+betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffers& b, const Operand& w, bool w_ahead, const InPlace* in_place) {
   Maps tm;
   Args a = {};
   common_args(a, s, b);
@@ -752,6 +764,11 @@ betty_status logits_statistics(cudaStream_t stream, const Shape& s, const Buffer
   a.part = b.part; a.part_y = b.part_y; a.y_entry = b.y_entry;
   BETTY_TRY(logits_maps(tm, a, s, b, w));
   a.ahead = w_ahead && s.rows <= 128;
+  if (in_place) {
+    a.rows = s.rows; a.target = in_place->target; a.id64 = in_place->id64; a.share = in_place->share;
+    const CUtensorMapDataType type = s.dtype == BETTY_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    if (!map_rows(&tm.m[M_X], type, 2, in_place->x, s.d, s.rows, in_place->ldx, BK, box_rows_of(s.rows))) return BETTY_ERR_CUDA;
+  }
   const int64_t tiles = div_up(s.rows, s.pairs ? 256 : 128) * div_up(s.vocab, s.width);
   // the operands' type is in the instruction descriptor: nothing else of the statistics depends on it
   if (s.pairs) return launch<2, 256, STATS, __nv_bfloat16, float>(stream, tm, a, tiles);
