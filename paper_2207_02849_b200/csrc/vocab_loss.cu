@@ -127,7 +127,7 @@ struct RowArgs {
   RowCoef* coef; float* row_scale;
   float inv_t, z_loss, smoothing;
   int fp16;
-  int lanes, workers, cols, want_dx, want_dw;  // the gradients' products
+  int lanes, workers, cols, want_dx, want_dw, twice;   // the gradients' products
   int64_t sum_rows;
   AlignRows align; int row_blocks;             // the blocks behind row_blocks copy W to 16-byte boundaries, where that is needed
 };
@@ -164,6 +164,7 @@ __device__ __forceinline__ void copy_segment(const RowArgs& a, int64_t from, int
   const uint16_t* in = a.x_in + from * a.ldx;
   uint16_t* out = a.x + to * a.dp;
   uint16_t* out2 = a.x_dw != a.x ? a.x_dw + to * a.dp : nullptr;
+  uint16_t* again = a.twice ? a.x_dw + (to + TWICE_ROWS) * a.dp : nullptr;
   constexpr int U = SEGMENT / 256;     // accesses in flight
   const int c0 = segment * SEGMENT + lane * 8;
   {
@@ -174,7 +175,7 @@ __device__ __forceinline__ void copy_segment(const RowArgs& a, int64_t from, int
     for (int u = 0; u < U; ++u) {
       const int c = c0 + 256 * u;
       if (c >= a.dp) break;
-      const uint4 v = shift8(raw[u], in, c, a.d);
+      uint4 v = shift8(raw[u], in, c, a.d);
       *(uint4*)(out + c) = v;
       if (out2) {
         uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -184,8 +185,10 @@ __device__ __forceinline__ void copy_segment(const RowArgs& a, int64_t from, int
           const __half2 h = __floats2half2_rn(f.x * scale, f.y * scale);
           w[k] = *(const uint32_t*)&h;
         }
-        *(uint4*)(out2 + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+        *(uint4*)(out2 + c) = v;
       }
+      if (again) *(uint4*)(again + c) = v;
     }
   }
 }
@@ -304,12 +307,12 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
       const int split = a.dloss && a.want_dx ? choose_split(a, before) : 1;
       if (lane == 0) { a.meta->n = before; a.meta->split = split; a.meta->dw_scale = lifted ? ldexpf(1.f, -least) : 1.f; }
     }
-    if (a.dloss)                       // a contraction over the rows takes them 16 at a time
-      for (int64_t r = before + warp; r < (before + 15) / 16 * 16; r += 8)
-        for (int c = lane * 8; c < a.dp; c += 256) {
-          *(uint4*)(a.x + r * a.dp + c) = make_uint4(0u, 0u, 0u, 0u);
-          if (a.x_dw != a.x) *(uint4*)(a.x_dw + r * a.dp + c) = make_uint4(0u, 0u, 0u, 0u);
-        }
+    if (a.dloss) {                     // a contraction over the rows takes them 16 at a time, or all that there is room for, twice
+      const int end = a.twice ? TWICE_ROWS : (before + 15) / 16 * 16, copies = a.twice ? 2 : 1;
+      for (int r = before + warp; r < end; r += 8)
+        for (int c = lane * 8; c < a.dp; c += 256)
+          for (int k = 0; k < copies; ++k) *(uint4*)(a.x_dw + (int64_t)(r + k * TWICE_ROWS) * a.dp + c) = make_uint4(0u, 0u, 0u, 0u);
+    }
   }
 }
 
@@ -422,7 +425,7 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
 // Row i of dX from the parts' sums of its copy, or zeros: blockDim.x threads take `width` columns of a row, four at a time each,
 // blockDim.y of them in a block of 256.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int lanes, int width, const Meta* meta, const int32_t* pos, const float* row_scale,
+__global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int lanes, int width, int twice, const Meta* meta, const int32_t* pos, const float* row_scale,
                                             const float* sums, T* dx, int64_t ld) {
   pdl_enter();
   const bool wide = ((uintptr_t)dx % (4 * sizeof(T))) == 0 && ld % 4 == 0;
@@ -440,6 +443,15 @@ __global__ void __launch_bounds__(256) k_dx(int64_t rows, int d, int64_t dp, int
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
       if (at >= 0) {
         v = *(const float4*)(in + c);
+        if (twice) {                   // the remainders' sums first: they are small
+          v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int s = 0; s < split; ++s) {
+            const float4 w = *(const float4*)(in + TWICE_ROWS * dp + s * stride + c);
+            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+          }
+          const float4 w = *(const float4*)(in + c);
+          v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
 #pragma unroll 8
         for (int s = 1; s < split; ++s) {
           const float4 w = *(const float4*)(in + s * stride + c);
@@ -625,7 +637,7 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   r.coef = b.coef; r.row_scale = b.row_scale;
   r.inv_t = 1.f / cfg->temperature; r.z_loss = cfg->z_loss; r.smoothing = cfg->smoothing; r.fp16 = cfg->dtype == BETTY_F16;
   r.lanes = s.product_pairs ? 256 : 128; r.workers = current_sm_count() / (s.product_pairs ? 2 : 1);
-  r.cols = s.piece < s.vocab ? s.piece : s.vocab; r.want_dx = s.want_dx; r.want_dw = s.want_dw; r.sum_rows = s.sum_rows;
+  r.cols = s.piece < s.vocab ? s.piece : s.vocab; r.want_dx = s.want_dx; r.want_dw = s.want_dw; r.twice = s.twice; r.sum_rows = s.sum_rows;
   // a block a row where there are few (the warps share it), about four rows a block up to four blocks an SM
   const int64_t sms = current_sm_count(), fours = (c.rows + 3) / 4, blocks = fours < sms ? (c.rows < sms ? c.rows : sms) : fours;
   r.row_blocks = (int)(blocks < most ? blocks : most);
@@ -650,11 +662,11 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
     const int64_t strips = (c.rows * ((cfg->d + width - 1) / width) + 256 / across - 1) / (256 / across);
     const dim3 grid((unsigned)(strips < most * 2 ? strips : most * 2)), block((unsigned)across, (unsigned)(256 / across));
     if (c.dx_dtype == BETTY_F32)
-      launch_pdl(k_dx<float>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (float*)c.dX, c.lddx);
+      launch_pdl(k_dx<float>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, s.twice, b.meta, b.pos, b.row_scale, b.dx, (float*)c.dX, c.lddx);
     else if (c.dx_dtype == BETTY_BF16)
-      launch_pdl(k_dx<__nv_bfloat16>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (__nv_bfloat16*)c.dX, c.lddx);
+      launch_pdl(k_dx<__nv_bfloat16>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, s.twice, b.meta, b.pos, b.row_scale, b.dx, (__nv_bfloat16*)c.dX, c.lddx);
     else
-      launch_pdl(k_dx<__half>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, b.meta, b.pos, b.row_scale, b.dx, (__half*)c.dX, c.lddx);
+      launch_pdl(k_dx<__half>, grid, block, 0, stream, c.rows, (int)cfg->d, s.dp, r.lanes, width, s.twice, b.meta, b.pos, b.row_scale, b.dx, (__half*)c.dX, c.lddx);
     BETTY_LAUNCH_CHECK();
   }
   return BETTY_OK;

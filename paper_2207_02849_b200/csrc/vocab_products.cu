@@ -60,6 +60,7 @@ struct Args {
   const RowCoef* coef;
   uint16_t* dz; int64_t ldz;
   // products
+  int twice;               // coefficients and products: remainders of the rounded coefficients, TWICE_ROWS rows behind them
   int want_dx, want_dw, add;          // add: dX's sums already hold the pieces before
   int w_blocked, dw_tma;
   void* dw; int64_t lddw;
@@ -231,6 +232,10 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
   return *(const uint32_t*)&v;
 }
 
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t v);
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t v) { return __bfloat1622float2(*(const __nv_bfloat162*)&v); }
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t v) { return __half22float2(*(const __half2*)&v); }
+
 __device__ __forceinline__ void store_2d(const CUtensorMap* tm, uint32_t from, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(from), "r"(x), "r"(y) : "memory");
 }
@@ -311,8 +316,10 @@ __device__ __forceinline__ void statistics(const Args& a, uint32_t acc, int c0, 
 }
 
 // 32 columns of a tile as coefficients of a row's gradient, packed in pairs; rows that do not count and columns that do not exist: 0
+// (rest: what the rounding took away, rounded itself; null: not wanted)
 template <typename T>
-__device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb, int end, bool live, const RowCoef& rc, Walk& w, uint32_t mine, uint32_t (&out)[16]) {
+__device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb, int end, bool live, const RowCoef& rc, Walk& w, uint32_t mine, uint32_t (&out)[16],
+                                             uint32_t* rest = nullptr) {
   const int lane = threadIdx.x & 31;
   uint32_t v[32];
   tmem_load32(v, acc);
@@ -346,6 +353,13 @@ __device__ __forceinline__ void coefficients(const Args& a, uint32_t acc, int cb
   }
 #pragma unroll
   for (int k = 0; k < 16; ++k) out[k] = pack2<T>(__uint_as_float(v[2 * k]), __uint_as_float(v[2 * k + 1]));
+  if (rest) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const float2 got = unpack2<T>(out[k]);
+      rest[k] = pack2<T>(__uint_as_float(v[2 * k]) - got.x, __uint_as_float(v[2 * k + 1]) - got.y);
+    }
+  }
 }
 
 template <typename T> struct IsF32 { static constexpr bool value = false; };
@@ -402,7 +416,8 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
   if (CG == 2) cluster_sync_all();     // the other's barriers exist before anything is signalled across the cluster
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = *tmem_slot;
-  const int n = MODE == STATS && a.rows ? a.rows : uniform(a.meta->n);
+  const int counted = MODE == STATS && a.rows ? a.rows : uniform(a.meta->n);
+  const int n = MODE == PRODUCTS && a.twice && counted ? 2 * TWICE_ROWS : counted;
   const Counts count = count_tiles<CG, NT, MODE>(a, n, MODE == PRODUCTS ? uniform(a.meta->split) : 1, workers);
 
   // The loading and the multiplying warp run their loops with all lanes, and one lane issues (see grouped.cu).
@@ -503,7 +518,7 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
     const int q = warp & 3, part = (warp - 2) >> 2;
     const uint32_t mine = s_u32(staging) + (uint32_t)(warp - 2) * 4096u;
     const float dw_scale = MODE == PRODUCTS ? a.meta->dw_scale : 1.f;
-    const int padded = (n + 15) / 16 * 16;               // rows of dz that a contraction over the rows takes
+    const int padded = MODE == GRAD && a.twice ? TWICE_ROWS : (n + 15) / 16 * 16;   // rows of dz that a contraction over the rows takes
     int j = 0;
     const int split_rows = count.row_tiles * (BM * CG);  // rows of one part of dX's sums
     for (int i = 0;; ++i) {
@@ -569,12 +584,16 @@ __device__ __forceinline__ void body(const Maps& tm, const Args& a) {
             for (int c = from; c < to; c += 32) {
               const int x = r.c0 + c;
               if (x >= a.cols) break;
-              uint32_t v[16];
-              coefficients<T>(a, acc + (uint32_t)c, shift + x, shift + min(min(x + 32, r.c0 + to), limit), live, rc, w, mine, v);
+              uint32_t v[16], rest[16];
+              const int end = shift + min(min(x + 32, r.c0 + to), limit);
+              coefficients<T>(a, acc + (uint32_t)c, shift + x, end, live, rc, w, mine, v, a.twice ? rest : nullptr);
               if (row < padded) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  if (c + 8 * k < to && x + 8 * k < a.cols) *(uint4*)(out + c + 8 * k) = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                for (int k = 0; k < 4; ++k) {
+                  if (c + 8 * k >= to || x + 8 * k >= a.cols) break;
+                  *(uint4*)(out + c + 8 * k) = make_uint4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+                  if (a.twice) *(uint4*)(out + TWICE_ROWS * a.ldz + c + 8 * k) = make_uint4(rest[4 * k], rest[4 * k + 1], rest[4 * k + 2], rest[4 * k + 3]);
+                }
               }
             }
           }
@@ -802,7 +821,8 @@ betty_status logits_gradients(cudaStream_t stream, const Shape& s, const Buffers
   pa.want_dx = s.want_dx; pa.want_dw = s.want_dw;
   pa.w_blocked = w.cols % 64 == 0;
   pa.dw = dw; pa.lddw = lddw;
-  const int a_box = s.product_pairs ? 128 : box_rows_of(s.rows);
+  const int a_box = s.product_pairs ? 128 : box_rows_of(s.twice ? 2 * TWICE_ROWS : s.rows);
+  la.twice = pa.twice = s.twice;
   pa.a_bytes = (uint32_t)a_box * BK * 2; pa.b_bytes = 128 * BK * 2;
   set_stages(pa);
   const Operand dz = {b.dz, s.piece, s.rpad, 1, s.piece, 0}, x = {b.x_dw, s.dp, s.rpad, 1, s.dp, 0};
@@ -861,6 +881,7 @@ void choose_shape(Shape& s, bool backward) {
   }
   s.product_pairs = 0;
   s.sum_rows = s.rpad;
+  s.twice = backward && rows <= TWICE_ROWS;
   if (!backward) return;
   const int64_t pair_tiles = div_up(s.d, 256) * ((s.want_dx ? div_up(rows, 256) : 0) + (s.want_dw ? div_up(s.piece, 256) : 0));
   s.product_pairs = rows > 128 && pair_tiles * 2 >= sms / 2;

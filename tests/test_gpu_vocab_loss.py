@@ -181,6 +181,26 @@ def test_half_precision_keeps_rows_of_small_weight():
         assert ref.near(dw, ww, ew + 200 * 2.0 ** -24 * dloss.abs().max())
 
 
+@pytest.mark.parametrize("rows,vocab,d", [(1, 700, 64), (5, 20000, 200), (24, 3000, 1025), (32, 999, 130)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_few_rows_keep_what_their_coefficients_lose(rows, vocab, d, dtype):
+    import paper_2207_02849_b200 as bt
+    x, w, target, dloss = _problem(rows, rows, vocab, d, dtype, ignored=0.2 if rows > 1 else 0.0)
+    cfg = _cfg(bt, vocab, d, dtype)
+    e = ref.Expected(x, w, ref.entries_ce(target, vocab, 0.0))
+    for room in (rows, 300):                       # a workspace for more rows changes nothing
+        ws = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, room))
+        ws.buf[256 + (-ws.buf.data_ptr()) % 256:] = 255
+        dx, dw = _nan(rows, d), _nan(vocab, d)
+        bt.betty_vocab_ce_backward(cfg, x, w, target, e.lse.float(), dloss, dx, dw, ws)
+        (wx, ex), (ww, ew) = e.gradients(dloss, roundings=2)
+        assert ref.near(dx, wx, ex) and ref.near(dw, ww, ew)
+        for a, b in (((dx, None), (None, dw)) if rows > 1 else ()):
+            one = [None if t is None else torch.full_like(t, float("nan")) for t in (a, b)]
+            bt.betty_vocab_ce_backward(cfg, x, w, target, e.lse.float(), dloss, *one, ws)
+            assert all(t is None or ref.near(t, *v) for t, v in zip(one, ((wx, ex), (ww, ew))))
+
+
 def _wide(pad, shift):
     def wrap(t):
         buf = torch.full((*t.shape[:-1], t.shape[-1] + pad + shift), float("nan"), dtype=t.dtype, device="cuda")

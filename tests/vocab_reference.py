@@ -62,8 +62,9 @@ class Expected:
         assert bool(((loss.double() - self.loss).abs() <= self.e_loss).all()), float(((loss.double() - self.loss).abs() - self.e_loss).max())
         assert bool((loss[~self.live] == 0).all()) and bool((lse[~self.live] == 0).all())
 
-    def gradients(self, dloss):
-        """(dx, how far it may be off before it is rounded), (dw, the same)."""
+    def gradients(self, dloss, roundings=1):
+        """(dx, how far it may be off before it is rounded), (dw, the same); roundings 2: what the first one takes away from dz is rounded
+        itself and taken along."""
         xd, wd, z, ez, ids, p, temperature, smoothing, z_loss = self._grad
         g = torch.where(self.live, dloss.double(), 0.0)[:, None] / temperature
         q = torch.exp(z - self.lse[:, None]) * (1 + 2 * z_loss * self.lse[:, None])
@@ -73,7 +74,7 @@ class Expected:
         size = g.abs() * (q.abs() + smoothing / self.vocab + share)
         e = g.abs() * q.abs() * (ez + 2.0 ** -18 + 2.0 ** -22 * (z.abs() + self.lse[:, None].abs())) + size * 2.0 ** -20
         step = 2.0 ** -32 * g.abs() * (1 + 2 * z_loss * self.lse[:, None].abs()) if self.dtype == torch.float16 else 0.0
-        e = torch.where(g != 0, e + UNIT[self.dtype] * 1.001 * (dz.abs() + e) + step, 0.0)
+        e = torch.where(g != 0, e + (UNIT[self.dtype] * 1.001) ** roundings * (dz.abs() + e) + step, 0.0)
         m = dz.abs() + e
         ex = e @ wd.abs() + (self.vocab / 16 + 64) * 2.0 ** -23 * (m @ wd.abs())
         ew = e.t() @ xd.abs() + (self.rows / 16 + 8) * 2.0 ** -23 * (m.t() @ xd.abs())
