@@ -526,7 +526,7 @@ static betty_status check(const Call& c, void* ws, size_t ws_bytes) {
   if (c.id_dtype != BETTY_I32 && c.id_dtype != BETTY_I64) return BETTY_ERR_DTYPE;
   if (distill && !float_bytes(c.teacher_dtype)) return BETTY_ERR_DTYPE;
   if (c.backward) {
-    if (!c.dX && !c.dW) return BETTY_ERR_INVALID_ARG;
+    if (c.rows && !c.dX && !c.dW) return BETTY_ERR_INVALID_ARG;   // of no rows dX has no values and may have no address
     if (c.dX && c.dx_dtype != BETTY_F32 && c.dx_dtype != c.cfg->dtype) return BETTY_ERR_DTYPE;
     if (c.dW && c.dw_dtype != BETTY_F32 && c.dw_dtype != c.cfg->dtype) return BETTY_ERR_DTYPE;
   }
