@@ -21,13 +21,14 @@ __device__ __forceinline__ float real(const void* p, int dtype, int64_t i) {
 // ------------------------------------------------------------------ a teacher's entries
 // A warp per row: the softmax of the row's logits over T, and its entries in ascending order of (id, place), by a bitonic sort of
 // 32-bit keys (22 bits of id, 10 of place) in registers: place 32 r + lane in register r.  An entry without an id of the
-// vocabulary or with a logit of -inf is none: what else its logit is is not looked at.  The same id twice stays two entries; their
-// shares add up where they are used.  (Sorted by a block in shared memory: 32 us for 8192 rows of 128.)
+// vocabulary or with a logit of -inf is none: what else its logit is is not looked at.  The maximum is taken away before T divides:
+// finite logits stay finite, or end as shares of zero, however large they are and however small T.  The same id twice stays two
+// entries; their shares add up where they are used.  (Sorted by a block in shared memory: 32 us for 8192 rows of 128.)
 struct EntryArgs {
   int64_t rows, vocab;
   const void* ids; int64_t ldi; int id64;
   const void* logits; int64_t ldt; int dtype;
-  int top; float inv_t;
+  int top; float c2;                           // log2(e) / T
   int2* out; int64_t out_row, out_place;       // from a row's entries to the next one's, from an entry to the next
   uint8_t* some;
 };
@@ -51,7 +52,7 @@ __global__ void __launch_bounds__(256) k_entries(const EntryArgs a) {
       const float x = real(a.logits, a.dtype, row * a.ldt + j);
       if (id >= 0 && id < a.vocab && x != -INFINITY) {
         key[r] = (uint32_t)id << 10 | (uint32_t)j;
-        t[r] = x * a.inv_t;
+        t[r] = x;
       }
     }
     m = fmaxf(m, t[r]);
@@ -61,7 +62,7 @@ __global__ void __launch_bounds__(256) k_entries(const EntryArgs a) {
   const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    t[r] = exp2f((t[r] - base) * LOG2E);
+    t[r] = exp2f((t[r] - base) * a.c2);
     s += t[r];
   }
 #pragma unroll
@@ -609,7 +610,7 @@ static betty_status evaluate(const Call& c, void* ws, size_t ws_bytes, void* str
   const int64_t ldx = c.rows == 1 ? pad8(cfg->d) : c.ldx;
   const bool in_place = !c.backward && c.rows <= IN_PLACE_ROWS && aligned16(c.X) && ldx % 8 == 0 && !r.align.rows;
   if (distill) {
-    const EntryArgs e = {c.rows, cfg->vocab, c.target, c.ldi, c.id_dtype == BETTY_I64, c.teacher, c.ldt, c.teacher_dtype, c.top, 1.f / cfg->temperature, in_place ? b.entry : b.entry_in,
+    const EntryArgs e = {c.rows, cfg->vocab, c.target, c.ldi, c.id_dtype == BETTY_I64, c.teacher, c.ldt, c.teacher_dtype, c.top, s.c2, in_place ? b.entry : b.entry_in,
                          in_place ? 1 : c.top, in_place ? s.rpad : 1, some};
     BETTY_TRY(sort_entries<1>(stream, e));
   }

@@ -2,7 +2,8 @@
 import pytest
 import torch
 
-from tests.test_gpu_vocab_loss import BF, F, _cfg, _ok
+from tests import vocab_reference as ref
+from tests.test_gpu_vocab_loss import BF, F, HF, _cfg, _nan, _ok, _problem
 
 pytestmark = pytest.mark.gpu
 
@@ -23,3 +24,37 @@ def test_an_empty_batch_without_a_weight_gradient():
             got = head.backward(w, kept, rows[0], wants)
             assert sorted(got) == sorted(wants) and ("u" not in got or got["u"].shape == (0, 64)) and ("w" not in got or bool((got["w"] == 0).all()))
     _ok(bt, head.ws)
+
+
+@pytest.mark.parametrize("teacher", [F, BF, HF])
+@pytest.mark.parametrize("temperature", [1e-3, 0.5, 1.0, 3.0])
+def test_teachers_with_logits_at_the_ends_of_their_type(teacher, temperature):
+    """Finite logits are entries however large they are: a mask of the type's lowest value beside others has no share, alone it is a uniform
+    distribution; the quotient by a temperature below one need not be a number of fp32.
+    A q below 2^-126 is subnormal and may count as zero: beside the reference's tolerances a coefficient may be off by 2^-126 |g| / T."""
+    import paper_2207_02849_b200 as bt
+    rows, vocab, d, top = 60, 500, 64, 8
+    x, w, _, dloss = _problem(5, rows, vocab, d, BF, boost=0.0)
+    g = torch.Generator().manual_seed(1)
+    ids = torch.stack([torch.randperm(vocab, generator=g)[:top] for _ in range(rows)]).cuda()
+    t = torch.randn(rows, top, generator=g)
+    low, high = torch.finfo(teacher).min, torch.finfo(teacher).max
+    t[0::6] = low
+    t[1::6, 2:] = low
+    t[2::6, 3] = high
+    t[3::6] = high
+    t[4::6, :4], t[4::6, 4:] = low, high
+    t = t.to(teacher).cuda()
+    cfg = _cfg(bt, vocab, d, BF, temperature=temperature)
+    ws = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, rows, top))
+    loss, lse, dx, dw = _nan(rows), _nan(rows), _nan(rows, d, dtype=BF), _nan(vocab, d, dtype=BF)
+    bt.betty_vocab_distill(cfg, x, w, ids, t, loss, lse, ws)
+    bt.betty_vocab_distill_backward(cfg, x, w, ids, t, lse, dloss, dx, dw, ws)
+    _ok(bt, ws)
+    e = ref.Expected(x, w, ref.entries_distill(ids, t, vocab, temperature), temperature, distill=True)
+    assert bool(e.live.all())
+    e.check_forward(loss, lse)
+    (wx, ex), (ww, ew) = e.gradients(dloss)
+    tiny = 2.0 ** -126 * dloss.double().abs()[:, None] / temperature
+    assert ref.near(dx, wx, ex + tiny * w.double().abs().sum(0))
+    assert ref.near(dw, ww, ew + (tiny * x.double().abs()).sum(0))
