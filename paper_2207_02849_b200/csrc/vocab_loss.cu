@@ -143,11 +143,9 @@ __device__ __forceinline__ bool counts(const RowArgs& a, const Mark& m) { return
 __device__ __forceinline__ float bound_of(const RowArgs& a, int64_t i, float g) {
   return fabsf(g * a.inv_t) * (a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * fabsf(a.lse[i]) : 1.f);
 }
-// exponent that brings a bound to [2^13, 2^14) (of bounds at the ends of the fp32 range: near it); of a bound that is zero or not
-// finite: none
-__device__ __forceinline__ int lift(float bound) {
-  return bound > 0.f && bound < INFINITY ? min(max(13 - ilogbf(bound), -100), 100) : 0;
-}
+// exponent that brings a bound to [2^13, 2^14); of bounds below 2^-113 only to 2^126 times themselves, 1 or more: 2^-126 is the smallest power
+// that the way back can multiply by.  Of a bound that is zero or not finite: none
+__device__ __forceinline__ int lift(float bound) { return bound > 0.f && bound < INFINITY ? min(13 - ilogbf(bound), 126) : 0; }
 static constexpr int NO_LIFT = 1 << 20;
 // Half precision: a row's coefficients are stored as dz 2^h, with h from the row's own bound, so that none of a row with a small
 // weight is lost; the sums dX take 2^-h back.  dW sums over rows of different h: with H the smallest, x is scaled by

@@ -58,3 +58,24 @@ def test_teachers_with_logits_at_the_ends_of_their_type(teacher, temperature):
     tiny = 2.0 ** -126 * dloss.double().abs()[:, None] / temperature
     assert ref.near(dx, wx, ex + tiny * w.double().abs().sum(0))
     assert ref.near(dw, ww, ew + (tiny * x.double().abs()).sum(0))
+
+
+@pytest.mark.parametrize("rows", [20, 200])
+@pytest.mark.parametrize("dtype,low,high,temperature", [(HF, 114, 118, 1.0), (BF, 114, 118, 1.0), (HF, -116, -112, 1.0), (HF, -14, -10, 1e30), (HF, 14, 18, 1e-30), (BF, 14, 18, 1e-30)])
+def test_weights_at_the_ends_of_the_range(rows, dtype, low, high, temperature):
+    """Gradients are as near, relative to their rows' weights over the temperature, as those of weights near one; results below the normal
+    numbers of fp32 may be zero."""
+    import paper_2207_02849_b200 as bt
+    vocab, d = 700, 72
+    x, w, target, _ = _problem(3, rows, vocab, d, dtype)
+    dloss = torch.logspace(low, high, rows, base=2.0, device="cuda") * torch.where(torch.arange(rows, device="cuda") % 2 == 0, 1.0, -1.0)
+    if temperature < 1.0:
+        w.zero_()                                  # logits that are zero whatever they are divided by
+    cfg = _cfg(bt, vocab, d, dtype, temperature=temperature)
+    ws = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, rows))
+    e = ref.Expected(x, w, ref.entries_ce(target, vocab, 0.0), temperature)
+    dx, dw = _nan(rows, d), _nan(vocab, d)
+    bt.betty_vocab_ce_backward(cfg, x, w, target, e.lse.float(), dloss, dx, dw, ws)
+    for got, (want, off) in zip((dx, dw), e.gradients(dloss)):
+        small = torch.where(want.abs() <= 2.0 ** -125, 2.0 ** -125, 0.0)
+        assert bool(((got.double() - want).abs() <= off + small).all())
