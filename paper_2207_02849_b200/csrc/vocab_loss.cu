@@ -326,6 +326,18 @@ struct LossArgs {
   // x in place: so many rows, each in its own place; which of them count
   int rows; const void* target; int id64; const uint8_t* some; float share;
 };
+// A sum that takes along what its additions round away: a thread adds up to 2048 parts (2^22 columns in half tiles of 128, 16 threads a
+// row), and parts that all round the same way would end 2^-15 off.  With it no sum of powers is a chain of more than 64 additions.  It is
+// taken once for the parts in flight, 16 of them in the 32-row form: part by part, eight in flight, 600 rows of 1000 parts took 6 us more.
+struct LongSum {
+  float s, lost;
+  __device__ __forceinline__ void scale(float f) { s *= f; lost *= f; }
+  __device__ __forceinline__ void add(float v) {
+    const float w = __fsub_rn(v, lost), t = __fadd_rn(s, w);
+    lost = __fsub_rn(__fsub_rn(t, s), w);
+    s = t;
+  }
+};
 // ROWS rows a block of 512 threads, which share a row's parts and entries: 32 rows for whole cache lines, 8 where there are few.
 // Measured: 8192 rows of 512 parts: 14.5 us with 32, 29 with 8; 8 rows of 572: 14 with 32.
 static constexpr int LOSS_THREADS = 512;
@@ -342,6 +354,7 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
   bool live = row < n;
   const bool ask = EARLY || live;
   float m = -INFINITY, s = 0.f, y = 0.f;
+  LongSum sum = {0.f, 0.f}, sum_y = {0.f, 0.f};
   // the first of a thread's entries is asked for before the parts
   const int64_t src = a.rows ? row : (ask ? a.src[row] : 0);
   float p0 = 0.f, y0 = 0.f;
@@ -356,7 +369,7 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
     live = !left_out;
   }
   if (ask) {
-    constexpr int U = EARLY ? 12 : 8;  // parts in flight
+    constexpr int U = EARLY ? 12 : 16; // parts in flight
     for (int i0 = slice; i0 < a.parts; i0 += SLICES * U) {
       float2 q[U];
 #pragma unroll
@@ -368,13 +381,25 @@ __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) most = fmaxf(most, q[u].x);
       const float base = most == -INFINITY ? 0.f : most;
-      s *= exp2f(m - base);
+      float e = 0.f;                   // of the parts in flight: plain additions, U at most one after the other
 #pragma unroll
-      for (int u = 0; u < U; ++u) s += q[u].y * exp2f(q[u].x - base);
+      for (int u = 0; u < U; ++u) e += q[u].y * exp2f(q[u].x - base);
+      sum.scale(exp2f(m - base));
+      sum.add(e);
       m = most;
     }
     if (a.part_y)
-      for (int i = slice; i < a.parts; i += SLICES) y += a.part_y[(int64_t)i * a.rpad + row];
+      for (int i0 = slice; i0 < a.parts; i0 += SLICES * 8) {
+        float e = 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int i = i0 + u * SLICES;
+          e += i < a.parts ? a.part_y[(int64_t)i * a.rpad + row] : 0.f;
+        }
+        sum_y.add(e);
+      }
+    s = sum.s;
+    y = sum_y.s;
   }
 #pragma unroll
   for (int o = ROWS; o < 32; o <<= 1) {

@@ -79,3 +79,26 @@ def test_weights_at_the_ends_of_the_range(rows, dtype, low, high, temperature):
     for got, (want, off) in zip((dx, dw), e.gradients(dloss)):
         small = torch.where(want.abs() <= 2.0 ** -125, 2.0 ** -125, 0.0)
         assert bool(((got.double() - want).abs() <= off + small).all())
+
+
+@pytest.mark.parametrize("rows", [40, 600])
+@pytest.mark.parametrize("smoothing", [0.0, 1.0])
+def test_sums_over_the_largest_vocabulary(rows, smoothing):
+    """Half tiles that all have the same sum, 1 + 127 exp(-0.65625): added one after the other, 2048 of them a thread, every addition rounds
+    the same way, and the logarithm ends 3.0e-5 off, where 1.2e-5 is allowed."""
+    import paper_2207_02849_b200 as bt
+    vocab, d = (1 << 22) - 128, 8
+    w = torch.zeros(vocab, d, dtype=BF, device="cuda")
+    w[:, 0] = -0.65625
+    w[::128, 0] = 0.0
+    x = torch.zeros(rows, d, dtype=BF, device="cuda")
+    x[:, 0] = 1.0
+    target = torch.full((rows,), 5, device="cuda")
+    cfg = _cfg(bt, vocab, d, BF, smoothing=smoothing)
+    ws = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, rows))
+    loss, lse = _nan(rows), _nan(rows)
+    bt.betty_vocab_ce(cfg, x, w, target, loss, lse, ws)
+    _ok(bt, ws)
+    one = ref.Expected(x[:1], w, ref.entries_ce(target[:1], vocab, smoothing), smoothing=smoothing)
+    assert float((lse.double() - one.lse).abs().max()) <= float(one.e_lse)
+    assert float((loss.double() - one.loss).abs().max()) <= float(one.e_loss)
