@@ -733,7 +733,7 @@ def _tokens(t: torch.Tensor, rows: int):
 
 
 def _on_current_device(*tensors) -> None:
-    """Kernels run on the current device: operands of another one are refused before anything is launched."""
+    """Kernels run on the current device: operands, results and a workspace of another one are refused before anything is launched."""
     here = _raw_device() if _raw_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() not in (here, -1):             # -1: not on a GPU, which is refused where its type is
@@ -753,7 +753,7 @@ def betty_vocab_ce(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, target: tor
                    ws: Workspace, stream=None) -> None:
     """loss, lse [rows] fp32: the rows' cross entropy with `target` (int32 or int64) and the logarithm of its normaliser."""
     rows = x.shape[0]
-    _on_current_device(x, w, target, loss, lse)
+    _on_current_device(x, w, target, loss, lse, ws.buf)
     _check(lib().betty_vocab_ce(*cfg._operands(x, w), *_tokens(target, rows), _row_values(loss, rows, "loss"),
                                 _row_values(lse, rows, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_ce")
 
@@ -762,7 +762,7 @@ def betty_vocab_ce_backward(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, ta
                             dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], ws: Workspace, stream=None) -> None:
     """dx, dw (None: not wanted) = the gradients of sum(dloss * loss)."""
     rows = x.shape[0]
-    _on_current_device(x, w, target, lse, dloss, dx, dw)
+    _on_current_device(x, w, target, lse, dloss, dx, dw, ws.buf)
     _check(lib().betty_vocab_ce_backward(*cfg._operands(x, w), *_tokens(target, rows),
                                          _row_values(lse, rows, "lse"), _row_values(dloss, rows, "dloss"), *cfg._results(dx, dw, rows), ws.ptr,
                                          ws.nbytes, _stream(stream)), "betty_vocab_ce_backward")
@@ -772,7 +772,7 @@ def betty_vocab_distill(cfg: VocabLoss, x: torch.Tensor, w: torch.Tensor, ids: t
                         lse: torch.Tensor, ws: Workspace, stream=None) -> None:
     """loss [rows] = KL(teacher || student) with the teacher's distribution over its entries (ids, teacher) [rows, top]."""
     rows = x.shape[0]
-    _on_current_device(x, w, ids, teacher, loss, lse)
+    _on_current_device(x, w, ids, teacher, loss, lse, ws.buf)
     _check(lib().betty_vocab_distill(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(loss, rows, "loss"),
                                      _row_values(lse, rows, "lse"), ws.ptr, ws.nbytes, _stream(stream)), "betty_vocab_distill")
 
@@ -781,7 +781,7 @@ def betty_vocab_distill_backward(cfg: VocabLoss, x: torch.Tensor, w: torch.Tenso
                                  dloss: torch.Tensor, dx: Optional[torch.Tensor], dw: Optional[torch.Tensor], ws: Workspace, stream=None) -> None:
     """dx, dw (None: not wanted) = the gradients of sum(dloss * loss)."""
     rows = x.shape[0]
-    _on_current_device(x, w, ids, teacher, lse, dloss, dx, dw)
+    _on_current_device(x, w, ids, teacher, lse, dloss, dx, dw, ws.buf)
     _check(lib().betty_vocab_distill_backward(*cfg._operands(x, w), *cfg._entries(ids, teacher, rows), _row_values(lse, rows, "lse"),
                                               _row_values(dloss, rows, "dloss"), *cfg._results(dx, dw, rows), ws.ptr, ws.nbytes, _stream(stream)),
            "betty_vocab_distill_backward")
