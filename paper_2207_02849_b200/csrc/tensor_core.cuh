@@ -167,52 +167,64 @@ static inline bool make_blocked_map(CUtensorMap* tm, int dtype, const Operand& o
 
 static inline int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
 
-// The values c .. c + 7 of a row of 16-bit values (c a multiple of 8), zeros behind its last: the two 16-byte words around them,
-// shifted together (never outside the row: its ends go value by value).  In two steps, so that the words of several are under way
-// together.
+// The values c .. c + 7 of a row of 16-bit values (c a multiple of 8), zeros behind its last, never outside the row: of a row that starts on
+// an 8-byte or 4-byte boundary as words of that size, of others the two 16-byte words around them, shifted together; the ends value
+// by value, each in a word of its own.  In two steps, so that the words of several accesses are under way together.
 struct Words { uint4 x, y; };
-__device__ __forceinline__ bool inside(const uint16_t* row, int c, int cols, int m) { return m ? c >= m && c - m + 16 <= cols : c + 8 <= cols; }
 __device__ __forceinline__ int before_word(const uint16_t* row) { return (int)((uintptr_t)row & 15) >> 1; }   // values between a 16-byte boundary and the row
+// whether whole words are read for c .. c + 7
+__device__ __forceinline__ bool inside(int c, int cols, int m) { return m & 1 ? c >= m && c - m + 16 <= cols : c + 8 <= cols; }
 __device__ __forceinline__ Words fetch8(const uint16_t* row, int c, int cols) {
   Words r = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
   const int m = before_word(row);
-  const bool in = inside(row, c, cols, m);
-  if (in) r.x = *(const uint4*)(row + c - m);
-  if (in && m) r.y = *(const uint4*)(row + c - m + 8);
+  if (inside(c, cols, m)) {
+    if (m & 1) {
+      r.x = *(const uint4*)(row + c - m);
+      r.y = *(const uint4*)(row + c - m + 8);
+    } else if (m & 2) {
+      const uint32_t* p = (const uint32_t*)(row + c);
+      r.x = make_uint4(p[0], p[1], p[2], p[3]);
+    } else {
+      const uint2 a = *(const uint2*)(row + c), b = *(const uint2*)(row + c + 4);
+      r.x = make_uint4(a.x, a.y, b.x, b.y);
+    }
+  } else if (c < cols) {
+    r.x.x = row[c];
+    if (c + 1 < cols) r.x.y = row[c + 1];
+    if (c + 2 < cols) r.x.z = row[c + 2];
+    if (c + 3 < cols) r.x.w = row[c + 3];
+    if (c + 4 < cols) r.y.x = row[c + 4];
+    if (c + 5 < cols) r.y.y = row[c + 5];
+    if (c + 6 < cols) r.y.z = row[c + 6];
+    if (c + 7 < cols) r.y.w = row[c + 7];
+  }
   return r;
 }
 __device__ __forceinline__ uint4 shift8(const Words& r, const uint16_t* row, int c, int cols) {
   const int m = before_word(row);
-  if (inside(row, c, cols, m)) {
-    uint32_t w[8] = {r.x.x, r.x.y, r.x.z, r.x.w, r.y.x, r.y.y, r.y.z, r.y.w};
+  if (!inside(c, cols, m)) return make_uint4(r.x.x | r.x.y << 16, r.x.z | r.x.w << 16, r.y.x | r.y.y << 16, r.y.z | r.y.w << 16);
+  if (!(m & 1)) return r.x;
+  uint32_t w[8] = {r.x.x, r.x.y, r.x.z, r.x.w, r.y.x, r.y.y, r.y.z, r.y.w};
 #pragma unroll
-    for (int k = 0; k < 6; ++k) w[k] = m & 4 ? w[k + 2] : w[k];
+  for (int k = 0; k < 6; ++k) w[k] = m & 4 ? w[k + 2] : w[k];
 #pragma unroll
-    for (int k = 0; k < 5; ++k) w[k] = m & 2 ? w[k + 1] : w[k];
+  for (int k = 0; k < 5; ++k) w[k] = m & 2 ? w[k + 1] : w[k];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = m & 1 ? __funnelshift_r(w[k], w[k + 1], 16) : w[k];
-    return make_uint4(w[0], w[1], w[2], w[3]);
-  }
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
-  if (c < cols) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (c + k < cols) w[k >> 1] |= (uint32_t)row[c + k] << (16 * (k & 1));
-  }
+  for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Copies a [rows, cols] matrix of 16-bit values to rows of `ld` values (a multiple of 8, from a 16-byte boundary), which is
 // what TMA reads; used for operands whose own rows do not start on 16-byte boundaries.  A warp takes a row at a time and a lane
-// eight values (85056 rows of 2461: 836 MB in 128 us, 6.5 TB/s; pieces of rows shared evenly among the lanes, or four segments of any
-// rows at a time, took 157 and 174 with their divisions).  Blocks of 256 threads.
+// eight values, U accesses under way together (pieces of rows shared evenly among the lanes, or four segments of any
+// rows at a time, took 157 and 174 us with their divisions where this takes 132).  Blocks of 256 threads.
 struct AlignRows {
   const uint16_t* src; int64_t ld_src, rows_per_group, group_stride, rows; int cols;
   uint16_t* dst; int ld;
 };
+template <int U>
 __device__ __forceinline__ void align_rows(const AlignRows& a, int64_t block, int64_t blocks) {
   const int lane = threadIdx.x & 31, cols = a.cols, ld = a.ld;
-  constexpr int U = 4;
   for (int64_t row = block * 8 + (threadIdx.x >> 5); row < a.rows; row += blocks * 8) {
     const uint16_t* p = a.rows_per_group == a.rows ? a.src + row * a.ld_src
                                                    : a.src + (row / a.rows_per_group) * a.group_stride + (row % a.rows_per_group) * a.ld_src;

@@ -226,7 +226,9 @@ __global__ void __launch_bounds__(ROW_THREADS) k_rows(const RowArgs a) {
   __shared__ float scales[ROW_THREADS];
   pdl_enter();
   if ((int)blockIdx.x >= a.row_blocks) {
-    align_rows(a.align, blockIdx.x - a.row_blocks, gridDim.x - a.row_blocks);
+    // narrow rows: fewer accesses (as in align.cu, with this kernel's registers): 60000 x 500 and a pass over it 41.5 instead of 45 us
+    if (a.align.ld <= 1280) align_rows<3>(a.align, blockIdx.x - a.row_blocks, gridDim.x - a.row_blocks);
+    else align_rows<4>(a.align, blockIdx.x - a.row_blocks, gridDim.x - a.row_blocks);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
