@@ -470,9 +470,12 @@ betty_status betty_vocab_ce(const betty_vocab_cfg* cfg, int64_t rows, const void
 /* Gradients of sum_i dloss_i loss_i, with lse from the forward call:
  *   dX_i = (dloss_i / T) sum_v dz_iv w_v,   dW_v = sum_i (dloss_i / T) dz_iv x_i,
  *   dz_iv = (1 + 2 zeta lse_i) exp(z_iv - lse_i) - (1 - e) [v = target_i] - e / vocab.
- * dX or dW may be NULL (not both, unless there are no rows).  Result types: BETTY_F32 or the operands' type.  dz is rounded to the operands' type before
- * the two products (of up to 32 rows what that takes away is taken along too).  A row that is left out, or whose dloss is 0, has a zero row in dX and no part in dW, whatever X holds there.
- * fp16: rows whose weights are less than 2^-20 of the largest lose accuracy in dW. */
+ * dX or dW may be NULL (not both, unless there are no rows).  Result types: BETTY_F32 or the operands' type.  dz is rounded
+ * to the operands' type before the two products (of up to 32 rows what that takes away is taken along too).  A row that is
+ * left out, or whose dloss is 0, has a zero row in dX and no part in dW, whatever X holds there.
+ * fp16: rows whose bound b_i = |dloss_i / T| (1 + 2 zeta |lse_i|) is less than 2^-6 of the largest, b, enter dW with x_i times a
+ * power of two, rounded again: an element is off by up to 2^-30 b |dz_iv| / (1 + 2 zeta |lse_i|) for each of them, whatever the size
+ * of x_i (values that stay normal numbers lose nothing).  dX is as near for all rows. */
 betty_status betty_vocab_ce_backward(const betty_vocab_cfg* cfg, int64_t rows, const void* X, int64_t ldx, const void* W, int64_t ldw,
                                      const void* target, int32_t target_dtype, const float* lse, const float* dloss, void* dX,
                                      int64_t lddx, int32_t dx_dtype, void* dW, int64_t lddw, int32_t dw_dtype, void* ws,

@@ -102,3 +102,29 @@ def test_sums_over_the_largest_vocabulary(rows, smoothing):
     one = ref.Expected(x[:1], w, ref.entries_ce(target[:1], vocab, smoothing), smoothing=smoothing)
     assert float((lse.double() - one.lse).abs().max()) <= float(one.e_lse)
     assert float((loss.double() - one.loss).abs().max()) <= float(one.e_loss)
+
+
+@pytest.mark.parametrize("size", [1.0, 0.03])
+@pytest.mark.parametrize("low", [-16, -22, -30])
+def test_half_precision_matrix_gradient_of_small_weights(size, low):
+    """Rows whose bound |dloss| (1 + 2 zeta |lse|) / T is 2^-6 of the largest or less, B: their coefficients are stored with bounds in
+    [2^7, 2^8), and x times a power of two, off by half of the type's smallest step, 2^-25, where it leaves the normal numbers.  Brought
+    back by at most B 2^-13, that is 2^-30 B of a row, times its |dz| over its bound."""
+    import paper_2207_02849_b200 as bt
+    rows, vocab, d = 300, 1200, 96
+    x, w, target, _ = _problem(21, rows, vocab, d, HF, ignored=0.0, boost=0.0)
+    x = (x.float() * size).to(HF)
+    dloss = torch.ones(rows, device="cuda")
+    dloss[2:] = torch.logspace(low, low + 3, rows - 2, base=2.0, device="cuda")
+    z_loss = 0.01
+    cfg = _cfg(bt, vocab, d, HF, z_loss=z_loss)
+    ws = bt.Workspace.of_bytes(bt.betty_vocab_workspace_size(cfg, rows))
+    e = ref.Expected(x, w, ref.entries_ce(target, vocab, 0.0), z_loss=z_loss)
+    dw = _nan(vocab, d)
+    bt.betty_vocab_ce_backward(cfg, x, w, target, e.lse.float(), dloss, None, dw, ws)
+    _, (ww, ew) = e.gradients(dloss)
+    factor = 1 + 2 * z_loss * e.lse.abs()
+    q = torch.exp(x.double() @ w.double().t() - e.lse[:, None])
+    dz = (q * factor[:, None]).scatter_add(1, target[:, None], -torch.ones(rows, 1, dtype=torch.float64, device="cuda"))
+    lost = 2.0 ** -30 * float((dloss.double() * factor).max()) * (dz[2:].abs() / factor[2:, None]).sum(0)[:, None] * 1.01
+    assert bool(((dw.double() - ww).abs() <= ew + lost).all()), float(((dw.double() - ww).abs() - ew - lost).max())
