@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from tests import vocab_reference as ref
-from tests.test_gpu_vocab_loss import BF, F, HF, _cfg, _nan, _ok, _problem
+from tests.test_gpu_vocab_loss import BF, F, HF, _cfg, _check_ce, _check_distill, _entries, _nan, _ok, _problem
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +128,35 @@ def test_half_precision_matrix_gradient_of_small_weights(size, low):
     dz = (q * factor[:, None]).scatter_add(1, target[:, None], -torch.ones(rows, 1, dtype=torch.float64, device="cuda"))
     lost = 2.0 ** -30 * float((dloss.double() * factor).max()) * (dz[2:].abs() / factor[2:, None]).sum(0)[:, None] * 1.01
     assert bool(((dw.double() - ww).abs() <= ew + lost).all()), float(((dw.double() - ww).abs() - ew - lost).max())
+
+
+def _pieces(rows, vocab):
+    """Columns of the vocabulary that are taken at a time: 2^27 coefficients, rows to multiples of 256, in pieces of about the same size."""
+    fits = (1 << 27) // (-(-rows // 256) * 256) // 256 * 256
+    return -(-(-(-vocab // -(-vocab // fits))) // 256) * 256
+
+
+@pytest.mark.parametrize("dtype,d,out", [(BF, 72, None), (HF, 72, F), (HF, 65, None), (BF, 67, F)])
+def test_distillation_over_several_pieces_of_the_vocabulary(dtype, d, out):
+    """Entries in each piece, on both sides of their borders, twice the same, and none."""
+    import paper_2207_02849_b200 as bt
+    rows, vocab, top = 16384, 20000, 9
+    piece = _pieces(rows, vocab)
+    assert piece < vocab
+    x, w, _, dloss = _problem(9, rows, vocab, d, dtype, boost=0.0)
+    ids, logits = _entries(2, rows, vocab, top, F, "any")
+    border = torch.tensor([0, piece - 1, piece, piece, 2 * piece - 1, 2 * piece, vocab - 1, vocab, -1])
+    ids[::3] = border
+    ids[1::7] = -1
+    _check_distill(bt, x, w, ids.cuda(), logits.cuda(), dloss, 1.5, out=out)
+
+
+@pytest.mark.parametrize("dtype,d,out", [(HF, 64, None), (HF, 67, None), (BF, 65, F)])
+def test_cross_entropy_over_several_pieces_of_the_vocabulary(dtype, d, out):
+    """Smoothed labels and z-loss, rows of all weights, results that are stored with and without TMA."""
+    import paper_2207_02849_b200 as bt
+    rows, vocab = 16384, 20000
+    x, w, target, dloss = _problem(10, rows, vocab, d, dtype)
+    piece = _pieces(rows, vocab)
+    target[:6] = torch.tensor([0, piece - 1, piece, 2 * piece - 1, 2 * piece, vocab - 1], device="cuda")
+    _check_ce(bt, x, w, target, dloss, out=out, smoothing=0.1, z_loss=1e-3)
