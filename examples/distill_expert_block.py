@@ -56,6 +56,20 @@ class Student:
         return grads
 
 
+def per_source_means(values, source, rows_of):
+    return torch.zeros_like(rows_of).index_add_(0, source, values) / rows_of
+
+
+def hypergradient(student, theta, v, train, source, rows_of, w, eps0, alpha):
+    """Of the upper cost by lambda, from the row losses at theta displaced along v, the upper cost's gradient: eps0 is the length of the
+    step.  source: the rows' sources; rows_of: how many rows each has; w = softmax(lambda)."""
+    eps = eps0 / torch.sqrt(sum(v[k].square().sum() for k in theta))
+    moved = [{k: theta[k] + s * eps * v[k] for k in theta} for s in (1.0, -1.0)]
+    costs = [per_source_means(student.losses(t, train)[0], source, rows_of) for t in moved]
+    d_lam = [w * (c - (w * c).sum()) for c in costs]             # dC/dlambda of a softmax-weighted sum
+    return -alpha * (d_lam[0] - d_lam[1]) / (2.0 * eps)
+
+
 def main(steps=40, n_experts=4, d=256, hidden=256, vocab=2000, rows=1024, top=16, sources=8, far=0.4, lr=2.0, lr_upper=200.0, eps0=0.02, alpha=1.0,
          seed=0, out=print):
     g = torch.Generator(device="cuda").manual_seed(seed)
@@ -81,21 +95,16 @@ def main(steps=40, n_experts=4, d=256, hidden=256, vocab=2000, rows=1024, top=16
     known = (offsets, x, z.argmax(1))
     lam = torch.zeros(sources, device="cuda")
     per_source = torch.zeros(sources, device="cuda").index_add_(0, source, torch.ones(rows, device="cuda"))
-    keys = tuple(theta)
 
     for step in range(steps):
         w = torch.softmax(lam, 0)
         _, kept = student.losses(theta, train)
         grads = student.gradient(train, kept, (w / per_source)[source])
-        for k in keys:
+        for k in theta:
             theta[k] -= lr * grads[k]
         loss, kept = student.losses(theta, known)
         v = student.gradient(known, kept, torch.full((rows,), 1.0 / rows, device="cuda"))
-        eps = eps0 / torch.sqrt(sum(v[k].square().sum() for k in keys))
-        moved = [{k: theta[k] + s * eps * v[k] for k in keys} for s in (1.0, -1.0)]
-        costs = [torch.zeros(sources, device="cuda").index_add_(0, source, student.losses(t, train)[0]) / per_source for t in moved]
-        d_lam = [w * (c - (w * c).sum()) for c in costs]             # dC/dlambda of a softmax-weighted sum
-        lam -= lr_upper * (-alpha * (d_lam[0] - d_lam[1]) / (2.0 * eps))
+        lam -= lr_upper * hypergradient(student, theta, v, train, source, per_source, w, eps0, alpha)
         if step % 10 == 0 or step == steps - 1:
             out(f"step {step:3d}  cross entropy of known rows {float(loss.mean()):.4f}  weight of mixed-up sources {float(torch.softmax(lam, 0)[: sources // 2].sum()):.3f}")
     for ws in (student.block.ws, student.head.ws):
