@@ -451,7 +451,10 @@ betty_status betty_grouped_workspace_size(const betty_grouped_cfg* cfg, int64_t 
  * The losses of a language model whose logits are products of its last hidden rows with a matrix of the vocabulary, forward
  * and backward, without the logits being kept: they are made again for the gradients, a piece of the vocabulary at a time.
  * Conventions as for the residual block's operators above; the losses are one number per row, so that a problem
- * above can weigh the rows (the row losses are then the gradient by the weights, and dloss the weights). */
+ * above can weigh the rows (the row losses are then the gradient by the weights, and dloss the weights).
+ * Accuracy: products of 16-bit values are exact and are added on the tensor cores, which truncate: a logit is within
+ * (d / 16 + 8) 2^-23 sum_k |x_ik w_vk| / T of the exact one, and lse and the losses are off by as much as their logits, 2^-17 and
+ * 2^-21 of the logits' size.  That is an absolute error: of a row that knows its token it can be any part of the loss. */
 typedef struct {
   int64_t vocab, d;      /* W is [vocab, d]; 1 .. 2^22 - 1 and 1 .. 2^16 */
   int32_t dtype;         /* X and W: BETTY_BF16 or BETTY_F16; fp32 accumulation */

@@ -2,7 +2,7 @@
 // C entries (see vocab_loss.cuh for the mathematics).
 //
 // What surrounds the products is bound by memory and small beside them, with few rows by latency: a copy of x in (8192 x 4096: 134 MB in 22
-// to 26 us), 8 bytes of statistics per row and half tile (8192 rows of 128 parts: 8 us), fp32 sums of dX out (201 MB in 45 to 50 us).
+// to 26 us), 8 bytes of statistics per row and half tile (8192 rows of 128 parts: 7 us), fp32 sums of dX out (201 MB in 45 to 50 us).
 #include "vocab_loss.cuh"
 
 namespace betty {
@@ -341,7 +341,7 @@ struct LongSum {
   }
 };
 // ROWS rows a block of 512 threads, which share a row's parts and entries: 32 rows for whole cache lines, 8 where there are few.
-// Measured: 8192 rows of 512 parts: 14.5 us with 32, 29 with 8; 8 rows of 572: 14 with 32.
+// Measured, with fewer parts in flight than now: 8192 rows of 512 parts: 14.5 us with 32 (now 10.4), 29 with 8; 8 rows of 572: 14 with 32.
 static constexpr int LOSS_THREADS = 512;
 template <int ROWS>
 __global__ void __launch_bounds__(LOSS_THREADS) k_losses(const LossArgs a) {

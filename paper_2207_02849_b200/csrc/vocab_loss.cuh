@@ -49,7 +49,8 @@ struct Shape {
 // The gradients' coefficients are rounded to the operands' type.  With so few rows that half of a contraction chunk over them is empty, what the
 // rounding took away is kept as rows of its own, this many behind the rounded ones (and the copies of x twice), and goes through
 // the same products, and the results are as near as their own last rounding (24 rows x 32000 x 2048, dX and dW in bf16 against 64
-// bits: 2.4e-3 -> 1.7e-3, for 93 -> 96 us).
+// bits: 2.4e-3 -> 1.7e-3, for 93 -> 96 us).  Room for 64 rows, in a second chunk, would do the same for 33 to 64 rows (2.4e-3 -> 1.7e-3, fp16
+// 3.1e-4 -> 2.1e-4), but not for nothing: 33, 48 and 64 rows take 93 us as they are and 107 to 108 with it, and fewer rows 108 instead of 96.
 static constexpr int TWICE_ROWS = 32;
 
 // ---- how the tiles of the gradients' products are spread ----
