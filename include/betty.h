@@ -454,7 +454,8 @@ betty_status betty_grouped_workspace_size(const betty_grouped_cfg* cfg, int64_t 
  * above can weigh the rows (the row losses are then the gradient by the weights, and dloss the weights).
  * Accuracy: products of 16-bit values are exact and are added on the tensor cores, which truncate: a logit is within
  * (d / 16 + 8) 2^-23 sum_k |x_ik w_vk| / T of the exact one, and lse and the losses are off by as much as their logits, 2^-17 and
- * 2^-21 of the logits' size.  That is an absolute error: of a row that knows its token it can be any part of the loss. */
+ * 2^-21 of the logits' size.  That is an absolute error: of a row that knows its token it can be any part of the loss.  In the
+ * gradients exp(z - lse) is off by the logit's error, relative, and with it the small difference that such a row's token has. */
 typedef struct {
   int64_t vocab, d;      /* W is [vocab, d]; 1 .. 2^22 - 1 and 1 .. 2^16 */
   int32_t dtype;         /* X and W: BETTY_BF16 or BETTY_F16; fp32 accumulation */
